@@ -331,6 +331,134 @@ scd_status_t scd_fit_solve_noalloc(const scd_model_t* model, int32_t branch, int
                                    void* const* w_dec, void* const* mu_enc, void* const* mu_dec,
                                    hipStream_t stream);
 
+/* ---- Serving the rebuilt cache: rotary positions, a paged 8-bit cache, attention over it -------
+ * What a consumer does with its KV cache once the codec has rebuilt it (the decode loop that follows
+ * Algorithm 1, Appendix F.2's cache positions): rows go into pages, new tokens' queries and keys are
+ * rotated to their positions, and the tokens attend to everything their request holds.  The calls
+ * below take a batch of new tokens: request b owns rows [cu_seqlens[b], cu_seqlens[b+1]) and already
+ * holds pos0[b] tokens, so row i of the request has position pos0[b] + i.
+ *
+ * scd_rows_t describes the rows of one tensor: channel c of head h of token t is element
+ * t * token_stride + h * head_stride + c of `data` (the model's dtype).  Any strides are taken, such
+ * as slices of a fused projection's rows or a head-major layout; rows whose addresses and strides
+ * are multiples of 16 bytes are read and written 16 bytes at a time.  `data` need only be aligned to
+ * its element (scd_rows_t is the exception to the 16-byte rule above). */
+typedef struct {
+  void* data;            /* DEVICE */
+  int32_t n_heads;
+  int64_t token_stride;  /* elements */
+  int64_t head_stride;   /* elements */
+} scd_rows_t;
+
+/* Rotary positions: pair i of a head (i < rotary_dim / 2) turns by p * w_i at position p.  Channels
+ * from rotary_dim on pass through.  HALF pairs channel i with i + rotary_dim / 2 (the codec's own
+ * layout), INTERLEAVED pairs 2i with 2i + 1.  With w_i = theta^(-2i / rotary_dim) the frequencies
+ * are, by `scaling`:
+ *   NONE      w_i
+ *   LINEAR    w_i / factor                                    (positions interpolated)
+ *   NTK       w_i of the base theta * factor^(rotary_dim / (rotary_dim - 2))
+ *   BY_PARTS  (1 - g) w_i / factor + g w_i, g = clamp((n - low) / (high - low), 0, 1) with
+ *             n = trained_positions w_i / 2 pi the turns pair i makes over the trained context
+ *   GIVEN     frequencies[i] (host array, read during scd_rotary_table)
+ * Cosines and sines are multiplied by attention_factor (1 = none). */
+typedef enum { SCD_ROTARY_HALF = 0, SCD_ROTARY_INTERLEAVED = 1 } scd_rotary_layout_t;
+typedef enum {
+  SCD_ROTARY_NONE = 0,
+  SCD_ROTARY_LINEAR = 1,
+  SCD_ROTARY_NTK = 2,
+  SCD_ROTARY_BY_PARTS = 3,
+  SCD_ROTARY_GIVEN = 4
+} scd_rotary_scaling_t;
+
+typedef struct {
+  int32_t head_dim;             /* even, at most 512 */
+  int32_t rotary_dim;           /* even, 2 <= rotary_dim <= head_dim */
+  int32_t layout;               /* scd_rotary_layout_t */
+  int32_t scaling;              /* scd_rotary_scaling_t */
+  double theta;                 /* > 1 */
+  double factor;                /* > 0; read by LINEAR, NTK, BY_PARTS */
+  double low, high;             /* low < high; read by BY_PARTS */
+  double attention_factor;      /* > 0 */
+  int64_t trained_positions;    /* >= 1; read by BY_PARTS */
+  const double* frequencies;    /* HOST [rotary_dim / 2]; read by GIVEN */
+} scd_rotary_t;
+
+/* Table of (cos, sin) for positions [0, max_position), fp32 [max_position][rotary_dim / 2][2],
+ * evaluated in fp64 and rounded once; built once per (rotary, max_position) and passed with the same
+ * pair to the calls below, which trust it as the codec's calls trust theirs. */
+size_t scd_rotary_table_bytes(const scd_rotary_t* rotary, int64_t max_position);
+scd_status_t scd_rotary_table(const scd_rotary_t* rotary, int64_t max_position, void* table,
+                              size_t table_bytes, hipStream_t stream);
+
+/* q_out = R(p) q and k_out = R(p) k for every row, in fp32, rounded once to dtype.  k and k_out may
+ * both be NULL.  transpose = 1 applies R(p)^T instead: the gradient of the call with respect to q and
+ * k, and, where attention_factor is 1, its inverse.  An output may be its input (same data and
+ * strides); otherwise outputs must not overlap inputs. */
+scd_status_t scd_rotary(const scd_rotary_t* rotary, const scd_batch_t* batch, const void* table,
+                        int64_t max_position, int32_t dtype, int32_t transpose,
+                        const scd_rows_t* q, const scd_rows_t* k, const scd_rows_t* q_out,
+                        const scd_rows_t* k_out, hipStream_t stream);
+
+/* Paged 8-bit cache of one layer.  A page holds page_tokens consecutive positions of one request, for
+ * every KV head: k_pages and v_pages are int8 [n_pages, n_kv_heads, page_tokens, head_dim], and a
+ * value stands for q * scale with the page's and head's scale in k_scales, v_scales
+ * [n_pages, n_kv_heads] (fp32).  page_table [n_seqs, max_pages] (device) names the page of each
+ * run of page_tokens positions of each request.  An entry outside [0, n_pages) is a hole: rows
+ * appended there are dropped, rows read there are zero, and attention leaves its positions out; so
+ * are positions from max_pages * page_tokens on and negative ones.  Pages that several requests name
+ * (a shared prefix) can be read, and must not be appended to.
+ * head_dim 32, 64 or 128; page_tokens 16, 32, 64 or 128. */
+typedef struct {
+  int32_t n_pages;
+  int32_t page_tokens;
+  int32_t n_kv_heads;
+  int32_t head_dim;
+  int32_t max_pages;
+  int8_t* k_pages;
+  int8_t* v_pages;
+  float* k_scales;
+  float* v_scales;
+  const int32_t* page_table;
+} scd_cache_t;
+
+/* Appends rows k, v [n_tokens, n_kv_heads, head_dim] at positions pos0[b] + i.  With `rotary` the
+ * keys are rotated to their positions on the way, in fp32, with no rounding before the quantisation
+ * (rotary NULL: as they are, for keys that the codec's decode or scd_rotary has rotated; table and
+ * max_position are then not read).
+ * For each page and head that new rows touch, with a = the largest magnitude of the new values:
+ *   scale = max(scale, a / 127)   (the old scale counts only if the page holds earlier positions)
+ *   q     = round(x / scale), ties to even, in [-127, 127]
+ * and where the scale grew the page's earlier values are rounded again to the new one (so a value is
+ * rounded at most once more per growth).  Scales below 2^-126 become 0 and their values 0.  A value
+ * that is not finite makes the scale of its page and head NaN, and with it all the page holds of that
+ * head, until the page is begun again.  Slots past the last row keep what they held. */
+scd_status_t scd_cache_append(const scd_cache_t* cache, const scd_batch_t* batch, int32_t dtype,
+                              const scd_rows_t* k, const scd_rows_t* v,
+                              const scd_rotary_t* rotary, const void* table,
+                              int64_t max_position, hipStream_t stream);
+
+/* Reads positions pos0[b] + i (pos0 NULL: from the start) of every request back as dense rows: what
+ * scd_encode takes from a producer that serves from pages.  Each value is q * scale in fp32, rounded
+ * once to dtype. */
+scd_status_t scd_cache_read(const scd_cache_t* cache, const scd_batch_t* batch, int32_t dtype,
+                            const scd_rows_t* k_out, const scd_rows_t* v_out, hipStream_t stream);
+
+/* Causal attention of the new tokens over the cache, which already holds them (append first).  For
+ * query row i of request b and query head h (of KV head h / (q.n_heads / n_kv_heads)):
+ *   out = sum_j p_j v_j,  p = softmax over j of softmax_scale * (q . k_j),  j in [0, pos0[b] + i]
+ * One token per request and whole prompts are the same call.  Sums, the running maximum and the
+ * softmax are fp32.  A row with no position to attend to (a hole at every one) is zero.
+ * q [n_tokens, n_heads, head_dim], n_heads a multiple of n_kv_heads; out alike, not overlapping q.
+ * `workspace` (device, 16-byte aligned, caller-owned, contents undefined on entry and exit) holds
+ * scd_cache_attend_workspace_bytes(cache, batch, q.n_heads) bytes; when that is 0 it may be NULL.
+ * The size depends on n_tokens, n_seqs, max_pages and the heads, not on device contents, so a
+ * captured call can be replayed while lengths grow.  Calls that may overlap need one each. */
+size_t scd_cache_attend_workspace_bytes(const scd_cache_t* cache, const scd_batch_t* batch,
+                                        int32_t n_q_heads);
+scd_status_t scd_cache_attend(const scd_cache_t* cache, const scd_batch_t* batch, int32_t dtype,
+                              double softmax_scale, const scd_rows_t* q, const scd_rows_t* out,
+                              void* workspace, size_t workspace_bytes, hipStream_t stream);
+
 /* ---- diagnostics ---------------------------------------------------------------------------- */
 const char* scd_status_string(scd_status_t status);
 /* Detail of the last non-OK status returned on the calling thread ("" if none). */

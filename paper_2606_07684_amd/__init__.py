@@ -11,6 +11,10 @@ meaning (``include/scd.h``):
 * :func:`scd_encode`       producer encode (Eq. encode_z_kv; Section 4.4.1)
 * :func:`scd_reuse_decode` consumer Reuse decode into the KV cache (Eq. decode_kv)
 * :func:`scd_patch_kv`     consumer Patch KV regeneration into the KV cache (Eq. kv_from_patch)
+* :func:`scd_rotary`       queries and keys rotated to their positions (or the gradient of that)
+* :func:`scd_cache_append` rows into a paged 8-bit cache, keys rotated on the way
+* :func:`scd_cache_read`   a paged cache's rows back as dense keys and values
+* :func:`scd_cache_attend` causal attention of new tokens over the paged 8-bit cache
 
 If the library is missing the first call raises: there is no fallback path.
 """
@@ -33,6 +37,9 @@ __all__ = [
     "DEFAULT_LAYERS_PER_GROUP", "scd_patch_fold", "prepare_patch_fold",
     "scd_patch_kv_from_codes", "prepare_patch_kv_from_codes", "scd_fit_solve_noalloc",
     "prepare_fit_solve_noalloc", "scd_fit_solve_noalloc_max_bytes",
+    "Rotary", "RotaryTable", "scd_rotary_table", "scd_rotary", "prepare_rotary", "PagedCache",
+    "scd_cache_append", "prepare_cache_append", "scd_cache_read", "prepare_cache_read",
+    "scd_cache_attend", "prepare_cache_attend", "scd_cache_attend_workspace_bytes",
 ]
 
 _PKG_DIR = os.path.dirname(os.path.abspath(__file__))
@@ -84,6 +91,46 @@ class _CBatch(ctypes.Structure):
     ]
 
 
+class _CRows(ctypes.Structure):
+    _fields_ = [
+        ("data", ctypes.c_void_p),
+        ("n_heads", ctypes.c_int32),
+        ("token_stride", ctypes.c_int64),
+        ("head_stride", ctypes.c_int64),
+    ]
+
+
+class _CRotary(ctypes.Structure):
+    _fields_ = [
+        ("head_dim", ctypes.c_int32),
+        ("rotary_dim", ctypes.c_int32),
+        ("layout", ctypes.c_int32),
+        ("scaling", ctypes.c_int32),
+        ("theta", ctypes.c_double),
+        ("factor", ctypes.c_double),
+        ("low", ctypes.c_double),
+        ("high", ctypes.c_double),
+        ("attention_factor", ctypes.c_double),
+        ("trained_positions", ctypes.c_int64),
+        ("frequencies", ctypes.POINTER(ctypes.c_double)),
+    ]
+
+
+class _CCache(ctypes.Structure):
+    _fields_ = [
+        ("n_pages", ctypes.c_int32),
+        ("page_tokens", ctypes.c_int32),
+        ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+        ("k_pages", ctypes.c_void_p),
+        ("v_pages", ctypes.c_void_p),
+        ("k_scales", ctypes.c_void_p),
+        ("v_scales", ctypes.c_void_p),
+        ("page_table", ctypes.c_void_p),
+    ]
+
+
 _VP = ctypes.c_void_p
 _PP = ctypes.POINTER(ctypes.c_void_p)
 _SIGS = {
@@ -130,6 +177,25 @@ _SIGS = {
     "scd_fit_solve_noalloc": (ctypes.c_int, [ctypes.POINTER(_CModel), ctypes.c_int32,
                                              ctypes.c_int64, ctypes.c_double, ctypes.c_int32]
                               + [_PP] * 6 + [_VP]),
+    "scd_rotary_table_bytes": (ctypes.c_size_t, [ctypes.POINTER(_CRotary), ctypes.c_int64]),
+    "scd_rotary_table": (ctypes.c_int, [ctypes.POINTER(_CRotary), ctypes.c_int64, _VP,
+                                        ctypes.c_size_t, _VP]),
+    "scd_rotary": (ctypes.c_int, [ctypes.POINTER(_CRotary), ctypes.POINTER(_CBatch), _VP,
+                                  ctypes.c_int64, ctypes.c_int32, ctypes.c_int32]
+                   + [ctypes.POINTER(_CRows)] * 4 + [_VP]),
+    "scd_cache_append": (ctypes.c_int, [ctypes.POINTER(_CCache), ctypes.POINTER(_CBatch),
+                                        ctypes.c_int32, ctypes.POINTER(_CRows),
+                                        ctypes.POINTER(_CRows), ctypes.POINTER(_CRotary), _VP,
+                                        ctypes.c_int64, _VP]),
+    "scd_cache_read": (ctypes.c_int, [ctypes.POINTER(_CCache), ctypes.POINTER(_CBatch),
+                                      ctypes.c_int32, ctypes.POINTER(_CRows),
+                                      ctypes.POINTER(_CRows), _VP]),
+    "scd_cache_attend_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(_CCache),
+                                                           ctypes.POINTER(_CBatch),
+                                                           ctypes.c_int32]),
+    "scd_cache_attend": (ctypes.c_int, [ctypes.POINTER(_CCache), ctypes.POINTER(_CBatch),
+                                        ctypes.c_int32, ctypes.c_double, ctypes.POINTER(_CRows),
+                                        ctypes.POINTER(_CRows), _VP, ctypes.c_size_t, _VP]),
 }
 EXPORTED_SYMBOLS = tuple(_SIGS)
 
@@ -751,3 +817,217 @@ def fit_reuse(model: Model, batch: Batch, rope: Optional[RopeTable], branch: int
                   w_enc, w_dec, mu_enc if center else None, mu_dec if center else None, ws, stream)
     return w_enc, w_dec, mu_enc, mu_dec, gram, colsum
 
+
+
+# ------------------------------------------------------------------------------------------------
+# Serving the rebuilt cache
+# ------------------------------------------------------------------------------------------------
+_LAYOUTS = {"half": 0, "interleaved": 1}
+_SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "by_parts": 3, "given": 4}
+
+
+@dataclasses.dataclass
+class Rotary:
+    """How a head's channel pairs turn with position (``scd_rotary_t``, where the formulas stand).
+    ``rotary_dim`` None: the whole head.  ``frequencies`` (radians per position of each pair) is
+    read with ``scaling="given"``."""
+    head_dim: int
+    theta: float
+    rotary_dim: Optional[int] = None
+    layout: str = "half"            # "half" or "interleaved"
+    scaling: str = "none"           # "none", "linear", "ntk", "by_parts" or "given"
+    factor: float = 1.0
+    low: float = 1.0
+    high: float = 32.0
+    trained_positions: int = 0
+    attention_factor: float = 1.0
+    frequencies: Optional[Sequence[float]] = None
+
+    def __post_init__(self):
+        if self.rotary_dim is None:
+            self.rotary_dim = self.head_dim
+        if self.layout not in _LAYOUTS:
+            raise ValueError("layout must be 'half' or 'interleaved'")
+        if self.scaling not in _SCALINGS:
+            raise ValueError(f"scaling must be one of {', '.join(_SCALINGS)}")
+        w = None
+        if self.scaling == "given":
+            if self.frequencies is None or len(self.frequencies) != self.rotary_dim // 2:
+                raise ValueError("frequencies must have rotary_dim / 2 entries")
+            w = (ctypes.c_double * len(self.frequencies))(*self.frequencies)
+        self._keep = w
+        self._c = _CRotary(self.head_dim, self.rotary_dim, _LAYOUTS[self.layout],
+                           _SCALINGS[self.scaling], float(self.theta), float(self.factor),
+                           float(self.low), float(self.high), float(self.attention_factor),
+                           int(self.trained_positions),
+                           None if w is None else ctypes.cast(w, ctypes.POINTER(ctypes.c_double)))
+
+
+@dataclasses.dataclass
+class RotaryTable:
+    """Device table filled by :func:`scd_rotary_table` for positions ``[0, max_position)``."""
+    buffer: torch.Tensor
+    max_position: int
+    rotary: Rotary
+
+
+@dataclasses.dataclass
+class PagedCache:
+    """One layer's paged 8-bit cache (``scd_cache_t``): ``k_pages``, ``v_pages`` int8
+    [n_pages, n_kv_heads, page_tokens, head_dim], ``k_scales``, ``v_scales`` fp32
+    [n_pages, n_kv_heads], ``page_table`` int32 [n_seqs, max_pages]."""
+    k_pages: torch.Tensor
+    v_pages: torch.Tensor
+    k_scales: torch.Tensor
+    v_scales: torch.Tensor
+    page_table: torch.Tensor
+
+    def __post_init__(self):
+        if self.k_pages.dim() != 4 or self.page_table.dim() != 2:
+            raise ValueError("pages must be [n_pages, n_kv_heads, page_tokens, head_dim], "
+                             "page_table [n_seqs, max_pages]")
+        n, h, size, d = self.k_pages.shape
+        for name, shape, dtype in (("k_pages", (n, h, size, d), torch.int8),
+                                   ("v_pages", (n, h, size, d), torch.int8),
+                                   ("k_scales", (n, h), torch.float32),
+                                   ("v_scales", (n, h), torch.float32),
+                                   ("page_table", tuple(self.page_table.shape), torch.int32)):
+            t = getattr(self, name)
+            if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape}")
+            if not t.is_cuda:
+                raise ValueError(f"{name} must be a CUDA tensor")
+        self._c = _CCache(n, size, h, d, self.page_table.shape[1], self.k_pages.data_ptr(),
+                          self.v_pages.data_ptr(), self.k_scales.data_ptr(),
+                          self.v_scales.data_ptr(), self.page_table.data_ptr())
+
+    @property
+    def n_kv_heads(self) -> int:
+        return self.k_pages.shape[1]
+
+    @property
+    def head_dim(self) -> int:
+        return self.k_pages.shape[3]
+
+
+def _dtype_code(t: torch.Tensor) -> int:
+    if t.dtype == torch.bfloat16:
+        return SCD_BF16
+    if t.dtype == torch.float32:
+        return SCD_F32
+    raise ValueError(f"rows have dtype {t.dtype}, expected bfloat16 or float32")
+
+
+def _rows(t: torch.Tensor, name: str, n_tokens: int, head_dim: int, dtype) -> _CRows:
+    """A [tokens, heads, head_dim] tensor of any token and head strides."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.dim() != 3 or t.shape[0] != n_tokens or t.shape[2] != head_dim:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected ({n_tokens}, heads, {head_dim})")
+    if t.stride(2) != 1:
+        raise ValueError(f"{name}: channels must be adjacent")
+    return _CRows(t.data_ptr(), t.shape[1], t.stride(0), t.stride(1))
+
+
+def _cache_batch(cache: PagedCache, batch: Batch):
+    if batch.n_seqs != cache.page_table.shape[0]:
+        raise ValueError(f"the batch has {batch.n_seqs} requests, page_table "
+                         f"{cache.page_table.shape[0]} rows")
+
+
+def scd_rotary_table(rotary: Rotary, max_position: int, device=None, stream=None) -> RotaryTable:
+    lib = load_library()
+    nbytes = int(lib.scd_rotary_table_bytes(ctypes.byref(rotary._c), int(max_position)))
+    if nbytes == 0:
+        detail = lib.scd_last_error().decode()
+        raise ValueError(f"invalid rotary or max_position: {detail or max_position}")
+    device = device or torch.device("cuda", torch.cuda.current_device())
+    buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    _check(lib.scd_rotary_table(ctypes.byref(rotary._c), int(max_position), buf.data_ptr(), nbytes,
+                                _stream(stream)))
+    return RotaryTable(buf, int(max_position), rotary)
+
+
+def prepare_rotary(table: RotaryTable, batch: Batch, q, k, q_out, k_out,
+                   transpose: bool = False) -> Prepared:
+    """q_out = R(p) q, k_out = R(p) k for rows [n_tokens, heads, head_dim] (k, k_out may be None);
+    transpose: R(p)^T, the gradient.  An output may be its input."""
+    lib = load_library()
+    d, T = table.rotary.head_dim, batch.n_tokens
+    rows = [None if t is None else _rows(t, n, T, d, q.dtype)
+            for t, n in ((q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out"))]
+    args = (ctypes.byref(table.rotary._c), ctypes.byref(batch._c), table.buffer.data_ptr(),
+            table.max_position, _dtype_code(q), 1 if transpose else 0,
+            *[None if r is None else ctypes.byref(r) for r in rows])
+    return Prepared(lib.scd_rotary, args, (table, batch, rows, q, k, q_out, k_out))
+
+
+def scd_rotary(table: RotaryTable, batch: Batch, q, k, q_out, k_out, transpose: bool = False,
+               stream=None) -> None:
+    prepare_rotary(table, batch, q, k, q_out, k_out, transpose)(stream)
+
+
+def prepare_cache_append(cache: PagedCache, batch: Batch, k, v,
+                         table: Optional[RotaryTable] = None) -> Prepared:
+    """Rows k, v [n_tokens, n_kv_heads, head_dim] into the cache at positions pos0[b] + i; with a
+    table the keys are rotated to them on the way."""
+    lib = load_library()
+    _cache_batch(cache, batch)
+    rows = [_rows(t, n, batch.n_tokens, cache.head_dim, k.dtype) for t, n in ((k, "k"), (v, "v"))]
+    args = (ctypes.byref(cache._c), ctypes.byref(batch._c), _dtype_code(k),
+            *[ctypes.byref(r) for r in rows],
+            None if table is None else ctypes.byref(table.rotary._c),
+            None if table is None else table.buffer.data_ptr(),
+            0 if table is None else table.max_position)
+    return Prepared(lib.scd_cache_append, args, (cache, batch, table, rows, k, v))
+
+
+def scd_cache_append(cache: PagedCache, batch: Batch, k, v, table: Optional[RotaryTable] = None,
+                     stream=None) -> None:
+    prepare_cache_append(cache, batch, k, v, table)(stream)
+
+
+def prepare_cache_read(cache: PagedCache, batch: Batch, k_out, v_out) -> Prepared:
+    """Positions pos0[b] + i of every request as dense rows [n_tokens, n_kv_heads, head_dim]."""
+    lib = load_library()
+    _cache_batch(cache, batch)
+    rows = [_rows(t, n, batch.n_tokens, cache.head_dim, k_out.dtype)
+            for t, n in ((k_out, "k_out"), (v_out, "v_out"))]
+    args = (ctypes.byref(cache._c), ctypes.byref(batch._c), _dtype_code(k_out),
+            *[ctypes.byref(r) for r in rows])
+    return Prepared(lib.scd_cache_read, args, (cache, batch, rows, k_out, v_out))
+
+
+def scd_cache_read(cache: PagedCache, batch: Batch, k_out, v_out, stream=None) -> None:
+    prepare_cache_read(cache, batch, k_out, v_out)(stream)
+
+
+def scd_cache_attend_workspace_bytes(cache: PagedCache, batch: Batch, n_q_heads: int) -> int:
+    return int(load_library().scd_cache_attend_workspace_bytes(
+        ctypes.byref(cache._c), ctypes.byref(batch._c), int(n_q_heads)))
+
+
+def prepare_cache_attend(cache: PagedCache, batch: Batch, q, out, scale: Optional[float] = None,
+                         workspace: Optional[torch.Tensor] = None) -> Prepared:
+    """Causal attention of rows q [n_tokens, heads, head_dim] over the cache, which holds them
+    already; ``scale`` None: head_dim^-1/2.  ``workspace`` None: one of
+    :func:`scd_cache_attend_workspace_bytes` is made and kept with the call."""
+    lib = load_library()
+    _cache_batch(cache, batch)
+    d = cache.head_dim
+    rows = [_rows(t, n, batch.n_tokens, d, q.dtype) for t, n in ((q, "q"), (out, "out"))]
+    if workspace is None:
+        nbytes = scd_cache_attend_workspace_bytes(cache, batch, q.shape[1])
+        workspace = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=q.device)
+    ws, nbytes = _workspace_arg(workspace)
+    args = (ctypes.byref(cache._c), ctypes.byref(batch._c), _dtype_code(q),
+            float(d ** -0.5 if scale is None else scale), *[ctypes.byref(r) for r in rows], ws,
+            nbytes)
+    return Prepared(lib.scd_cache_attend, args, (cache, batch, rows, q, out, workspace))
+
+
+def scd_cache_attend(cache: PagedCache, batch: Batch, q, out, scale: Optional[float] = None,
+                     workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    prepare_cache_attend(cache, batch, q, out, scale, workspace)(stream)

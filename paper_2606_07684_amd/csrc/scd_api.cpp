@@ -12,13 +12,14 @@
 #include <string>
 #include <vector>
 
+#include "scd_host.h"
 #include "scd_kernels.h"
 
 namespace {
-
 thread_local std::string g_last_error;
+}
 
-scd_status_t fail(scd_status_t s, const char* fmt, ...) {
+scd_status_t scd::fail(scd_status_t s, const char* fmt, ...) {
   char buf[512];
   va_list ap;
   va_start(ap, fmt);
@@ -28,12 +29,30 @@ scd_status_t fail(scd_status_t s, const char* fmt, ...) {
   return s;
 }
 
-scd_status_t ok() {
+scd_status_t scd::ok() {
   g_last_error.clear();
   return SCD_OK;
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool scd::aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+scd_status_t scd::check_batch(const scd_batch_t* b) {
+  if (b == nullptr) return fail(SCD_ERR_NULL, "batch is NULL");
+  if (b->n_seqs < 1) return fail(SCD_ERR_SHAPE, "n_seqs must be >= 1 (got %d)", b->n_seqs);
+  if (b->n_tokens < 0) return fail(SCD_ERR_SHAPE, "n_tokens must be >= 0");
+  if (b->n_tokens > (int64_t{1} << 31) - 1)
+    return fail(SCD_ERR_UNSUPPORTED, "n_tokens above 2^31 - 1");
+  if (b->cu_seqlens == nullptr && b->n_seqs != 1)
+    return fail(SCD_ERR_NULL, "cu_seqlens is NULL but n_seqs = %d", b->n_seqs);
+  return SCD_OK;
+}
+
+using scd::aligned16;
+using scd::check_batch;
+using scd::fail;
+using scd::ok;
+
+namespace {
 
 scd_status_t check_model(const scd_model_t* m) {
   if (m == nullptr) return fail(SCD_ERR_NULL, "model is NULL");
@@ -66,17 +85,6 @@ scd_status_t check_rank(const char* what, int layer, int32_t r, int32_t hi) {
   return SCD_OK;
 }
 
-scd_status_t check_batch(const scd_batch_t* b) {
-  if (b == nullptr) return fail(SCD_ERR_NULL, "batch is NULL");
-  if (b->n_seqs < 1) return fail(SCD_ERR_SHAPE, "n_seqs must be >= 1 (got %d)", b->n_seqs);
-  if (b->n_tokens < 0) return fail(SCD_ERR_SHAPE, "n_tokens must be >= 0");
-  if (b->n_tokens > (int64_t{1} << 31) - 1)
-    return fail(SCD_ERR_UNSUPPORTED, "n_tokens above 2^31 - 1");
-  if (b->cu_seqlens == nullptr && b->n_seqs != 1)
-    return fail(SCD_ERR_NULL, "cu_seqlens is NULL but n_seqs = %d", b->n_seqs);
-  return SCD_OK;
-}
-
 scd_status_t check_rope(const void* table, int64_t max_position) {
   if (table == nullptr) return fail(SCD_ERR_WORKSPACE, "RoPE table is NULL");
   if (!aligned16(table)) return fail(SCD_ERR_ALIGN, "RoPE table is not 16-byte aligned");
@@ -106,12 +114,6 @@ scd_status_t opt_ptr(const void* const* arr, int layer, const char* name, const 
     return fail(SCD_ERR_ALIGN, "%s[%d] is not 16-byte aligned", name, layer);
   return SCD_OK;
 }
-
-#define SCD_TRY(expr)                  \
-  do {                                 \
-    const scd_status_t s_ = (expr);    \
-    if (s_ != SCD_OK) return s_;       \
-  } while (0)
 
 // Packs jobs into launches (launch_jobs).
 class JobPacker {

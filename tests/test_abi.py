@@ -513,3 +513,163 @@ def test_rope_table_is_checked_against_the_model(lib):
     with pytest.raises(ValueError, match="theta"):
         scd._rope_args(theta, m)
     assert scd._rope_args(None, m) == (None, 0)
+
+
+# ---- serving operators ---------------------------------------------------------------------------
+def _rotary(**kw):
+    base = dict(head_dim=64, theta=1e4)
+    base.update(kw)
+    return scd.Rotary(**base)
+
+
+def _crows(data=FAKE, heads=2, token=128, head=64):
+    return scd._CRows(data, heads, token, head)
+
+
+def _ccache(**kw):
+    base = dict(n_pages=4, page_tokens=16, n_kv_heads=2, head_dim=64, max_pages=3, k_pages=FAKE, v_pages=FAKE,
+                k_scales=FAKE, v_scales=FAKE, page_table=FAKE)
+    base.update(kw)
+    return scd._CCache(*base.values())
+
+
+def _ref(x):
+    return None if x is None else ctypes.byref(x)
+
+
+def test_rotary_table_validation(lib):
+    r = _rotary()
+    assert lib.scd_rotary_table_bytes(ctypes.byref(r._c), 100) == 100 * 32 * 8
+    assert lib.scd_rotary_table_bytes(ctypes.byref(_rotary(rotary_dim=16)._c), 7) == 7 * 8 * 8
+    for bad in (dict(head_dim=0), dict(head_dim=63), dict(head_dim=514), dict(rotary_dim=66), dict(rotary_dim=3),
+                dict(rotary_dim=0), dict(theta=1.0), dict(theta=float("inf")), dict(attention_factor=0.0),
+                dict(scaling="linear", factor=0.0), dict(scaling="ntk", factor=2.0, rotary_dim=2),
+                dict(scaling="by_parts", factor=2.0, trained_positions=0),
+                dict(scaling="by_parts", factor=2.0, trained_positions=9, low=4.0, high=4.0),
+                dict(scaling="by_parts", factor=float("nan"), trained_positions=9)):
+        c = _rotary(**bad)._c
+        assert lib.scd_rotary_table_bytes(ctypes.byref(c), 100) == 0, bad
+        assert lib.scd_rotary_table(ctypes.byref(c), 100, FAKE, 1 << 30, None) in (SHAPE, UNSUP), bad
+    assert lib.scd_rotary_table_bytes(None, 100) == 0
+    assert lib.scd_rotary_table_bytes(ctypes.byref(r._c), 0) == 0
+    assert lib.scd_rotary_table(None, 100, FAKE, 1 << 30, None) == NULL
+    assert lib.scd_rotary_table(ctypes.byref(r._c), 100, None, 1 << 30, None) == WS
+    assert lib.scd_rotary_table(ctypes.byref(r._c), 100, FAKE + 4, 1 << 30, None) == ALIGN
+    assert lib.scd_rotary_table(ctypes.byref(r._c), 0, FAKE, 1 << 30, None) == WS
+    assert lib.scd_rotary_table(ctypes.byref(r._c), 100, FAKE, 100 * 32 * 8 - 1, None) == WS
+    g = _rotary(scaling="given", frequencies=[1.0] * 32)
+    g._c.frequencies = None
+    assert lib.scd_rotary_table(ctypes.byref(g._c), 100, FAKE, 1 << 30, None) == NULL
+    c = _rotary()._c
+    c.layout = 2
+    assert lib.scd_rotary_table(ctypes.byref(c), 100, FAKE, 1 << 30, None) == SHAPE
+    c.layout, c.scaling = 0, 5
+    assert lib.scd_rotary_table(ctypes.byref(c), 100, FAKE, 1 << 30, None) == SHAPE
+    with pytest.raises(ValueError):
+        _rotary(layout="pairs")
+    with pytest.raises(ValueError):
+        _rotary(scaling="dynamic")
+    with pytest.raises(ValueError):
+        _rotary(scaling="given", frequencies=[1.0])
+
+
+def _run_rotary(lib, r=None, batch=None, table=FAKE, maxp=100, dtype=1, q=_crows(), k=_crows(), qo=_crows(FAKE + 4096),
+                ko=_crows(FAKE + 8192)):
+    r, batch = r or _rotary(), batch or _batch()
+    st = lib.scd_rotary(ctypes.byref(r._c), ctypes.byref(batch._c), table, maxp, dtype, 0, _ref(q), _ref(k), _ref(qo),
+                        _ref(ko), None)
+    return st, lib.scd_last_error().decode()
+
+
+def test_rotary_validation(lib):
+    assert _run_rotary(lib, batch=_batch(n_tokens=0))[0] == OK
+    assert _run_rotary(lib, batch=_batch(n_tokens=0), q=_crows(None), qo=_crows(None), k=None, ko=None)[0] == OK
+    assert lib.scd_rotary(None, ctypes.byref(_batch()._c), FAKE, 9, 1, 0, None, None, None, None, None) == NULL
+    assert _run_rotary(lib, batch=_batch(n_seqs=2, cu=None))[0] == NULL
+    assert _run_rotary(lib, table=None)[0] == WS
+    assert _run_rotary(lib, maxp=0)[0] == WS
+    assert _run_rotary(lib, dtype=2)[0] == SHAPE
+    assert _run_rotary(lib, q=None)[0] == NULL
+    assert _run_rotary(lib, ko=None)[0] == NULL
+    assert _run_rotary(lib, k=None)[0] == NULL
+    assert _run_rotary(lib, q=_crows(None))[0] == NULL
+    assert _run_rotary(lib, q=_crows(FAKE + 1))[0] == ALIGN
+    assert _run_rotary(lib, q=_crows(FAKE + 2), dtype=0)[0] == ALIGN
+    assert _run_rotary(lib, qo=_crows(heads=3, token=192))[0] == SHAPE
+    assert _run_rotary(lib, q=_crows(heads=0), qo=_crows(heads=0))[0] == SHAPE
+    assert _run_rotary(lib, q=_crows(token=-1))[0] == SHAPE
+    for over in (dict(token=0), dict(head=0), dict(head=63), dict(token=127)):  # written rows overlap
+        st, msg = _run_rotary(lib, qo=_crows(FAKE + 4096, **over))
+        assert st == SHAPE and "q_out: rows overlap" in msg, over
+    st, msg = _run_rotary(lib, qo=_crows(FAKE, token=256))  # in place with other strides
+    assert st == SHAPE and "in place" in msg
+
+
+def _append(lib, cache=None, batch=None, dtype=1, k=_crows(), v=_crows(), r=None, table=FAKE, maxp=100):
+    cache, batch = cache or _ccache(), batch or _batch()
+    st = lib.scd_cache_append(ctypes.byref(cache), ctypes.byref(batch._c), dtype, _ref(k), _ref(v),
+                              None if r is None else ctypes.byref(r._c), table, maxp, None)
+    return st, lib.scd_last_error().decode()
+
+
+def test_cache_append_and_read_validation(lib):
+    none = _batch(n_tokens=0)
+    assert _append(lib, batch=none, k=_crows(None), v=_crows(None))[0] == OK
+    assert _append(lib, batch=none, r=_rotary())[0] == OK
+    assert lib.scd_cache_append(None, ctypes.byref(none._c), 1, None, None, None, None, 0, None) == NULL
+    for bad, want in ((dict(n_pages=0), SHAPE), (dict(max_pages=0), SHAPE), (dict(n_kv_heads=0), SHAPE),
+                      (dict(head_dim=80), UNSUP), (dict(page_tokens=48), UNSUP), (dict(page_tokens=256), UNSUP),
+                      (dict(k_pages=None), NULL), (dict(v_scales=None), NULL), (dict(page_table=None), NULL),
+                      (dict(v_pages=FAKE + 8), ALIGN), (dict(k_scales=FAKE + 4), ALIGN)):
+        assert _append(lib, cache=_ccache(**bad))[0] == want, bad
+        b, rows = _batch(), _crows()
+        assert lib.scd_cache_read(ctypes.byref(_ccache(**bad)), ctypes.byref(b._c), 1, ctypes.byref(rows),
+                                  ctypes.byref(rows), None) == want, bad
+    assert _append(lib, k=None)[0] == NULL
+    assert _append(lib, v=_crows(heads=3))[0] == SHAPE
+    assert _append(lib, dtype=9)[0] == SHAPE
+    assert _append(lib, r=_rotary(head_dim=128))[0] == SHAPE
+    assert _append(lib, r=_rotary(), table=None)[0] == WS
+    assert _append(lib, r=_rotary(theta=0.5))[0] == SHAPE
+
+    def read(ko=_crows(), vo=_crows(FAKE + 65536), batch=None):
+        b = batch or _batch()
+        return lib.scd_cache_read(ctypes.byref(_ccache()), ctypes.byref(b._c), 1, _ref(ko), _ref(vo), None)
+
+    assert read(batch=none) == OK
+    assert read(ko=None) == NULL
+    assert read(vo=_crows(None)) == NULL
+    assert read(ko=_crows(heads=1)) == SHAPE
+    assert read(vo=_crows(token=64)) == SHAPE
+    assert read(batch=_batch(n_tokens=-1)) == SHAPE
+
+
+def _attend(lib, cache=None, batch=None, dtype=1, scale=0.125, q=_crows(heads=4, token=256),
+            out=_crows(FAKE + 65536, heads=4, token=256), ws=FAKE, ws_bytes=1 << 40):
+    cache, batch = cache or _ccache(), batch or _batch()
+    st = lib.scd_cache_attend(ctypes.byref(cache), ctypes.byref(batch._c), dtype, scale, _ref(q), _ref(out), ws,
+                              ws_bytes, None)
+    return st, lib.scd_last_error().decode()
+
+
+def test_cache_attend_validation(lib):
+    assert _attend(lib, batch=_batch(n_tokens=0), ws=None, ws_bytes=0)[0] == OK
+    assert lib.scd_cache_attend(None, None, 1, 1.0, None, None, None, 0, None) == NULL
+    assert _attend(lib, cache=_ccache(head_dim=96))[0] == UNSUP
+    assert _attend(lib, scale=float("nan"))[0] == SHAPE
+    assert _attend(lib, scale=1e300)[0] == SHAPE
+    assert _attend(lib, dtype=3)[0] == SHAPE
+    assert _attend(lib, q=None)[0] == NULL
+    assert _attend(lib, q=_crows(heads=3, token=256))[0] == SHAPE
+    assert _attend(lib, out=_crows(heads=2))[0] == SHAPE
+    assert _attend(lib, out=_crows(heads=4, token=255))[0] == SHAPE
+    assert _attend(lib, batch=_batch(n_seqs=0))[0] == SHAPE
+    # the workspace: its size follows from the arguments alone, and too little is refused
+    cache, batch = _ccache(max_pages=4096), _batch(n_tokens=1)
+    need = lib.scd_cache_attend_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch._c), 4)
+    if need > 0:
+        assert _attend(lib, cache=cache, batch=batch, ws=None)[0] == NULL
+        assert _attend(lib, cache=cache, batch=batch, ws=FAKE + 8)[0] == ALIGN
+        assert _attend(lib, cache=cache, batch=batch, ws_bytes=need - 1)[0] == SHAPE
+    assert lib.scd_cache_attend_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch._c), 3) == 0
+    assert lib.scd_cache_attend_workspace_bytes(None, ctypes.byref(batch._c), 4) == 0
