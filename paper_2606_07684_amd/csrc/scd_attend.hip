@@ -2,95 +2,545 @@
 //
 // out = sum_j p_j v_j with p the softmax over the cached positions of scale * (q . k_j), in one pass
 // with a running maximum and sum: when the maximum grows from m to m', what is summed so far is
-// multiplied by e^(m - m').
+// multiplied by e^(m - m').  Both products run on the matrix cores with fp32 accumulation:
+//  - cached values are whole numbers of at most 127, exact in fp16 and bf16; a page's key scale
+//    multiplies the scores, its value scale the weights, so no value is scaled one by one.
+//  - scores in fp16: a query row is multiplied by the power of two that brings its largest element to
+//    2^14 (its scores by the inverse).  bf16 rows are then exact down to 2^-28 of that element; fp32
+//    rows are split into two parts (22 bits and their sign).
+//  - sums over values in bf16, the weights split into two parts for bf16 output (16 bits; its own
+//    rounding has 8) and three for fp32: the parts keep the whole exponent range, so a channel in
+//    which the heaviest positions are zero still has its bits.
+//  - a value scale is f 2^e with f in [1, 2).  The running maximum is that of log2 of the weight plus
+//    e, what a position can add to the sum; the softmax's own sum takes the weights times 2^-e.
+#include <algorithm>
+
 #include "scd_serve_device.h"
 
 namespace scd {
 using namespace dev;
 
-// One wave per query row: 64 positions at a time, one a lane for the scores, then one after another
-// for the sum over values.
-template <typename T, int kDim>
-__global__ __launch_bounds__(64) void cache_attend_kernel(CacheAttendParams p, int64_t units) {
-  __shared__ float q[kDim], weight[64];
-  __shared__ int64_t row_at[64];
-  const int lane = threadIdx.x;
-  constexpr int kOwn = (kDim + 63) / 64;
-  const bool owner = lane < kDim;
-  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    const int64_t t = unit / p.q.n_heads;
-    const int head = static_cast<int>(unit - t * p.q.n_heads), h = head / p.group;
-    const int b = request_of(p.batch, t, lane);
-    const Span s = span_of(p.batch, b);
-    const int64_t n = t - s.begin + s.pos0 + 1;  // positions it attends to
-    const T* src = reinterpret_cast<const T*>(p.q.data) + t * p.q.token + head * p.q.head;
-    for (int c = lane; c < kDim; c += 64) q[c] = load1(src + c) * p.scale;
-    __syncthreads();
-    float m = -INFINITY, l = 0.f, acc[kOwn] = {};
-    for (int64_t j0 = 0; j0 < n; j0 += 64) {
-      const int64_t j = j0 + lane;
-      const int page = j < n ? page_of(p.cache, b, j) : -1;
-      float score = -INFINITY;
-      if (page >= 0) {
-        row_at[lane] = page_at(p.cache, page, h, kDim) + (j & (p.cache.page - 1)) * kDim;
-        const uint4* k = reinterpret_cast<const uint4*>(p.cache.k + row_at[lane]);
-        float sum = 0.f;
-        for (int c = 0; c < kDim / 16; ++c) {
-          const uint4 w = k[c];
-          const uint32_t word[4] = {w.x, w.y, w.z, w.w};
-          for (int i = 0; i < 16; ++i)
-            sum += q[16 * c + i] * static_cast<float>(static_cast<int8_t>(word[i >> 2] >> (8 * (i & 3))));
-        }
-        score = sum * p.cache.k_scale[static_cast<int64_t>(page) * p.cache.heads + h];
-        if (score != score) score = INFINITY;  // NaN: the row becomes NaN
-      }
-      float top = score;
-      for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-      top = fmaxf(top, m);
-      if (top == -INFINITY) continue;
-      const float w = page >= 0 ? expf(score - top) : 0.f;
-      const float fade = expf(m - top);
-      m = top;
-      float sum = w;
-      for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-      l = l * fade + sum;
-      __syncthreads();
-      weight[lane] = page >= 0 ? w * p.cache.v_scale[static_cast<int64_t>(page) * p.cache.heads + h] : 0.f;
-      if (page < 0) row_at[lane] = -1;
-      __syncthreads();
-      if (owner) {
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef const __attribute__((address_space(4))) int32_t* uniform_ints_t;
+typedef const __attribute__((address_space(4))) float* uniform_floats_t;
+
+constexpr float kLog2e = 1.44269504f;
+constexpr int kLift = 14;  // the largest element of a query row is brought to 2^kLift
+constexpr int kLeastExponent = -90;  // of a value scale: 2^90 times 2^31 positions fits the sum
+
+__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ inline f32x4 mfma16(const f16x8& a, const f16x8& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+__device__ inline f32x4 mfma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// Two bytes (sign bit flipped: value + 128) with 0x64 above each are the halves 1152 + value; less
+// 1152 they are the values.
+__device__ inline uint32_t halves(uint32_t biased) {
+  const f16x2 offset = {static_cast<_Float16>(-1152.f), static_cast<_Float16>(-1152.f)};
+  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, biased) + offset);
+}
+// Eight adjacent bytes as fp16.
+__device__ inline f16x8 bytes_as_f16(uint32_t a, uint32_t b) {
+  a ^= 0x80808080u;
+  b ^= 0x80808080u;
+  u32x4 w;
+  w[0] = halves(__builtin_amdgcn_perm(0x64646464u, a, 0x04010400u));
+  w[1] = halves(__builtin_amdgcn_perm(0x64646464u, a, 0x04030402u));
+  w[2] = halves(__builtin_amdgcn_perm(0x64646464u, b, 0x04010400u));
+  w[3] = halves(__builtin_amdgcn_perm(0x64646464u, b, 0x04030402u));
+  return __builtin_bit_cast(f16x8, w);
+}
+// Byte kByte of eight words as bf16: fp32 of a byte is exact in its upper half.
+template <int kByte> __device__ inline float byte_as_f32(uint32_t w) {
+  return static_cast<float>(static_cast<int8_t>(w >> (8 * kByte)));
+}
+template <int kByte> __device__ inline bf16x8 byte_column_as_bf16(const uint32_t (&w)[8]) {
+  u32x4 r;
 #pragma unroll
-        for (int i = 0; i < kOwn; ++i) {
-          float a = acc[i] * fade;
-          for (int jj = 0; jj < 64; ++jj)
-            if (row_at[jj] >= 0) a += weight[jj] * static_cast<float>(p.cache.v[row_at[jj] + lane + 64 * i]);
-          acc[i] = a;
+  for (int i = 0; i < 4; ++i)
+    r[i] = __builtin_amdgcn_perm(__float_as_uint(byte_as_f32<kByte>(w[2 * i + 1])),
+                                 __float_as_uint(byte_as_f32<kByte>(w[2 * i])), 0x07060302u);
+  return __builtin_bit_cast(bf16x8, r);
+}
+
+// Positions the page table can name (cut off where positions would pass 31 bits).
+__device__ inline int64_t positions_held(const PagedCache& c) {
+  const int64_t n = static_cast<int64_t>(c.cols) << c.page_log2, most = (int64_t{1} << 31) - 64;
+  return n < most ? n : most;
+}
+
+// Rows of one tile: query rows (token, head of the group) of one request and KV head.
+struct Tile {
+  int b;
+  int64_t row0;      // first row, in the request
+  int rows;          // rows of the tile that exist
+  int64_t first;     // packed row of the request's first token
+  int64_t pos0;
+};
+
+// Tiles of kRows rows of all requests, one after another.
+template <int kRows>
+__device__ inline bool tile_of(const CacheAttendParams& p, int64_t index, LocateLds& lds, int tid, Tile& t) {
+  Located at{0, index};
+  const auto rows_of = [&](int b) -> int64_t {
+    const Span s = span_of(p.batch, b);
+    return (s.end - s.begin) * p.group;
+  };
+  if (!locate(p.batch.n_seqs, index, lds, tid,
+              [&](int b) { return (rows_of(b) + kRows - 1) / kRows; }, at))
+    return false;
+  const Span s = span_of(p.batch, at.b);
+  t.b = at.b;
+  t.row0 = at.local * kRows;
+  const int64_t left = (s.end - s.begin) * p.group - t.row0;
+  t.rows = static_cast<int>(left < kRows ? left : kRows);
+  t.first = s.begin;
+  t.pos0 = s.pos0;
+  return true;
+}
+__host__ __device__ inline int64_t tiles_bound(int64_t n_tokens, int32_t n_seqs, int group, int rows) {
+  const int64_t requests = n_seqs < n_tokens ? n_seqs : n_tokens;
+  return n_tokens * group / rows + requests;
+}
+
+// Splits of a tile that has `blocks` blocks of 32 positions, when a launch has up to `most`: at least
+// two blocks for each of a workgroup's four waves.
+__device__ inline int splits_of(int64_t blocks, int most) {
+  const int64_t n = (blocks + 7) / 8;
+  return static_cast<int>(n < 1 ? 1 : (n < most ? n : most));
+}
+
+// One workgroup per tile of 16 kBlocks query rows, KV head and share of the positions.  Its four waves
+// take blocks of 32 positions in turn, straight from the pages into registers in the layout of the
+// matrix operands, so no value passes through LDS:
+//   scores^T [32 x 16] = K Q^T: a lane holds positions (4g + i, 16 + 4g + i) of one query row, which
+//   is the operand layout of   out^T [d x 16] += V^T P^T   with the positions in that order.
+// The contraction over channels, and the order of the output channels over the matrix rows, are
+// permuted so that every lane reads adjacent bytes.
+template <typename T, int kDim, int kBlocks>
+__global__ __launch_bounds__(256) void cache_attend_rows_kernel(CacheAttendParams p, int most_splits,
+                                                               int64_t units, float* partial,
+                                                               float* partial_ml) {
+  constexpr int kParts = sizeof(T) == 2 ? 1 : 2;    // of a query element
+  constexpr int kWeights = sizeof(T) == 2 ? 2 : 3;  // of a weight
+  constexpr int kRows = 16 * kBlocks;
+  constexpr int kSteps = kDim / 32;   // matrix steps over channels
+  constexpr int kOut = kDim / 16;     // output channels a lane holds of each of its four matrix rows
+  constexpr int kPitch = kDim + 4;
+  __shared__ LocateLds locate_lds;
+  __shared__ float joined[4][16][kPitch];
+  __shared__ float joined_m[4][kRows], joined_l[4][kRows];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int r = lane & 15, g = lane >> 4;
+  const uniform_ints_t table = (uniform_ints_t)(p.cache.table);
+  const uniform_floats_t k_scale = (uniform_floats_t)(p.cache.k_scale);
+  const uniform_floats_t v_scale = (uniform_floats_t)(p.cache.v_scale);
+
+  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const int h = static_cast<int>(unit % p.cache.heads);
+    const int64_t rest = unit / p.cache.heads;
+    const int split = static_cast<int>(rest % most_splits);
+    Tile t;
+    if (!tile_of<kRows>(p, rest / most_splits, locate_lds, tid, t)) return;
+    const int64_t last_row = t.row0 + t.rows - 1;
+    int64_t seen = t.pos0 + last_row / p.group + 1;  // positions the tile's last row attends to
+    const int64_t held = positions_held(p.cache);
+    seen = seen < 0 ? 0 : (seen < held ? seen : held);
+    const int64_t blocks = (seen + 31) >> 5;
+    const int splits = splits_of(blocks, most_splits);
+    if (split >= splits) continue;
+    const int begin = static_cast<int>(blocks * split / splits), end = static_cast<int>(blocks * (split + 1) / splits);
+    const int64_t free_until = t.pos0 + t.row0 / p.group + 1;  // positions every row attends to
+
+    // queries
+    f16x8 q[kBlocks][kParts][kSteps];
+    float factor[kBlocks];
+    int limit[kBlocks];  // last position of the lane's row
+#pragma unroll
+    for (int n = 0; n < kBlocks; ++n) {
+      int64_t row = t.row0 + 16 * n + r;
+      row = row > last_row ? last_row : row;
+      const int64_t token = row / p.group;
+      const int head = h * p.group + static_cast<int>(row - token * p.group);
+      const T* src = reinterpret_cast<const T*>(p.q.data) + (t.first + token) * p.q.token + head * p.q.head + g * (kDim / 4);
+      float x[kSteps][8];
+      float top = 0.f;
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        load8(src + 8 * s, p.q.wide, x[s]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[s][j]));
+      }
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      int e = (__float_as_uint(top) >> 23) & 255;
+      e = e < kLift + 1 ? kLift + 1 : (e > 254 ? 254 : e);
+      const float lift = __uint_as_float(static_cast<uint32_t>(254 + kLift - e) << 23);
+      factor[n] = __uint_as_float(static_cast<uint32_t>(e - kLift) << 23) * (p.scale * kLog2e);
+      const int64_t reach = t.pos0 + token;
+      limit[n] = static_cast<int>(reach < held ? reach : held);
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float v = x[s][j] * lift;
+          const _Float16 hi = static_cast<_Float16>(v);
+          q[n][0][s][j] = hi;
+          if constexpr (kParts == 2) q[n][1][s][j] = static_cast<_Float16>(v - static_cast<float>(hi));
+        }
+    }
+
+    f32x4 acc[kBlocks][kOut];
+    float m[kBlocks], l[kBlocks];
+#pragma unroll
+    for (int n = 0; n < kBlocks; ++n) {
+      m[n] = -INFINITY;
+      l[n] = 0.f;
+#pragma unroll
+      for (int c = 0; c < kOut; ++c) acc[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    for (int block = begin + wave; block < end; block += 4) {
+      const int at = block << 5;
+      // the block's two halves of 16 positions lie in one page each
+      int page[2];
+      float ks[2], vs[2];
+      const int8_t *kb[2], *vb[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int pos = at + 16 * i;
+        int64_t col = pos >> p.cache.page_log2;
+        const bool inside = col < p.cache.cols;
+        col = inside ? col : 0;
+        int id = table[static_cast<int64_t>(t.b) * p.cache.cols + col];
+        page[i] = inside && id >= 0 && id < p.cache.n_pages ? id : -1;
+        id = page[i] < 0 ? 0 : id;
+        const int64_t s = static_cast<int64_t>(id) * p.cache.heads + h;
+        ks[i] = page[i] < 0 ? 0.f : k_scale[s];
+        vs[i] = page[i] < 0 ? 0.f : v_scale[s];
+        const int64_t byte = page_at(p.cache, id, h, kDim) + (pos & (p.cache.page - 1)) * kDim;
+        kb[i] = p.cache.k + byte;
+        vb[i] = p.cache.v + byte;
+      }
+      // keys: position r of each half, channels g * kDim / 4 on
+      uint32_t kw[2][kDim / 16];
+      uint32_t vw[kDim / 64 > 0 ? kDim / 64 : 1][8];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int8_t* src = kb[i] + r * kDim + g * (kDim / 4);
+        if constexpr (kDim >= 64) {
+#pragma unroll
+          for (int c = 0; c < kDim / 64; ++c) {
+            const uint4 w = *reinterpret_cast<const uint4*>(src + 16 * c);
+            kw[i][4 * c] = w.x; kw[i][4 * c + 1] = w.y; kw[i][4 * c + 2] = w.z; kw[i][4 * c + 3] = w.w;
+          }
+        } else {
+          const uint2 w = *reinterpret_cast<const uint2*>(src);
+          kw[i][0] = w.x; kw[i][1] = w.y;
+        }
+      }
+      // values: channels kOut * r on, of positions 4g + j of each half
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int8_t* src = vb[i] + (4 * g + j) * kDim + kOut * r;
+          if constexpr (kDim == 128) {
+            const uint2 w = *reinterpret_cast<const uint2*>(src);
+            vw[0][4 * i + j] = w.x;
+            vw[1][4 * i + j] = w.y;
+          } else if constexpr (kDim == 64) {
+            vw[0][4 * i + j] = *reinterpret_cast<const uint32_t*>(src);
+          } else {
+            vw[0][4 * i + j] = *reinterpret_cast<const uint16_t*>(src);
+          }
+        }
+      // scores
+      f32x4 score[kBlocks][2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int n = 0; n < kBlocks; ++n) score[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = 0; s < kSteps; ++s) {
+          const f16x8 k = bytes_as_f16(kw[i][2 * s], kw[i][2 * s + 1]);
+#pragma unroll
+          for (int n = 0; n < kBlocks; ++n)
+#pragma unroll
+            for (int part = 0; part < kParts; ++part) score[n][i] = mfma16(k, q[n][part][s], score[n][i]);
+        }
+      }
+      // value scales as f 2^e (e at least kLeastExponent, where f may be below 1 or 0)
+      float part_scale[2], exponent[2], back[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        int e = (__float_as_uint(vs[i]) >> 23) & 255;
+        e = e < 127 + kLeastExponent ? 127 + kLeastExponent : (e > 253 ? 253 : e);
+        back[i] = __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
+        part_scale[i] = vs[i] * back[i];
+        exponent[i] = static_cast<float>(e - 127);
+      }
+      const bool masked = at + 32 > free_until || page[0] < 0 || page[1] < 0;
+      bf16x8 w[kBlocks][kWeights];
+#pragma unroll
+      for (int n = 0; n < kBlocks; ++n) {
+        float x[8];
+        bool hidden[8];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float f = ks[i] * factor[n];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            x[4 * i + j] = fmaf(score[n][i][j], f, exponent[i]);
+            hidden[4 * i + j] = masked && (page[i] < 0 || at + 16 * i + 4 * g + j > limit[n]);
+            if (hidden[4 * i + j]) x[4 * i + j] = -INFINITY;
+          }
+        }
+        float top = m[n];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, x[j]);
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float base = top == -INFINITY ? 0.f : top;
+        const float fade = exp2_fast(m[n] - base);
+        m[n] = top;
+        float sum[2] = {0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float e = exp2_fast(x[j] - base);
+          sum[j >> 2] += e;
+          float v = hidden[j] ? 0.f : e * part_scale[j >> 2];
+#pragma unroll
+          for (int k = 0; k < kWeights; ++k) {
+            w[n][k][j] = static_cast<__bf16>(v);
+            v -= static_cast<float>(w[n][k][j]);
+          }
+        }
+        l[n] = l[n] * fade + sum[0] * back[0] + sum[1] * back[1];
+#pragma unroll
+        for (int c = 0; c < kOut; ++c) acc[n][c] *= fade;
+      }
+      // values
+      const auto out = [&](auto byte, int word) {
+        constexpr int kByte = decltype(byte)::value;
+        const bf16x8 v = byte_column_as_bf16<kByte>(vw[word]);
+#pragma unroll
+        for (int n = 0; n < kBlocks; ++n)
+#pragma unroll
+          for (int part = 0; part < kWeights; ++part)
+            acc[n][4 * word + kByte] = mfma16(v, w[n][part], acc[n][4 * word + kByte]);
+      };
+      out(IntC<0>{}, 0);
+      out(IntC<1>{}, 0);
+      if constexpr (kOut >= 4) {
+        out(IntC<2>{}, 0);
+        out(IntC<3>{}, 0);
+      }
+      if constexpr (kOut == 8) {
+        out(IntC<0>{}, 1);
+        out(IntC<1>{}, 1);
+        out(IntC<2>{}, 1);
+        out(IntC<3>{}, 1);
+      }
+    }
+
+    // join the waves, 16 rows at a time
+#pragma unroll
+    for (int n = 0; n < kBlocks; ++n) {
+      l[n] += __shfl_xor(l[n], 16);
+      l[n] += __shfl_xor(l[n], 32);
+      if (g == 0) {
+        joined_m[wave][16 * n + r] = m[n];
+        joined_l[wave][16 * n + r] = l[n];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < kBlocks; ++n) {
+      float top = joined_m[0][16 * n + r];
+      for (int v = 1; v < 4; ++v) top = fmaxf(top, joined_m[v][16 * n + r]);
+      const float mine = exp2_fast(m[n] - (top == -INFINITY ? 0.f : top));
+      float* dst = joined[wave][r];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < kOut; ++c) dst[kOut * (4 * g + i) + c] = acc[n][c][i] * mine;
+      __syncthreads();
+      for (int item = tid; item < 16 * (kDim / 8); item += 256) {
+        const int row = item / (kDim / 8), chunk = item % (kDim / 8);
+        if (16 * n + row < t.rows) {
+          float f[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            f[j] = 0.f;
+            for (int v = 0; v < 4; ++v) f[j] += joined[v][row][8 * chunk + j];
+          }
+          float rm = joined_m[0][16 * n + row];
+          for (int v = 1; v < 4; ++v) rm = fmaxf(rm, joined_m[v][16 * n + row]);
+          const float base = rm == -INFINITY ? 0.f : rm;
+          float rl = 0.f;
+          for (int v = 0; v < 4; ++v) rl += joined_l[v][16 * n + row] * exp2_fast(joined_m[v][16 * n + row] - base);
+          if (splits == 1) {
+            const int64_t token = (t.row0 + 16 * n + row) / p.group;
+            const int head = h * p.group + static_cast<int>(t.row0 + 16 * n + row - token * p.group);
+            const float inv_l = rl != 0.f ? 1.f / rl : 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] *= inv_l;
+            store8(reinterpret_cast<T*>(p.out.data) + (t.first + token) * p.out.token + head * p.out.head + 8 * chunk,
+                   p.out.wide, f);
+          } else {
+            const int64_t at = unit * kRows + 16 * n + row;
+            store8(partial + at * kDim + 8 * chunk, true, f);
+            if (chunk == 0) *reinterpret_cast<float2*>(partial_ml + 2 * at) = make_float2(rm, rl);
+          }
         }
       }
       __syncthreads();
     }
-    T* dst = reinterpret_cast<T*>(p.out.data) + t * p.out.token + head * p.out.head;
-    if (owner)
-      for (int i = 0; i < kOwn; ++i) store1(dst + lane + 64 * i, l != 0.f ? acc[i] / l : 0.f);
+  }
+}
+
+// Joins the shares of every row that was split: one workgroup per row, its threads over channels
+// (four each) and shares.
+template <typename T, int kDim, int kRows>
+__global__ __launch_bounds__(256) void cache_attend_join_kernel(CacheAttendParams p, int most_splits,
+                                                               int64_t units, const float* partial,
+                                                               const float* partial_ml) {
+  constexpr int kLanes = kDim / 4, kShares = 256 / kLanes;
+  __shared__ LocateLds locate_lds;
+  __shared__ float4 sums[kShares][kLanes];
+  __shared__ float tops[kShares], totals[kShares];
+  const int tid = threadIdx.x, c = tid % kLanes, share = tid / kLanes;
+  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const int row = static_cast<int>(unit % kRows);
+    const int h = static_cast<int>(unit / kRows % p.cache.heads);
+    const int64_t index = unit / kRows / p.cache.heads;
+    Tile t;
+    if (!tile_of<kRows>(p, index, locate_lds, tid, t)) return;
+    if (row >= t.rows) continue;
+    int64_t seen = t.pos0 + (t.row0 + t.rows - 1) / p.group + 1;
+    const int64_t held = positions_held(p.cache);
+    seen = seen < 0 ? 0 : (seen < held ? seen : held);
+    const int splits = splits_of((seen + 31) >> 5, most_splits);
+    if (splits == 1) continue;
+    const int64_t first = (index * most_splits * p.cache.heads + h) * kRows + row;
+    const int64_t step = static_cast<int64_t>(p.cache.heads) * kRows;
+    float top = -INFINITY, total = 0.f;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = share; s < splits; s += kShares) {
+      const int64_t at = first + s * step;
+      const float2 ml = *reinterpret_cast<const float2*>(partial_ml + 2 * at);
+      const float4 x = *reinterpret_cast<const float4*>(partial + at * kDim + 4 * c);
+      const float now = fmaxf(top, ml.x), base = now == -INFINITY ? 0.f : now;
+      const float fade = exp2_fast(top - base), w = exp2_fast(ml.x - base);
+      top = now;
+      total = total * fade + ml.y * w;
+      sum.x = sum.x * fade + x.x * w;
+      sum.y = sum.y * fade + x.y * w;
+      sum.z = sum.z * fade + x.z * w;
+      sum.w = sum.w * fade + x.w * w;
+    }
+    sums[share][c] = sum;
+    if (c == 0) {
+      tops[share] = top;
+      totals[share] = total;
+    }
+    __syncthreads();
+    if (share == 0) {
+      float all = tops[0];
+      for (int s = 1; s < kShares; ++s) all = fmaxf(all, tops[s]);
+      const float base = all == -INFINITY ? 0.f : all;
+      float f[4] = {0.f, 0.f, 0.f, 0.f}, l = 0.f;
+      for (int s = 0; s < kShares; ++s) {
+        const float w = exp2_fast(tops[s] - base);
+        l += totals[s] * w;
+        f[0] += sums[s][c].x * w;
+        f[1] += sums[s][c].y * w;
+        f[2] += sums[s][c].z * w;
+        f[3] += sums[s][c].w * w;
+      }
+      const int64_t token = (t.row0 + row) / p.group;
+      const int head = h * p.group + static_cast<int>(t.row0 + row - token * p.group);
+      T* dst = reinterpret_cast<T*>(p.out.data) + (t.first + token) * p.out.token + head * p.out.head + 4 * c;
+      const float inv = l != 0.f ? 1.f / l : 0.f;
+      for (int j = 0; j < 4; ++j) store1(dst + j, f[j] * inv);
+    }
     __syncthreads();
   }
 }
 
-size_t attend_workspace(const PagedCache&, const SeqBatch&, int, int) { return 0; }
+// How a call is laid out over workgroups, from its arguments alone.
+struct AttendPlan {
+  int blocks;        // 16-row blocks of a tile
+  int splits;        // most shares of a tile
+  int64_t tiles;     // bound
+};
+static AttendPlan attend_plan(const PagedCache& c, const SeqBatch& b, int group, bool bf16) {
+  AttendPlan plan;
+  const int64_t requests = b.n_seqs < b.n_tokens ? b.n_seqs : b.n_tokens;
+  const int64_t mean = b.n_tokens * group / requests;  // rows of a request and KV head
+  plan.blocks = mean <= 16 ? 1 : (mean <= 32 || !bf16) ? 2 : 4;
+  plan.tiles = tiles_bound(b.n_tokens, b.n_seqs, group, 16 * plan.blocks);
+  const int64_t most = (static_cast<int64_t>(c.cols) * c.page + 255) / 256;
+  const int64_t want = (2048 + plan.tiles * c.heads - 1) / (plan.tiles * c.heads);
+  plan.splits = static_cast<int>(want < most ? want : most);
+  return plan;
+}
 
-template <typename T>
-static hipError_t launch_attend_as(int head_dim, const CacheAttendParams& p, hipStream_t stream) {
-  const int64_t units = p.batch.n_tokens * p.q.n_heads;
-  const dim3 grid(static_cast<unsigned>(units < kMaxGrid ? units : kMaxGrid)), block(64);
-  if (head_dim == 128) hipLaunchKernelGGL((cache_attend_kernel<T, 128>), grid, block, 0, stream, p, units);
-  else if (head_dim == 64) hipLaunchKernelGGL((cache_attend_kernel<T, 64>), grid, block, 0, stream, p, units);
-  else hipLaunchKernelGGL((cache_attend_kernel<T, 32>), grid, block, 0, stream, p, units);
+size_t attend_workspace(const PagedCache& c, const SeqBatch& b, int group, int head_dim) {
+  size_t most = 0;
+  for (int bf16 = 0; bf16 < 2; ++bf16) {
+    const AttendPlan plan = attend_plan(c, b, group, bf16 != 0);
+    if (plan.splits == 1) continue;
+    const size_t rows = static_cast<size_t>(plan.tiles * c.heads * plan.splits) * (16 * plan.blocks);
+    most = std::max(most, rows * (head_dim + 2) * sizeof(float));
+  }
+  return most;
+}
+
+template <typename T, int kDim, int kBlocks>
+static hipError_t launch_rows_as(const AttendPlan& plan, const CacheAttendParams& p, float* workspace,
+                                 hipStream_t stream) {
+  const int64_t units = plan.tiles * p.cache.heads * plan.splits;
+  float* ml = workspace + units * 16 * kBlocks * kDim;
+  const auto grid = [](int64_t n) { return dim3(static_cast<unsigned>(n < kMaxGrid ? n : kMaxGrid)); };
+  hipLaunchKernelGGL((cache_attend_rows_kernel<T, kDim, kBlocks>), grid(units), dim3(256), 0, stream, p,
+                     plan.splits, units, workspace, ml);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || plan.splits == 1) return e;
+  const int64_t rows = plan.tiles * p.cache.heads * 16 * kBlocks;
+  hipLaunchKernelGGL((cache_attend_join_kernel<T, kDim, 16 * kBlocks>), grid(rows), dim3(256), 0, stream, p,
+                     plan.splits, rows, workspace, ml);
   return hipGetLastError();
 }
 
-hipError_t launch_cache_attend(bool bf16, int head_dim, const CacheAttendParams& p, void*,
+template <typename T, int kDim>
+static hipError_t launch_attend_as(const CacheAttendParams& p, float* workspace, hipStream_t stream) {
+  const AttendPlan plan = attend_plan(p.cache, p.batch, p.group, sizeof(T) == 2);
+  if (plan.blocks == 1) return launch_rows_as<T, kDim, 1>(plan, p, workspace, stream);
+  if constexpr (sizeof(T) == 2)
+    if (plan.blocks == 4) return launch_rows_as<T, kDim, 4>(plan, p, workspace, stream);
+  return launch_rows_as<T, kDim, 2>(plan, p, workspace, stream);
+}
+
+hipError_t launch_cache_attend(bool bf16, int head_dim, const CacheAttendParams& p, void* workspace,
                                hipStream_t stream) {
-  return bf16 ? launch_attend_as<uint16_t>(head_dim, p, stream) : launch_attend_as<float>(head_dim, p, stream);
+  float* ws = static_cast<float*>(workspace);
+  if (bf16)
+    return head_dim == 128 ? launch_attend_as<uint16_t, 128>(p, ws, stream)
+           : head_dim == 64 ? launch_attend_as<uint16_t, 64>(p, ws, stream)
+                            : launch_attend_as<uint16_t, 32>(p, ws, stream);
+  return head_dim == 128 ? launch_attend_as<float, 128>(p, ws, stream)
+         : head_dim == 64 ? launch_attend_as<float, 64>(p, ws, stream)
+                          : launch_attend_as<float, 32>(p, ws, stream);
 }
 
 }  // namespace scd
