@@ -316,8 +316,8 @@ class RopeTable:
 
 
 def _stream(stream) -> Optional[int]:
-    if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+    if stream is None:  # torch.cuda.current_stream().cuda_stream, without making a Stream object
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream

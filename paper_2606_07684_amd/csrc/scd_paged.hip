@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheAppendParams p, 
     const int kv = static_cast<int>(unit & 1);
     const int h = static_cast<int>((unit >> 1) % p.cache.heads);
     Located at;
-    const bool found = locate(p.batch.n_seqs, (unit >> 1) / p.cache.heads, lds, tid, [&](int b) -> int64_t {
+    const bool found = locate<256>(p.batch.n_seqs, (unit >> 1) / p.cache.heads, lds, tid, [&](int b) -> int64_t {
       const Span s = span_of(p.batch, b);
       const int64_t end = s.pos0 + s.end - s.begin;
       return s.end > s.begin && end > 0 ? ((end - 1) >> lg) - ((s.pos0 < 0 ? 0 : s.pos0) >> lg) + 1 : 0;

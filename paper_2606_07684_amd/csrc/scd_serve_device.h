@@ -57,21 +57,21 @@ __device__ inline int64_t page_at(const PagedCache& c, int page, int head, int d
 }
 
 // Work units of requests one after another, count(b) of each: the request and the place in it of
-// `unit`, or false past the last.  Every thread of the workgroup (256) calls it and gets the answer.
+// `unit`, or false past the last.  Every thread of the workgroup calls it and gets the answer.
 struct Located {
   int b;
   int64_t local;
 };
 struct LocateLds {
-  int64_t wave_sum[4];
+  int64_t wave_sum[16];
   int64_t local;
   int b;
 };
-template <typename Count>
+template <int kThreads, typename Count>
 __device__ inline bool locate(int n_seqs, int64_t unit, LocateLds& lds, int tid, Count count,
                               Located& out) {
   const int lane = tid & 63, wave = tid >> 6;
-  for (int base = 0; base < n_seqs; base += 256) {
+  for (int base = 0; base < n_seqs; base += kThreads) {
     const int64_t mine = base + tid < n_seqs ? count(base + tid) : 0;
     int64_t sum = mine;
     for (int o = 1; o < 64; o <<= 1) {
@@ -83,7 +83,7 @@ __device__ inline bool locate(int n_seqs, int64_t unit, LocateLds& lds, int tid,
     if (lane == 63) lds.wave_sum[wave] = sum;
     __syncthreads();
     int64_t before = 0, total = 0;
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < kThreads / 64; ++w) {
       if (w < wave) before += lds.wave_sum[w];
       total += lds.wave_sum[w];
     }
