@@ -89,21 +89,16 @@ struct Tile {
 // Tiles of kRows rows of all requests, one after another.
 template <int kRows, int kThreads = 256>
 __device__ inline bool tile_of(const CacheAttendParams& p, int64_t index, LocateLds& lds, int tid, Tile& t) {
-  Located at{0, index};
-  const auto rows_of = [&](int b) -> int64_t {
-    const Span s = span_of(p.batch, b);
-    return (s.end - s.begin) * p.group;
-  };
-  if (!locate<kThreads>(p.batch.n_seqs, index, lds, tid,
-              [&](int b) { return (rows_of(b) + kRows - 1) / kRows; }, at))
+  Located at;
+  if (!locate<kThreads>(p.batch, index, lds, tid,
+                        [&](const Span& s) { return ((s.end - s.begin) * p.group + kRows - 1) / kRows; }, at))
     return false;
-  const Span s = span_of(p.batch, at.b);
   t.b = at.b;
   t.row0 = at.local * kRows;
-  const int64_t left = (s.end - s.begin) * p.group - t.row0;
+  const int64_t left = (at.span.end - at.span.begin) * p.group - t.row0;
   t.rows = static_cast<int>(left < kRows ? left : kRows);
-  t.first = s.begin;
-  t.pos0 = s.pos0;
+  t.first = at.span.begin;
+  t.pos0 = at.span.pos0;
   return true;
 }
 __host__ __device__ inline int64_t tiles_bound(int64_t n_tokens, int32_t n_seqs, int group, int rows) {

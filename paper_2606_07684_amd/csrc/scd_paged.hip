@@ -7,39 +7,48 @@ using namespace dev;
 // Scales below this are 0, so that 1 / scale is finite.
 constexpr float kSmallestScale = 1.17549435e-38f;
 
-// Eight channels from 8 * chunk of a row, turned to position `pos`.
-template <typename T>
-__device__ inline void turned8(const Turn& turn, const T* row, bool wide, int chunk, int64_t pos,
-                               float* x) {
-  load8(row + 8 * chunk, wide, x);
-  if (turn.table == nullptr || 8 * chunk >= turn.dim) return;
-  pos = pos < 0 ? 0 : (pos >= turn.max_pos ? turn.max_pos - 1 : pos);
-  const int half = turn.dim / 2;
-  const float2* cs = turn.table + pos * half;
-  float unused;
-  if (turn.interleaved) {
+// How a row's 16-channel items turn.
+enum class TurnKind : int {
+  kNone,         // as they are
+  kHalf,         // item i < dim / 16: channels 8i.. and dim / 2 + 8i.., the two halves of 8 pairs
+  kInterleaved,  // item i: channels 16i.., 8 adjacent pairs
+  kOdd           // rotary_dim not a multiple of 16: channels 16i.., each with its partner wherever it is
+};
+
+// First channels of the two 8-channel groups of an item.
+template <TurnKind kKind>
+__device__ inline int2 item_channels(const Turn& turn, int item) {
+  if (kKind == TurnKind::kHalf && 16 * item < turn.dim) return make_int2(8 * item, turn.dim / 2 + 8 * item);
+  return make_int2(16 * item, 16 * item + 8);
+}
+// An item's 16 channels turned by the table's row `cs` (its 8 pairs in registers but for kOdd).
+template <TurnKind kKind, typename T>
+__device__ inline void turn_item(const Turn& turn, const T* row, int item, const float2 (&cs)[8],
+                                 const float2* table_row, float (&x)[16]) {
+  if constexpr (kKind == TurnKind::kHalf) {
+    if (16 * item < turn.dim) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (8 * chunk + 2 * i < turn.dim)
-        turn_pair(x[2 * i], x[2 * i + 1], cs[4 * chunk + i], x[2 * i], x[2 * i + 1]);
-    return;
-  }
-  if (half % 8 == 0) {  // the other halves of the eight pairs are adjacent too
-    float y[8];
-    const bool first = 8 * chunk < half;
-    const int at = first ? 8 * chunk : 8 * chunk - half;
-    load8(row + (first ? 8 * chunk + half : at), wide, y);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (first) turn_pair(x[i], y[i], cs[at + i], x[i], unused);
-      else turn_pair(y[i], x[i], cs[at + i], unused, x[i]);
+      for (int i = 0; i < 8; ++i) turn_pair(x[i], x[8 + i], cs[i], x[i], x[8 + i]);
     }
-    return;
-  }
-  for (int i = 0; i < 8; ++i) {
-    const int c = 8 * chunk + i;
-    if (c < half) turn_pair(x[i], load1(row + c + half), cs[c], x[i], unused);
-    else if (c < turn.dim) turn_pair(load1(row + c - half), x[i], cs[c - half], unused, x[i]);
+  } else if constexpr (kKind == TurnKind::kInterleaved) {
+    if (16 * item < turn.dim) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) turn_pair(x[2 * i], x[2 * i + 1], cs[i], x[2 * i], x[2 * i + 1]);
+    }
+  } else if constexpr (kKind == TurnKind::kOdd) {
+    float unused;
+    const int half = turn.dim / 2;
+    for (int i = 0; i < 16; ++i) {
+      const int c = 16 * item + i;
+      if (c >= turn.dim) break;
+      if (turn.interleaved) {
+        if (c % 2 == 0) turn_pair(x[i], x[i + 1], table_row[c / 2], x[i], x[i + 1]);
+      } else if (c < half) {
+        turn_pair(x[i], load1(row + c + half), table_row[c], x[i], unused);
+      } else {
+        turn_pair(load1(row + c - half), x[i], table_row[c - half], unused, x[i]);
+      }
+    }
   }
 }
 
@@ -57,95 +66,258 @@ __device__ inline void unpack4(uint32_t w, float* f) {
   f[3] = static_cast<float>(static_cast<int32_t>(w) >> 24);
 }
 
-// One workgroup per page that new rows touch, KV head and branch.  The page's new rows (at most
-// kSteps x 8 channels a thread) stay in registers between the maximum and the quantisation, so every
-// row is read once.
-template <typename T, int kDim, int kSteps>
-__global__ __launch_bounds__(256) void cache_append_kernel(CacheAppendParams p, int64_t units) {
-  constexpr int kChunks = kDim / 8, kRows = 256 / kChunks;
-  __shared__ LocateLds lds;
-  __shared__ float wave_top[4];
-  const int tid = threadIdx.x, chunk = tid % kChunks;
+// Sixteen channels of a row as they lie in memory, to be turned and quantised later.
+template <typename T> struct RawItem;
+template <> struct RawItem<uint16_t> {
+  uint4 a, b;
+  __device__ void load(const uint16_t* row, int2 c, bool wide) {
+    if (wide) {
+      a = *reinterpret_cast<const uint4*>(row + c.x);
+      b = *reinterpret_cast<const uint4*>(row + c.y);
+    } else {
+      uint32_t w[8];
+      for (int i = 0; i < 8; ++i) {
+        const uint16_t* p = row + (i < 4 ? c.x + 2 * i : c.y + 2 * (i - 4));
+        w[i] = p[0] | static_cast<uint32_t>(p[1]) << 16;
+      }
+      a = make_uint4(w[0], w[1], w[2], w[3]);
+      b = make_uint4(w[4], w[5], w[6], w[7]);
+    }
+  }
+  __device__ void get(float (&x)[16]) const {
+    unpack8(a, x);
+    unpack8(b, x + 8);
+  }
+};
+template <> struct RawItem<float> {
+  float x[16];
+  __device__ void load(const float* row, int2 c, bool wide) {
+    load8(row + c.x, wide, x);
+    load8(row + c.y, wide, x + 8);
+  }
+  __device__ void get(float (&y)[16]) const {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) y[i] = x[i];
+  }
+};
+
+// The new rows of one page that a workgroup appends, [lo, hi) of its slots.
+struct PageRows {
+  Located at;
+  int64_t base;  // position of the page's first slot
+  int lo, hi;
+  int page;      // -1: a hole
+};
+template <int kThreads>
+__device__ inline bool page_rows(const CacheAppendParams& p, int64_t index, LocateLds& lds, int tid, PageRows& r) {
   const int lg = p.cache.page_log2;
-  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    const int kv = static_cast<int>(unit & 1);
-    const int h = static_cast<int>((unit >> 1) % p.cache.heads);
-    Located at;
-    const bool found = locate<256>(p.batch.n_seqs, (unit >> 1) / p.cache.heads, lds, tid, [&](int b) -> int64_t {
-      const Span s = span_of(p.batch, b);
-      const int64_t end = s.pos0 + s.end - s.begin;
-      return s.end > s.begin && end > 0 ? ((end - 1) >> lg) - ((s.pos0 < 0 ? 0 : s.pos0) >> lg) + 1 : 0;
-    }, at);
-    if (!found) return;
-    const Span s = span_of(p.batch, at.b);
-    const int64_t from = s.pos0 < 0 ? 0 : s.pos0;
-    const int64_t base = ((from >> lg) + at.local) << lg;  // position of the page's first slot
-    const int64_t end = s.pos0 + s.end - s.begin;
-    const int lo = static_cast<int>(from > base ? from - base : 0);
-    const int hi = static_cast<int>(end - base < p.cache.page ? end - base : p.cache.page);
-    const int page = page_of(p.cache, at.b, base);
-    if (page < 0) continue;
-    const Rows& rows = p.rows[kv];
-    const T* src = reinterpret_cast<const T*>(rows.data) + h * rows.head;
-    int8_t* dst = (kv ? p.cache.v : p.cache.k) + page_at(p.cache, page, h, kDim);
-    float* scale_at = (kv ? p.cache.v_scale : p.cache.k_scale) + static_cast<int64_t>(page) * p.cache.heads + h;
-    Turn turn = p.turn;
-    if (kv) turn.table = nullptr;
-    float x[kSteps][8];
+  if (!locate<kThreads>(p.batch, index, lds, tid, [&](const Span& s) -> int64_t {
+        const int64_t end = s.pos0 + s.end - s.begin;
+        return s.end > s.begin && end > 0 ? ((end - 1) >> lg) - ((s.pos0 < 0 ? 0 : s.pos0) >> lg) + 1 : 0;
+      }, r.at))
+    return false;
+  const Span& s = r.at.span;
+  const int64_t from = s.pos0 < 0 ? 0 : s.pos0, end = s.pos0 + s.end - s.begin;
+  r.base = ((from >> lg) + r.at.local) << lg;
+  r.lo = static_cast<int>(from > r.base ? from - r.base : 0);
+  r.hi = static_cast<int>(end - r.base < p.cache.page ? end - r.base : p.cache.page);
+  r.page = page_of(p.cache, r.at.b, r.base);
+  return true;
+}
+// Table row of a position (at or past the table's end: its last).
+__device__ inline const float2* table_row(const Turn& turn, int64_t pos) {
+  return turn.table + (pos >= turn.max_pos ? turn.max_pos - 1 : pos) * (turn.dim / 2);
+}
+template <TurnKind kKind>
+__device__ inline void load_pairs(const Turn& turn, int64_t pos, int item, float2 (&cs)[8]) {
+  if constexpr (kKind == TurnKind::kHalf || kKind == TurnKind::kInterleaved) {
+    if (16 * item >= turn.dim) return;
+    const float4* src = reinterpret_cast<const float4*>(table_row(turn, pos) + 8 * item);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float4 w = src[j];
+      cs[2 * j] = make_float2(w.x, w.y);
+      cs[2 * j + 1] = make_float2(w.z, w.w);
+    }
+  }
+}
+// The largest magnitude of 16 values with the largest so far; NaN once one is not finite.
+__device__ inline float top_of(const float (&x)[16], float top) {
+  bool finite = true;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    top = fmaxf(top, fabsf(x[j]));
+    finite = finite && fabsf(x[j]) <= 3.40282347e38f;
+  }
+  return finite ? top : __builtin_nanf("");
+}
+__device__ inline float larger_or_nan(float a, float b) { return a > b || a != a ? a : b; }
+__device__ inline float wave_top_of(float top) {
+  const bool finite = __all(top == top);
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  return finite ? top : __builtin_nanf("");
+}
+// Scale of a page and head that had `held` (0: none) and takes values up to `top`.
+__device__ inline float scale_with(float held, float top) {
+  const float scale = larger_or_nan(top * (1.f / 127.f), held);
+  return scale < kSmallestScale ? 0.f : scale;
+}
+__device__ inline void requantise(int8_t* at, float ratio) {
+  uint4* w = reinterpret_cast<uint4*>(at);
+  const uint4 v = *w;
+  float f[16];
+  unpack4(v.x, f);
+  unpack4(v.y, f + 4);
+  unpack4(v.z, f + 8);
+  unpack4(v.w, f + 12);
+#pragma unroll
+  for (int j = 0; j < 16; ++j) f[j] *= ratio;
+  *w = make_uint4(pack4(f), pack4(f + 4), pack4(f + 8), pack4(f + 12));
+}
+template <TurnKind kKind>
+__device__ inline void store_item(int8_t* row, int2 at, float (&x)[16], float inv) {
+#pragma unroll
+  for (int j = 0; j < 16; ++j) x[j] *= inv;
+  const uint4 v = make_uint4(pack4(x), pack4(x + 4), pack4(x + 8), pack4(x + 12));
+  if (kKind == TurnKind::kHalf) {
+    *reinterpret_cast<uint2*>(row + at.x) = make_uint2(v.x, v.y);
+    *reinterpret_cast<uint2*>(row + at.y) = make_uint2(v.z, v.w);
+  } else {
+    *reinterpret_cast<uint4*>(row + at.x) = v;
+  }
+}
+
+// Many rows: a workgroup takes one branch (keys or values) of one page, one item of 16 channels a thread, and
+// heads_per of its heads one after another.  A head's rows stay in registers between the maximum and the
+// quantisation, the next head's are on their way meanwhile, and a thread's cosines and sines serve all heads.
+// Bound by HBM: rows are read once, in the model's type, and written once, in 8 bits.
+template <typename T, int kDim, int kThreads, TurnKind kKind>
+__device__ inline void append_page(const CacheAppendParams& p, int kv, int first_head, int last_head,
+                                   const PageRows& r, float (*wave_top)[kThreads / 64], int tid) {
+  constexpr int kItems = kDim / 16;
+  const int item = tid % kItems, slot = tid / kItems;
+  const Rows& rows = p.rows[kv];
+  const T* row = reinterpret_cast<const T*>(rows.data) + (r.at.span.begin + r.base + slot - r.at.span.pos0) * rows.token;
+  int8_t* pages = kv ? p.cache.v : p.cache.k;
+  float* scales = (kv ? p.cache.v_scale : p.cache.k_scale) + static_cast<int64_t>(r.page) * p.cache.heads;
+  const int2 at = item_channels<kKind>(p.turn, item);
+  const bool mine = slot >= r.lo && slot < r.hi;
+  RawItem<T> raw;
+  float2 cs[8];
+  if (mine) {
+    raw.load(row + first_head * rows.head, at, rows.wide);
+    load_pairs<kKind>(p.turn, r.base + slot, item, cs);
+  }
+  float old = r.lo > 0 ? scales[first_head] : 0.f;
+  for (int h = first_head; h < last_head; ++h) {
+    float x[16];
     float top = 0.f;
-    bool finite = true;
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-      const int slot = i * kRows + tid / kChunks;
-      if (slot >= lo && slot < hi) {
-        const int64_t pos = base + slot;
-        turned8(turn, src + (s.begin + pos - s.pos0) * rows.token, rows.wide, chunk, pos, x[i]);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          top = fmaxf(top, fabsf(x[i][j]));
-          finite = finite && fabsf(x[i][j]) <= 3.40282347e38f;
-        }
-      }
+    if (mine) {
+      raw.get(x);
+      turn_item<kKind>(p.turn, row, item, cs, nullptr, x);
+      top = top_of(x, top);
     }
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    finite = __all(finite);
-    if ((tid & 63) == 0) wave_top[tid >> 6] = finite ? top : __builtin_nanf("");
-    const float old = lo > 0 ? *scale_at : 0.f;
-    __syncthreads();
-    float scale = old;
-    for (int w = 0; w < 4; ++w) {
-      const float a = wave_top[w] * (1.f / 127.f);
-      scale = a > scale || a != a ? a : scale;
+    const float held = old;
+    if (h + 1 < last_head) {
+      if (mine) raw.load(row + (h + 1) * rows.head, at, rows.wide);
+      old = r.lo > 0 ? scales[h + 1] : 0.f;
     }
-    if (scale < kSmallestScale) scale = 0.f;
+    top = wave_top_of(top);
+    float* tops = wave_top[h & 1];
+    if ((tid & 63) == 0) tops[tid >> 6] = top;
+    lds_barrier();  // the loads on their way stay so
+    float all = tops[0];
+#pragma unroll
+    for (int w = 1; w < kThreads / 64; ++w) all = larger_or_nan(tops[w], all);
+    const float scale = scale_with(held, all);
     const float inv = scale > 0.f ? 1.f / scale : 0.f;
-    if (tid == 0) *scale_at = scale;
-    if (scale > old && lo > 0) {  // earlier rows to the new scale
-      const float ratio = old * inv;
-#pragma unroll
-      for (int i = 0; i < kSteps; ++i) {
-        const int slot = i * kRows + tid / kChunks;
-        if (slot < lo) {
-          uint2* w = reinterpret_cast<uint2*>(dst + slot * kDim + 8 * chunk);
-          uint2 v = *w;
-          float f[8];
-          unpack4(v.x, f);
-          unpack4(v.y, f + 4);
-          for (int j = 0; j < 8; ++j) f[j] *= ratio;
-          *w = make_uint2(pack4(f), pack4(f + 4));
-        }
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i) {
-      const int slot = i * kRows + tid / kChunks;
-      if (slot >= lo && slot < hi) {
-        float f[8];
-        for (int j = 0; j < 8; ++j) f[j] = x[i][j] * inv;
-        *reinterpret_cast<uint2*>(dst + slot * kDim + 8 * chunk) = make_uint2(pack4(f), pack4(f + 4));
-      }
-    }
+    if (tid == 0) scales[h] = scale;
+    int8_t* dst = pages + page_at(p.cache, r.page, h, kDim) + slot * kDim;
+    if (mine) store_item<kKind>(dst, at, x, inv);
+    else if (slot < r.lo && scale > held) requantise(dst + 16 * item, held * inv);
+  }
+}
+
+template <typename T, int kDim, int kThreads, TurnKind kKind>
+__global__ __launch_bounds__(kThreads) void cache_append_pages_kernel(CacheAppendParams p, int heads_per, int shares,
+                                                                     int64_t units) {
+  __shared__ LocateLds lds;
+  __shared__ float wave_top[2][kThreads / 64];
+  const int tid = threadIdx.x;
+  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const int64_t rest = unit >> 1;
+    const int kv = static_cast<int>(unit & 1);
+    const int first_head = static_cast<int>(rest % shares) * heads_per;
+    const int last_head = first_head + heads_per < p.cache.heads ? first_head + heads_per : p.cache.heads;
+    PageRows r;
+    if (!page_rows<kThreads>(p, rest / shares, lds, tid, r)) return;
+    if (r.page < 0) continue;
+    if (kv) append_page<T, kDim, kThreads, TurnKind::kNone>(p, kv, first_head, last_head, r, wave_top, tid);
+    else append_page<T, kDim, kThreads, kKind>(p, kv, first_head, last_head, r, wave_top, tid);
     __syncthreads();  // wave_top is written again
+  }
+}
+
+// A few rows of a page (and any number where rotary_dim is odd in 16s): a wave takes one branch of one page and
+// head, 64 items at a time, first for the maximum and then for the quantisation, the first 64 read once.
+template <typename T, int kDim, TurnKind kKind>
+__device__ inline void append_few(const CacheAppendParams& p, int kv, int h, const PageRows& r, int lane) {
+  constexpr int kItems = kDim / 16;
+  const Rows& rows = p.rows[kv];
+  const T* src = reinterpret_cast<const T*>(rows.data) + (r.at.span.begin + r.base - r.at.span.pos0) * rows.token + h * rows.head;
+  float* scale_at = (kv ? p.cache.v_scale : p.cache.k_scale) + static_cast<int64_t>(r.page) * p.cache.heads + h;
+  int8_t* dst = (kv ? p.cache.v : p.cache.k) + page_at(p.cache, r.page, h, kDim);
+  const int first = r.lo * kItems, last = r.hi * kItems;
+  const int item = lane % kItems;  // 64 is a multiple of kItems
+  const int2 at = item_channels<kKind>(p.turn, item);
+  const auto fetch = [&](int i, float (&x)[16]) {
+    const int slot = i / kItems;
+    const T* row = src + slot * rows.token;
+    RawItem<T> raw;
+    float2 cs[8];
+    raw.load(row, at, rows.wide);
+    load_pairs<kKind>(p.turn, r.base + slot, item, cs);
+    raw.get(x);
+    turn_item<kKind>(p.turn, row, item, cs, kKind == TurnKind::kOdd ? table_row(p.turn, r.base + slot) : nullptr, x);
+  };
+  const float held = r.lo > 0 ? *scale_at : 0.f;
+  float x[16];
+  float top = 0.f;
+  if (first + lane < last) {
+    fetch(first + lane, x);
+    top = top_of(x, top);
+  }
+  for (int i = first + 64 + lane; i < last; i += 64) {
+    float y[16];
+    fetch(i, y);
+    top = larger_or_nan(top_of(y, 0.f), top);
+  }
+  top = wave_top_of(top);
+  const float scale = scale_with(held, top);
+  const float inv = scale > 0.f ? 1.f / scale : 0.f;
+  if (lane == 0) *scale_at = scale;
+  if (first + lane < last) store_item<kKind>(dst + (first + lane) / kItems * kDim, at, x, inv);
+  for (int i = first + 64 + lane; i < last; i += 64) {
+    fetch(i, x);
+    store_item<kKind>(dst + i / kItems * kDim, at, x, inv);
+  }
+  if (scale > held)
+    for (int i = lane; i < first; i += 64) requantise(dst + i * 16, held * inv);
+}
+
+template <typename T, int kDim, TurnKind kKind>
+__global__ __launch_bounds__(256) void cache_append_few_kernel(CacheAppendParams p, int shares, int64_t units) {
+  __shared__ LocateLds lds;
+  const int tid = threadIdx.x;
+  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    // four of the 2 n_kv_heads (branch, head) pairs a workgroup, keys first
+    const int pair = static_cast<int>(unit % shares) * 4 + __builtin_amdgcn_readfirstlane(tid >> 6);
+    PageRows r;
+    if (!page_rows<256>(p, unit / shares, lds, tid, r)) return;
+    if (r.page < 0 || pair >= 2 * p.cache.heads) continue;
+    const int kv = pair >= p.cache.heads;
+    if (kv) append_few<T, kDim, TurnKind::kNone>(p, kv, pair - p.cache.heads, r, tid & 63);
+    else append_few<T, kDim, kKind>(p, kv, pair, r, tid & 63);
   }
 }
 
@@ -156,10 +328,9 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheReadParams p) {
   const int lane = threadIdx.x & 63;
   for (int64_t t = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6); t < p.batch.n_tokens;
        t += static_cast<int64_t>(gridDim.x) * 4) {
-    const int b = request_of(p.batch, t, lane);
-    const Span s = span_of(p.batch, b);
-    const int64_t pos = t - s.begin + s.pos0;
-    const int page = page_of(p.cache, b, pos);
+    const Owner owner = owner_of(p.batch, t, lane);
+    const int64_t pos = t - owner.begin + owner.pos0;
+    const int page = page_of(p.cache, owner.b, pos);
     for (int idx = lane; idx < 2 * p.cache.heads * kChunks; idx += 64) {
       const int kv = idx >= p.cache.heads * kChunks;
       const int h = idx / kChunks - (kv ? p.cache.heads : 0), chunk = idx % kChunks;
@@ -185,21 +356,55 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheReadParams p) {
   }
 }
 
+// Pages that a batch touches, at most: a request's n rows lie in at most (n - 2) / page + 2 of them.
+static int64_t pages_bound(const SeqBatch& b, int page) {
+  const int64_t requests = b.n_seqs < b.n_tokens ? b.n_seqs : b.n_tokens;
+  const int64_t bound = b.n_tokens / page + 2 * requests;
+  return bound < b.n_tokens ? bound : b.n_tokens;
+}
+static dim3 grid_of(int64_t units) { return dim3(static_cast<unsigned>(units < kMaxGrid / 4 ? units : kMaxGrid / 4)); }
+
+template <typename T, int kDim, TurnKind kKind>
+static hipError_t launch_append_few(const CacheAppendParams& p, hipStream_t stream) {
+  const int shares = (2 * p.cache.heads + 3) / 4;
+  const int64_t units = pages_bound(p.batch, p.cache.page) * shares;
+  hipLaunchKernelGGL((cache_append_few_kernel<T, kDim, kKind>), grid_of(units), dim3(256), 0, stream, p, shares, units);
+  return hipGetLastError();
+}
+
+template <typename T, int kDim, int kPage, TurnKind kKind>
+static hipError_t launch_append_pages(const CacheAppendParams& p, hipStream_t stream) {
+  constexpr int kThreads = kPage * kDim / 16 < 64 ? 64 : kPage * kDim / 16;
+  const int64_t pages = pages_bound(p.batch, kPage);
+  // As many heads to a workgroup as leave 1024 workgroups.
+  const int64_t most = pages * 2 * p.cache.heads / 1024;
+  const int heads_per = static_cast<int>(most < 1 ? 1 : (most < p.cache.heads ? most : p.cache.heads));
+  const int shares = (p.cache.heads + heads_per - 1) / heads_per;
+  const int64_t units = pages * shares * 2;
+  hipLaunchKernelGGL((cache_append_pages_kernel<T, kDim, kThreads, kKind>), grid_of(units), dim3(kThreads), 0, stream, p,
+                     heads_per, shares, units);
+  return hipGetLastError();
+}
+
+template <typename T, int kDim, TurnKind kKind>
+static hipError_t launch_append_kind(const CacheAppendParams& p, hipStream_t stream) {
+  const int64_t requests = p.batch.n_seqs < p.batch.n_tokens ? p.batch.n_seqs : p.batch.n_tokens;
+  if (kKind == TurnKind::kOdd || p.batch.n_tokens < 8 * requests) return launch_append_few<T, kDim, kKind>(p, stream);
+  if constexpr (kKind != TurnKind::kOdd) {
+    if (p.cache.page == 16) return launch_append_pages<T, kDim, 16, kKind>(p, stream);
+    if (p.cache.page == 32) return launch_append_pages<T, kDim, 32, kKind>(p, stream);
+    if (p.cache.page == 64) return launch_append_pages<T, kDim, 64, kKind>(p, stream);
+    return launch_append_pages<T, kDim, 128, kKind>(p, stream);
+  }
+  return hipSuccess;
+}
+
 template <typename T, int kDim>
 static hipError_t launch_append_as(const CacheAppendParams& p, hipStream_t stream) {
-  // Pages touched: a request's n rows lie in at most (n - 2) / page + 2 of them.
-  const int64_t n = p.batch.n_tokens, requests = p.batch.n_seqs < n ? p.batch.n_seqs : n;
-  const int64_t pages = n / p.cache.page + 2 * requests;
-  const int64_t units = (pages < n ? pages : n) * p.cache.heads * 2;
-  const dim3 grid(static_cast<unsigned>(units < kMaxGrid ? units : kMaxGrid)), block(256);
-  const int steps = p.cache.page * kDim / 2048;
-  switch (steps <= 1 ? 1 : steps) {
-    case 1: hipLaunchKernelGGL((cache_append_kernel<T, kDim, 1>), grid, block, 0, stream, p, units); break;
-    case 2: hipLaunchKernelGGL((cache_append_kernel<T, kDim, 2>), grid, block, 0, stream, p, units); break;
-    case 4: hipLaunchKernelGGL((cache_append_kernel<T, kDim, 4>), grid, block, 0, stream, p, units); break;
-    default: hipLaunchKernelGGL((cache_append_kernel<T, kDim, 8>), grid, block, 0, stream, p, units); break;
-  }
-  return hipGetLastError();
+  if (p.turn.table == nullptr) return launch_append_kind<T, kDim, TurnKind::kNone>(p, stream);
+  if (p.turn.dim % 16 != 0) return launch_append_kind<T, kDim, TurnKind::kOdd>(p, stream);
+  return p.turn.interleaved ? launch_append_kind<T, kDim, TurnKind::kInterleaved>(p, stream)
+                            : launch_append_kind<T, kDim, TurnKind::kHalf>(p, stream);
 }
 
 hipError_t launch_cache_append(bool bf16, int head_dim, const CacheAppendParams& p,

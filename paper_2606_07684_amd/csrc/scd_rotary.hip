@@ -31,9 +31,8 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryParams p, int items_p
        unit += static_cast<int64_t>(gridDim.x) * 4) {
     const int64_t t = unit / parts;
     const int idx = static_cast<int>(unit - t * parts) * 64 + lane;
-    const int b = request_of(p.batch, t, lane);
-    const Span span = span_of(p.batch, b);
-    int64_t pos = t - span.begin + span.pos0;
+    const Owner owner = owner_of(p.batch, t, lane);
+    int64_t pos = t - owner.begin + owner.pos0;
     pos = pos < 0 ? 0 : (pos >= p.turn.max_pos ? p.turn.max_pos - 1 : pos);
     if (idx >= heads * items_per_head) continue;
     int h = idx / items_per_head;

@@ -27,12 +27,17 @@ __device__ inline Span span_of(const SeqBatch& s, int b) {
   return r;
 }
 
-// Request of row t (the same for the whole wave): the last b with cu[b] <= t.  Each step reads 64
-// boundaries at once, so 64 requests take one memory access and 4096 two.
-__device__ inline int request_of(const SeqBatch& s, int64_t t, int lane) {
-  if (s.cu == nullptr || s.n_seqs == 1) return 0;
+// Request, first row and held tokens of row t (the same for the whole wave): the last b with cu[b] <= t.
+// Each step reads 64 boundaries at once, and the last one the held tokens with them, so 64 requests
+// take one memory access and 4096 two.
+struct Owner {
+  int b;
+  int64_t begin, pos0;
+};
+__device__ inline Owner owner_of(const SeqBatch& s, int64_t t, int lane) {
+  if (s.cu == nullptr) return Owner{0, 0, s.pos0 != nullptr ? s.pos0[0] : 0};
   int lo = 0, n = s.n_seqs;
-  while (n > 1) {
+  while (n > 64) {
     const int step = (n + 63) >> 6;
     const int i = lane * step;
     const bool under = i < n && (i == 0 || s.cu[lo + i] <= t);
@@ -40,7 +45,10 @@ __device__ inline int request_of(const SeqBatch& s, int64_t t, int lane) {
     lo += at;
     n = n - at < step ? n - at : step;
   }
-  return lo;
+  const int start = lane < n ? s.cu[lo + lane] : 0;
+  const int held = lane < n && s.pos0 != nullptr ? s.pos0[lo + lane] : 0;
+  const int at = __builtin_amdgcn_readfirstlane(__popcll(__ballot(lane < n && (lane == 0 || start <= t))) - 1);
+  return Owner{lo + at, __builtin_amdgcn_readlane(start, at), __builtin_amdgcn_readlane(held, at)};
 }
 
 // Page of position p of request b, or -1: out of the table, or a hole.
@@ -56,30 +64,39 @@ __device__ inline int64_t page_at(const PagedCache& c, int page, int head, int d
   return (static_cast<int64_t>(page) * c.heads + head) * (c.page * static_cast<int64_t>(d));
 }
 
-// Work units of requests one after another, count(b) of each: the request and the place in it of
-// `unit`, or false past the last.  Every thread of the workgroup calls it and gets the answer.
+// Work units of requests one after another, count(span) of each: the request and its rows, and the
+// place among its units, of `unit`; false past the last.  Every thread of the workgroup calls it and
+// gets the answer.
 struct Located {
-  int b;
+  Span span;
   int64_t local;
+  int b;
 };
 struct LocateLds {
   int64_t wave_sum[16];
-  int64_t local;
-  int b;
+  Located found;
 };
 template <int kThreads, typename Count>
-__device__ inline bool locate(int n_seqs, int64_t unit, LocateLds& lds, int tid, Count count,
+__device__ inline bool locate(const SeqBatch& s, int64_t unit, LocateLds& lds, int tid, Count count,
                               Located& out) {
+  if (s.n_seqs == 1) {
+    out.b = 0;
+    out.local = unit;
+    out.span = span_of(s, 0);
+    return unit < count(out.span);
+  }
   const int lane = tid & 63, wave = tid >> 6;
-  for (int base = 0; base < n_seqs; base += kThreads) {
-    const int64_t mine = base + tid < n_seqs ? count(base + tid) : 0;
+  for (int base = 0; base < s.n_seqs; base += kThreads) {
+    Span span{0, 0, 0};
+    if (base + tid < s.n_seqs) span = span_of(s, base + tid);
+    const int64_t mine = count(span);
     int64_t sum = mine;
     for (int o = 1; o < 64; o <<= 1) {
       const int64_t other = __shfl_up(sum, o);
       if (lane >= o) sum += other;
     }
     __syncthreads();  // the last round's readers are done
-    if (tid == 0) lds.b = -1;
+    if (tid == 0) lds.found.b = -1;
     if (lane == 63) lds.wave_sum[wave] = sum;
     __syncthreads();
     int64_t before = 0, total = 0;
@@ -88,13 +105,10 @@ __device__ inline bool locate(int n_seqs, int64_t unit, LocateLds& lds, int tid,
       total += lds.wave_sum[w];
     }
     const int64_t first = before + sum - mine;
-    if (unit >= first && unit < first + mine) {
-      lds.b = base + tid;
-      lds.local = unit - first;
-    }
+    if (unit >= first && unit < first + mine) lds.found = Located{span, unit - first, base + tid};
     __syncthreads();
-    if (lds.b >= 0) {
-      out = Located{lds.b, lds.local};
+    if (lds.found.b >= 0) {
+      out = lds.found;
       return true;
     }
     unit -= total;
