@@ -203,61 +203,67 @@ __global__ __launch_bounds__(256) void cache_attend_rows_kernel(CacheAttendParam
       for (int c = 0; c < kOut; ++c) acc[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    for (int block = begin + wave; block < end; block += 4) {
-      const int at = block << 5;
-      // the block's two halves of 16 positions lie in one page each
-      int page[2];
-      float ks[2], vs[2];
-      const int8_t *kb[2], *vb[2];
+    // Blocks are fetched one ahead of the arithmetic, their pages' numbers another one ahead.
+    const auto pages_of = [&](int block) {
+      int2 id;
+      int* const out[2] = {&id.x, &id.y};
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int pos = at + 16 * i;
-        int64_t col = pos >> p.cache.page_log2;
-        const bool inside = col < p.cache.cols;
-        col = inside ? col : 0;
-        int id = table[static_cast<int64_t>(t.b) * p.cache.cols + col];
-        page[i] = inside && id >= 0 && id < p.cache.n_pages ? id : -1;
-        id = page[i] < 0 ? 0 : id;
-        const int64_t s = static_cast<int64_t>(id) * p.cache.heads + h;
-        ks[i] = page[i] < 0 ? 0.f : k_scale[s];
-        vs[i] = page[i] < 0 ? 0.f : v_scale[s];
-        const int64_t byte = page_at(p.cache, id, h, kDim) + (pos & (p.cache.page - 1)) * kDim;
-        kb[i] = p.cache.k + byte;
-        vb[i] = p.cache.v + byte;
+        const int col = ((block << 5) + 16 * i) >> p.cache.page_log2;
+        *out[i] = col < p.cache.cols ? table[static_cast<int64_t>(t.b) * p.cache.cols + col] : -1;
       }
-      // keys: position r of each half, channels g * kDim / 4 on
+      return id;
+    };
+    struct Fetched {
       uint32_t kw[2][kDim / 16];
       uint32_t vw[kDim / 64 > 0 ? kDim / 64 : 1][8];
+      float ks[2], vs[2];
+      bool hole[2];
+    };
+    const auto fetch = [&](Fetched& f, int block, int2 ids) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int8_t* src = kb[i] + r * kDim + g * (kDim / 4);
+        int id = i == 0 ? ids.x : ids.y;
+        f.hole[i] = id < 0 || id >= p.cache.n_pages;
+        id = f.hole[i] ? 0 : id;
+        const int64_t at = static_cast<int64_t>(id) * p.cache.heads + h;
+        f.ks[i] = f.hole[i] ? 0.f : k_scale[at];
+        f.vs[i] = f.hole[i] ? 0.f : v_scale[at];
+        const int64_t byte = page_at(p.cache, id, h, kDim) + ((((block << 5) + 16 * i) & (p.cache.page - 1)) * kDim);
+        // keys: position r of the half, channels g * kDim / 4 on
+        const int8_t* src = p.cache.k + byte + (r * kDim + g * (kDim / 4));
         if constexpr (kDim >= 64) {
 #pragma unroll
           for (int c = 0; c < kDim / 64; ++c) {
             const uint4 w = *reinterpret_cast<const uint4*>(src + 16 * c);
-            kw[i][4 * c] = w.x; kw[i][4 * c + 1] = w.y; kw[i][4 * c + 2] = w.z; kw[i][4 * c + 3] = w.w;
+            f.kw[i][4 * c] = w.x; f.kw[i][4 * c + 1] = w.y; f.kw[i][4 * c + 2] = w.z; f.kw[i][4 * c + 3] = w.w;
           }
         } else {
           const uint2 w = *reinterpret_cast<const uint2*>(src);
-          kw[i][0] = w.x; kw[i][1] = w.y;
+          f.kw[i][0] = w.x; f.kw[i][1] = w.y;
         }
-      }
-      // values: channels kOut * r on, of positions 4g + j of each half
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
+        // values: channels kOut * r on, of positions 4g + j of the half
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const int8_t* src = vb[i] + (4 * g + j) * kDim + kOut * r;
+          src = p.cache.v + byte + ((4 * g + j) * kDim + kOut * r);
           if constexpr (kDim == 128) {
             const uint2 w = *reinterpret_cast<const uint2*>(src);
-            vw[0][4 * i + j] = w.x;
-            vw[1][4 * i + j] = w.y;
+            f.vw[0][4 * i + j] = w.x;
+            f.vw[1][4 * i + j] = w.y;
           } else if constexpr (kDim == 64) {
-            vw[0][4 * i + j] = *reinterpret_cast<const uint32_t*>(src);
+            f.vw[0][4 * i + j] = *reinterpret_cast<const uint32_t*>(src);
           } else {
-            vw[0][4 * i + j] = *reinterpret_cast<const uint16_t*>(src);
+            f.vw[0][4 * i + j] = *reinterpret_cast<const uint16_t*>(src);
           }
         }
+      }
+    };
+    const auto attend = [&](const Fetched& fetched, int block) {
+      const int at = block << 5;
+      const auto& kw = fetched.kw;
+      const auto& vw = fetched.vw;
+      const float (&ks)[2] = fetched.ks;
+      const float (&vs)[2] = fetched.vs;
       // scores
       f32x4 score[kBlocks][2];
 #pragma unroll
@@ -283,7 +289,7 @@ __global__ __launch_bounds__(256) void cache_attend_rows_kernel(CacheAttendParam
         part_scale[i] = vs[i] * back[i];
         exponent[i] = static_cast<float>(e - 127);
       }
-      const bool masked = at + 32 > free_until || page[0] < 0 || page[1] < 0;
+      const bool masked = at + 32 > free_until || fetched.hole[0] || fetched.hole[1];
       bf16x8 w[kBlocks][kWeights];
 #pragma unroll
       for (int n = 0; n < kBlocks; ++n) {
@@ -295,7 +301,7 @@ __global__ __launch_bounds__(256) void cache_attend_rows_kernel(CacheAttendParam
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             x[4 * i + j] = fmaf(score[n][i][j], f, exponent[i]);
-            hidden[4 * i + j] = masked && (page[i] < 0 || at + 16 * i + 4 * g + j > limit[n]);
+            hidden[4 * i + j] = masked && (fetched.hole[i] || at + 16 * i + 4 * g + j > limit[n]);
             if (hidden[4 * i + j]) x[4 * i + j] = -INFINITY;
           }
         }
@@ -344,6 +350,28 @@ __global__ __launch_bounds__(256) void cache_attend_rows_kernel(CacheAttendParam
         out(IntC<1>{}, 1);
         out(IntC<2>{}, 1);
         out(IntC<3>{}, 1);
+      }
+    };
+    int block = begin + wave;
+    if (block < end) {
+      Fetched now, next;
+      fetch(now, block, pages_of(block));
+      int2 ids = pages_of(block + 4);
+      while (true) {
+        if (block + 4 < end) {
+          fetch(next, block + 4, ids);
+          ids = pages_of(block + 8);
+        }
+        attend(now, block);
+        block += 4;
+        if (block >= end) break;
+        if (block + 4 < end) {
+          fetch(now, block + 4, ids);
+          ids = pages_of(block + 8);
+        }
+        attend(next, block);
+        block += 4;
+        if (block >= end) break;
       }
     }
 
