@@ -449,10 +449,13 @@ scd_status_t scd_cache_read(const scd_cache_t* cache, const scd_batch_t* batch, 
  * One token per request and whole prompts are the same call.  Sums, the running maximum and the
  * softmax are fp32.  A row with no position to attend to (a hole at every one) is zero.
  * q [n_tokens, n_heads, head_dim], n_heads a multiple of n_kv_heads; out alike, not overlapping q.
- * `workspace` (device, 16-byte aligned, caller-owned, contents undefined on entry and exit) holds
- * scd_cache_attend_workspace_bytes(cache, batch, q.n_heads) bytes; when that is 0 it may be NULL.
- * The size depends on n_tokens, n_seqs, max_pages and the heads, not on device contents, so a
+ * `workspace` (device, 16-byte aligned, caller-owned) holds
+ * scd_cache_attend_workspace_bytes(cache, batch, q.n_heads) bytes; when that is 0 it may be NULL.  Its
+ * first SCD_ATTEND_COUNTER_BYTES (or all of it, if less) must be zero before its first use; every call
+ * leaves them zero, so one buffer serves calls of any shapes one after another, and the rest may hold
+ * anything.  The size depends on n_tokens, n_seqs, max_pages and the heads, not on device contents, so a
  * captured call can be replayed while lengths grow.  Calls that may overlap need one each. */
+#define SCD_ATTEND_COUNTER_BYTES 2048
 size_t scd_cache_attend_workspace_bytes(const scd_cache_t* cache, const scd_batch_t* batch,
                                         int32_t n_q_heads);
 scd_status_t scd_cache_attend(const scd_cache_t* cache, const scd_batch_t* batch, int32_t dtype,

@@ -19,7 +19,7 @@ ARCH = "gfx950"
 
 SOURCES = ["scd_gemm.hip", "scd_patch.hip", "scd_decode.hip", "scd_encode.hip", "scd_fit.hip",
            "scd_fold.hip", "scd_api.cpp", "scd_rotary.hip", "scd_paged.hip", "scd_attend.hip",
-           "scd_serve_api.cpp"]
+           "scd_attend_rows.hip", "scd_attend_prompt.hip", "scd_serve_api.cpp"]
 
 FLAGS = [
     f"--offload-arch={ARCH}",

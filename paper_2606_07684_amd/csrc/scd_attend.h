@@ -1,0 +1,122 @@
+// Causal attention of new tokens over the paged 8-bit cache (gfx950): what its two kernels share.
+//
+// out = sum_j p_j v_j with p the softmax over the cached positions of scale * (q . k_j), in one pass
+// with a running maximum and sum: when the maximum grows from m to m', what is summed so far is
+// multiplied by e^(m - m').  Both products run on the matrix cores with fp32 accumulation:
+//  - cached values are whole numbers of at most 127, exact in fp16 and bf16; a page's key scale
+//    multiplies the scores, its value scale the weights, so no value is scaled one by one.
+//  - scores in fp16: a query row is multiplied by the power of two that brings its largest element to
+//    2^14 (its scores by the inverse).  bf16 rows are then exact down to 2^-28 of that element; fp32
+//    rows are split into two parts (22 bits and their sign).
+//  - sums over values in bf16, the weights split into two parts for bf16 output (16 bits; its own
+//    rounding has 8) and three for fp32: the parts keep the whole exponent range, so a channel in
+//    which the heaviest positions are zero still has its bits.
+//  - a value scale is f 2^e with f in [1, 2).  The running maximum is that of log2 of the weight plus
+//    e, what a position can add to the sum; the softmax's own sum takes the weights times 2^-e.
+#pragma once
+
+#include "scd_serve_device.h"
+
+namespace scd {
+namespace dev {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef const __attribute__((address_space(4))) int32_t* uniform_ints_t;
+typedef const __attribute__((address_space(4))) float* uniform_floats_t;
+
+constexpr float kLog2e = 1.44269504f;
+constexpr int kLift = 14;  // the largest element of a query row is brought to 2^kLift
+constexpr int kLeastExponent = -90;  // of a value scale: 2^90 times 2^31 positions fits the sum
+
+__device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+// The larger of x and the other half-wave's x.
+__device__ inline float max_of_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+// The largest of x over the lanes of the same place in every 16.
+__device__ inline float max_of_quarters(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return max_of_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ inline f32x4 mfma16(const f16x8& a, const f16x8& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
+__device__ inline f32x4 mfma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// Two bytes (sign bit flipped: value + 128) with 0x64 above each are the halves 1152 + value; less
+// 1152 they are the values.
+__device__ inline uint32_t halves(uint32_t biased) {
+  const f16x2 offset = {static_cast<_Float16>(-1152.f), static_cast<_Float16>(-1152.f)};
+  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, biased) + offset);
+}
+// Eight adjacent bytes as fp16.
+__device__ inline f16x8 bytes_as_f16(uint32_t a, uint32_t b) {
+  a ^= 0x80808080u;
+  b ^= 0x80808080u;
+  u32x4 w;
+  w[0] = halves(__builtin_amdgcn_perm(0x64646464u, a, 0x04010400u));
+  w[1] = halves(__builtin_amdgcn_perm(0x64646464u, a, 0x04030402u));
+  w[2] = halves(__builtin_amdgcn_perm(0x64646464u, b, 0x04010400u));
+  w[3] = halves(__builtin_amdgcn_perm(0x64646464u, b, 0x04030402u));
+  return __builtin_bit_cast(f16x8, w);
+}
+// Byte kByte of eight words as bf16: fp32 of a byte is exact in its upper half.
+template <int kByte> __device__ inline float byte_as_f32(uint32_t w) {
+  return static_cast<float>(static_cast<int8_t>(w >> (8 * kByte)));
+}
+template <int kByte> __device__ inline bf16x8 byte_column_as_bf16(const uint32_t (&w)[8]) {
+  u32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    r[i] = __builtin_amdgcn_perm(__float_as_uint(byte_as_f32<kByte>(w[2 * i + 1])),
+                                 __float_as_uint(byte_as_f32<kByte>(w[2 * i])), 0x07060302u);
+  return __builtin_bit_cast(bf16x8, r);
+}
+
+// Positions the page table can name (cut off where positions would pass 31 bits).
+__device__ inline int64_t positions_held(const PagedCache& c) {
+  const int64_t n = static_cast<int64_t>(c.cols) << c.page_log2, most = (int64_t{1} << 31) - 64;
+  return n < most ? n : most;
+}
+
+// Query rows of a request and KV head: row i is head h * group + i % group of its token i / group.  A call
+// has less than 2^31 of them in all.
+struct Request {
+  int begin, end;  // packed rows of its tokens
+  int pos0;
+};
+__device__ inline Request request_at(const SeqBatch& s, int b) {
+  const Span span = span_of(s, b);
+  return Request{static_cast<int>(span.begin), static_cast<int>(span.end), static_cast<int>(span.pos0)};
+}
+// Blocks of 32 positions up to the one of the request's token `token`.
+__device__ inline int blocks_to(int64_t held, int pos0, int token) {
+  const int64_t seen = static_cast<int64_t>(pos0) + token + 1;
+  return static_cast<int>(((seen < 0 ? 0 : (seen < held ? seen : held)) + 31) >> 5);
+}
+// Last position a token attends to, as far as it can be held.
+__device__ inline int reach_of(int64_t held, int pos0, int token) {
+  const int64_t pos = static_cast<int64_t>(pos0) + token;
+  return static_cast<int>(pos < -1 ? -1 : (pos < held ? pos : held));
+}
+
+}  // namespace dev
+
+// Workspace: a count for each workgroup of a launch (0 between calls), then partial sums.
+constexpr int kRowsWorkers = 512;
+constexpr size_t kCounterBytes = kRowsWorkers * sizeof(int);
+
+// Workgroups for a few rows of a request (tiles of 16, 32 or 64 rows): waves of one, and most of a launch.
+__host__ __device__ constexpr int rows_waves(int rows) { return rows == 16 ? 8 : 4; }
+constexpr int rows_workers(int rows) { return rows == 16 ? kRowsWorkers / 2 : kRowsWorkers; }
+constexpr int kUncutSteps = 4;    // mean steps of a segment up to which it stays whole
+
+constexpr int kPromptWaves = 8, kPromptRows = 32 * kPromptWaves;
+
+}  // namespace scd

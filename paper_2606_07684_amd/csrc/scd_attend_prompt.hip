@@ -1,0 +1,423 @@
+// Attention of whole prompts over the paged 8-bit cache (gfx950).
+#include "scd_attend.h"
+
+namespace scd {
+using namespace dev;
+
+// Rows of one tile: query rows (token, head of the group) of one request and KV head.
+struct Tile {
+  int b;
+  int64_t row0;      // first row, in the request
+  int rows;          // rows of the tile that exist
+  int64_t first;     // packed row of the request's first token
+  int64_t pos0;
+};
+
+template <int kRows>
+__device__ inline void set_tile(const CacheAttendParams& p, const Span& span, int b, int64_t index, Tile& t) {
+  t.b = b;
+  t.row0 = index * kRows;
+  const int64_t left = (span.end - span.begin) * p.group - t.row0;
+  t.rows = static_cast<int>(left < kRows ? left : kRows);
+  t.first = span.begin;
+  t.pos0 = span.pos0;
+}
+// Tiles of kRows rows of all requests, one after another.
+template <int kRows>
+__device__ inline int64_t tiles_in(const CacheAttendParams& p, const Span& s) {
+  return ((s.end - s.begin) * p.group + kRows - 1) / kRows;
+}
+template <int kRows, int kThreads>
+__device__ inline bool tile_of(const CacheAttendParams& p, int64_t index, LocateLds& lds, int tid, Tile& t) {
+  Located at;
+  if (!locate<kThreads>(p.batch, index, lds, tid, [&](const Span& s) { return tiles_in<kRows>(p, s); }, at))
+    return false;
+  set_tile<kRows>(p, at.span, at.b, at.local, t);
+  return true;
+}
+// Splits of a tile that has `blocks` blocks of 32 positions, when a launch has up to `most`: at least
+// two blocks for each of a workgroup's four waves.
+__device__ inline int splits_of(int64_t blocks, int most) {
+  const int64_t n = (blocks + 7) / 8;
+  return static_cast<int>(n < 1 ? 1 : (n < most ? n : most));
+}
+
+// One workgroup per tile of 32 kWaves query rows, KV head and share of the positions.  64 positions at
+// a time are converted to fp16 once, into LDS (keys as rows, values transposed), and every wave takes
+// them for its 32 rows: scores^T [64 x 32] = K Q^T, then out^T [d x 32] += V^T P^T on 32 x 32 x 16
+// matrix steps, the weights going from the one to the other in registers.  Weights are one fp16 part
+// of 11 bits (2^kPromptLift is the largest; below 2^-24 of that they lose bits), and the softmax's sum
+// takes them as rounded, so their rounding has no bias.
+constexpr int kPromptLift = 11;   // the running maximum may lag by kPromptSlack: 2^15 fits fp16
+constexpr float kPromptSlack = 4.f;
+constexpr int kPromptTokens = 64;
+constexpr int kListed = 1024;     // groups of 16 positions whose pages and scales are held in LDS
+
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+
+__device__ inline f32x16 mfma32(const f16x8& a, const f16x8& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+// Byte kByte of four words as fp16.
+template <int kByte> __device__ inline uint2 byte_column_as_f16(const uint32_t (&w)[4]) {
+  constexpr uint32_t sel = 0x0c000c04u + 0x00010001u * kByte;  // bytes: kByte of the first, 0, of the second, 0
+  return make_uint2(halves(__builtin_amdgcn_perm(w[0], w[1], sel) ^ 0x64806480u),
+                    halves(__builtin_amdgcn_perm(w[2], w[3], sel) ^ 0x64806480u));
+}
+template <int kDim, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(CacheAttendParams p, int most_splits,
+                                                                            int64_t units, float* partial,
+                                                                            float* partial_ml) {
+  typedef uint16_t T;
+  constexpr int kRows = 32 * kWaves, kThreads = 64 * kWaves;
+  constexpr int kSteps = kDim / 16, kOut = kDim / 32;
+  constexpr int kPitchK = kDim + 8, kPitchV = kPromptTokens + 8;   // halves
+  constexpr int kPieces = kPromptTokens * kDim / 16;                // 16-byte pieces of either branch
+  constexpr int kLoads = (kPieces + kThreads - 1) / kThreads;
+  struct Group {
+    int page;
+    float key_scale, exponent, back;
+  };
+  __shared__ LocateLds locate_lds;
+  __shared__ _Float16 keys[2][kPromptTokens][kPitchK];
+  __shared__ _Float16 values[2][kDim][kPitchV];
+  __shared__ Group groups[kListed];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  const int r = lane & 31, half = lane >> 5;
+
+  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const int h = static_cast<int>(unit % p.cache.heads);
+    const int64_t rest = unit / p.cache.heads;
+    const int split = static_cast<int>(rest % most_splits);
+    Tile t;
+    if (!tile_of<kRows, kThreads>(p, rest / most_splits, locate_lds, tid, t)) return;
+    const int64_t last_row = t.row0 + t.rows - 1;
+    const int64_t held = positions_held(p.cache);
+    int64_t seen = t.pos0 + last_row / p.group + 1;
+    seen = seen < 0 ? 0 : (seen < held ? seen : held);
+    const int64_t blocks = (seen + 31) >> 5;
+    const int splits = splits_of(blocks, most_splits);
+    if (split >= splits) continue;
+    const int begin = static_cast<int>(blocks * split / splits) << 5;
+    const int end = static_cast<int>(blocks * (split + 1) / splits) << 5;
+
+    // queries, lifted as in the kernel above; a negative scale turns their sign
+    f16x8 q[kSteps];
+    float factor;
+    int limit, free_until, wave_end;
+    {
+      const int64_t wave_row = t.row0 + 32 * wave;
+      const int64_t wave_last = wave_row + 31 < last_row ? wave_row + 31 : last_row;
+      int64_t row = wave_row + r;
+      row = row > last_row ? last_row : row;
+      const int64_t token = row / p.group;
+      const int head = h * p.group + static_cast<int>(row - token * p.group);
+      const T* src = reinterpret_cast<const T*>(p.q.data) + (t.first + token) * p.q.token + head * p.q.head + 8 * half;
+      float x[kSteps][8];
+      float top = 0.f;
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        load8(src + 16 * s, p.q.wide, x[s]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[s][j]));
+      }
+      top = max_of_halves(top);
+      int e = (__float_as_uint(top) >> 23) & 255;
+      e = e < kLift + 1 ? kLift + 1 : (e > 254 ? 254 : e);
+      float lift = __uint_as_float(static_cast<uint32_t>(254 + kLift - e) << 23);
+      if (p.scale < 0.f) lift = -lift;
+      factor = __uint_as_float(static_cast<uint32_t>(e - kLift) << 23) * (fabsf(p.scale) * kLog2e);
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) q[s][j] = static_cast<_Float16>(x[s][j] * lift);
+      const auto position = [&](int64_t row) {
+        const int64_t pos = t.pos0 + row / p.group;
+        return static_cast<int>(pos < -1 ? -1 : (pos < held ? pos : held));
+      };
+      limit = position(row);
+      free_until = uniform(position(wave_row)) + 1;
+      wave_end = wave_row > last_row ? 0 : uniform(position(wave_last)) + 1;
+    }
+
+    f32x16 acc[kOut];
+#pragma unroll
+    for (int c = 0; c < kOut; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[c][i] = 0.f;
+    float m = -INFINITY, l = 0.f;
+
+    for (int chunk = begin; chunk < end; chunk += 16 * kListed) {
+      const int chunk_end = chunk + 16 * kListed < end ? chunk + 16 * kListed : end;
+      const int tiles = (chunk_end - chunk + kPromptTokens - 1) / kPromptTokens;
+      // pages and scales of the chunk's groups; a hole, and what lies past the end, weighs nothing
+      for (int i = tid; i < 4 * tiles; i += kThreads) {
+        const int pos = chunk + 16 * i;
+        Group group{0, 0.f, -INFINITY, 0.f};
+        const int page = pos < chunk_end ? page_of(p.cache, t.b, pos) : -1;
+        if (page >= 0) {
+          const int64_t at = static_cast<int64_t>(page) * p.cache.heads + h;
+          float vs = p.cache.v_scale[at];
+          vs = vs < 7.8886091e-31f ? 7.8886091e-31f : vs;  // 2^-100: 2^27 positions fit the sum
+          group = Group{page, p.cache.k_scale[at], __builtin_amdgcn_logf(vs), 1.f / vs};
+        }
+        groups[i] = group;
+      }
+      __syncthreads();
+
+      uint4 kraw[kLoads];
+      uint32_t vraw[kLoads][4];
+      const auto load = [&](int tile) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          const int piece = i * kThreads + tid;
+          if (kPieces % kThreads != 0 && piece >= kPieces) break;
+          const int key = piece / (kDim / 16);
+          int page = uniform(groups[4 * tile + uniform(key >> 4)].page);
+          const int64_t in_page = (chunk + kPromptTokens * tile + 16 * uniform(key >> 4)) & (p.cache.page - 1);
+          const int8_t* src = p.cache.k + page_at(p.cache, page, h, kDim) + in_page * kDim;
+          kraw[i] = *reinterpret_cast<const uint4*>(src + (key & 15) * kDim + 16 * (piece % (kDim / 16)));
+          const int four = piece / (kDim / 4);  // four positions, four channels
+          page = uniform(groups[4 * tile + uniform(four >> 2)].page);
+          const int64_t in_page_v = (chunk + kPromptTokens * tile + 16 * uniform(four >> 2)) & (p.cache.page - 1);
+          src = p.cache.v + page_at(p.cache, page, h, kDim) + in_page_v * kDim + 4 * (piece % (kDim / 4));
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            vraw[i][j] = *reinterpret_cast<const uint32_t*>(src + (4 * (four & 3) + j) * kDim);
+        }
+      };
+      const auto store = [&](int buffer) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          const int piece = i * kThreads + tid;
+          if (kPieces % kThreads != 0 && piece >= kPieces) break;
+          _Float16* dst = &keys[buffer][piece / (kDim / 16)][16 * (piece % (kDim / 16))];
+          *reinterpret_cast<f16x8*>(dst) = bytes_as_f16(kraw[i].x, kraw[i].y);
+          *reinterpret_cast<f16x8*>(dst + 8) = bytes_as_f16(kraw[i].z, kraw[i].w);
+          // positions 16t + 8a + 4b + (0..3) stand at 16t + 8b + 4a: the order of the score registers
+          const int four = piece / (kDim / 4), c = 4 * (piece % (kDim / 4));
+          const int at = 16 * (four >> 2) + 8 * (four & 1) + 4 * ((four >> 1) & 1);
+          *reinterpret_cast<uint2*>(&values[buffer][c][at]) = byte_column_as_f16<0>(vraw[i]);
+          *reinterpret_cast<uint2*>(&values[buffer][c + 1][at]) = byte_column_as_f16<1>(vraw[i]);
+          *reinterpret_cast<uint2*>(&values[buffer][c + 2][at]) = byte_column_as_f16<2>(vraw[i]);
+          *reinterpret_cast<uint2*>(&values[buffer][c + 3][at]) = byte_column_as_f16<3>(vraw[i]);
+        }
+      };
+
+      load(0);
+      store(0);
+      if (tiles > 1) load(1);
+      __syncthreads();
+      for (int tile = 0; tile < tiles; ++tile) {
+        const int buffer = tile & 1, at = chunk + kPromptTokens * tile;
+        if (tile + 1 < tiles) store(buffer ^ 1);
+        if (tile + 2 < tiles) load(tile + 2);
+        if (at < wave_end) {
+          f32x16 score[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) score[i][j] = 0.f;
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s)
+              score[i] = mfma32(*reinterpret_cast<const f16x8*>(&keys[buffer][32 * i + r][16 * s + 8 * half]), q[s], score[i]);
+          }
+          float f[4], exponent[4], back[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const Group group = groups[4 * tile + i];
+            f[i] = group.key_scale * factor;
+            exponent[i] = group.exponent;
+            back[i] = group.back;
+          }
+          const bool masked = at + kPromptTokens > free_until;
+          if (masked) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int j = 0; j < 16; ++j)
+                if (at + 32 * i + 8 * (j >> 2) + 4 * half + (j & 3) > limit) score[i][j] = -INFINITY;
+          }
+          float top = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float best = score[i >> 1][8 * (i & 1)];
+#pragma unroll
+            for (int j = 1; j < 8; ++j) best = fmaxf(best, score[i >> 1][8 * (i & 1) + j]);
+            if (best > -INFINITY) top = fmaxf(top, fmaf(best, f[i], exponent[i]));
+          }
+          top = max_of_halves(top);
+          if (__any(top > m + kPromptSlack)) {
+            const float now = fmaxf(m, top);
+            const float fade = exp2_fast(m - (now == -INFINITY ? 0.f : now));
+            m = now;
+            l *= fade;
+#pragma unroll
+            for (int c = 0; c < kOut; ++c)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) acc[c][i] *= fade;
+          }
+          const float base = (m == -INFINITY ? 0.f : m) - kPromptLift;
+          f16x8 w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float offset = exponent[i] - base;
+            float sum = 0.f;
+            u32x4 packed;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              float e[2];
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const float s = score[i >> 1][8 * (i & 1) + 2 * j + k];
+                e[k] = exp2_fast(fmaf(s, f[i], offset));
+                if (masked && s == -INFINITY) e[k] = 0.f;
+              }
+              const auto pair = __builtin_amdgcn_cvt_pkrtz(e[0], e[1]);
+              packed[j] = __builtin_bit_cast(uint32_t, pair);
+              sum = __builtin_amdgcn_fdot2(pair, decltype(pair){1, 1}, sum, false);
+            }
+            w[i] = __builtin_bit_cast(f16x8, packed);
+            if (sum != 0.f) l = fmaf(sum, back[i], l);
+          }
+#pragma unroll
+          for (int c = 0; c < kOut; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              acc[c] = mfma32(*reinterpret_cast<const f16x8*>(&values[buffer][32 * c + r][16 * i + 8 * half]), w[i], acc[c]);
+        }
+        __syncthreads();
+      }
+    }
+
+    l += __shfl_xor(l, 32);
+    const int64_t row = t.row0 + 32 * wave + r;
+    if (row <= last_row) {
+      if (splits == 1) {
+        const int64_t token = row / p.group;
+        const int head = h * p.group + static_cast<int>(row - token * p.group);
+        T* dst = reinterpret_cast<T*>(p.out.data) + (t.first + token) * p.out.token + head * p.out.head;
+        const float inv = l != 0.f ? 1.f / l : 0.f;
+#pragma unroll
+        for (int c = 0; c < kOut; ++c)
+#pragma unroll
+          for (int a = 0; a < 4; ++a) {
+            const int at = 32 * c + 8 * a + 4 * half;
+            const uint2 v = make_uint2(pack_bf16x2(acc[c][4 * a] * inv, acc[c][4 * a + 1] * inv),
+                                       pack_bf16x2(acc[c][4 * a + 2] * inv, acc[c][4 * a + 3] * inv));
+            if (p.out.wide) {
+              *reinterpret_cast<uint2*>(dst + at) = v;
+            } else {
+              dst[at] = static_cast<uint16_t>(v.x);
+              dst[at + 1] = static_cast<uint16_t>(v.x >> 16);
+              dst[at + 2] = static_cast<uint16_t>(v.y);
+              dst[at + 3] = static_cast<uint16_t>(v.y >> 16);
+            }
+          }
+      } else {
+        const int64_t at = unit * kRows + 32 * wave + r;
+#pragma unroll
+        for (int c = 0; c < kOut; ++c)
+#pragma unroll
+          for (int a = 0; a < 4; ++a)
+            *reinterpret_cast<float4*>(partial + at * kDim + 32 * c + 8 * a + 4 * half) =
+                make_float4(acc[c][4 * a], acc[c][4 * a + 1], acc[c][4 * a + 2], acc[c][4 * a + 3]);
+        if (half == 0) *reinterpret_cast<float2*>(partial_ml + 2 * at) = make_float2(m, l);
+      }
+    }
+  }
+}
+
+// Joins the shares of every row that was split: one workgroup per row, its threads over channels
+// (four each) and shares.
+template <typename T, int kDim, int kRows>
+__global__ __launch_bounds__(256) void cache_attend_join_kernel(CacheAttendParams p, int most_splits,
+                                                               int64_t units, const float* partial,
+                                                               const float* partial_ml) {
+  constexpr int kLanes = kDim / 4, kShares = 256 / kLanes;
+  __shared__ LocateLds locate_lds;
+  __shared__ float4 sums[kShares][kLanes];
+  __shared__ float tops[kShares], totals[kShares];
+  const int tid = threadIdx.x, c = tid % kLanes, share = tid / kLanes;
+  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    const int row = static_cast<int>(unit % kRows);
+    const int h = static_cast<int>(unit / kRows % p.cache.heads);
+    const int64_t index = unit / kRows / p.cache.heads;
+    Tile t;
+    if (!tile_of<kRows, 256>(p, index, locate_lds, tid, t)) return;
+    if (row >= t.rows) continue;
+    int64_t seen = t.pos0 + (t.row0 + t.rows - 1) / p.group + 1;
+    const int64_t held = positions_held(p.cache);
+    seen = seen < 0 ? 0 : (seen < held ? seen : held);
+    const int splits = splits_of((seen + 31) >> 5, most_splits);
+    if (splits == 1) continue;
+    const int64_t first = (index * most_splits * p.cache.heads + h) * kRows + row;
+    const int64_t step = static_cast<int64_t>(p.cache.heads) * kRows;
+    float top = -INFINITY, total = 0.f;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s = share; s < splits; s += kShares) {
+      const int64_t at = first + s * step;
+      const float2 ml = *reinterpret_cast<const float2*>(partial_ml + 2 * at);
+      const float4 x = *reinterpret_cast<const float4*>(partial + at * kDim + 4 * c);
+      const float now = fmaxf(top, ml.x), base = now == -INFINITY ? 0.f : now;
+      const float fade = exp2_fast(top - base), w = exp2_fast(ml.x - base);
+      top = now;
+      total = total * fade + ml.y * w;
+      sum.x = sum.x * fade + x.x * w;
+      sum.y = sum.y * fade + x.y * w;
+      sum.z = sum.z * fade + x.z * w;
+      sum.w = sum.w * fade + x.w * w;
+    }
+    sums[share][c] = sum;
+    if (c == 0) {
+      tops[share] = top;
+      totals[share] = total;
+    }
+    __syncthreads();
+    if (share == 0) {
+      float all = tops[0];
+      for (int s = 1; s < kShares; ++s) all = fmaxf(all, tops[s]);
+      const float base = all == -INFINITY ? 0.f : all;
+      float f[4] = {0.f, 0.f, 0.f, 0.f}, l = 0.f;
+      for (int s = 0; s < kShares; ++s) {
+        const float w = exp2_fast(tops[s] - base);
+        l += totals[s] * w;
+        f[0] += sums[s][c].x * w;
+        f[1] += sums[s][c].y * w;
+        f[2] += sums[s][c].z * w;
+        f[3] += sums[s][c].w * w;
+      }
+      const int64_t token = (t.row0 + row) / p.group;
+      const int head = h * p.group + static_cast<int>(t.row0 + row - token * p.group);
+      T* dst = reinterpret_cast<T*>(p.out.data) + (t.first + token) * p.out.token + head * p.out.head + 4 * c;
+      const float inv = l != 0.f ? 1.f / l : 0.f;
+      for (int j = 0; j < 4; ++j) store1(dst + j, f[j] * inv);
+    }
+    __syncthreads();
+  }
+}
+
+template <int kDim>
+static hipError_t launch_prompt_as(const CacheAttendParams& p, int64_t tiles, int splits, float* workspace,
+                                   hipStream_t stream) {
+  const int64_t units = tiles * p.cache.heads * splits;
+  workspace += kCounterBytes / sizeof(float);  // the counts of the other kernel stay zero
+  float* ml = workspace + units * kPromptRows * kDim;
+  const auto grid = [](int64_t n) { return dim3(static_cast<unsigned>(n < kMaxGrid / 2 ? n : kMaxGrid / 2)); };
+  hipLaunchKernelGGL((cache_attend_prompt_kernel<kDim, kPromptWaves>), grid(units), dim3(64 * kPromptWaves), 0,
+                     stream, p, splits, units, workspace, ml);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || splits == 1) return e;
+  const int64_t rows = tiles * p.cache.heads * kPromptRows;
+  hipLaunchKernelGGL((cache_attend_join_kernel<uint16_t, kDim, kPromptRows>), grid(rows), dim3(256), 0, stream, p,
+                     splits, rows, workspace, ml);
+  return hipGetLastError();
+}
+
+hipError_t launch_attend_prompt(int head_dim, const CacheAttendParams& p, int64_t tiles, int splits, float* workspace,
+                                hipStream_t stream) {
+  return head_dim == 128 ? launch_prompt_as<128>(p, tiles, splits, workspace, stream)
+                         : launch_prompt_as<64>(p, tiles, splits, workspace, stream);
+}
+
+}  // namespace scd

@@ -61,12 +61,26 @@ struct CacheReadParams {
   Rows rows[2];
 };
 
+// Division of 0 <= n < 2^31 by a number known on the host: a product, a sum and a shift.
+struct FastDiv {
+  uint32_t mul = 1, shift = 0;
+  FastDiv() = default;
+  explicit FastDiv(uint32_t d) {
+    while ((uint64_t{1} << shift) < d) ++shift;
+    mul = static_cast<uint32_t>((((uint64_t{1} << shift) - d) << 32) / d + 1);
+  }
+  __device__ int of(int n) const {
+    return static_cast<int>((__umulhi(static_cast<uint32_t>(n), mul) + static_cast<uint32_t>(n)) >> shift);
+  }
+};
+
 struct CacheAttendParams {
   PagedCache cache;
   SeqBatch batch;
   Rows q, out;
   int32_t group;        // query heads per KV head
   float scale;
+  FastDiv by_group, by_heads;  // by group, by cache.heads
 };
 
 constexpr int kMaxTurnPairs = 256;
@@ -85,6 +99,12 @@ hipError_t launch_cache_append(bool bf16, int head_dim, const CacheAppendParams&
                                hipStream_t stream);
 hipError_t launch_cache_read(bool bf16, int head_dim, const CacheReadParams& p, hipStream_t stream);
 
+// A few rows of every request (tiles of 16, 32 or 64 of them) in `workers` workgroups, or whole prompts (bf16,
+// head_dim 64 or 128) in up to `splits` shares of each of `tiles` tiles and KV head.
+hipError_t launch_attend_rows(bool bf16, int head_dim, int rows, const CacheAttendParams& p, int workers, int step_log2,
+                              float* workspace, hipStream_t stream);
+hipError_t launch_attend_prompt(int head_dim, const CacheAttendParams& p, int64_t tiles, int splits, float* workspace,
+                                hipStream_t stream);
 size_t attend_workspace(const PagedCache& c, const SeqBatch& b, int group, int head_dim);
 hipError_t launch_cache_attend(bool bf16, int head_dim, const CacheAttendParams& p,
                                void* workspace, hipStream_t stream);

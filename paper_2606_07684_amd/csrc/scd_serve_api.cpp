@@ -274,6 +274,8 @@ scd_status_t scd_cache_attend(const scd_cache_t* cache, const scd_batch_t* batch
     return fail(SCD_ERR_SHAPE, "q has %d heads, not a multiple of n_kv_heads %d", q->n_heads,
                 cache->n_kv_heads);
   if (q->n_heads > 65536) return fail(SCD_ERR_UNSUPPORTED, "more than 65536 query heads");
+  if (batch->n_tokens * q->n_heads >= int64_t{1} << 31)
+    return fail(SCD_ERR_UNSUPPORTED, "n_tokens * n_heads reaches 2^31");
   SCD_TRY(check_rows(out, "out", q->n_heads, cache->head_dim, dtype, batch->n_tokens, true));
   if (batch->n_tokens == 0) return ok();
   const size_t need = scd_cache_attend_workspace_bytes(cache, batch, q->n_heads);
@@ -288,6 +290,8 @@ scd_status_t scd_cache_attend(const scd_cache_t* cache, const scd_batch_t* batch
   p.out = rows_of(out, dtype);
   p.group = q->n_heads / cache->n_kv_heads;
   p.scale = static_cast<float>(softmax_scale);
+  p.by_group = scd::FastDiv(p.group);
+  p.by_heads = scd::FastDiv(cache->n_kv_heads);
   return launched(scd::launch_cache_attend(dtype == SCD_BF16, cache->head_dim, p, workspace, stream),
                   "cache attend");
 }
