@@ -145,18 +145,15 @@ __device__ inline bool share_of(const CacheAttendParams& p, const RowsLayout& la
   return true;
 }
 
-// What a workgroup leaves for another, perhaps on another XCD whose L2 does not see this one's: stores and
-// loads of agent scope go past both, and a store has arrived once it is waited for.  (A fence of agent scope
-// would do, but writes back and invalidates a whole L2 each time: three times the run time of 512
-// workgroups.)
+// What a workgroup leaves for another, perhaps on another XCD whose L2 does not see this one's: stores of agent
+// scope go through to memory, and have arrived once they are waited for; the one that reads them invalidates its
+// caches first.  (A release fence would do for the stores, but writes back a whole L2 each time, at three times
+// the run time of 512 workgroups.)
 __device__ inline void leave2(float* p, float a, float b) {
   const uint64_t v = static_cast<uint64_t>(__float_as_uint(a)) | static_cast<uint64_t>(__float_as_uint(b)) << 32;
   __hip_atomic_store(reinterpret_cast<uint64_t*>(p), v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-__device__ inline float2 take2(const float* p) {
-  const uint64_t v = __hip_atomic_load(reinterpret_cast<const uint64_t*>(p), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  return make_float2(__uint_as_float(static_cast<uint32_t>(v)), __uint_as_float(static_cast<uint32_t>(v >> 32)));
-}
+__device__ inline float2 take2(const float* p) { return *reinterpret_cast<const float2*>(p); }
 
 // Sums a workgroup leaves for a row that it does not finish: rows of two slots a worker (0: of a segment that
 // began before its share, 1: of one that goes on after it), then their maxima and sums, then a count a worker
@@ -183,10 +180,11 @@ __global__ __launch_bounds__(64 * rows_waves(kRows), rows_waves(kRows) / 4) void
   constexpr int kOut = kDim / 16;     // output channels a lane holds of each of its four matrix rows
   constexpr int kPitch = kDim + 4;
   constexpr int kPairs = kDim / 2;
+  constexpr int kAhead = 1;          // blocks on their way
   __shared__ ShareLds<kThreads> share_lds;
   __shared__ float joined[kWaves][16][kPitch];
   __shared__ float joined_m[kWaves][kRows], joined_l[kWaves][kRows];
-  __shared__ float team_sums[kThreads][3];
+  __shared__ __attribute__((aligned(16))) float team_sums[kThreads][8];
   __shared__ int arrived;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int r = lane & 15, g = lane >> 4;
@@ -225,7 +223,7 @@ __global__ __launch_bounds__(64 * rows_waves(kRows), rows_waves(kRows) / 4) void
       limit[n] = reach_of(held, pos0, token);
     }
 
-    // Blocks are fetched one ahead of the arithmetic, their pages' numbers another one ahead.
+    // Blocks are fetched kAhead ahead of the arithmetic, their pages' numbers another one ahead.
     const auto pages_of = [&](int block) {
       int2 id;
       int* const out[2] = {&id.x, &id.y};
@@ -281,11 +279,13 @@ __global__ __launch_bounds__(64 * rows_waves(kRows), rows_waves(kRows) / 4) void
       }
     };
     int block = begin + wave;
-    Fetched now, next;
+    Fetched ring[kAhead + 1];
     int2 ids;
     if (block < end) {
-      fetch(now, block, pages_of(block));
-      ids = pages_of(block + kWaves);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i)
+        if (block + i * kWaves < end) fetch(ring[i], block + i * kWaves, pages_of(block + i * kWaves));
+      ids = pages_of(block + kAhead * kWaves);
     }
 
     // queries, lifted and split
@@ -428,20 +428,14 @@ __global__ __launch_bounds__(64 * rows_waves(kRows), rows_waves(kRows) / 4) void
         out(IntC<3>{}, 1);
       }
     };
-    if (block < end) {
-      while (true) {
-        if (block + kWaves < end) {
-          fetch(next, block + kWaves, ids);
-          ids = pages_of(block + 2 * kWaves);
+    while (block < end) {
+#pragma unroll
+      for (int i = 0; i <= kAhead; ++i) {
+        if (block + kAhead * kWaves < end) {
+          fetch(ring[(i + kAhead) % (kAhead + 1)], block + kAhead * kWaves, ids);
+          ids = pages_of(block + (kAhead + 1) * kWaves);
         }
-        attend(now, block);
-        block += kWaves;
-        if (block >= end) break;
-        if (block + kWaves < end) {
-          fetch(now, block + kWaves, ids);
-          ids = pages_of(block + 2 * kWaves);
-        }
-        attend(next, block);
+        attend(ring[i], block);
         block += kWaves;
         if (block >= end) break;
       }
@@ -520,8 +514,9 @@ __global__ __launch_bounds__(64 * rows_waves(kRows), rows_waves(kRows) / 4) void
         arrived = __hip_atomic_fetch_add(partial.count + first, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       lds_barrier();
       if (arrived == last - first) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
         if (tid == 0) __hip_atomic_store(partial.count + first, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        // Pairs of channels of every row, and where they leave threads over, several threads a pair's parts.
+        // Four channels of every row, and where they leave threads over, several threads a four's parts.
         // The parts' maxima and sums go through LDS where it holds them.
         const int parts = last - first + 1;
         const auto row_from = [&](int i, int row) { return static_cast<int64_t>(2 * (first + i) + (i == 0)) * kRows + row; };
@@ -533,43 +528,52 @@ __global__ __launch_bounds__(64 * rows_waves(kRows), rows_waves(kRows) / 4) void
             staged[i] = take2(partial.ml + 2 * row_from(part, i - part * rows));
           }
         lds_barrier();
-        const int items = rows * kPairs;
+        constexpr int kFours = kDim / 4;
+        const int items = rows * kFours;
         const int teams = items >= kThreads ? 1 : kThreads / items;
         for (int item0 = 0; item0 < items; item0 += kThreads) {
           const int item = item0 + (teams == 1 ? tid : tid % items), team = teams == 1 ? 0 : tid / items;
           const bool busy = item < items && team < teams;
-          const int row = busy ? item / kPairs : 0, c = 2 * (item % kPairs);
+          const int row = busy ? item / kFours : 0, c = 4 * (item % kFours);
           const auto ml_of = [&](int i) { return fits ? staged[i * rows + row] : take2(partial.ml + 2 * row_from(i, row)); };
-          float x = 0.f, y = 0.f, sum = 0.f;
+          f32x4 x = {0.f, 0.f, 0.f, 0.f};
+          float sum = 0.f;
           if (busy) {
             float top = -INFINITY;
             for (int i = 0; i < parts; ++i) top = fmaxf(top, ml_of(i).x);
             const float base = top == -INFINITY ? 0.f : top;
-#pragma unroll 8
-            for (int i = team; i < parts; i += teams) {
-              const float2 v = take2(partial.rows + row_from(i, row) * kDim + c);
-              const float2 ml = ml_of(i);
-              const float w = exp2_fast(ml.x - base);
-              sum += ml.y * w;
-              x += v.x * w;
-              y += v.y * w;
+            constexpr int kBatch = 8;  // parts on their way at once
+            for (int i0 = team; i0 < parts; i0 += kBatch * teams) {
+              f32x4 v[kBatch];
+#pragma unroll
+              for (int k = 0; k < kBatch; ++k) {
+                const int i = i0 + k * teams;
+                v[k] = *reinterpret_cast<const f32x4*>(partial.rows + row_from(i < parts ? i : i0, row) * kDim + c);
+              }
+#pragma unroll
+              for (int k = 0; k < kBatch; ++k) {
+                const int i = i0 + k * teams;
+                const float2 ml = ml_of(i < parts ? i : i0);
+                const float w = i < parts ? exp2_fast(ml.x - base) : 0.f;
+                sum += ml.y * w;
+                x += v[k] * w;
+              }
             }
           }
           if (teams > 1) {
-            team_sums[tid][0] = x;
-            team_sums[tid][1] = y;
-            team_sums[tid][2] = sum;
+            *reinterpret_cast<f32x4*>(team_sums[tid]) = x;
+            team_sums[tid][4] = sum;
             lds_barrier();
             if (team == 0)
               for (int k = 1; k < teams; ++k) {
-                x += team_sums[k * items + item][0];
-                y += team_sums[k * items + item][1];
-                sum += team_sums[k * items + item][2];
+                x += *reinterpret_cast<const f32x4*>(team_sums[k * items + item]);
+                sum += team_sums[k * items + item][4];
               }
           }
           if (busy && team == 0) {
             const float inv = sum != 0.f ? 1.f / sum : 0.f;
-            store2(row, c, x * inv, y * inv);
+            store2(row, c, x[0] * inv, x[1] * inv);
+            store2(row, c + 2, x[2] * inv, x[3] * inv);
           }
         }
         lds_barrier();
