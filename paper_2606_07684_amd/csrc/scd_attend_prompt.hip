@@ -74,14 +74,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
   constexpr int kPitchK = kDim + 8, kPitchV = kPromptTokens + 8;   // halves
   constexpr int kPieces = kPromptTokens * kDim / 16;                // 16-byte pieces of either branch
   constexpr int kLoads = (kPieces + kThreads - 1) / kThreads;
-  struct Group {
-    int page;
-    float key_scale, exponent, back;
-  };
   __shared__ LocateLds locate_lds;
   __shared__ _Float16 keys[2][kPromptTokens][kPitchK];
   __shared__ _Float16 values[2][kDim][kPitchV];
-  __shared__ Group groups[kListed];
+  __shared__ float4 scales[kListed];   // of keys; log2 and inverse of that of values
+  __shared__ int64_t places[kListed];  // byte of a group's first position, in either branch's pages
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int r = lane & 31, half = lane >> 5;
 
@@ -153,40 +150,46 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
       // pages and scales of the chunk's groups; a hole, and what lies past the end, weighs nothing
       for (int i = tid; i < 4 * tiles; i += kThreads) {
         const int pos = chunk + 16 * i;
-        Group group{0, 0.f, -INFINITY, 0.f};
-        const int page = pos < chunk_end ? page_of(p.cache, t.b, pos) : -1;
+        float4 scale = make_float4(0.f, -INFINITY, 0.f, 0.f);
+        int page = pos < chunk_end ? page_of(p.cache, t.b, pos) : -1;
         if (page >= 0) {
           const int64_t at = static_cast<int64_t>(page) * p.cache.heads + h;
           float vs = p.cache.v_scale[at];
           vs = vs < 7.8886091e-31f ? 7.8886091e-31f : vs;  // 2^-100: 2^27 positions fit the sum
-          group = Group{page, p.cache.k_scale[at], __builtin_amdgcn_logf(vs), 1.f / vs};
+          scale = make_float4(p.cache.k_scale[at], __builtin_amdgcn_logf(vs), 1.f / vs, 0.f);
+        } else {
+          page = 0;
         }
-        groups[i] = group;
+        scales[i] = scale;
+        places[i] = page_at(p.cache, page, h, kDim) + (pos & (p.cache.page - 1)) * kDim;
       }
       __syncthreads();
 
+      // Raw bytes on their way to LDS: keys of one tile, values of the one before it.
       uint4 kraw[kLoads];
       uint32_t vraw[kLoads][4];
-      const auto load = [&](int tile) {
+      // A thread's pieces of either branch lie in the same groups of 16 positions.
+      const auto load_keys = [&](int tile) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
           const int piece = i * kThreads + tid;
           if (kPieces % kThreads != 0 && piece >= kPieces) break;
-          const int key = piece / (kDim / 16);
-          int page = uniform(groups[4 * tile + uniform(key >> 4)].page);
-          const int64_t in_page = (chunk + kPromptTokens * tile + 16 * uniform(key >> 4)) & (p.cache.page - 1);
-          const int8_t* src = p.cache.k + page_at(p.cache, page, h, kDim) + in_page * kDim;
-          kraw[i] = *reinterpret_cast<const uint4*>(src + (key & 15) * kDim + 16 * (piece % (kDim / 16)));
-          const int four = piece / (kDim / 4);  // four positions, four channels
-          page = uniform(groups[4 * tile + uniform(four >> 2)].page);
-          const int64_t in_page_v = (chunk + kPromptTokens * tile + 16 * uniform(four >> 2)) & (p.cache.page - 1);
-          src = p.cache.v + page_at(p.cache, page, h, kDim) + in_page_v * kDim + 4 * (piece % (kDim / 4));
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            vraw[i][j] = *reinterpret_cast<const uint32_t*>(src + (4 * (four & 3) + j) * kDim);
+          const int8_t* src = p.cache.k + places[4 * tile + piece / kDim] + (piece / (kDim / 16) & 15) * kDim + 16 * (piece % (kDim / 16));
+          kraw[i] = *reinterpret_cast<const uint4*>(src);
         }
       };
-      const auto store = [&](int buffer) {
+      const auto load_values = [&](int tile) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          const int piece = i * kThreads + tid;
+          if (kPieces % kThreads != 0 && piece >= kPieces) break;
+          const int four = piece / (kDim / 4);  // four positions, four channels
+          const int8_t* src = p.cache.v + places[4 * tile + piece / kDim] + 4 * (four & 3) * kDim + 4 * (piece % (kDim / 4));
+#pragma unroll
+          for (int j = 0; j < 4; ++j) vraw[i][j] = *reinterpret_cast<const uint32_t*>(src + j * kDim);
+        }
+      };
+      const auto store_keys = [&](int buffer) {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
           const int piece = i * kThreads + tid;
@@ -194,100 +197,163 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
           _Float16* dst = &keys[buffer][piece / (kDim / 16)][16 * (piece % (kDim / 16))];
           *reinterpret_cast<f16x8*>(dst) = bytes_as_f16(kraw[i].x, kraw[i].y);
           *reinterpret_cast<f16x8*>(dst + 8) = bytes_as_f16(kraw[i].z, kraw[i].w);
-          // positions 16t + 8a + 4b + (0..3) stand at 16t + 8b + 4a: the order of the score registers
+        }
+      };
+      const auto store_values = [&](int buffer) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          const int piece = i * kThreads + tid;
+          if (kPieces % kThreads != 0 && piece >= kPieces) break;
+          // Positions 16t + 8a + 4b + (0..3) stand at 16t + 8b + 4a, the order of the score registers, and
+          // channel c's pieces of 8 are exchanged by bits of c, so that the 32 lanes of a store, four channels
+          // apart, reach all banks.
           const int four = piece / (kDim / 4), c = 4 * (piece % (kDim / 4));
-          const int at = 16 * (four >> 2) + 8 * (four & 1) + 4 * ((four >> 1) & 1);
+          const int eight = (2 * (four >> 2) + (four & 1)) ^ (c >> 4 & 7), at = 8 * eight + 4 * ((four >> 1) & 1);
           *reinterpret_cast<uint2*>(&values[buffer][c][at]) = byte_column_as_f16<0>(vraw[i]);
           *reinterpret_cast<uint2*>(&values[buffer][c + 1][at]) = byte_column_as_f16<1>(vraw[i]);
           *reinterpret_cast<uint2*>(&values[buffer][c + 2][at]) = byte_column_as_f16<2>(vraw[i]);
           *reinterpret_cast<uint2*>(&values[buffer][c + 3][at]) = byte_column_as_f16<3>(vraw[i]);
         }
       };
+      const auto stage = [&](int tile) {
+        if (tile + 1 < tiles) store_keys((tile + 1) & 1);
+        if (tile < tiles) store_values(tile & 1);
+        if (tile + 2 < tiles) load_keys(tile + 2);
+        if (tile + 1 < tiles) load_values(tile + 1);
+      };
 
-      load(0);
-      store(0);
-      if (tiles > 1) load(1);
-      __syncthreads();
-      for (int tile = 0; tile < tiles; ++tile) {
-        const int buffer = tile & 1, at = chunk + kPromptTokens * tile;
-        if (tile + 1 < tiles) store(buffer ^ 1);
-        if (tile + 2 < tiles) load(tile + 2);
-        if (at < wave_end) {
-          f32x16 score[2];
+      f32x16 score[2];
+      f16x8 w[4];
+      const auto live = [&](int tile) { return chunk + kPromptTokens * tile < wave_end; };
+      // Operands are read kReads matrix steps before the one that takes them, in this order: left to itself
+      // the compiler keeps one or two and waits for LDS at every step.
+      constexpr int kReads = 6;
+      const auto steps = [&](auto count, auto operand, auto step) {
+        constexpr int kCount = decltype(count)::value;
+        f16x8 a[kReads];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kReads; ++i) a[i] = operand(i);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < kCount; ++i) {
+          step(i, a[i % kReads]);
+          if (i + kReads < kCount) a[i % kReads] = operand(i + kReads);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      };
+      const auto products = [&](int tile) {
+        if (tile > 0 && live(tile - 1)) {
+          const _Float16* rows = values[(tile - 1) & 1][r];
+          const auto operand = [&](int i) {  // of channel 32c + r, its piece 2t + half
+            const int c = i % kOut, eight = (2 * (i / kOut) + half) ^ ((2 * c + (r >> 4)) & 7);
+            return *reinterpret_cast<const f16x8*>(rows + 32 * c * kPitchV + 8 * eight);
+          };
+          steps(IntC<4 * kOut>{}, operand,
+                [&](int i, const f16x8& a) { acc[i % kOut] = mfma32(a, w[i / kOut], acc[i % kOut]); });
+        }
+        if (tile < tiles && live(tile)) {
+          const _Float16* rows = &keys[tile & 1][r][8 * half];
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int j = 0; j < 16; ++j) score[i][j] = 0.f;
+          steps(IntC<2 * kSteps>{}, [&](int i) { return *reinterpret_cast<const f16x8*>(rows + 32 * (i % 2) * kPitchK + 16 * (i / 2)); },
+                [&](int i, const f16x8& a) { score[i % 2] = mfma32(a, q[i / 2], score[i % 2]); });
+        }
+      };
+      const auto weights = [&](int tile) {
+        const int at = chunk + kPromptTokens * tile;
+        if (at >= wave_end) return;
+        float f[4], exponent[4], back[4];
 #pragma unroll
-            for (int s = 0; s < kSteps; ++s)
-              score[i] = mfma32(*reinterpret_cast<const f16x8*>(&keys[buffer][32 * i + r][16 * s + 8 * half]), q[s], score[i]);
-          }
-          float f[4], exponent[4], back[4];
+        for (int i = 0; i < 4; ++i) {
+          const float4 scale = scales[4 * tile + i];
+          f[i] = scale.x * factor;
+          exponent[i] = scale.y;
+          back[i] = scale.z;
+        }
+        const bool masked = at + kPromptTokens > free_until;
+        const int shown = limit - at - 4 * half;  // compared with constants, not with a register each
+        const auto hide = [&](float with) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const Group group = groups[4 * tile + i];
-            f[i] = group.key_scale * factor;
-            exponent[i] = group.exponent;
-            back[i] = group.back;
-          }
-          const bool masked = at + kPromptTokens > free_until;
-          if (masked) {
+          for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
+            for (int j = 0; j < 16; ++j)
+              if (32 * i + 8 * (j >> 2) + (j & 3) > shown) score[i][j] = with;
+        };
+        if (masked) hide(-INFINITY);
+        float top = -INFINITY;
 #pragma unroll
-              for (int j = 0; j < 16; ++j)
-                if (at + 32 * i + 8 * (j >> 2) + 4 * half + (j & 3) > limit) score[i][j] = -INFINITY;
-          }
-          float top = -INFINITY;
+        for (int i = 0; i < 4; ++i) {
+          float best = score[i >> 1][8 * (i & 1)];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float best = score[i >> 1][8 * (i & 1)];
-#pragma unroll
-            for (int j = 1; j < 8; ++j) best = fmaxf(best, score[i >> 1][8 * (i & 1) + j]);
-            if (best > -INFINITY) top = fmaxf(top, fmaf(best, f[i], exponent[i]));
-          }
-          top = max_of_halves(top);
-          if (__any(top > m + kPromptSlack)) {
-            const float now = fmaxf(m, top);
-            const float fade = exp2_fast(m - (now == -INFINITY ? 0.f : now));
-            m = now;
-            l *= fade;
-#pragma unroll
-            for (int c = 0; c < kOut; ++c)
-#pragma unroll
-              for (int i = 0; i < 16; ++i) acc[c][i] *= fade;
-          }
-          const float base = (m == -INFINITY ? 0.f : m) - kPromptLift;
-          f16x8 w[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float offset = exponent[i] - base;
-            float sum = 0.f;
-            u32x4 packed;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              float e[2];
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const float s = score[i >> 1][8 * (i & 1) + 2 * j + k];
-                e[k] = exp2_fast(fmaf(s, f[i], offset));
-                if (masked && s == -INFINITY) e[k] = 0.f;
-              }
-              const auto pair = __builtin_amdgcn_cvt_pkrtz(e[0], e[1]);
-              packed[j] = __builtin_bit_cast(uint32_t, pair);
-              sum = __builtin_amdgcn_fdot2(pair, decltype(pair){1, 1}, sum, false);
-            }
-            w[i] = __builtin_bit_cast(f16x8, packed);
-            if (sum != 0.f) l = fmaf(sum, back[i], l);
-          }
+          for (int j = 1; j < 8; ++j) best = fmaxf(best, score[i >> 1][8 * (i & 1) + j]);
+          if (best > -INFINITY) top = fmaxf(top, fmaf(best, f[i], exponent[i]));
+        }
+        top = max_of_halves(top);
+        if (__any(top > m + kPromptSlack)) {
+          const float now = fmaxf(m, top);
+          const float fade = exp2_fast(m - (now == -INFINITY ? 0.f : now));
+          m = now;
+          l *= fade;
 #pragma unroll
           for (int c = 0; c < kOut; ++c)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              acc[c] = mfma32(*reinterpret_cast<const f16x8*>(&values[buffer][32 * c + r][16 * i + 8 * half]), w[i], acc[c]);
+            for (int i = 0; i < 16; ++i) acc[c][i] *= fade;
         }
-        __syncthreads();
+        const float base = (m == -INFINITY ? 0.f : m) - kPromptLift;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float offset = exponent[i] - base;
+#pragma unroll
+          for (int j = 8 * (i & 1); j < 8 * (i & 1) + 8; ++j) score[i >> 1][j] = exp2_fast(fmaf(score[i >> 1][j], f[i], offset));
+        }
+        if (masked) hide(0.f);  // whatever the scale: one that is not a number stays with the rows that see it
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float sum = 0.f;
+          u32x4 packed;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const auto pair = __builtin_amdgcn_cvt_pkrtz(score[i >> 1][8 * (i & 1) + 2 * j], score[i >> 1][8 * (i & 1) + 2 * j + 1]);
+            packed[j] = __builtin_bit_cast(uint32_t, pair);
+            sum = __builtin_amdgcn_fdot2(pair, decltype(pair){1, 1}, sum, false);
+          }
+          w[i] = __builtin_bit_cast(f16x8, packed);
+          if (sum != 0.f) l = fmaf(sum, back[i], l);
+        }
+      };
+
+      // The waves of a SIMD, one of either half of the workgroup, take turns: while one keeps the matrix cores
+      // busy the other works on its weights and stages bytes.  Between two barriers, in slots 2j and 2j + 1,
+      // the first and the second half read the keys of tile j and the values of tile j - 1, and the keys of
+      // tile j + 1 and the values of tile j are stored to the other buffers.
+      const auto slot_end = [] {
+        __builtin_amdgcn_sched_barrier(0);
+        lds_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      load_keys(0);
+      store_keys(0);
+      if (tiles > 1) load_keys(1);
+      load_values(0);
+      lds_barrier();
+      const bool second = wave >= kWaves / 2;
+      if (second) {
+        stage(0);
+        slot_end();
       }
+      for (int tile = 0; tile <= tiles; ++tile) {
+        __builtin_amdgcn_s_setprio(1);
+        products(tile);
+        __builtin_amdgcn_s_setprio(0);
+        slot_end();
+        if (tile < tiles) weights(tile);
+        stage(second ? tile + 1 : tile);
+        slot_end();
+      }
+      if (!second) slot_end();
+      __syncthreads();
     }
 
     l += __shfl_xor(l, 32);
