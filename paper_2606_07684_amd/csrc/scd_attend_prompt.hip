@@ -169,22 +169,31 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
       uint4 kraw[kLoads];
       uint32_t vraw[kLoads][4];
       // A thread's pieces of either branch lie in the same groups of 16 positions.
-      const auto load_keys = [&](int tile) {
+      int64_t place[kLoads], place_after[kLoads];  // of the tiles that values and keys are fetched of next
+      const auto find = [&](int tile) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          place[i] = place_after[i];
+          const int group = 4 * tile + (i * kThreads + tid) / kDim;
+          place_after[i] = places[group < 4 * tiles ? group : 0];
+        }
+      };
+      const auto load_keys = [&] {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
           const int piece = i * kThreads + tid;
           if (kPieces % kThreads != 0 && piece >= kPieces) break;
-          const int8_t* src = p.cache.k + places[4 * tile + piece / kDim] + (piece / (kDim / 16) & 15) * kDim + 16 * (piece % (kDim / 16));
+          const int8_t* src = p.cache.k + place_after[i] + (piece / (kDim / 16) & 15) * kDim + 16 * (piece % (kDim / 16));
           kraw[i] = *reinterpret_cast<const uint4*>(src);
         }
       };
-      const auto load_values = [&](int tile) {
+      const auto load_values = [&] {
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) {
           const int piece = i * kThreads + tid;
           if (kPieces % kThreads != 0 && piece >= kPieces) break;
           const int four = piece / (kDim / 4);  // four positions, four channels
-          const int8_t* src = p.cache.v + places[4 * tile + piece / kDim] + 4 * (four & 3) * kDim + 4 * (piece % (kDim / 4));
+          const int8_t* src = p.cache.v + place[i] + 4 * (four & 3) * kDim + 4 * (piece % (kDim / 4));
 #pragma unroll
           for (int j = 0; j < 4; ++j) vraw[i][j] = *reinterpret_cast<const uint32_t*>(src + j * kDim);
         }
@@ -218,8 +227,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
       const auto stage = [&](int tile) {
         if (tile + 1 < tiles) store_keys((tile + 1) & 1);
         if (tile < tiles) store_values(tile & 1);
-        if (tile + 2 < tiles) load_keys(tile + 2);
-        if (tile + 1 < tiles) load_values(tile + 1);
+        if (tile + 2 < tiles) load_keys();
+        if (tile + 1 < tiles) load_values();
+        find(tile + 3);
       };
 
       f32x16 score[2];
@@ -273,8 +283,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
           back[i] = scale.z;
         }
         const bool masked = at + kPromptTokens > free_until;
-        const int shown = limit - at - 4 * half;  // compared with constants, not with a register each
         const auto hide = [&](float with) {
+          int shown = limit - at - 4 * half;  // compared with constants, not with a register each
+          asm volatile("" : "+v"(shown));     // and only where something is hidden
 #pragma unroll
           for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -333,10 +344,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
         lds_barrier();
         __builtin_amdgcn_sched_barrier(0);
       };
-      load_keys(0);
+      find(0);
+      find(0);
+      load_keys();
       store_keys(0);
-      if (tiles > 1) load_keys(1);
-      load_values(0);
+      find(1);
+      if (tiles > 1) load_keys();
+      load_values();
+      find(2);
       lds_barrier();
       const bool second = wave >= kWaves / 2;
       if (second) {
