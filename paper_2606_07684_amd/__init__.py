@@ -1010,18 +1010,19 @@ def scd_cache_attend_workspace_bytes(cache: PagedCache, batch: Batch, n_q_heads:
 
 
 def prepare_cache_attend(cache: PagedCache, batch: Batch, q, out, scale: Optional[float] = None,
-                         workspace: Optional[torch.Tensor] = None) -> Prepared:
+                         workspace: Optional[torch.Tensor] = None, stream=None) -> Prepared:
     """Causal attention of rows q [n_tokens, heads, head_dim] over the cache, which holds them
     already; ``scale`` None: head_dim^-1/2.  ``workspace`` (zero before its first use; every call leaves
-    it ready for the next) None: one of :func:`scd_cache_attend_workspace_bytes` is made and kept with
-    the call."""
+    it ready for the next) None: one of :func:`scd_cache_attend_workspace_bytes` is made, zeroed on
+    ``stream`` (or the current one), which the calls then belong to, and kept with the call."""
     lib = load_library()
     _cache_batch(cache, batch)
     d = cache.head_dim
     rows = [_rows(t, n, batch.n_tokens, d, q.dtype) for t, n in ((q, "q"), (out, "out"))]
     if workspace is None:
         nbytes = scd_cache_attend_workspace_bytes(cache, batch, q.shape[1])
-        workspace = torch.zeros(max(nbytes, 16), dtype=torch.uint8, device=q.device)
+        with torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream), device=q.device)):
+            workspace = torch.zeros(max(nbytes, 16), dtype=torch.uint8, device=q.device)
     ws, nbytes = _workspace_arg(workspace)
     args = (ctypes.byref(cache._c), ctypes.byref(batch._c), _dtype_code(q),
             float(d ** -0.5 if scale is None else scale), *[ctypes.byref(r) for r in rows], ws,
@@ -1031,4 +1032,4 @@ def prepare_cache_attend(cache: PagedCache, batch: Batch, q, out, scale: Optiona
 
 def scd_cache_attend(cache: PagedCache, batch: Batch, q, out, scale: Optional[float] = None,
                      workspace: Optional[torch.Tensor] = None, stream=None) -> None:
-    prepare_cache_attend(cache, batch, q, out, scale, workspace)(stream)
+    prepare_cache_attend(cache, batch, q, out, scale, workspace, stream)(stream)

@@ -112,11 +112,12 @@ __device__ inline int reach_of(int64_t held, int pos0, int token) {
 constexpr int kRowsWorkers = 512;
 constexpr size_t kCounterBytes = kRowsWorkers * sizeof(int);
 
-// Workgroups for a few rows of a request (tiles of 16, 32 or 64 rows): waves of one, and most of a launch.
+// Workgroups for a few rows of a request (tiles of 16 or 32 rows): waves of one, and most of a launch.
 __host__ __device__ constexpr int rows_waves(int rows) { return rows == 16 ? 8 : 4; }
 constexpr int rows_workers(int rows) { return rows == 16 ? kRowsWorkers / 2 : kRowsWorkers; }
 constexpr int kUncutSteps = 4;    // mean steps of a segment up to which it stays whole
 
 constexpr int kPromptWaves = 8, kPromptRows = 32 * kPromptWaves;
+constexpr int kMostSplits = 64;   // shares of a prompt's tile
 
 }  // namespace scd

@@ -21,14 +21,14 @@ static AttendPlan attend_plan(const PagedCache& c, const SeqBatch& b, int group,
   AttendPlan plan{};
   const int64_t requests = b.n_seqs < b.n_tokens ? b.n_seqs : b.n_tokens;
   const int64_t mean = b.n_tokens * group / requests;  // rows of a request and KV head
-  const bool prompt = bf16 && head_dim >= 64 && mean >= kPromptRows;
-  plan.rows = prompt ? kPromptRows : mean <= 16 ? 16 : (mean <= 32 || !bf16) ? 32 : 64;
+  const bool prompt = bf16 && head_dim >= 64 && mean >= kPromptRows / 2;
+  plan.rows = prompt ? kPromptRows : mean <= 16 ? 16 : 32;
   plan.tiles = b.n_tokens * group / plan.rows + requests;
   const int64_t positions = static_cast<int64_t>(c.cols) * c.page, segments = plan.tiles * c.heads;
   const size_t row = static_cast<size_t>(head_dim + 2) * sizeof(float);
   if (prompt) {
     const int64_t most = (positions + 255) / 256, want = (256 + segments - 1) / segments;
-    plan.splits = static_cast<int>(want < most ? want : most);
+    plan.splits = static_cast<int>(std::min<int64_t>(std::min(want, most), kMostSplits));
     if (plan.splits > 1) plan.bytes = kCounterBytes + segments * plan.splits * plan.rows * row;
     return plan;
   }

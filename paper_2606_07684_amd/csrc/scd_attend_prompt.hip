@@ -66,7 +66,7 @@ template <int kByte> __device__ inline uint2 byte_column_as_f16(const uint32_t (
 }
 template <int kDim, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(CacheAttendParams p, int most_splits,
-                                                                            int64_t units, float* partial,
+                                                                            int64_t tiles, float* partial,
                                                                             float* partial_ml) {
   typedef uint16_t T;
   constexpr int kRows = 32 * kWaves, kThreads = 64 * kWaves;
@@ -82,12 +82,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int r = lane & 31, half = lane >> 5;
 
+  const int64_t units = tiles * p.cache.heads * most_splits;
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
     const int h = static_cast<int>(unit % p.cache.heads);
     const int64_t rest = unit / p.cache.heads;
     const int split = static_cast<int>(rest % most_splits);
     Tile t;
-    if (!tile_of<kRows, kThreads>(p, rest / most_splits, locate_lds, tid, t)) return;
+    // the last tiles, which see the most positions, first
+    if (!tile_of<kRows, kThreads>(p, tiles - 1 - rest / most_splits, locate_lds, tid, t)) continue;
     const int64_t last_row = t.row0 + t.rows - 1;
     const int64_t held = positions_held(p.cache);
     int64_t seen = t.pos0 + last_row / p.group + 1;
@@ -409,70 +411,58 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
   }
 }
 
-// Joins the shares of every row that was split: one workgroup per row, its threads over channels
-// (four each) and shares.
-template <typename T, int kDim, int kRows>
-__global__ __launch_bounds__(256) void cache_attend_join_kernel(CacheAttendParams p, int most_splits,
-                                                               int64_t units, const float* partial,
-                                                               const float* partial_ml) {
-  constexpr int kLanes = kDim / 4, kShares = 256 / kLanes;
+// Joins the shares of the tiles that were split: one workgroup per 16 rows, four channels a thread, eight shares
+// on their way at once.
+template <int kDim>
+__global__ __launch_bounds__(256) void cache_attend_join_kernel(CacheAttendParams p, int most_splits, int64_t tiles,
+                                                               const float* partial, const float* partial_ml) {
+  constexpr int kFours = kDim / 4, kParts = kPromptRows / 16, kBatch = 8;
   __shared__ LocateLds locate_lds;
-  __shared__ float4 sums[kShares][kLanes];
-  __shared__ float tops[kShares], totals[kShares];
-  const int tid = threadIdx.x, c = tid % kLanes, share = tid / kLanes;
+  __shared__ float2 ml[kMostSplits][16];
+  const int tid = threadIdx.x;
+  const int64_t units = tiles * p.cache.heads * kParts;
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    const int row = static_cast<int>(unit % kRows);
-    const int h = static_cast<int>(unit / kRows % p.cache.heads);
-    const int64_t index = unit / kRows / p.cache.heads;
+    const int row0 = static_cast<int>(unit % kParts) * 16;
+    const int h = static_cast<int>(unit / kParts % p.cache.heads);
+    const int64_t index = unit / kParts / p.cache.heads;
     Tile t;
-    if (!tile_of<kRows, 256>(p, index, locate_lds, tid, t)) return;
-    if (row >= t.rows) continue;
-    int64_t seen = t.pos0 + (t.row0 + t.rows - 1) / p.group + 1;
-    const int64_t held = positions_held(p.cache);
-    seen = seen < 0 ? 0 : (seen < held ? seen : held);
-    const int splits = splits_of((seen + 31) >> 5, most_splits);
+    if (!tile_of<kPromptRows, 256>(p, index, locate_lds, tid, t)) return;
+    if (row0 >= t.rows) continue;
+    const int splits = splits_of(blocks_to(positions_held(p.cache), static_cast<int>(t.pos0),
+                                           p.by_group.of(static_cast<int>(t.row0) + t.rows - 1)), most_splits);
     if (splits == 1) continue;
-    const int64_t first = (index * most_splits * p.cache.heads + h) * kRows + row;
-    const int64_t step = static_cast<int64_t>(p.cache.heads) * kRows;
-    float top = -INFINITY, total = 0.f;
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s = share; s < splits; s += kShares) {
-      const int64_t at = first + s * step;
-      const float2 ml = *reinterpret_cast<const float2*>(partial_ml + 2 * at);
-      const float4 x = *reinterpret_cast<const float4*>(partial + at * kDim + 4 * c);
-      const float now = fmaxf(top, ml.x), base = now == -INFINITY ? 0.f : now;
-      const float fade = exp2_fast(top - base), w = exp2_fast(ml.x - base);
-      top = now;
-      total = total * fade + ml.y * w;
-      sum.x = sum.x * fade + x.x * w;
-      sum.y = sum.y * fade + x.y * w;
-      sum.z = sum.z * fade + x.z * w;
-      sum.w = sum.w * fade + x.w * w;
-    }
-    sums[share][c] = sum;
-    if (c == 0) {
-      tops[share] = top;
-      totals[share] = total;
-    }
+    const int64_t first = ((tiles - 1 - index) * most_splits * p.cache.heads + h) * kPromptRows + row0;
+    const int64_t step = static_cast<int64_t>(p.cache.heads) * kPromptRows;
+    const int rows = t.rows - row0 < 16 ? t.rows - row0 : 16;
+    for (int i = tid; i < splits * 16; i += 256)
+      if (i % 16 < rows) ml[i / 16][i % 16] = *reinterpret_cast<const float2*>(partial_ml + 2 * (first + i / 16 * step + i % 16));
     __syncthreads();
-    if (share == 0) {
-      float all = tops[0];
-      for (int s = 1; s < kShares; ++s) all = fmaxf(all, tops[s]);
-      const float base = all == -INFINITY ? 0.f : all;
-      float f[4] = {0.f, 0.f, 0.f, 0.f}, l = 0.f;
-      for (int s = 0; s < kShares; ++s) {
-        const float w = exp2_fast(tops[s] - base);
-        l += totals[s] * w;
-        f[0] += sums[s][c].x * w;
-        f[1] += sums[s][c].y * w;
-        f[2] += sums[s][c].z * w;
-        f[3] += sums[s][c].w * w;
+    for (int item = tid; item < rows * kFours; item += 256) {
+      const int row = item / kFours, c = 4 * (item % kFours);
+      float top = -INFINITY;
+      for (int s = 0; s < splits; ++s) top = fmaxf(top, ml[s][row].x);
+      const float base = top == -INFINITY ? 0.f : top;
+      f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+      float l = 0.f;
+      for (int s0 = 0; s0 < splits; s0 += kBatch) {
+        f32x4 v[kBatch];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k)
+          v[k] = *reinterpret_cast<const f32x4*>(partial + (first + (s0 + k < splits ? s0 + k : s0) * step + row) * kDim + c);
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+          const float2 x = ml[s0 + k < splits ? s0 + k : s0][row];
+          const float w = s0 + k < splits ? exp2_fast(x.x - base) : 0.f;
+          l += x.y * w;
+          sum += v[k] * w;
+        }
       }
-      const int64_t token = (t.row0 + row) / p.group;
-      const int head = h * p.group + static_cast<int>(t.row0 + row - token * p.group);
-      T* dst = reinterpret_cast<T*>(p.out.data) + (t.first + token) * p.out.token + head * p.out.head + 4 * c;
+      const int at = static_cast<int>(t.row0) + row0 + row, token = p.by_group.of(at);
+      uint16_t* dst = reinterpret_cast<uint16_t*>(p.out.data) + (t.first + token) * p.out.token +
+                      (h * p.group + at - token * p.group) * p.out.head + c;
       const float inv = l != 0.f ? 1.f / l : 0.f;
-      for (int j = 0; j < 4; ++j) store1(dst + j, f[j] * inv);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) store1(dst + j, sum[j] * inv);
     }
     __syncthreads();
   }
@@ -486,12 +476,11 @@ static hipError_t launch_prompt_as(const CacheAttendParams& p, int64_t tiles, in
   float* ml = workspace + units * kPromptRows * kDim;
   const auto grid = [](int64_t n) { return dim3(static_cast<unsigned>(n < kMaxGrid / 2 ? n : kMaxGrid / 2)); };
   hipLaunchKernelGGL((cache_attend_prompt_kernel<kDim, kPromptWaves>), grid(units), dim3(64 * kPromptWaves), 0,
-                     stream, p, splits, units, workspace, ml);
+                     stream, p, splits, tiles, workspace, ml);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || splits == 1) return e;
-  const int64_t rows = tiles * p.cache.heads * kPromptRows;
-  hipLaunchKernelGGL((cache_attend_join_kernel<uint16_t, kDim, kPromptRows>), grid(rows), dim3(256), 0, stream, p,
-                     splits, rows, workspace, ml);
+  hipLaunchKernelGGL((cache_attend_join_kernel<kDim>), grid(tiles * p.cache.heads * (kPromptRows / 16)), dim3(256), 0,
+                     stream, p, splits, tiles, workspace, ml);
   return hipGetLastError();
 }
 

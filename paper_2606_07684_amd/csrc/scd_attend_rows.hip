@@ -609,8 +609,6 @@ static hipError_t launch_rows_as(const CacheAttendParams& p, const RowsLayout& l
 template <typename T, int kDim>
 static hipError_t launch_rows_dim(int rows, const CacheAttendParams& p, const RowsLayout& layout, float* workspace,
                                   hipStream_t stream) {
-  if constexpr (sizeof(T) == 2)
-    if (rows == 64) return launch_rows_as<T, kDim, 64>(p, layout, workspace, stream);
   return rows == 32 ? launch_rows_as<T, kDim, 32>(p, layout, workspace, stream)
                     : launch_rows_as<T, kDim, 16>(p, layout, workspace, stream);
 }
