@@ -187,9 +187,9 @@ __device__ inline void store_item(int8_t* row, int2 at, float (&x)[16], float in
   }
 }
 
-// Many rows: a workgroup takes one branch (keys or values) of one page, one item of 16 channels a thread, and
-// heads_per of its heads one after another.  A head's rows stay in registers between the maximum and the
-// quantisation, the next head's are on their way meanwhile, and a thread's cosines and sines serve all heads.
+// Many rows: a workgroup takes one page, one item of 16 channels a thread, and pairs_per of its (branch, head)
+// pairs one after another.  A head's rows stay in registers between the maximum and the
+// quantisation, the next two heads' are on their way meanwhile, and a thread's cosines and sines serve all heads.
 // Bound by HBM: rows are read once, in the model's type, and written once, in 8 bits.
 template <typename T, int kDim, int kThreads, TurnKind kKind>
 __device__ inline void append_page(const CacheAppendParams& p, int kv, int first_head, int last_head,
@@ -202,28 +202,36 @@ __device__ inline void append_page(const CacheAppendParams& p, int kv, int first
   float* scales = (kv ? p.cache.v_scale : p.cache.k_scale) + static_cast<int64_t>(r.page) * p.cache.heads;
   const int2 at = item_channels<kKind>(p.turn, item);
   const bool mine = slot >= r.lo && slot < r.hi;
-  RawItem<T> raw;
+  RawItem<T> raw[2];
+  float old[2];
   float2 cs[8];
-  if (mine) {
-    raw.load(row + first_head * rows.head, at, rows.wide);
-    load_pairs<kKind>(p.turn, r.base + slot, item, cs);
-  }
-  float old = r.lo > 0 ? scales[first_head] : 0.f;
-  for (int h = first_head; h < last_head; ++h) {
+  const auto fetch = [&](int h) {
+    if (h >= last_head) return;
+    const int k = (h - first_head) & 1;
+    if (mine) {
+      if (k == 0) raw[0].load(row + h * rows.head, at, rows.wide);
+      else raw[1].load(row + h * rows.head, at, rows.wide);
+    }
+    const float scale = r.lo > 0 ? scales[h] : 0.f;
+    if (k == 0) old[0] = scale;
+    else old[1] = scale;
+  };
+  fetch(first_head);
+  fetch(first_head + 1);
+  if (mine) load_pairs<kKind>(p.turn, r.base + slot, item, cs);
+  const auto append_head = [&](auto which, int h) {
+    constexpr int k = decltype(which)::value;
     float x[16];
     float top = 0.f;
     if (mine) {
-      raw.get(x);
+      raw[k].get(x);
       turn_item<kKind>(p.turn, row, item, cs, nullptr, x);
       top = top_of(x, top);
     }
-    const float held = old;
-    if (h + 1 < last_head) {
-      if (mine) raw.load(row + (h + 1) * rows.head, at, rows.wide);
-      old = r.lo > 0 ? scales[h + 1] : 0.f;
-    }
+    const float held = old[k];
+    fetch(h + 2);
     top = wave_top_of(top);
-    float* tops = wave_top[h & 1];
+    float* tops = wave_top[k];
     if ((tid & 63) == 0) tops[tid >> 6] = top;
     lds_barrier();  // the loads on their way stay so
     float all = tops[0];
@@ -235,25 +243,32 @@ __device__ inline void append_page(const CacheAppendParams& p, int kv, int first
     int8_t* dst = pages + page_at(p.cache, r.page, h, kDim) + slot * kDim;
     if (mine) store_item<kKind>(dst, at, x, inv);
     else if (slot < r.lo && scale > held) requantise(dst + 16 * item, held * inv);
+  };
+  for (int h = first_head; h < last_head; h += 2) {
+    append_head(IntC<0>{}, h);
+    if (h + 1 < last_head) append_head(IntC<1>{}, h + 1);
   }
 }
 
 template <typename T, int kDim, int kThreads, TurnKind kKind>
-__global__ __launch_bounds__(kThreads) void cache_append_pages_kernel(CacheAppendParams p, int heads_per, int shares,
+__global__ __launch_bounds__(kThreads) void cache_append_pages_kernel(CacheAppendParams p, int pairs_per, int shares,
                                                                      int64_t units) {
   __shared__ LocateLds lds;
   __shared__ float wave_top[2][kThreads / 64];
   const int tid = threadIdx.x;
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
-    const int64_t rest = unit >> 1;
-    const int kv = static_cast<int>(unit & 1);
-    const int first_head = static_cast<int>(rest % shares) * heads_per;
-    const int last_head = first_head + heads_per < p.cache.heads ? first_head + heads_per : p.cache.heads;
+    // of the 2 n_kv_heads (branch, head) pairs, keys first
+    const int heads = p.cache.heads, first = static_cast<int>(unit % shares) * pairs_per;
+    const int last = first + pairs_per < 2 * heads ? first + pairs_per : 2 * heads;
     PageRows r;
-    if (!page_rows<kThreads>(p, rest / shares, lds, tid, r)) return;
+    if (!page_rows<kThreads>(p, unit / shares, lds, tid, r)) return;
     if (r.page < 0) continue;
-    if (kv) append_page<T, kDim, kThreads, TurnKind::kNone>(p, kv, first_head, last_head, r, wave_top, tid);
-    else append_page<T, kDim, kThreads, kKind>(p, kv, first_head, last_head, r, wave_top, tid);
+    if (first < heads)
+      append_page<T, kDim, kThreads, kKind>(p, 0, first, last < heads ? last : heads, r, wave_top, tid);
+    if (last > heads) {
+      __syncthreads();
+      append_page<T, kDim, kThreads, TurnKind::kNone>(p, 1, first > heads ? first - heads : 0, last - heads, r, wave_top, tid);
+    }
     __syncthreads();  // wave_top is written again
   }
 }
@@ -376,13 +391,14 @@ template <typename T, int kDim, int kPage, TurnKind kKind>
 static hipError_t launch_append_pages(const CacheAppendParams& p, hipStream_t stream) {
   constexpr int kThreads = kPage * kDim / 16 < 64 ? 64 : kPage * kDim / 16;
   const int64_t pages = pages_bound(p.batch, kPage);
-  // As many heads to a workgroup as leave 1024 workgroups.
-  const int64_t most = pages * 2 * p.cache.heads / 1024;
-  const int heads_per = static_cast<int>(most < 1 ? 1 : (most < p.cache.heads ? most : p.cache.heads));
-  const int shares = (p.cache.heads + heads_per - 1) / heads_per;
-  const int64_t units = pages * shares * 2;
+  // As many pairs to a workgroup as leave 512 workgroups: what a workgroup pays once (finding its page, its rows'
+  // cosines and sines) is about what two pairs cost.
+  const int64_t pairs = 2 * p.cache.heads, most = pages * pairs / 512;
+  const int pairs_per = static_cast<int>(most < 1 ? 1 : (most < pairs ? most : pairs));
+  const int shares = static_cast<int>((pairs + pairs_per - 1) / pairs_per);
+  const int64_t units = pages * shares;
   hipLaunchKernelGGL((cache_append_pages_kernel<T, kDim, kThreads, kKind>), grid_of(units), dim3(kThreads), 0, stream, p,
-                     heads_per, shares, units);
+                     pairs_per, shares, units);
   return hipGetLastError();
 }
 
