@@ -52,12 +52,15 @@ __device__ inline void turn_item(const Turn& turn, const T* row, int item, const
   }
 }
 
-__device__ inline int quantised(float x) {
-  return static_cast<int>(fminf(fmaxf(rintf(x), -127.f), 127.f));
-}
+// Four values of at most 127 in magnitude (and a rounding) rounded to whole numbers, ties to even, as bytes:
+// 1.5 * 2^23 more, a float's last bits are the number's.  The sum must not take the caller's product in.
 __device__ inline uint32_t pack4(const float* f) {
-  return (quantised(f[0]) & 255) | (quantised(f[1]) & 255) << 8 | (quantised(f[2]) & 255) << 16 |
-         static_cast<uint32_t>(quantised(f[3]) & 255) << 24;
+#pragma clang fp contract(off)
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(f[i] + 12582912.f);
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(w[3], w[2], 0x0c0c0400u),
+                               __builtin_amdgcn_perm(w[1], w[0], 0x0c0c0400u), 0x05040100u);
 }
 __device__ inline void unpack4(uint32_t w, float* f) {
   f[0] = static_cast<float>(static_cast<int8_t>(w));
@@ -141,28 +144,30 @@ __device__ inline void load_pairs(const Turn& turn, int64_t pos, int item, float
     }
   }
 }
-// The largest magnitude of 16 values with the largest so far; NaN once one is not finite.
-__device__ inline float top_of(const float (&x)[16], float top) {
-  bool finite = true;
+// Magnitudes are compared as the bits of fp32 less the sign: what is not finite is above all that is.
+__device__ inline uint32_t top_of(const float (&x)[16], uint32_t top) {
 #pragma unroll
   for (int j = 0; j < 16; ++j) {
-    top = fmaxf(top, fabsf(x[j]));
-    finite = finite && fabsf(x[j]) <= 3.40282347e38f;
+    const uint32_t bits = __float_as_uint(x[j]) & 0x7fffffffu;
+    top = bits > top ? bits : top;
   }
-  return finite ? top : __builtin_nanf("");
+  return top;
 }
-__device__ inline float larger_or_nan(float a, float b) { return a > b || a != a ? a : b; }
-__device__ inline float wave_top_of(float top) {
-  const bool finite = __all(top == top);
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-  return finite ? top : __builtin_nanf("");
+__device__ inline uint32_t wave_top_of(uint32_t top) {
+  for (int o = 32; o > 0; o >>= 1) {
+    const uint32_t other = __shfl_xor(top, o);
+    top = other > top ? other : top;
+  }
+  return top;
 }
-// Scale of a page and head that had `held` (0: none) and takes values up to `top`.
-__device__ inline float scale_with(float held, float top) {
-  const float scale = larger_or_nan(top * (1.f / 127.f), held);
+// Scale of a page and head that had `held` (0: none) and takes magnitudes up to that of the bits `top`.
+__device__ inline float scale_with(float held, uint32_t top) {
+  const float a = top < 0x7f800000u ? __uint_as_float(top) * (1.f / 127.f) : __builtin_nanf("");
+  const float scale = a > held || a != a ? a : held;
   return scale < kSmallestScale ? 0.f : scale;
 }
 __device__ inline void requantise(int8_t* at, float ratio) {
+#pragma clang fp contract(off)
   uint4* w = reinterpret_cast<uint4*>(at);
   const uint4 v = *w;
   float f[16];
@@ -176,6 +181,7 @@ __device__ inline void requantise(int8_t* at, float ratio) {
 }
 template <TurnKind kKind>
 __device__ inline void store_item(int8_t* row, int2 at, float (&x)[16], float inv) {
+#pragma clang fp contract(off)
 #pragma unroll
   for (int j = 0; j < 16; ++j) x[j] *= inv;
   const uint4 v = make_uint4(pack4(x), pack4(x + 4), pack4(x + 8), pack4(x + 12));
@@ -193,7 +199,7 @@ __device__ inline void store_item(int8_t* row, int2 at, float (&x)[16], float in
 // Bound by HBM: rows are read once, in the model's type, and written once, in 8 bits.
 template <typename T, int kDim, int kThreads, TurnKind kKind>
 __device__ inline void append_page(const CacheAppendParams& p, int kv, int first_head, int last_head,
-                                   const PageRows& r, float (*wave_top)[kThreads / 64], int tid) {
+                                   const PageRows& r, uint32_t (*wave_top)[kThreads / 64], int tid) {
   constexpr int kItems = kDim / 16;
   const int item = tid % kItems, slot = tid / kItems;
   const Rows& rows = p.rows[kv];
@@ -222,7 +228,7 @@ __device__ inline void append_page(const CacheAppendParams& p, int kv, int first
   const auto append_head = [&](auto which, int h) {
     constexpr int k = decltype(which)::value;
     float x[16];
-    float top = 0.f;
+    uint32_t top = 0;
     if (mine) {
       raw[k].get(x);
       turn_item<kKind>(p.turn, row, item, cs, nullptr, x);
@@ -231,12 +237,12 @@ __device__ inline void append_page(const CacheAppendParams& p, int kv, int first
     const float held = old[k];
     fetch(h + 2);
     top = wave_top_of(top);
-    float* tops = wave_top[k];
+    uint32_t* tops = wave_top[k];
     if ((tid & 63) == 0) tops[tid >> 6] = top;
     lds_barrier();  // the loads on their way stay so
-    float all = tops[0];
+    uint32_t all = tops[0];
 #pragma unroll
-    for (int w = 1; w < kThreads / 64; ++w) all = larger_or_nan(tops[w], all);
+    for (int w = 1; w < kThreads / 64; ++w) all = tops[w] > all ? tops[w] : all;
     const float scale = scale_with(held, all);
     const float inv = scale > 0.f ? 1.f / scale : 0.f;
     if (tid == 0) scales[h] = scale;
@@ -254,7 +260,7 @@ template <typename T, int kDim, int kThreads, TurnKind kKind>
 __global__ __launch_bounds__(kThreads) void cache_append_pages_kernel(CacheAppendParams p, int pairs_per, int shares,
                                                                      int64_t units) {
   __shared__ LocateLds lds;
-  __shared__ float wave_top[2][kThreads / 64];
+  __shared__ uint32_t wave_top[2][kThreads / 64];
   const int tid = threadIdx.x;
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
     // of the 2 n_kv_heads (branch, head) pairs, keys first
@@ -297,7 +303,7 @@ __device__ inline void append_few(const CacheAppendParams& p, int kv, int h, con
   };
   const float held = r.lo > 0 ? *scale_at : 0.f;
   float x[16];
-  float top = 0.f;
+  uint32_t top = 0;
   if (first + lane < last) {
     fetch(first + lane, x);
     top = top_of(x, top);
@@ -305,7 +311,7 @@ __device__ inline void append_few(const CacheAppendParams& p, int kv, int h, con
   for (int i = first + 64 + lane; i < last; i += 64) {
     float y[16];
     fetch(i, y);
-    top = larger_or_nan(top_of(y, 0.f), top);
+    top = top_of(y, top);
   }
   top = wave_top_of(top);
   const float scale = scale_with(held, top);
