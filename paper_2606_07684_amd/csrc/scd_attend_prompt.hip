@@ -239,7 +239,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
       const auto live = [&](int tile) { return chunk + kPromptTokens * tile < wave_end; };
       // Operands are read kReads matrix steps before the one that takes them, in this order: left to itself
       // the compiler keeps one or two and waits for LDS at every step.
-      constexpr int kReads = 6;
+      constexpr int kReads = 4;
       const auto steps = [&](auto count, auto operand, auto step) {
         constexpr int kCount = decltype(count)::value;
         f16x8 a[kReads];
