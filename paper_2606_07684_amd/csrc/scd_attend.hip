@@ -14,7 +14,7 @@ struct AttendPlan {
   int64_t tiles;     // bound
   int splits;        // prompts: most shares of a tile
   int workers;       // a few rows: workgroups
-  int step_log2;     // a few rows: a step is this many doublings of a block for each wave
+  int step_log2;     // a few rows: blocks of a step
   size_t bytes;      // workspace
 };
 static AttendPlan attend_plan(const PagedCache& c, const SeqBatch& b, int group, int head_dim, bool bf16) {
@@ -22,7 +22,7 @@ static AttendPlan attend_plan(const PagedCache& c, const SeqBatch& b, int group,
   const int64_t requests = b.n_seqs < b.n_tokens ? b.n_seqs : b.n_tokens;
   const int64_t mean = b.n_tokens * group / requests;  // rows of a request and KV head
   const bool prompt = bf16 && head_dim >= 64 && mean >= kPromptRows / 2;
-  plan.rows = prompt ? kPromptRows : mean <= 16 ? 16 : 32;
+  plan.rows = prompt ? kPromptRows : kRowTile;
   plan.tiles = b.n_tokens * group / plan.rows + requests;
   const int64_t positions = static_cast<int64_t>(c.cols) * c.page, segments = plan.tiles * c.heads;
   const size_t row = static_cast<size_t>(head_dim + 2) * sizeof(float);
@@ -33,10 +33,10 @@ static AttendPlan attend_plan(const PagedCache& c, const SeqBatch& b, int group,
     return plan;
   }
   const auto steps = [&] { return (positions + (int64_t{32} << plan.step_log2) - 1) >> (5 + plan.step_log2); };
-  plan.step_log2 = rows_waves(plan.rows) == 8 ? 3 : 2;
+  while (1 << plan.step_log2 < kRowWaves) ++plan.step_log2;
   while (segments * steps() >= int64_t{1} << 31 && steps() > 1) ++plan.step_log2;  // the kernel counts in 31 bits
   const int64_t able = steps() <= kUncutSteps ? segments : segments * steps();
-  plan.workers = static_cast<int>(std::min<int64_t>(able, rows_workers(plan.rows)));
+  plan.workers = static_cast<int>(std::min<int64_t>(able, kRowsWorkers));
   if (steps() > kUncutSteps) plan.bytes = kCounterBytes + 2 * plan.workers * plan.rows * row;
   return plan;
 }
@@ -50,7 +50,7 @@ hipError_t launch_cache_attend(bool bf16, int head_dim, const CacheAttendParams&
   const AttendPlan plan = attend_plan(p.cache, p.batch, p.group, head_dim, bf16);
   float* ws = static_cast<float*>(workspace);
   if (plan.rows == kPromptRows) return launch_attend_prompt(head_dim, p, plan.tiles, plan.splits, ws, stream);
-  return launch_attend_rows(bf16, head_dim, plan.rows, p, plan.workers, plan.step_log2, ws, stream);
+  return launch_attend_rows(bf16, head_dim, p, plan.workers, plan.step_log2, ws, stream);
 }
 
 }  // namespace scd

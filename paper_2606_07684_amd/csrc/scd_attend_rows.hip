@@ -17,9 +17,10 @@ struct RowsLayout {
   int step_log2;  // blocks of a step
 };
 
-template <int kRows>
+constexpr int kThreads = 64 * kRowWaves;
+
 __device__ inline int tiles_of(const CacheAttendParams& p, const Request& r) {
-  return ((r.end - r.begin) * p.group + kRows - 1) / kRows;
+  return ((r.end - r.begin) * p.group + kRowTile - 1) / kRowTile;
 }
 __device__ inline int steps_of(const CacheAttendParams& p, const RowsLayout& layout, int64_t held, const Request& r) {
   const int n = (blocks_to(held, r.pos0, r.end - r.begin - 1) + (1 << layout.step_log2) - 1) >> layout.step_log2;
@@ -44,14 +45,13 @@ struct Share {
     return w;
   }
 };
-template <int kThreads> struct ShareLds {
+struct ShareLds {
   int2 wave_sum[kThreads / 64];
   Request request;
   int b, local;
 };
-template <int kRows, int kThreads>
-__device__ inline bool share_of(const CacheAttendParams& p, const RowsLayout& layout, int64_t held,
-                                ShareLds<kThreads>& lds, int tid, Share& s) {
+__device__ inline bool share_of(const CacheAttendParams& p, const RowsLayout& layout, int64_t held, ShareLds& lds,
+                                int tid, Share& s) {
   const int n = p.batch.n_seqs, lane = tid & 63, wave = tid >> 6;
   struct Scan {
     Request request;
@@ -60,7 +60,7 @@ __device__ inline bool share_of(const CacheAttendParams& p, const RowsLayout& la
   const auto scan = [&](int base) {
     Scan c;
     c.request = base + tid < n ? request_at(p.batch, base + tid) : Request{0, 0, 0};
-    c.mine.x = tiles_of<kRows>(p, c.request) * p.cache.heads;
+    c.mine.x = tiles_of(p, c.request) * p.cache.heads;
     c.mine.y = c.mine.x * steps_of(p, layout, held, c.request);
     int2 sum = c.mine;
     for (int o = 1; o < 64; o <<= 1) {
@@ -91,7 +91,7 @@ __device__ inline bool share_of(const CacheAttendParams& p, const RowsLayout& la
   int2 all;
   if (n == 1) {
     c.request = request_at(p.batch, 0);
-    all.x = tiles_of<kRows>(p, c.request) * p.cache.heads;
+    all.x = tiles_of(p, c.request) * p.cache.heads;
     all.y = all.x * steps_of(p, layout, held, c.request);
   } else {
     c = scan(0);
@@ -170,10 +170,9 @@ struct Partials {
 //   is the operand layout of   out^T [d x 16] += V^T P^T   with the positions in that order.
 // The contraction over channels, and the order of the output channels over the matrix rows, are
 // permuted so that every lane reads adjacent bytes.
-template <typename T, int kDim, int kRows>
-__global__ __launch_bounds__(64 * rows_waves(kRows), rows_waves(kRows) / 4) void cache_attend_rows_kernel(
-    CacheAttendParams p, RowsLayout layout, Partials partial) {
-  constexpr int kBlocks = kRows / 16, kWaves = rows_waves(kRows), kThreads = 64 * kWaves;
+template <typename T, int kDim>
+__global__ __launch_bounds__(kThreads, 2) void cache_attend_rows_kernel(CacheAttendParams p, RowsLayout layout,
+                                                                       Partials partial) {
   constexpr int kParts = sizeof(T) == 2 ? 1 : 2;    // of a query element
   constexpr int kWeights = sizeof(T) == 2 ? 2 : 3;  // of a weight
   constexpr int kSteps = kDim / 32;   // matrix steps over channels
@@ -181,9 +180,9 @@ __global__ __launch_bounds__(64 * rows_waves(kRows), rows_waves(kRows) / 4) void
   constexpr int kPitch = kDim + 4;
   constexpr int kPairs = kDim / 2;
   constexpr int kAhead = 1;          // blocks on their way
-  __shared__ ShareLds<kThreads> share_lds;
-  __shared__ float joined[kWaves][16][kPitch];
-  __shared__ float joined_m[kWaves][kRows], joined_l[kWaves][kRows];
+  __shared__ ShareLds share_lds;
+  __shared__ float joined[kRowWaves][16][kPitch];
+  __shared__ float joined_m[kRowWaves][kRowTile], joined_l[kRowWaves][kRowTile];
   __shared__ __attribute__((aligned(16))) float team_sums[kThreads][8];
   __shared__ int arrived;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
@@ -194,16 +193,16 @@ __global__ __launch_bounds__(64 * rows_waves(kRows), rows_waves(kRows) / 4) void
   const int64_t held = positions_held(p.cache);
 
   Share share;
-  if (!share_of<kRows, kThreads>(p, layout, held, share_lds, tid, share)) return;
+  if (!share_of(p, layout, held, share_lds, tid, share)) return;
   int seg_steps = share.cut ? steps_of(p, layout, held, share.request) : 1;
 
   while (true) {
     const int b = share.b, pos0 = share.request.pos0, step = share.step;
     const int step_end = seg_steps - step < share.end - share.unit ? seg_steps : step + share.end - share.unit;
     const int tile = p.by_heads.of(share.segment), h = share.segment - tile * p.cache.heads;
-    const int row0 = tile * kRows;
+    const int row0 = tile * kRowTile;
     const int all_rows = (share.request.end - share.request.begin) * p.group;
-    const int rows = all_rows - row0 < kRows ? all_rows - row0 : kRows;
+    const int rows = all_rows - row0 < kRowTile ? all_rows - row0 : kRowTile;
     const int last_row = row0 + rows - 1;
     const int blocks = blocks_to(held, pos0, p.by_group.of(last_row));
     const int begin = share.cut ? (step << layout.step_log2 < blocks ? step << layout.step_log2 : blocks) : 0;
@@ -211,16 +210,15 @@ __global__ __launch_bounds__(64 * rows_waves(kRows), rows_waves(kRows) / 4) void
     const int free_until = reach_of(held, pos0, p.by_group.of(row0)) + 1;  // positions every row attends to
 
     // queries, as they lie in memory
-    float qx[kBlocks][kSteps][8];
-    int limit[kBlocks];  // last position of the lane's row
-#pragma unroll
-    for (int n = 0; n < kBlocks; ++n) {
-      const int row = row0 + 16 * n + r < last_row ? row0 + 16 * n + r : last_row;
+    float qx[kSteps][8];
+    int limit;  // last position of the lane's row
+    {
+      const int row = row0 + r < last_row ? row0 + r : last_row;
       const int token = p.by_group.of(row), head = h * p.group + row - token * p.group;
       const T* src = reinterpret_cast<const T*>(p.q.data) + (share.request.begin + token) * p.q.token + head * p.q.head + g * (kDim / 4);
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) load8(src + 8 * s, p.q.wide, qx[n][s]);
-      limit[n] = reach_of(held, pos0, token);
+      for (int s = 0; s < kSteps; ++s) load8(src + 8 * s, p.q.wide, qx[s]);
+      limit = reach_of(held, pos0, token);
     }
 
     // Blocks are fetched kAhead ahead of the arithmetic, their pages' numbers another one ahead.
@@ -284,45 +282,39 @@ __global__ __launch_bounds__(64 * rows_waves(kRows), rows_waves(kRows) / 4) void
     if (block < end) {
 #pragma unroll
       for (int i = 0; i < kAhead; ++i)
-        if (block + i * kWaves < end) fetch(ring[i], block + i * kWaves, pages_of(block + i * kWaves));
-      ids = pages_of(block + kAhead * kWaves);
+        if (block + i * kRowWaves < end) fetch(ring[i], block + i * kRowWaves, pages_of(block + i * kRowWaves));
+      ids = pages_of(block + kAhead * kRowWaves);
     }
 
     // queries, lifted and split
-    f16x8 q[kBlocks][kParts][kSteps];
-    float factor[kBlocks];
-#pragma unroll
-    for (int n = 0; n < kBlocks; ++n) {
+    f16x8 q[kParts][kSteps];
+    float factor;
+    {
       float top = 0.f;
 #pragma unroll
       for (int s = 0; s < kSteps; ++s)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(qx[n][s][j]));
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(qx[s][j]));
       top = max_of_quarters(top);
       int e = (__float_as_uint(top) >> 23) & 255;
       e = e < kLift + 1 ? kLift + 1 : (e > 254 ? 254 : e);
       const float lift = __uint_as_float(static_cast<uint32_t>(254 + kLift - e) << 23);
-      factor[n] = __uint_as_float(static_cast<uint32_t>(e - kLift) << 23) * (p.scale * kLog2e);
+      factor = __uint_as_float(static_cast<uint32_t>(e - kLift) << 23) * (p.scale * kLog2e);
 #pragma unroll
       for (int s = 0; s < kSteps; ++s)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const float v = qx[n][s][j] * lift;
+          const float v = qx[s][j] * lift;
           const _Float16 hi = static_cast<_Float16>(v);
-          q[n][0][s][j] = hi;
-          if constexpr (kParts == 2) q[n][1][s][j] = static_cast<_Float16>(v - static_cast<float>(hi));
+          q[0][s][j] = hi;
+          if constexpr (kParts == 2) q[1][s][j] = static_cast<_Float16>(v - static_cast<float>(hi));
         }
     }
 
-    f32x4 acc[kBlocks][kOut];
-    float m[kBlocks], l[kBlocks];
+    f32x4 acc[kOut];
+    float m = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int n = 0; n < kBlocks; ++n) {
-      m[n] = -INFINITY;
-      l[n] = 0.f;
-#pragma unroll
-      for (int c = 0; c < kOut; ++c) acc[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    for (int c = 0; c < kOut; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
 
     const auto attend = [&](const Fetched& fetched, int block) {
       const int at = block << 5;
@@ -331,18 +323,15 @@ __global__ __launch_bounds__(64 * rows_waves(kRows), rows_waves(kRows) / 4) void
       const float (&ks)[2] = fetched.ks;
       const float (&vs)[2] = fetched.vs;
       // scores
-      f32x4 score[kBlocks][2];
+      f32x4 score[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-#pragma unroll
-        for (int n = 0; n < kBlocks; ++n) score[n][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        score[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < kSteps; ++s) {
           const f16x8 k = bytes_as_f16(kw[i][2 * s], kw[i][2 * s + 1]);
 #pragma unroll
-          for (int n = 0; n < kBlocks; ++n)
-#pragma unroll
-            for (int part = 0; part < kParts; ++part) score[n][i] = mfma16(k, q[n][part][s], score[n][i]);
+          for (int part = 0; part < kParts; ++part) score[i] = mfma16(k, q[part][s], score[i]);
         }
       }
       // value scales as f 2^e (e at least kLeastExponent, where f may be below 1 or 0)
@@ -356,64 +345,58 @@ __global__ __launch_bounds__(64 * rows_waves(kRows), rows_waves(kRows) / 4) void
         exponent[i] = static_cast<float>(e - 127);
       }
       const bool masked = at + 32 > free_until || fetched.hole[0] || fetched.hole[1];
-      bf16x8 w[kBlocks][kWeights];
+      const auto hidden = [&](int j) { return fetched.hole[j >> 2] || at + 16 * (j >> 2) + 4 * g + (j & 3) > limit; };
+      float x[8];
 #pragma unroll
-      for (int n = 0; n < kBlocks; ++n) {
-        const auto hidden = [&](int j) { return fetched.hole[j >> 2] || at + 16 * (j >> 2) + 4 * g + (j & 3) > limit[n]; };
-        float x[8];
+      for (int i = 0; i < 2; ++i) {
+        const float f = ks[i] * factor;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const float f = ks[i] * factor[n];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) x[4 * i + j] = fmaf(score[n][i][j], f, exponent[i]);
-        }
-        if (masked) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (hidden(j)) x[j] = -INFINITY;
-        }
-        float top = m[n];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) top = fmaxf(top, x[j]);
-        top = max_of_quarters(top);
-        const float base = top == -INFINITY ? 0.f : top;
-        if (__any(top > m[n])) {
-          const float fade = exp2_fast(m[n] - base);
-          m[n] = top;
-          l[n] *= fade;
-#pragma unroll
-          for (int c = 0; c < kOut; ++c) acc[n][c] *= fade;
-        }
-        float sum[2] = {0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float e = exp2_fast(x[j] - base);
-          sum[j >> 2] += e;
-          x[j] = e * part_scale[j >> 2];
-        }
-        if (masked) {  // nor does a scale that is not a number reach rows that do not see it
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            if (hidden(j)) x[j] = 0.f;
-        }
+        for (int j = 0; j < 4; ++j) x[4 * i + j] = fmaf(score[i][j], f, exponent[i]);
+      }
+      if (masked) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-#pragma unroll
-          for (int k = 0; k < kWeights; ++k) {
-            w[n][k][j] = static_cast<__bf16>(x[j]);
-            x[j] -= static_cast<float>(w[n][k][j]);
-          }
-        l[n] += sum[0] * back[0] + sum[1] * back[1];
+          if (hidden(j)) x[j] = -INFINITY;
       }
+      float top = m;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) top = fmaxf(top, x[j]);
+      top = max_of_quarters(top);
+      const float base = top == -INFINITY ? 0.f : top;
+      if (__any(top > m)) {
+        const float fade = exp2_fast(m - base);
+        m = top;
+        l *= fade;
+#pragma unroll
+        for (int c = 0; c < kOut; ++c) acc[c] *= fade;
+      }
+      float sum[2] = {0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float e = exp2_fast(x[j] - base);
+        sum[j >> 2] += e;
+        x[j] = e * part_scale[j >> 2];
+      }
+      l += sum[0] * back[0] + sum[1] * back[1];
+      if (masked) {  // nor does a scale that is not a number reach rows that do not see it
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (hidden(j)) x[j] = 0.f;
+      }
+      bf16x8 w[kWeights];
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int k = 0; k < kWeights; ++k) {
+          w[k][j] = static_cast<__bf16>(x[j]);
+          x[j] -= static_cast<float>(w[k][j]);
+        }
       // values
       const auto out = [&](auto byte, int word) {
         constexpr int kByte = decltype(byte)::value;
         const bf16x8 v = byte_column_as_bf16<kByte>(vw[word]);
 #pragma unroll
-        for (int n = 0; n < kBlocks; ++n)
-#pragma unroll
-          for (int part = 0; part < kWeights; ++part)
-            acc[n][4 * word + kByte] = mfma16(v, w[n][part], acc[n][4 * word + kByte]);
+        for (int part = 0; part < kWeights; ++part) acc[4 * word + kByte] = mfma16(v, w[part], acc[4 * word + kByte]);
       };
       out(IntC<0>{}, 0);
       out(IntC<1>{}, 0);
@@ -431,17 +414,17 @@ __global__ __launch_bounds__(64 * rows_waves(kRows), rows_waves(kRows) / 4) void
     while (block < end) {
 #pragma unroll
       for (int i = 0; i <= kAhead; ++i) {
-        if (block + kAhead * kWaves < end) {
-          fetch(ring[(i + kAhead) % (kAhead + 1)], block + kAhead * kWaves, ids);
-          ids = pages_of(block + (kAhead + 1) * kWaves);
+        if (block + kAhead * kRowWaves < end) {
+          fetch(ring[(i + kAhead) % (kAhead + 1)], block + kAhead * kRowWaves, ids);
+          ids = pages_of(block + (kAhead + 1) * kRowWaves);
         }
         attend(ring[i], block);
-        block += kWaves;
+        block += kRowWaves;
         if (block >= end) break;
       }
     }
 
-    // join the waves, 16 rows at a time
+    // join the waves
     const bool whole = step == 0 && step_end == seg_steps;
     const int slot = 2 * share.worker + (step == 0);
     const auto store2 = [&](int row, int c, float x, float y) {
@@ -456,54 +439,47 @@ __global__ __launch_bounds__(64 * rows_waves(kRows), rows_waves(kRows) / 4) void
         *reinterpret_cast<float2*>(dst) = make_float2(x, y);
       }
     };
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (g == 0) {
+      joined_m[wave][r] = m;
+      joined_l[wave][r] = l;
+    }
+    lds_barrier();
+    if (r < rows) {
+      float top = joined_m[0][r];
+      for (int v = 1; v < kRowWaves; ++v) top = fmaxf(top, joined_m[v][r]);
+      const float mine = exp2_fast(m - (top == -INFINITY ? 0.f : top));
+      float* dst = joined[wave][r];
 #pragma unroll
-    for (int n = 0; n < kBlocks; ++n) {
-      l[n] += __shfl_xor(l[n], 16);
-      l[n] += __shfl_xor(l[n], 32);
-      if (g == 0) {
-        joined_m[wave][16 * n + r] = m[n];
-        joined_l[wave][16 * n + r] = l[n];
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < kOut; ++c) dst[kOut * (4 * g + i) + c] = acc[c][i] * mine;
+    }
+    lds_barrier();
+    for (int item = tid; item < rows * kPairs; item += kThreads) {
+      const int row = item / kPairs, c = 2 * (item % kPairs);
+      float x = 0.f, y = 0.f, top = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int v = 0; v < kRowWaves; ++v) {
+        const float2 f = *reinterpret_cast<const float2*>(&joined[v][row][c]);
+        x += f.x;
+        y += f.y;
+        top = fmaxf(top, joined_m[v][row]);
+      }
+      const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+      for (int v = 0; v < kRowWaves; ++v) sum += joined_l[v][row] * exp2_fast(joined_m[v][row] - base);
+      if (whole) {
+        const float inv = sum != 0.f ? 1.f / sum : 0.f;
+        store2(row, c, x * inv, y * inv);
+      } else {
+        const int64_t to = static_cast<int64_t>(slot) * kRowTile + row;
+        leave2(partial.rows + to * kDim + c, x, y);
+        if (c == 0) leave2(partial.ml + 2 * to, top, sum);
       }
     }
     lds_barrier();
-#pragma unroll
-    for (int n = 0; n < kBlocks; ++n) {
-      if (16 * n + r < rows) {
-        float top = joined_m[0][16 * n + r];
-        for (int v = 1; v < kWaves; ++v) top = fmaxf(top, joined_m[v][16 * n + r]);
-        const float mine = exp2_fast(m[n] - (top == -INFINITY ? 0.f : top));
-        float* dst = joined[wave][r];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int c = 0; c < kOut; ++c) dst[kOut * (4 * g + i) + c] = acc[n][c][i] * mine;
-      }
-      lds_barrier();
-      const int items = (rows - 16 * n < 16 ? rows - 16 * n : 16) * kPairs;
-      for (int item = tid; item < items; item += kThreads) {
-        const int row = item / kPairs, c = 2 * (item % kPairs);
-        float x = 0.f, y = 0.f, top = -INFINITY, sum = 0.f;
-#pragma unroll
-        for (int v = 0; v < kWaves; ++v) {
-          const float2 f = *reinterpret_cast<const float2*>(&joined[v][row][c]);
-          x += f.x;
-          y += f.y;
-          top = fmaxf(top, joined_m[v][16 * n + row]);
-        }
-        const float base = top == -INFINITY ? 0.f : top;
-#pragma unroll
-        for (int v = 0; v < kWaves; ++v) sum += joined_l[v][16 * n + row] * exp2_fast(joined_m[v][16 * n + row] - base);
-        if (whole) {
-          const float inv = sum != 0.f ? 1.f / sum : 0.f;
-          store2(16 * n + row, c, x * inv, y * inv);
-        } else {
-          const int64_t to = static_cast<int64_t>(slot) * kRows + 16 * n + row;
-          leave2(partial.rows + to * kDim + c, x, y);
-          if (c == 0) leave2(partial.ml + 2 * to, top, sum);
-        }
-      }
-      lds_barrier();
-    }
 
     if (!whole) {
       const int seg_begin = share.unit - step;
@@ -519,9 +495,9 @@ __global__ __launch_bounds__(64 * rows_waves(kRows), rows_waves(kRows) / 4) void
         // Four channels of every row, and where they leave threads over, several threads a four's parts.
         // The parts' maxima and sums go through LDS where it holds them.
         const int parts = last - first + 1;
-        const auto row_from = [&](int i, int row) { return static_cast<int64_t>(2 * (first + i) + (i == 0)) * kRows + row; };
+        const auto row_from = [&](int i, int row) { return static_cast<int64_t>(2 * (first + i) + (i == 0)) * kRowTile + row; };
         float2* const staged = reinterpret_cast<float2*>(&joined[0][0][0]);
-        const bool fits = parts * rows <= kWaves * 16 * kPitch / 2;
+        const bool fits = parts * rows <= kRowWaves * 16 * kPitch / 2;
         if (fits)
           for (int i = tid; i < parts * rows; i += kThreads) {
             const int part = i / rows;
@@ -583,7 +559,7 @@ __global__ __launch_bounds__(64 * rows_waves(kRows), rows_waves(kRows) / 4) void
     share.unit += step_end - step;
     if (share.unit >= share.end) break;
     share.step = 0;
-    if (++share.segment == tiles_of<kRows>(p, share.request) * p.cache.heads) {
+    if (++share.segment == tiles_of(p, share.request) * p.cache.heads) {
       share.segment = 0;
       do {
         if (++share.b >= p.batch.n_seqs) return;
@@ -595,34 +571,27 @@ __global__ __launch_bounds__(64 * rows_waves(kRows), rows_waves(kRows) / 4) void
   }
 }
 
-template <typename T, int kDim, int kRows>
+template <typename T, int kDim>
 static hipError_t launch_rows_as(const CacheAttendParams& p, const RowsLayout& layout, float* workspace, hipStream_t stream) {
   Partials partial;
   partial.count = reinterpret_cast<int*>(workspace);
   partial.rows = workspace + kCounterBytes / sizeof(float);
-  partial.ml = partial.rows + static_cast<int64_t>(2) * layout.most_workers * kRows * kDim;
-  hipLaunchKernelGGL((cache_attend_rows_kernel<T, kDim, kRows>), dim3(layout.most_workers), dim3(64 * rows_waves(kRows)), 0,
-                     stream, p, layout, partial);
+  partial.ml = partial.rows + static_cast<int64_t>(2) * layout.most_workers * kRowTile * kDim;
+  hipLaunchKernelGGL((cache_attend_rows_kernel<T, kDim>), dim3(layout.most_workers), dim3(kThreads), 0, stream, p, layout,
+                     partial);
   return hipGetLastError();
 }
 
-template <typename T, int kDim>
-static hipError_t launch_rows_dim(int rows, const CacheAttendParams& p, const RowsLayout& layout, float* workspace,
-                                  hipStream_t stream) {
-  return rows == 32 ? launch_rows_as<T, kDim, 32>(p, layout, workspace, stream)
-                    : launch_rows_as<T, kDim, 16>(p, layout, workspace, stream);
-}
-
-hipError_t launch_attend_rows(bool bf16, int head_dim, int rows, const CacheAttendParams& p, int workers, int step_log2,
+hipError_t launch_attend_rows(bool bf16, int head_dim, const CacheAttendParams& p, int workers, int step_log2,
                               float* workspace, hipStream_t stream) {
   const RowsLayout layout{workers, step_log2};
   if (bf16)
-    return head_dim == 128 ? launch_rows_dim<uint16_t, 128>(rows, p, layout, workspace, stream)
-           : head_dim == 64 ? launch_rows_dim<uint16_t, 64>(rows, p, layout, workspace, stream)
-                            : launch_rows_dim<uint16_t, 32>(rows, p, layout, workspace, stream);
-  return head_dim == 128 ? launch_rows_dim<float, 128>(rows, p, layout, workspace, stream)
-         : head_dim == 64 ? launch_rows_dim<float, 64>(rows, p, layout, workspace, stream)
-                          : launch_rows_dim<float, 32>(rows, p, layout, workspace, stream);
+    return head_dim == 128 ? launch_rows_as<uint16_t, 128>(p, layout, workspace, stream)
+           : head_dim == 64 ? launch_rows_as<uint16_t, 64>(p, layout, workspace, stream)
+                            : launch_rows_as<uint16_t, 32>(p, layout, workspace, stream);
+  return head_dim == 128 ? launch_rows_as<float, 128>(p, layout, workspace, stream)
+         : head_dim == 64 ? launch_rows_as<float, 64>(p, layout, workspace, stream)
+                          : launch_rows_as<float, 32>(p, layout, workspace, stream);
 }
 
 }  // namespace scd

@@ -99,9 +99,9 @@ hipError_t launch_cache_append(bool bf16, int head_dim, const CacheAppendParams&
                                hipStream_t stream);
 hipError_t launch_cache_read(bool bf16, int head_dim, const CacheReadParams& p, hipStream_t stream);
 
-// A few rows of every request (tiles of 16 or 32 of them) in `workers` workgroups, or whole prompts (bf16,
+// A few rows of every request in `workers` workgroups, steps of 2^step_log2 blocks, or whole prompts (bf16,
 // head_dim 64 or 128) in up to `splits` shares of each of `tiles` tiles and KV head.
-hipError_t launch_attend_rows(bool bf16, int head_dim, int rows, const CacheAttendParams& p, int workers, int step_log2,
+hipError_t launch_attend_rows(bool bf16, int head_dim, const CacheAttendParams& p, int workers, int step_log2,
                               float* workspace, hipStream_t stream);
 hipError_t launch_attend_prompt(int head_dim, const CacheAttendParams& p, int64_t tiles, int splits, float* workspace,
                                 hipStream_t stream);
