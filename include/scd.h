@@ -402,8 +402,8 @@ scd_status_t scd_rotary(const scd_rotary_t* rotary, const scd_batch_t* batch, co
 /* Paged 8-bit cache of one layer.  A page holds page_tokens consecutive positions of one request, for
  * every KV head: k_pages and v_pages are int8 [n_pages, n_kv_heads, page_tokens, head_dim], and a
  * value stands for q * scale with the page's and head's scale in k_scales, v_scales
- * [n_pages, n_kv_heads] (fp32).  page_table [n_seqs, max_pages] (device) names the page of each
- * run of page_tokens positions of each request.  An entry outside [0, n_pages) is a hole: rows
+ * [n_pages, n_kv_heads] (fp32).  page_table [n_seqs, max_pages] (device, aligned to its entries, so
+ * rows of a larger table will do) names the page of each run of page_tokens positions of each request.  An entry outside [0, n_pages) is a hole: rows
  * appended there are dropped, rows read there are zero, and attention leaves its positions out; so
  * are positions from max_pages * page_tokens on and negative ones.  Pages that several requests name
  * (a shared prefix) can be read, and must not be appended to.

@@ -416,7 +416,9 @@ static hipError_t launch_append_kind(const CacheAppendParams& p, hipStream_t str
     if (p.cache.page == 16) return launch_append_pages<T, kDim, 16, kKind>(p, stream);
     if (p.cache.page == 32) return launch_append_pages<T, kDim, 32, kKind>(p, stream);
     if (p.cache.page == 64) return launch_append_pages<T, kDim, 64, kKind>(p, stream);
-    return launch_append_pages<T, kDim, 128, kKind>(p, stream);
+    // fp32 rows of 128 channels would leave 1024 threads no registers
+    if constexpr (sizeof(T) == 4 && kDim == 128) return launch_append_few<T, kDim, kKind>(p, stream);
+    else return launch_append_pages<T, kDim, 128, kKind>(p, stream);
   }
   return hipSuccess;
 }

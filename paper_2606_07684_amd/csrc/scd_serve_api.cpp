@@ -111,11 +111,14 @@ scd_status_t check_cache(const scd_cache_t* c) {
     const void* p;
     const char* name;
   } need[] = {{c->k_pages, "k_pages"}, {c->v_pages, "v_pages"}, {c->k_scales, "k_scales"},
-              {c->v_scales, "v_scales"}, {c->page_table, "page_table"}};
+              {c->v_scales, "v_scales"}};
   for (const auto& n : need) {
     if (n.p == nullptr) return fail(SCD_ERR_NULL, "%s is NULL", n.name);
     if (!aligned16(n.p)) return fail(SCD_ERR_ALIGN, "%s is not 16-byte aligned", n.name);
   }
+  if (c->page_table == nullptr) return fail(SCD_ERR_NULL, "page_table is NULL");
+  if (reinterpret_cast<uintptr_t>(c->page_table) % 4 != 0)
+    return fail(SCD_ERR_ALIGN, "page_table is not aligned to its entries");
   return SCD_OK;
 }
 
