@@ -449,6 +449,8 @@ scd_status_t scd_cache_read(const scd_cache_t* cache, const scd_batch_t* batch, 
  * One token per request and whole prompts are the same call.  Sums, the running maximum and the
  * softmax are fp32.  A row with no position to attend to (a hole at every one) is zero.
  * q [n_tokens, n_heads, head_dim], n_heads a multiple of n_kv_heads; out alike, not overlapping q.
+ * n_tokens * n_heads must be below 2^31 (else SCD_ERR_UNSUPPORTED), and cached positions from 2^31 - 64
+ * on are left out.
  * `workspace` (device, 16-byte aligned, caller-owned) holds
  * scd_cache_attend_workspace_bytes(cache, batch, q.n_heads) bytes; when that is 0 it may be NULL.  Its
  * first SCD_ATTEND_COUNTER_BYTES (or all of it, if less) must be zero before its first use; every call

@@ -20,6 +20,7 @@ If the library is missing the first call raises: there is no fallback path.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import dataclasses
 import os
@@ -822,6 +823,7 @@ def fit_reuse(model: Model, batch: Batch, rope: Optional[RopeTable], branch: int
 # ------------------------------------------------------------------------------------------------
 # Serving the rebuilt cache
 # ------------------------------------------------------------------------------------------------
+ATTEND_COUNTER_BYTES = 2048  # SCD_ATTEND_COUNTER_BYTES: of a workspace, zero before its first use
 _LAYOUTS = {"half": 0, "interleaved": 1}
 _SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "by_parts": 3, "given": 4}
 
@@ -1012,17 +1014,20 @@ def scd_cache_attend_workspace_bytes(cache: PagedCache, batch: Batch, n_q_heads:
 def prepare_cache_attend(cache: PagedCache, batch: Batch, q, out, scale: Optional[float] = None,
                          workspace: Optional[torch.Tensor] = None, stream=None) -> Prepared:
     """Causal attention of rows q [n_tokens, heads, head_dim] over the cache, which holds them
-    already; ``scale`` None: head_dim^-1/2.  ``workspace`` (zero before its first use; every call leaves
-    it ready for the next) None: one of :func:`scd_cache_attend_workspace_bytes` is made, zeroed on
-    ``stream`` (or the current one), which the calls then belong to, and kept with the call."""
+    already; ``scale`` None: head_dim^-1/2.  ``workspace`` (its first ATTEND_COUNTER_BYTES zero before
+    its first use; every call leaves it ready for the next) None: one of
+    :func:`scd_cache_attend_workspace_bytes` is made, zeroed on ``stream`` (or the current one), which
+    the calls then belong to, and kept with the call."""
     lib = load_library()
     _cache_batch(cache, batch)
     d = cache.head_dim
     rows = [_rows(t, n, batch.n_tokens, d, q.dtype) for t, n in ((q, "q"), (out, "out"))]
     if workspace is None:
         nbytes = scd_cache_attend_workspace_bytes(cache, batch, q.shape[1])
-        with torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream), device=q.device)):
-            workspace = torch.zeros(max(nbytes, 16), dtype=torch.uint8, device=q.device)
+        with (contextlib.nullcontext() if stream is None else
+              torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream), device=q.device))):
+            workspace = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=q.device)
+            workspace[:ATTEND_COUNTER_BYTES].zero_()
     ws, nbytes = _workspace_arg(workspace)
     args = (ctypes.byref(cache._c), ctypes.byref(batch._c), _dtype_code(q),
             float(d ** -0.5 if scale is None else scale), *[ctypes.byref(r) for r in rows], ws,

@@ -8,11 +8,9 @@
 //  - scores in fp16: a query row is multiplied by the power of two that brings its largest element to
 //    2^14 (its scores by the inverse).  bf16 rows are then exact down to 2^-28 of that element; fp32
 //    rows are split into two parts (22 bits and their sign).
-//  - sums over values in bf16, the weights split into two parts for bf16 output (16 bits; its own
-//    rounding has 8) and three for fp32: the parts keep the whole exponent range, so a channel in
-//    which the heaviest positions are zero still has its bits.
-//  - a value scale is f 2^e with f in [1, 2).  The running maximum is that of log2 of the weight plus
-//    e, what a position can add to the sum; the softmax's own sum takes the weights times 2^-e.
+//  - a page's value scale goes into the exponent: the running maximum is that of log2 of a position's weight
+//    times its value scale, what it can add to the sum, so weights on the matrix cores are never out of range; the
+//    softmax's own sum takes them divided by the scale again.
 #pragma once
 
 #include "scd_serve_device.h"
@@ -118,6 +116,9 @@ constexpr size_t kCounterBytes = kRowsWorkers * sizeof(int);
 // waves a workgroup join more on the spot, but four, two workgroups a CU, hide one's ends behind the other: 64
 // requests over 16 KV heads of 64 take 111 and 86 us.)
 constexpr int kRowTile = 16, kRowWaves = 4, kUncutSteps = 4;
+// Mean parts of a segment, at most: one workgroup joins them.  (16, 64 and 128 are no faster than the 24 us of one
+// request of 32K positions over 4 heads.)
+constexpr int kMostParts = 32;
 
 constexpr int kPromptWaves = 8, kPromptRows = 32 * kPromptWaves;
 constexpr int kMostSplits = 64;   // shares of a prompt's tile

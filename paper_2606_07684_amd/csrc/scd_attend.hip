@@ -20,13 +20,17 @@ struct AttendPlan {
 static AttendPlan attend_plan(const PagedCache& c, const SeqBatch& b, int group, int head_dim, bool bf16) {
   AttendPlan plan{};
   const int64_t requests = b.n_seqs < b.n_tokens ? b.n_seqs : b.n_tokens;
-  const int64_t mean = b.n_tokens * group / requests;  // rows of a request and KV head
+  // Rows of a request and KV head, on average.  From half a tile of the prompts' kernel on it takes the call (32
+  // tokens of 32 heads over 8 behind 1000: 22 us, and 45 us as a few rows in tiles of 64); it has bf16 rows of 64
+  // and 128 channels only.
+  const int64_t mean = b.n_tokens * group / requests;
   const bool prompt = bf16 && head_dim >= 64 && mean >= kPromptRows / 2;
   plan.rows = prompt ? kPromptRows : kRowTile;
   plan.tiles = b.n_tokens * group / plan.rows + requests;
   const int64_t positions = static_cast<int64_t>(c.cols) * c.page, segments = plan.tiles * c.heads;
   const size_t row = static_cast<size_t>(head_dim + 2) * sizeof(float);
   if (prompt) {
+    // Shares of at least 256 positions, as many as give the chip's 256 CUs a workgroup each.
     const int64_t most = (positions + 255) / 256, want = (256 + segments - 1) / segments;
     plan.splits = static_cast<int>(std::min<int64_t>(std::min(want, most), kMostSplits));
     if (plan.splits > 1) plan.bytes = kCounterBytes + segments * plan.splits * plan.rows * row;
@@ -35,7 +39,7 @@ static AttendPlan attend_plan(const PagedCache& c, const SeqBatch& b, int group,
   const auto steps = [&] { return (positions + (int64_t{32} << plan.step_log2) - 1) >> (5 + plan.step_log2); };
   while (1 << plan.step_log2 < kRowWaves) ++plan.step_log2;
   while (segments * steps() >= int64_t{1} << 31 && steps() > 1) ++plan.step_log2;  // the kernel counts in 31 bits
-  const int64_t able = steps() <= kUncutSteps ? segments : segments * steps();
+  const int64_t able = steps() <= kUncutSteps ? segments : segments * std::min<int64_t>(steps(), kMostParts);
   plan.workers = static_cast<int>(std::min<int64_t>(able, kRowsWorkers));
   if (steps() > kUncutSteps) plan.bytes = kCounterBytes + 2 * plan.workers * plan.rows * row;
   return plan;

@@ -5,12 +5,20 @@
 // workgroup, so requests of any lengths load the chip evenly.  A workgroup that does not hold all of a segment
 // leaves its sums in the workspace, and the last to do so joins them, in the order of the positions, so
 // results do not depend on which is last.  Where segments are short on average they are not cut.
+//
+// Weights are split into two bf16 parts for bf16 output (16 bits; its own rounding has 8) and three for fp32: the
+// parts keep the whole exponent range, so a channel in which the heaviest positions are zero still has its bits.
+//
+// Bound by the pages' bytes where segments are long: one token of 16 requests of 1K to 16K positions, 32 heads over
+// 8 of 128, takes 66 us (295 MB, 4.4 TB/s; a large copy moves 5.2).  Of a wave's 430 instructions a block of 32
+// positions some 180 turn bytes into operands, so with two waves a SIMD arithmetic alone would take about a third of
+// that.  Short contexts are latency: 333 positions of one request take 8.5 us, 2.3 to find the work and fetch
+// its first block, 2.7 for the blocks, 2 to join the waves, the rest the launch.  One request of 32K positions
+// over 4 heads takes 24 us, 7 of them the join of its 128 parts by 4 workgroups.
 #include "scd_attend.h"
 
 namespace scd {
 using namespace dev;
-
-constexpr int kMostParts = 32;    // mean parts of a segment, at most: one workgroup joins them
 
 struct RowsLayout {
   int most_workers;

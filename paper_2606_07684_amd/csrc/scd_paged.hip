@@ -196,7 +196,9 @@ __device__ inline void store_item(int8_t* row, int2 at, float (&x)[16], float in
 // Many rows: a workgroup takes one page, one item of 16 channels a thread, and pairs_per of its (branch, head)
 // pairs one after another.  A head's rows stay in registers between the maximum and the
 // quantisation, the next two heads' are on their way meanwhile, and a thread's cosines and sines serve all heads.
-// Bound by HBM: rows are read once, in the model's type, and written once, in 8 bits.
+// Bound by HBM: rows are read once, in the model's type, and written once, in 8 bits.  8192 rows of 8 heads of 128 in
+// bf16, keys rotated, take 15 us (50 MB, 3.3 TB/s: one round of workgroups, so its start and end weigh); 111,169
+// rows 150 to 175 us (683 MB, 3.9 to 4.5 TB/s).
 template <typename T, int kDim, int kThreads, TurnKind kKind>
 __device__ inline void append_page(const CacheAppendParams& p, int kv, int first_head, int last_head,
                                    const PageRows& r, uint32_t (*wave_top)[kThreads / 64], int tid) {
@@ -280,7 +282,8 @@ __global__ __launch_bounds__(kThreads) void cache_append_pages_kernel(CacheAppen
 }
 
 // A few rows of a page (and any number where rotary_dim is odd in 16s): a wave takes one branch of one page and
-// head, 64 items at a time, first for the maximum and then for the quantisation, the first 64 read once.
+// head, 64 items at a time, first for the maximum and then for the quantisation, the first 64 read once.  Latency:
+// one row of each of 64 requests, 8 heads of 128, takes 5 us, as a workgroup a page 10.
 template <typename T, int kDim, TurnKind kKind>
 __device__ inline void append_few(const CacheAppendParams& p, int kv, int h, const PageRows& r, int lane) {
   constexpr int kItems = kDim / 16;
@@ -342,7 +345,8 @@ __global__ __launch_bounds__(256) void cache_append_few_kernel(CacheAppendParams
   }
 }
 
-// One wave per row: both branches of every head, 16 channels a lane at a time.
+// One wave per row: both branches of every head, 16 channels a lane at a time.  Bound by HBM: 111,169 rows of 8 heads
+// of 128 into bf16 take 145 us (683 MB, 4.7 TB/s).
 template <typename T, int kDim>
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheReadParams p) {
   constexpr int kChunks = kDim / 16;
@@ -410,6 +414,7 @@ static hipError_t launch_append_pages(const CacheAppendParams& p, hipStream_t st
 
 template <typename T, int kDim, TurnKind kKind>
 static hipError_t launch_append_kind(const CacheAppendParams& p, hipStream_t stream) {
+  // Fewer than 8 rows a request would leave most of a page's workgroup idle.
   const int64_t requests = p.batch.n_seqs < p.batch.n_tokens ? p.batch.n_seqs : p.batch.n_tokens;
   if (kKind == TurnKind::kOdd || p.batch.n_tokens < 8 * requests) return launch_append_few<T, kDim, kKind>(p, stream);
   if constexpr (kKind != TurnKind::kOdd) {

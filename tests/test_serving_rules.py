@@ -23,8 +23,8 @@ def _bytes(n_tokens, n_seqs, q_heads, kv_heads=8, head_dim=128, page=64, columns
     (dict(n_tokens=1, n_seqs=1, q_heads=32, columns=8), 0),
     # one more column: 8 segments in 9 .. steps: two slots of 16 rows for each of the workgroups
     (dict(n_tokens=1, n_seqs=1, q_heads=32, columns=9), 2048 + 2 * (8 * 5) * 16 * 130 * 4),
-    # a long table: as many workgroups as a launch has
-    (dict(n_tokens=1, n_seqs=1, q_heads=32, columns=512), 2048 + 2 * 512 * 16 * 130 * 4),
+    # a long table: 32 parts of each segment, or as many workgroups as a launch has
+    (dict(n_tokens=1, n_seqs=1, q_heads=32, columns=512), 2048 + 2 * (8 * 32) * 16 * 130 * 4),
     (dict(n_tokens=64, n_seqs=64, q_heads=32, columns=512), 2048 + 2 * 512 * 16 * 130 * 4),
     (dict(n_tokens=0, n_seqs=1, q_heads=32), 0)])
 def test_workspace_of_a_few_rows(args, want):
