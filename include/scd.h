@@ -403,10 +403,10 @@ scd_status_t scd_rotary(const scd_rotary_t* rotary, const scd_batch_t* batch, co
  * every KV head: k_pages and v_pages are int8 [n_pages, n_kv_heads, page_tokens, head_dim], and a
  * value stands for q * scale with the page's and head's scale in k_scales, v_scales
  * [n_pages, n_kv_heads] (fp32).  page_table [n_seqs, max_pages] (device, aligned to its entries, so
- * rows of a larger table will do) names the page of each run of page_tokens positions of each request.  An entry outside [0, n_pages) is a hole: rows
- * appended there are dropped, rows read there are zero, and attention leaves its positions out; so
- * are positions from max_pages * page_tokens on and negative ones.  Pages that several requests name
- * (a shared prefix) can be read, and must not be appended to.
+ * rows of a larger table will do) names the page of each run of page_tokens positions of each request.
+ * An entry outside [0, n_pages) is a hole: rows appended there are dropped, rows read there are zero,
+ * and attention leaves its positions out; so are positions from max_pages * page_tokens on and negative
+ * ones.  Pages that several requests name (a shared prefix) can be read, and must not be appended to.
  * head_dim 32, 64 or 128; page_tokens 16, 32, 64 or 128. */
 typedef struct {
   int32_t n_pages;

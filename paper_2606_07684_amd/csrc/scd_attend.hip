@@ -20,9 +20,11 @@ struct AttendPlan {
 static AttendPlan attend_plan(const PagedCache& c, const SeqBatch& b, int group, int head_dim, bool bf16) {
   AttendPlan plan{};
   const int64_t requests = b.n_seqs < b.n_tokens ? b.n_seqs : b.n_tokens;
-  // Rows of a request and KV head, on average.  From half a tile of the prompts' kernel on it takes the call (32
-  // tokens of 32 heads over 8 behind 1000: 22 us, and 45 us as a few rows in tiles of 64); it has bf16 rows of 64
-  // and 128 channels only.
+  // Rows of a request and KV head, on average.  From half a tile of the prompts' kernel on it takes the call, where it
+  // has the type and head_dim.  New tokens behind 1000 each, 32 heads over 8 of 128, us as a few rows / as a prompt:
+  //   1 request    8 13.8 / 18.4    16 15.4 / 19.4    32  27.9 / 21.8    64  25.8 / 27.2
+  //   16 requests  8 32.4 / 37.1    16 25.8 / 39.5    32  46.2 / 45.2    64  89.4 / 52.0
+  //   64 requests  8 52.0 / 68.7    16 97.7 / 70.6    32 180.6 / 86.2    64 349.4 / 118.2
   const int64_t mean = b.n_tokens * group / requests;
   const bool prompt = bf16 && head_dim >= 64 && mean >= kPromptRows / 2;
   plan.rows = prompt ? kPromptRows : kRowTile;

@@ -283,7 +283,7 @@ __global__ __launch_bounds__(kThreads) void cache_append_pages_kernel(CacheAppen
 
 // A few rows of a page (and any number where rotary_dim is odd in 16s): a wave takes one branch of one page and
 // head, 64 items at a time, first for the maximum and then for the quantisation, the first 64 read once.  Latency:
-// one row of each of 64 requests, 8 heads of 128, takes 5 us, as a workgroup a page 10.
+// one row of each of 64 requests, 8 heads of 128, takes 5 us.
 template <typename T, int kDim, TurnKind kKind>
 __device__ inline void append_few(const CacheAppendParams& p, int kv, int h, const PageRows& r, int lane) {
   constexpr int kItems = kDim / 16;
@@ -414,9 +414,13 @@ static hipError_t launch_append_pages(const CacheAppendParams& p, hipStream_t st
 
 template <typename T, int kDim, TurnKind kKind>
 static hipError_t launch_append_kind(const CacheAppendParams& p, hipStream_t stream) {
-  // Fewer than 8 rows a request would leave most of a page's workgroup idle.
+  // Few rows leave most of a page's workgroup idle, many keep a head's one wave at its page for long.  Rotated bf16
+  // rows of 8 heads of 128 in pages of 64, us as a wave a head / a workgroup a page:
+  //   1 request    16 rows 5.1 / 5.1    32 rows 5.9 / 5.1     64 rows 7.6 / 5.2
+  //   16 requests  16 rows 5.7 / 6.4    32 rows 6.8 / 7.7    128 rows 11.5 / 9.1
+  //   64 requests  16 rows 6.1 / 8.7    32 rows 8.6 / 12.0   128 rows 18.3 / 18.6
   const int64_t requests = p.batch.n_seqs < p.batch.n_tokens ? p.batch.n_seqs : p.batch.n_tokens;
-  if (kKind == TurnKind::kOdd || p.batch.n_tokens < 8 * requests) return launch_append_few<T, kDim, kKind>(p, stream);
+  if (kKind == TurnKind::kOdd || p.batch.n_tokens < 32 * requests) return launch_append_few<T, kDim, kKind>(p, stream);
   if constexpr (kKind != TurnKind::kOdd) {
     if (p.cache.page == 16) return launch_append_pages<T, kDim, 16, kKind>(p, stream);
     if (p.cache.page == 32) return launch_append_pages<T, kDim, 32, kKind>(p, stream);

@@ -131,6 +131,21 @@ def test_append_few_and_many_rows(lens, held, heads):
     check_append(cache, before, table, cu, held, (kx, f64(v)))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,held,size", [([32, 31], [0, 50], 64), ([32, 32], [5, 60], 64), ([31], [17], 16),
+                                            ([140, 1, 1, 1, 1], [9, 0, 63, 64, 3], 64), ([150], [5], 128)])
+def test_append_on_both_sides_of_32_rows_a_request(dtype, lens, held, size):
+    table, n_pages = table_of(np.random.default_rng(5), lens, held, size)
+    cache = make_cache(3, size, 128, n_pages, table)
+    batch, cu = batch_of(lens, held)
+    k, v = (randn(s, sum(lens), 3, 128).to(DT[dtype]) for s in (1, 2))
+    turns = scd.scd_rotary_table(scd.Rotary(128, 5e5), 1000)
+    before = state(cache)
+    scd.scd_cache_append(cache, batch, k, v, turns)
+    kx = O.rotate(f64(k), positions(lens, held), O.frequencies(128, 5e5))
+    check_append(cache, before, table, cu, held, (kx, f64(v)))
+
+
 def test_append_of_a_long_batch_reads_back():
     """Enough pages that a workgroup takes several heads of both branches, ragged, against the append of every
     request alone."""
