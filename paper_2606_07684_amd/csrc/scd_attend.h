@@ -110,12 +110,12 @@ __device__ inline int reach_of(int64_t held, int pos0, int token) {
 constexpr int kRowsWorkers = 512;
 constexpr size_t kCounterBytes = kRowsWorkers * sizeof(int);
 
-// A few rows of a request: rows of a tile, waves of a workgroup, and mean steps of a segment up to which it stays
-// whole.  (Tiles of 32 and 64 rows halve the conversions but leave one wave a SIMD its registers: 64 requests of 5
-// rows over 8 KV heads of 128 and up to 4K positions take 136 us in tiles of 32 and 122 us in tiles of 16.  Eight
-// waves a workgroup join more on the spot, but four, two workgroups a CU, hide one's ends behind the other: 64
-// requests over 16 KV heads of 64 take 111 and 86 us.)
-constexpr int kRowTile = 16, kRowWaves = 4, kUncutSteps = 4;
+// A few rows of a request: rows of a tile, waves of a workgroup, steps of the longest segment up to which all stay
+// whole, and workgroups whose parts cost a step to leave and join.  (Tiles of 32 and 64 rows halve the conversions but
+// leave one wave a SIMD its registers: 64 requests of 5 rows over 8 KV heads of 128 and up to 4K positions take 136 us
+// in tiles of 32 and 122 us in tiles of 16.  Eight waves a workgroup join more on the spot, but four, two workgroups a
+// CU, hide one's ends behind the other: 64 requests over 16 KV heads of 64 take 111 and 86 us.)
+constexpr int kRowTile = 16, kRowWaves = 4, kUncutSteps = 4, kWorkersAStep = 40;
 // Mean parts of a segment, at most: one workgroup joins them.  (16, 64 and 128 are no faster than the 24 us of one
 // request of 32K positions over 4 heads.)
 constexpr int kMostParts = 32;

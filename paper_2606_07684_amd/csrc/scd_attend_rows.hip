@@ -4,7 +4,7 @@
 // tile of query rows and a KV head.  All steps, one segment after another, are cut into equal shares, one a
 // workgroup, so requests of any lengths load the chip evenly.  A workgroup that does not hold all of a segment
 // leaves its sums in the workspace, and the last to do so joins them, in the order of the positions, so
-// results do not depend on which is last.  Where segments are short on average they are not cut.
+// results do not depend on which is last.  Where that would cost more than it evens out, segments stay whole.
 //
 // Weights are split into two bf16 parts for bf16 output (16 bits; its own rounding has 8) and three for fp32: the
 // parts keep the whole exponent range, so a channel in which the heaviest positions are zero still has its bits.
@@ -55,6 +55,7 @@ struct Share {
 };
 struct ShareLds {
   int2 wave_sum[kThreads / 64];
+  int wave_longest[kThreads / 64];
   Request request;
   int b, local;
 };
@@ -64,25 +65,33 @@ __device__ inline bool share_of(const CacheAttendParams& p, const RowsLayout& la
   struct Scan {
     Request request;
     int2 mine, first, all;  // segments and steps: of this thread's request, before it, of all threads'
+    int longest;            // steps of a segment of any of them, at most
   };
   const auto scan = [&](int base) {
     Scan c;
     c.request = base + tid < n ? request_at(p.batch, base + tid) : Request{0, 0, 0};
     c.mine.x = tiles_of(p, c.request) * p.cache.heads;
-    c.mine.y = c.mine.x * steps_of(p, layout, held, c.request);
+    const int steps = steps_of(p, layout, held, c.request);
+    c.mine.y = c.mine.x * steps;
     int2 sum = c.mine;
+    int longest = c.mine.x > 0 ? steps : 0;
     for (int o = 1; o < 64; o <<= 1) {
-      const int x = __shfl_up(sum.x, o), y = __shfl_up(sum.y, o);
+      const int x = __shfl_up(sum.x, o), y = __shfl_up(sum.y, o), z = __shfl_up(longest, o);
       if (lane >= o) {
+        longest = max(longest, z);
         sum.x += x;
         sum.y += y;
       }
     }
     __syncthreads();  // the last round's readers are done
-    if (lane == 63) lds.wave_sum[wave] = sum;
+    if (lane == 63) {
+      lds.wave_sum[wave] = sum;
+      lds.wave_longest[wave] = longest;
+    }
     __syncthreads();
     c.first = make_int2(sum.x - c.mine.x, sum.y - c.mine.y);
     c.all = make_int2(0, 0);
+    c.longest = 0;
 #pragma unroll
     for (int w = 0; w < kThreads / 64; ++w) {
       const int2 v = lds.wave_sum[w];
@@ -92,31 +101,46 @@ __device__ inline bool share_of(const CacheAttendParams& p, const RowsLayout& la
       }
       c.all.x += v.x;
       c.all.y += v.y;
+      c.longest = max(c.longest, lds.wave_longest[w]);
     }
     return c;
   };
   Scan c;
   int2 all;
+  int longest;
   if (n == 1) {
     c.request = request_at(p.batch, 0);
     all.x = tiles_of(p, c.request) * p.cache.heads;
-    all.y = all.x * steps_of(p, layout, held, c.request);
+    longest = steps_of(p, layout, held, c.request);
+    all.y = all.x * longest;
   } else {
     c = scan(0);
     all = c.all;
+    longest = c.longest;
     for (int base = kThreads; base < n; base += kThreads) {
       c = scan(base);
       all.x += c.all.x;
       all.y += c.all.y;
+      longest = max(longest, c.longest);
     }
   }
   all.x = uniform(all.x);
   all.y = uniform(all.y);
-  s.cut = all.y > kUncutSteps * static_cast<int64_t>(all.x);
+  longest = uniform(longest);
+  const int64_t parts = kMostParts * static_cast<int64_t>(all.x);
+  const int able = static_cast<int>(parts < layout.most_workers ? parts : layout.most_workers);
+  if (able < 1) return false;
+  // Whole segments take the longest of them (several, if a workgroup has as many); shares the mean, and what leaving
+  // and joining them costs, about two steps and one more for every 40 workgroups that do.  Tokens of requests with as
+  // many positions each, 32 heads over 8, us whole / cut:
+  //   1 of 1    600 11.3 / 9.7     1000 14.8 / 10.5               4 of 4    600 13.0 / 14.5    1000 16.8 / 16.2
+  //   16 of 16  600 12.3 / 26.6    1000 17.3 / 24.0    2000 27.0 / 28.6
+  //   8 of 16   600 13.3 / 30.6    1000 18.5 / 32.4    2000 28.8 / 39.9    4000 47.8 / 54.4
+  const int64_t whole = static_cast<int64_t>((all.x + layout.most_workers - 1) / layout.most_workers) * longest;
+  const int sharers = able < all.y ? able : all.y;
+  s.cut = longest > kUncutSteps && whole > all.y / sharers + 2 + sharers / kWorkersAStep;
   s.total = s.cut ? all.y : all.x;
-  const int64_t able = s.cut ? kMostParts * static_cast<int64_t>(all.x) : s.total;
-  s.workers = static_cast<int>(able < layout.most_workers ? able : layout.most_workers);
-  s.workers = s.workers < s.total ? s.workers : s.total;
+  s.workers = able < s.total ? able : s.total;
   s.worker = blockIdx.x;
   if (s.worker >= s.workers) return false;
   s.each = s.total / s.workers;

@@ -116,6 +116,21 @@ def test_captured_attention_grows_into_cut_segments():
         check_attend(cache, [1, 1], [s + grow for s in start], table, q, "bf16")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,held", [
+    ([2] * 16, [590 + i for i in range(16)]),           # 128 segments of 5 steps: whole
+    ([4] * 16, [100 * i for i in range(16)]),           # ragged, up to 13 steps: whole
+    ([1] * 40 + [2], [20 + i for i in range(40)] + [9000]),  # one long among short ones: cut, into many parts
+    ([1] * 70, [120] * 69 + [700]),                     # segments of one step, the longest 6: whole
+    ([0, 3, 0, 0], [9, 4000, 7, 8000])])                # the longest has no new token
+def test_uneven_requests_whole_and_cut(dtype, lens, held):
+    """Both sides of the rule between whole segments and equal shares, uneven requests among them."""
+    table, n_pages = table_of(np.random.default_rng(4), lens, held, 32)
+    cache = make_cache(4, 32, 64, n_pages, table, seed=3)
+    q = (randn(8, sum(lens), 16, 64) * 2).to(DT[dtype])
+    check_attend(cache, lens, held, table, q, dtype)
+
+
 @pytest.mark.parametrize("lens,held", [([8, 7], [0, 3]), ([8, 8], [5, 60]), ([1] * 7 + [60], [0] * 8), ([700], [33])])
 @pytest.mark.parametrize("heads", [1, 3, 8])
 def test_append_few_and_many_rows(lens, held, heads):
