@@ -21,10 +21,13 @@ static AttendPlan attend_plan(const PagedCache& c, const SeqBatch& b, int group,
   AttendPlan plan{};
   const int64_t requests = b.n_seqs < b.n_tokens ? b.n_seqs : b.n_tokens;
   // Rows of a request and KV head, on average.  From half a tile of the prompts' kernel on it takes the call, where it
-  // has the type and head_dim.  New tokens behind 1000 each, 32 heads over 8 of 128, us as a few rows / as a prompt:
-  //   1 request    8 13.8 / 18.4    16 15.4 / 19.4    32  27.9 / 21.8    64  25.8 / 27.2
-  //   16 requests  8 32.4 / 37.1    16 25.8 / 39.5    32  46.2 / 45.2    64  89.4 / 52.0
-  //   64 requests  8 52.0 / 68.7    16 97.7 / 70.6    32 180.6 / 86.2    64 349.4 / 118.2
+  // has the type and head_dim.  New tokens of each request, 32 heads over 8 of 128, us as a few rows / as a prompt:
+  //   1 request behind  1000   8 14.0 / 18.4   16 15.8 / 19.4   32  17.0 / 21.8   64  17.3 / 27.2
+  //   1 request behind  8000                                    32  42.3 / 36.0   64  56.4 / 41.8
+  //   1 request behind 30000                                    32  81.3 / 52.8   64 127.9 / 86.8
+  //   16 requests, 1000        8 19.3 / 37.1   16 26.4 / 39.5   32  47.6 / 45.2   64  89.1 / 52.0
+  //   64 requests, 1000        8 52.7 / 68.7   16 97.1 / 70.6   32 182.1 / 86.2   64 350.5 / 118.2
+  // What a request holds already is known on the device only, so it is not part of the rule.
   const int64_t mean = b.n_tokens * group / requests;
   const bool prompt = bf16 && head_dim >= 64 && mean >= kPromptRows / 2;
   plan.rows = prompt ? kPromptRows : kRowTile;
