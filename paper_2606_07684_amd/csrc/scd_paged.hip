@@ -213,6 +213,7 @@ __device__ inline void append_page(const CacheAppendParams& p, int kv, int first
   RawItem<T> raw[2];
   float old[2];
   float2 cs[8];
+  float scale_before = 0.f;
   const auto fetch = [&](int h) {
     if (h >= last_head) return;
     const int k = (h - first_head) & 1;
@@ -247,7 +248,10 @@ __device__ inline void append_page(const CacheAppendParams& p, int kv, int first
     for (int w = 1; w < kThreads / 64; ++w) all = tops[w] > all ? tops[w] : all;
     const float scale = scale_with(held, all);
     const float inv = scale > 0.f ? 1.f / scale : 0.f;
-    if (tid == 0) scales[h] = scale;
+    // A head's scale is stored a barrier late: a wave that has no new rows of the page comes to this one with its load
+    // of the old scale on its way still, but not to the next, before which it needs it.
+    if (tid == 0 && h > first_head) scales[h - 1] = scale_before;
+    scale_before = scale;
     int8_t* dst = pages + page_at(p.cache, r.page, h, kDim) + slot * kDim;
     if (mine) store_item<kKind>(dst, at, x, inv);
     else if (slot < r.lo && scale > held) requantise(dst + 16 * item, held * inv);
@@ -256,6 +260,8 @@ __device__ inline void append_page(const CacheAppendParams& p, int kv, int first
     append_head(IntC<0>{}, h);
     if (h + 1 < last_head) append_head(IntC<1>{}, h + 1);
   }
+  lds_barrier();  // and wave_top is written again
+  if (tid == 0) scales[last_head - 1] = scale_before;
 }
 
 template <typename T, int kDim, int kThreads, TurnKind kKind>
@@ -273,11 +279,8 @@ __global__ __launch_bounds__(kThreads) void cache_append_pages_kernel(CacheAppen
     if (r.page < 0) continue;
     if (first < heads)
       append_page<T, kDim, kThreads, kKind>(p, 0, first, last < heads ? last : heads, r, wave_top, tid);
-    if (last > heads) {
-      __syncthreads();
+    if (last > heads)
       append_page<T, kDim, kThreads, TurnKind::kNone>(p, 1, first > heads ? first - heads : 0, last - heads, r, wave_top, tid);
-    }
-    __syncthreads();  // wave_top is written again
   }
 }
 
