@@ -151,8 +151,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
       for (int i = 0; i < 16; ++i) acc[c][i] = 0.f;
     float m = -INFINITY, l = 0.f;
 
-    for (int chunk = begin; chunk < end; chunk += 16 * kListed) {
-      const int chunk_end = chunk + 16 * kListed < end ? chunk + 16 * kListed : end;
+    for (int chunk = begin, chunk_end; chunk < end; chunk = chunk_end) {
+      chunk_end = end - chunk < 16 * kListed ? end : chunk + 16 * kListed;  // no further: end may be close to 2^31
       const int tiles = (chunk_end - chunk + kPromptTokens - 1) / kPromptTokens;
       // pages and scales of the chunk's groups; a hole, and what lies past the end, weighs nothing
       for (int i = tid; i < 4 * tiles; i += kThreads) {

@@ -28,7 +28,7 @@ struct RowsLayout {
 constexpr int kThreads = 64 * kRowWaves;
 
 __device__ inline int tiles_of(const CacheAttendParams& p, const Request& r) {
-  return ((r.end - r.begin) * p.group + kRowTile - 1) / kRowTile;
+  return static_cast<int>((static_cast<uint32_t>((r.end - r.begin) * p.group) + kRowTile - 1) / kRowTile);
 }
 __device__ inline int steps_of(const CacheAttendParams& p, const RowsLayout& layout, int64_t held, const Request& r) {
   const int n = (blocks_to(held, r.pos0, r.end - r.begin - 1) + (1 << layout.step_log2) - 1) >> layout.step_log2;
@@ -259,7 +259,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_rows_kernel(CacheAtt
       int* const out[2] = {&id.x, &id.y};
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int col = ((block << 5) + 16 * i) >> p.cache.page_log2;
+        // in groups of 16 positions: a block looked up ahead may begin past 31 bits
+        const int col = (2 * block + i) >> (p.cache.page_log2 - 4);
         *out[i] = col < p.cache.cols ? table[static_cast<int64_t>(b) * p.cache.cols + col] : -1;
       }
       return id;
