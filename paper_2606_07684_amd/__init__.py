@@ -324,6 +324,13 @@ def _stream(stream) -> Optional[int]:
     return stream.cuda_stream
 
 
+def _torch_stream(stream, device) -> torch.cuda.Stream:
+    """A stream given as ``_stream`` takes it.  The default stream is 0, of which ExternalStream would
+    make a stream of its own, in no order with it."""
+    raw = _stream(stream)
+    return torch.cuda.ExternalStream(raw, device=device) if raw else torch.cuda.default_stream(device)
+
+
 def _ptr_array(tensors, n_layers: int, name: str, shapes: dict, dtype) -> ctypes.Array:
     """Host array of device pointers for one per-layer argument (None entries -> NULL)."""
     if tensors is None:
@@ -1024,8 +1031,7 @@ def prepare_cache_attend(cache: PagedCache, batch: Batch, q, out, scale: Optiona
     rows = [_rows(t, n, batch.n_tokens, d, q.dtype) for t, n in ((q, "q"), (out, "out"))]
     if workspace is None:
         nbytes = scd_cache_attend_workspace_bytes(cache, batch, q.shape[1])
-        with (contextlib.nullcontext() if stream is None else
-              torch.cuda.stream(torch.cuda.ExternalStream(_stream(stream), device=q.device))):
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(_torch_stream(stream, q.device)):
             workspace = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=q.device)
             workspace[:ATTEND_COUNTER_BYTES].zero_()
     ws, nbytes = _workspace_arg(workspace)
