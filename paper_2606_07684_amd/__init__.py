@@ -959,6 +959,19 @@ def scd_rotary_table(rotary: Rotary, max_position: int, device=None, stream=None
     return RotaryTable(buf, int(max_position), rotary)
 
 
+def _turns_args(table: RotaryTable):
+    """Arguments of a table large enough for its max_position: the library reads
+    max_position * rotary_dim / 2 (cos, sin) pairs from it."""
+    buf = table.buffer
+    if not isinstance(buf, torch.Tensor) or not buf.is_cuda or not buf.is_contiguous():
+        raise ValueError("rotary table buffer must be a contiguous CUDA tensor")
+    need = int(load_library().scd_rotary_table_bytes(ctypes.byref(table.rotary._c), int(table.max_position)))
+    if need == 0 or buf.numel() * buf.element_size() < need:
+        raise ValueError(f"rotary table holds {buf.numel() * buf.element_size()} bytes; "
+                         f"max_position {table.max_position} needs {need}")
+    return ctypes.byref(table.rotary._c), buf.data_ptr(), int(table.max_position)
+
+
 def prepare_rotary(table: RotaryTable, batch: Batch, q, k, q_out, k_out,
                    transpose: bool = False) -> Prepared:
     """q_out = R(p) q, k_out = R(p) k for rows [n_tokens, heads, head_dim] (k, k_out may be None);
@@ -967,8 +980,8 @@ def prepare_rotary(table: RotaryTable, batch: Batch, q, k, q_out, k_out,
     d, T = table.rotary.head_dim, batch.n_tokens
     rows = [None if t is None else _rows(t, n, T, d, q.dtype)
             for t, n in ((q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out"))]
-    args = (ctypes.byref(table.rotary._c), ctypes.byref(batch._c), table.buffer.data_ptr(),
-            table.max_position, _dtype_code(q), 1 if transpose else 0,
+    rotary, turns, maxp = _turns_args(table)
+    args = (rotary, ctypes.byref(batch._c), turns, maxp, _dtype_code(q), 1 if transpose else 0,
             *[None if r is None else ctypes.byref(r) for r in rows])
     return Prepared(lib.scd_rotary, args, (table, batch, rows, q, k, q_out, k_out))
 
@@ -986,10 +999,7 @@ def prepare_cache_append(cache: PagedCache, batch: Batch, k, v,
     _cache_batch(cache, batch)
     rows = [_rows(t, n, batch.n_tokens, cache.head_dim, k.dtype) for t, n in ((k, "k"), (v, "v"))]
     args = (ctypes.byref(cache._c), ctypes.byref(batch._c), _dtype_code(k),
-            *[ctypes.byref(r) for r in rows],
-            None if table is None else ctypes.byref(table.rotary._c),
-            None if table is None else table.buffer.data_ptr(),
-            0 if table is None else table.max_position)
+            *[ctypes.byref(r) for r in rows], *((None, None, 0) if table is None else _turns_args(table)))
     return Prepared(lib.scd_cache_append, args, (cache, batch, table, rows, k, v))
 
 
