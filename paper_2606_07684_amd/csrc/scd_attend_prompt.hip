@@ -45,9 +45,10 @@ __device__ inline int splits_of(int64_t blocks, int most) {
 // One workgroup per tile of 32 kWaves query rows, KV head and share of the positions.  64 positions at
 // a time are converted to fp16 once, into LDS (keys as rows, values transposed), and every wave takes
 // them for its 32 rows: scores^T [64 x 32] = K Q^T, then out^T [d x 32] += V^T P^T on 32 x 32 x 16
-// matrix steps, the weights going from the one to the other in registers.  Weights are one fp16 part
-// of 11 bits (2^kPromptLift is the largest; below 2^-24 of that they lose bits), and the softmax's sum
-// takes them as rounded, so their rounding has no bias.
+// matrix steps, the weights going from the one to the other in registers.  The softmax's sum takes the weights
+// in fp32.  The values' take them as one fp16 part: 11 bits, rounded to the nearest, which is finer than the
+// output's own 8 and needs one matrix step; 2^kPromptLift is the largest, and below 2^-25 of that a weight
+// (times its value scale, so what it can add to the output) loses bits.
 //
 // Bound by the vector units beside the matrix cores: per 64 positions a SIMD's two waves take 2048 cycles of matrix
 // steps, about 3000 of exponentials, conversions and maxima, and the CU's LDS 2600 of reads and stores; taking turns
@@ -333,9 +334,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
           u32x4 packed;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const auto pair = __builtin_amdgcn_cvt_pkrtz(score[i >> 1][8 * (i & 1) + 2 * j], score[i >> 1][8 * (i & 1) + 2 * j + 1]);
-            packed[j] = __builtin_bit_cast(uint32_t, pair);
-            sum = __builtin_amdgcn_fdot2(pair, decltype(pair){1, 1}, sum, false);
+            const float a = score[i >> 1][8 * (i & 1) + 2 * j], b = score[i >> 1][8 * (i & 1) + 2 * j + 1];
+            packed[j] = __builtin_bit_cast(uint32_t, f16x2{static_cast<_Float16>(a), static_cast<_Float16>(b)});
+            sum += a + b;
           }
           w[i] = __builtin_bit_cast(f16x8, packed);
           if (sum != 0.f) l = fmaf(sum, back[i], l);
