@@ -9,8 +9,8 @@
 //    2^14 (its scores by the inverse).  bf16 rows are then exact down to 2^-28 of that element; fp32
 //    rows are split into two parts (22 bits and their sign).
 //  - a page's value scale goes into the exponent: the running maximum is that of log2 of a position's weight
-//    times its value scale, what it can add to the sum, so weights on the matrix cores are never out of range; the
-//    softmax's own sum takes them divided by the scale again.
+//    times its value scale, what it can add to the output, so the weights that add most to it have all their bits on the
+//    matrix cores whatever the scales; the softmax's own sum takes them divided by the scale again.
 #pragma once
 
 #include "scd_serve_device.h"
@@ -29,6 +29,7 @@ constexpr int kLeastExponent = -90;  // of a value scale: 2^90 times 2^31 positi
 
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ inline float uniform(float x) { return __int_as_float(uniform(__float_as_int(x))); }
 // The larger of x and the other half-wave's x.
 __device__ inline float max_of_halves(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -75,6 +76,16 @@ template <int kByte> __device__ inline bf16x8 byte_column_as_bf16(const uint32_t
     r[i] = __builtin_amdgcn_perm(__float_as_uint(byte_as_f32<kByte>(w[2 * i + 1])),
                                  __float_as_uint(byte_as_f32<kByte>(w[2 * i])), 0x07060302u);
   return __builtin_bit_cast(bf16x8, r);
+}
+
+// What a share of a row's positions leaves for the join beside its own output: its sum l 2^n, as an exponent and a
+// fraction in [1/2, 1) (or 0), so that weights of shares are at most 1 whatever their sizes.
+__device__ inline float2 part_sum(float n, float l) {
+  return make_float2(n + static_cast<float>(__builtin_amdgcn_frexp_expf(l)), __builtin_amdgcn_frexp_mantf(l));
+}
+// Base of the exponents of shares, `top` the largest: shares of weights of 1 / most at most cannot exceed the largest of them.
+__device__ inline float join_base(float top, int most) {
+  return (top == -INFINITY ? 0.f : top) + static_cast<float>(32 - __builtin_clz(most - 1));
 }
 
 // Positions the page table can name (cut off where positions would pass 31 bits).

@@ -45,8 +45,8 @@ __device__ inline int splits_of(int64_t blocks, int most) {
 // One workgroup per tile of 32 kWaves query rows, KV head and share of the positions.  64 positions at
 // a time are converted to fp16 once, into LDS (keys as rows, values transposed), and every wave takes
 // them for its 32 rows: scores^T [64 x 32] = K Q^T, then out^T [d x 32] += V^T P^T on 32 x 32 x 16
-// matrix steps, the weights going from the one to the other in registers.  The softmax's sum takes the weights
-// in fp32.  The values' take them as one fp16 part: 11 bits, rounded to the nearest, which is finer than the
+// matrix steps, the weights going from the one to the other in registers.  The softmax's sum is
+// fp32.  The values take their weights as one fp16 part: 11 bits, rounded to the nearest, which is finer than the
 // output's own 8 and needs one matrix step; 2^kPromptLift is the largest, and below 2^-25 of that a weight
 // (times its value scale, so what it can add to the output) loses bits.
 //
@@ -56,6 +56,10 @@ __device__ inline int splits_of(int64_t blocks, int most) {
 // TFLOP/s, where a library product of 8192^3 reaches 1175.
 constexpr int kPromptLift = 11;   // the running maximum may lag by kPromptSlack: 2^15 fits fp16
 constexpr float kPromptSlack = 4.f;
+// The softmax's sum of a chunk is taken of the weights that the values take, divided by the value scales, where these are
+// less than 2^kAlike apart (and from the loudest page of earlier chunks): a position that fp32's range leaves out is then
+// below 2^-57 of the heaviest.  Otherwise, and where a scale is 0, the sum is of exponentials of its own.
+constexpr float kAlike = 40.f;
 constexpr int kPromptTokens = 64;
 constexpr int kListed = 1024;     // groups of 16 positions whose pages and scales are held in LDS
 
@@ -73,7 +77,7 @@ template <int kByte> __device__ inline uint2 byte_column_as_f16(const uint32_t (
 template <int kDim, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(CacheAttendParams p, int most_splits,
                                                                             int64_t tiles, float* partial,
-                                                                            float* partial_ml) {
+                                                                            float* partial_sum) {
   typedef uint16_t T;
   constexpr int kRows = 32 * kWaves, kThreads = 64 * kWaves;
   constexpr int kSteps = kDim / 16, kOut = kDim / 32;
@@ -83,7 +87,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
   __shared__ LocateLds locate_lds;
   __shared__ _Float16 keys[2][kPromptTokens][kPitchK];
   __shared__ _Float16 values[2][kDim][kPitchV];
-  __shared__ float4 scales[kListed];   // of keys; log2 and inverse of that of values
+  __shared__ float4 scales[kListed];   // of keys; log2 of that of values, and its inverse to the loudest; -inf for a hole
+  __shared__ float2 range[kWaves];
   __shared__ int64_t places[kListed];  // byte of a group's first position, in either branch's pages
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   const int r = lane & 31, half = lane >> 5;
@@ -150,28 +155,49 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
     for (int c = 0; c < kOut; ++c)
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[c][i] = 0.f;
-    float m = -INFINITY, l = 0.f;
+    float m = -INFINITY;           // base of the weights: log2 of a weight times its value scale
+    float n = -INFINITY, l = 0.f;  // the softmax's sum, l 2^n, but for the present chunk's
+    float l_even = 0.f;            // that of the present chunk, l_even 2^(m - loudest), if its pages are alike
 
     for (int chunk = begin, chunk_end; chunk < end; chunk = chunk_end) {
       chunk_end = end - chunk < 16 * kListed ? end : chunk + 16 * kListed;  // no further: end may be close to 2^31
       const int tiles = (chunk_end - chunk + kPromptTokens - 1) / kPromptTokens;
-      // pages and scales of the chunk's groups; a hole, and what lies past the end, weighs nothing
+      // Pages and scales of the chunk's groups; a hole, and what lies past the end, weighs nothing.  Nor do values of a
+      // scale of 0 (the least other one is 2^-126), which still have their part in the sum.
+      float least = INFINITY, most = -INFINITY;
       for (int i = tid; i < 4 * tiles; i += kThreads) {
         const int pos = chunk + 16 * i;
-        float4 scale = make_float4(0.f, -INFINITY, 0.f, 0.f);
+        float4 scale = make_float4(0.f, -INFINITY, 0.f, -INFINITY);
         int page = pos < chunk_end ? page_of(p.cache, t.b, pos) : -1;
         if (page >= 0) {
           const int64_t at = static_cast<int64_t>(page) * p.cache.heads + h;
-          float vs = p.cache.v_scale[at];
-          vs = vs < 7.8886091e-31f ? 7.8886091e-31f : vs;  // 2^-100: 2^27 positions fit the sum
-          scale = make_float4(p.cache.k_scale[at], __builtin_amdgcn_logf(vs), 1.f / vs, 0.f);
+          const float vs = p.cache.v_scale[at];
+          scale = make_float4(p.cache.k_scale[at], vs < 1.17549435e-38f ? -INFINITY : __builtin_amdgcn_logf(vs), 0.f, 0.f);
+          least = scale.y > -INFINITY ? fminf(least, scale.y) : -INFINITY;  // nor is one that is not a number like others
+          most = fmaxf(most, scale.y);
         } else {
           page = 0;
         }
         scales[i] = scale;
         places[i] = page_at(p.cache, page, h, kDim) + (pos & (p.cache.page - 1)) * kDim;
       }
+      for (int o = 32; o > 0; o >>= 1) {
+        least = fminf(least, __shfl_xor(least, o));
+        most = fmaxf(most, __shfl_xor(most, o));
+      }
+      if (lane == 0) range[wave] = make_float2(least, most);
       __syncthreads();
+      for (int i = 0; i < kWaves; ++i) {
+        least = fminf(least, range[i].x);
+        most = fmaxf(most, range[i].y);
+      }
+      const float loudest = uniform(most);
+      const bool alike = loudest - uniform(least) < kAlike;
+      for (int i = tid; i < 4 * tiles; i += kThreads)
+        if (alike && scales[i].w == 0.f) scales[i].z = exp2_fast(loudest - scales[i].y);
+      __syncthreads();
+      // and rows whose weights have the base of an earlier chunk's far louder pages
+      const bool even = alike && !__any(m - n - loudest > kAlike);
 
       // Raw bytes on their way to LDS: keys of one tile, values of the one before it.
       uint4 kraw[kLoads];
@@ -301,6 +327,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
               if (32 * i + 8 * (j >> 2) + (j & 3) > shown) score[i][j] = with;
         };
         if (masked) hide(-INFINITY);
+        if (__builtin_expect(!even, 0)) {  // the softmax's sum by exponentials of its own
+          float top = n;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 8 * (i & 1); j < 8 * (i & 1) + 8; ++j)
+              if (score[i >> 1][j] > -INFINITY) top = fmaxf(top, fmaf(score[i >> 1][j], f[i], scales[4 * tile + i].w));
+          if (top > -INFINITY) {
+            l *= exp2_fast(n - top);
+            n = top;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int j = 8 * (i & 1); j < 8 * (i & 1) + 8; ++j)
+                if (score[i >> 1][j] > -INFINITY) l += exp2_fast(fmaf(score[i >> 1][j], f[i], scales[4 * tile + i].w) - n);
+          }
+        }
         float top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -314,7 +357,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
           const float now = fmaxf(m, top);
           const float fade = exp2_fast(m - (now == -INFINITY ? 0.f : now));
           m = now;
-          l *= fade;
+          l_even *= fade;
 #pragma unroll
           for (int c = 0; c < kOut; ++c)
 #pragma unroll
@@ -339,7 +382,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
             sum += a + b;
           }
           w[i] = __builtin_bit_cast(f16x8, packed);
-          if (sum != 0.f) l = fmaf(sum, back[i], l);
+          if (sum != 0.f) l_even = fmaf(sum, back[i], l_even);
         }
       };
 
@@ -376,24 +419,38 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
         slot_end();
       }
       if (!second) slot_end();
+      if (even && l_even != 0.f) {
+        const float alone = m - loudest, now = fmaxf(n, alone);
+        l = l * exp2_fast(n - now) + l_even * (1.f / (1 << kPromptLift)) * exp2_fast(alone - now);
+        n = now;
+      }
+      l_even = 0.f;
       __syncthreads();
     }
 
+    // out = acc 2^(m - n - kPromptLift) / l, in two steps as the power may be out of range
+    const float both = max_of_halves(n);
+    if (both > -INFINITY) l *= exp2_fast(n - both);
     l += __shfl_xor(l, 32);
+    const float power = both > -INFINITY ? exp2_fast(0.5f * (m - both - kPromptLift)) : 0.f;
+    const float inv = l != 0.f ? power / l : 0.f;
+#pragma unroll
+    for (int c = 0; c < kOut; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[c][i] = acc[c][i] * inv * power;
     const int64_t row = t.row0 + 32 * wave + r;
     if (row <= last_row) {
       if (splits == 1) {
         const int64_t token = row / p.group;
         const int head = h * p.group + static_cast<int>(row - token * p.group);
         T* dst = reinterpret_cast<T*>(p.out.data) + (t.first + token) * p.out.token + head * p.out.head;
-        const float inv = l != 0.f ? 1.f / l : 0.f;
 #pragma unroll
         for (int c = 0; c < kOut; ++c)
 #pragma unroll
           for (int a = 0; a < 4; ++a) {
             const int at = 32 * c + 8 * a + 4 * half;
-            const uint2 v = make_uint2(pack_bf16x2(acc[c][4 * a] * inv, acc[c][4 * a + 1] * inv),
-                                       pack_bf16x2(acc[c][4 * a + 2] * inv, acc[c][4 * a + 3] * inv));
+            const uint2 v = make_uint2(pack_bf16x2(acc[c][4 * a], acc[c][4 * a + 1]),
+                                       pack_bf16x2(acc[c][4 * a + 2], acc[c][4 * a + 3]));
             if (p.out.wide) {
               *reinterpret_cast<uint2*>(dst + at) = v;
             } else {
@@ -411,7 +468,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
           for (int a = 0; a < 4; ++a)
             *reinterpret_cast<float4*>(partial + at * kDim + 32 * c + 8 * a + 4 * half) =
                 make_float4(acc[c][4 * a], acc[c][4 * a + 1], acc[c][4 * a + 2], acc[c][4 * a + 3]);
-        if (half == 0) *reinterpret_cast<float2*>(partial_ml + 2 * at) = make_float2(m, l);
+        if (half == 0) *reinterpret_cast<float2*>(partial_sum + 2 * at) = part_sum(both, l);
       }
     }
   }
@@ -421,10 +478,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
 // on their way at once.
 template <int kDim>
 __global__ __launch_bounds__(256) void cache_attend_join_kernel(CacheAttendParams p, int most_splits, int64_t tiles,
-                                                               const float* partial, const float* partial_ml) {
+                                                               const float* partial, const float* partial_sum) {
   constexpr int kFours = kDim / 4, kParts = kPromptRows / 16, kBatch = 8;
   __shared__ LocateLds locate_lds;
-  __shared__ float2 ml[kMostSplits][16];
+  __shared__ float2 sums[kMostSplits][16];
   const int tid = threadIdx.x;
   const int64_t units = tiles * p.cache.heads * kParts;
   for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
@@ -441,13 +498,14 @@ __global__ __launch_bounds__(256) void cache_attend_join_kernel(CacheAttendParam
     const int64_t step = static_cast<int64_t>(p.cache.heads) * kPromptRows;
     const int rows = t.rows - row0 < 16 ? t.rows - row0 : 16;
     for (int i = tid; i < splits * 16; i += 256)
-      if (i % 16 < rows) ml[i / 16][i % 16] = *reinterpret_cast<const float2*>(partial_ml + 2 * (first + i / 16 * step + i % 16));
+      if (i % 16 < rows)
+        sums[i / 16][i % 16] = *reinterpret_cast<const float2*>(partial_sum + 2 * (first + i / 16 * step + i % 16));
     __syncthreads();
     for (int item = tid; item < rows * kFours; item += 256) {
       const int row = item / kFours, c = 4 * (item % kFours);
       float top = -INFINITY;
-      for (int s = 0; s < splits; ++s) top = fmaxf(top, ml[s][row].x);
-      const float base = top == -INFINITY ? 0.f : top;
+      for (int s = 0; s < splits; ++s) top = fmaxf(top, sums[s][row].x);
+      const float base = join_base(top, kMostSplits);
       f32x4 sum = {0.f, 0.f, 0.f, 0.f};
       float l = 0.f;
       for (int s0 = 0; s0 < splits; s0 += kBatch) {
@@ -457,9 +515,9 @@ __global__ __launch_bounds__(256) void cache_attend_join_kernel(CacheAttendParam
           v[k] = *reinterpret_cast<const f32x4*>(partial + (first + (s0 + k < splits ? s0 + k : s0) * step + row) * kDim + c);
 #pragma unroll
         for (int k = 0; k < kBatch; ++k) {
-          const float2 x = ml[s0 + k < splits ? s0 + k : s0][row];
-          const float w = s0 + k < splits ? exp2_fast(x.x - base) : 0.f;
-          l += x.y * w;
+          const float2 x = sums[s0 + k < splits ? s0 + k : s0][row];
+          const float w = s0 + k < splits ? x.y * exp2_fast(x.x - base) : 0.f;
+          l += w;
           sum += v[k] * w;
         }
       }
@@ -479,14 +537,14 @@ static hipError_t launch_prompt_as(const CacheAttendParams& p, int64_t tiles, in
                                    hipStream_t stream) {
   const int64_t units = tiles * p.cache.heads * splits;
   workspace += kCounterBytes / sizeof(float);  // the counts of the other kernel stay zero
-  float* ml = workspace + units * kPromptRows * kDim;
+  float* sums = workspace + units * kPromptRows * kDim;
   const auto grid = [](int64_t n) { return dim3(static_cast<unsigned>(n < kMaxGrid / 2 ? n : kMaxGrid / 2)); };
   hipLaunchKernelGGL((cache_attend_prompt_kernel<kDim, kPromptWaves>), grid(units), dim3(64 * kPromptWaves), 0,
-                     stream, p, splits, tiles, workspace, ml);
+                     stream, p, splits, tiles, workspace, sums);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || splits == 1) return e;
   hipLaunchKernelGGL((cache_attend_join_kernel<kDim>), grid(tiles * p.cache.heads * (kPromptRows / 16)), dim3(256), 0,
-                     stream, p, splits, tiles, workspace, ml);
+                     stream, p, splits, tiles, workspace, sums);
   return hipGetLastError();
 }
 

@@ -107,6 +107,70 @@ def test_wide_ranges(dtype, d, lens, held, scale):
     check(cache, table, lens, held, q, dtype, scale, prompt=prompt)
 
 
+@pytest.mark.parametrize("dtype,d,lens,held", SHAPES[4:])
+@pytest.mark.parametrize("loud", [1e6, 1e15, 1e25, 1e35])
+def test_pages_of_zeros_beside_loud_ones(dtype, d, lens, held, loud):
+    cache, table, q, prompt = world(dtype, d, lens, held)
+    for b in range(2):
+        cache.v_scales[ints(table[b, 0::3]).long()] *= loud
+        ids = ints(table[b, 1::3]).long()
+        cache.v_scales[ids] = 0.0
+        cache.v_pages[ids] = 0
+    check(cache, table, lens, held, q, dtype, prompt=prompt)
+
+
+@pytest.mark.parametrize("dtype,d,lens,held", SHAPES)
+@pytest.mark.parametrize("power", [-118, -110, -100, 60, 110])
+def test_scales_near_the_ends_of_their_range(dtype, d, lens, held, power):
+    """All values of about 2^power: their scales have no ordinary page beside them."""
+    cache, table, q, prompt = world(dtype, d, lens, held)
+    cache.v_scales.mul_(2.0 ** (power // 2)).mul_(2.0 ** (power - power // 2))
+    check(cache, table, lens, held, q, dtype, prompt=prompt)
+
+
+@pytest.mark.parametrize("dtype,tokens,kv_heads,heads,zeros,ordinary", [
+    ("bf16", 2048, 8, 32, 19000, 2500),    # prompts, no shares: a workgroup goes over all positions
+    ("bf16", 64, 1, 8, 600000, 1500),      # prompts in 64 shares
+    ("bf16", 1, 8, 32, 40000, 100), ("f32", 1, 2, 2, 300000, 77)])
+def test_many_positions_of_zeros(dtype, tokens, kv_heads, heads, zeros, ordinary):
+    """A long run of pages of zeros (scale 0) in front of ordinary ones; scores rise by just under 4 log2 units after the
+    first 64 positions, so that every position weighs 15 times what the first ones do."""
+    size, d, total = 64, 64, zeros // 64 * 64 + ordinary
+    n_pages = -(-total // size)
+    table = np.random.default_rng(2).permutation(n_pages)[None]
+    cache = make_cache(kv_heads, size, d, n_pages, table, seed=3)
+    cache.k_pages.zero_()
+    cache.k_pages[..., 0] = 1
+    cache.k_pages[int(table[0, 0]), :, :, 0] = 0
+    cache.k_scales.fill_(3.9 * float(np.log(2.0)))
+    ids = ints(table[0, :zeros // size]).long()
+    cache.v_pages[ids] = 0
+    cache.v_scales[ids] = 0.0
+    q = randn(8, tokens, heads, d).to(DT[dtype])
+    q[..., 0] = 1.0
+    rows = sorted({0, tokens // 3, tokens - 1})
+    check(cache, table, [tokens], [total - tokens], q, dtype, scale=1.0, rows=rows, prompt=tokens > 1)
+
+
+@pytest.mark.parametrize("dtype,tokens,kv_heads,heads", [("bf16", 2048, 8, 32)])
+@pytest.mark.parametrize("gains", [(1.0, 1e18, 1.0), (1e18, 1.0, 0.0), (0.0, 1.0, 1e-18), (1.0, 0.0, 1.0), (1e18, 1.0, 1e18)])
+def test_long_runs_of_pages_far_apart(dtype, tokens, kv_heads, heads, gains):
+    """Value scales that change every 16384 positions, as many as a workgroup of the prompts' kernel lists at once."""
+    size, d, run = 64, 64, 16384
+    total = 3 * run - 1000
+    n_pages = -(-total // size)
+    table = np.random.default_rng(2).permutation(n_pages)[None]
+    cache = make_cache(kv_heads, size, d, n_pages, table, seed=3)
+    for i, gain in enumerate(gains):
+        ids = ints(table[0, i * run // size:(i + 1) * run // size]).long()
+        cache.v_scales[ids] *= gain
+        if gain == 0.0:
+            cache.v_pages[ids] = 0
+    q = randn(8, tokens, heads, d).to(DT[dtype])
+    rows = sorted({0, tokens // 3, tokens - 1})
+    check(cache, table, [tokens], [total - tokens], q, dtype, rows=rows, prompt=tokens > 1)
+
+
 @pytest.mark.parametrize("dtype,lens,held", [("bf16", [90, 80, 100], [100, 64, 3]), ("bf16", [90, 80, 100], [400, 64, 3]),
                                              ("bf16", [5, 40, 1], [100, 96, 3]), ("f32", [90, 80, 100], [100, 64, 3])])
 def test_nan_stays_with_the_rows_that_see_it(dtype, lens, held):
