@@ -187,14 +187,19 @@ __device__ inline void leave2(float* p, float a, float b) {
 }
 __device__ inline float2 take2(const float* p) { return *reinterpret_cast<const float2*>(p); }
 
-// Sums a workgroup leaves for a row that it does not finish: rows of two slots a worker (0: of a segment that
-// began before its share, 1: of one that goes on after it), then their maxima and sums, then a count a worker
-// of the parts left of the segment that begins in its share.  Counts are 0 between calls.
+// What a workgroup leaves of a row that it does not finish: rows of two slots a worker (0: of a segment that
+// began before its share, 1: of one that goes on after it), outputs of their own positions, then their softmax's sums
+// (part_sum), then a count a worker of the parts left of the segment that begins in its share.  Counts are 0 between calls.
 struct Partials {
   float* rows;
-  float* ml;
+  float* sums;
   int* count;
 };
+
+// Powers of two that the value scales of a part's pages may lie from the first one's for the softmax's sum to be taken of the
+// weights that the values take, divided by the scales: a position that fp32's range leaves out is then below 2^-77 of the
+// heaviest.  Otherwise the sum is of exponentials of its own.
+constexpr int kNear = 24;
 
 // The waves take a step's blocks straight from the pages into registers in the layout of the
 // matrix operands, so no value passes through LDS:
@@ -214,7 +219,8 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_rows_kernel(CacheAtt
   constexpr int kAhead = 1;          // blocks on their way
   __shared__ ShareLds share_lds;
   __shared__ float joined[kRowWaves][16][kPitch];
-  __shared__ float joined_m[kRowWaves][kRowTile], joined_l[kRowWaves][kRowTile];
+  __shared__ float joined_m[kRowWaves][kRowTile];
+  __shared__ float2 joined_sum[kRowWaves][kRowTile];
   __shared__ __attribute__((aligned(16))) float team_sums[kThreads][8];
   __shared__ int arrived;
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
@@ -229,17 +235,17 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_rows_kernel(CacheAtt
   int seg_steps = share.cut ? steps_of(p, layout, held, share.request) : 1;
 
   while (true) {
-    const int b = share.b, pos0 = share.request.pos0, step = share.step;
+    const int b = uniform(share.b), pos0 = share.request.pos0, step = share.step;
     const int step_end = seg_steps - step < share.end - share.unit ? seg_steps : step + share.end - share.unit;
-    const int tile = p.by_heads.of(share.segment), h = share.segment - tile * p.cache.heads;
+    const int tile = uniform(p.by_heads.of(share.segment)), h = uniform(share.segment - tile * p.cache.heads);
     const int row0 = tile * kRowTile;
     const int all_rows = (share.request.end - share.request.begin) * p.group;
     const int rows = all_rows - row0 < kRowTile ? all_rows - row0 : kRowTile;
     const int last_row = row0 + rows - 1;
     const int blocks = blocks_to(held, pos0, p.by_group.of(last_row));
     const int begin = share.cut ? (step << layout.step_log2 < blocks ? step << layout.step_log2 : blocks) : 0;
-    const int end = share.cut && step_end << layout.step_log2 < blocks ? step_end << layout.step_log2 : blocks;
-    const int free_until = reach_of(held, pos0, p.by_group.of(row0)) + 1;  // positions every row attends to
+    const int end = uniform(share.cut && step_end << layout.step_log2 < blocks ? step_end << layout.step_log2 : blocks);
+    const int free_until = uniform(reach_of(held, pos0, p.by_group.of(row0)) + 1);  // positions every row attends to
 
     // queries, as they lie in memory
     float qx[kSteps][8];
@@ -309,7 +315,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_rows_kernel(CacheAtt
         }
       }
     };
-    int block = begin + wave;
+    int block = uniform(begin) + wave;
     Fetched ring[kAhead + 1];
     int2 ids;
     if (block < end) {
@@ -345,7 +351,11 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_rows_kernel(CacheAtt
     }
 
     f32x4 acc[kOut];
-    float m = -INFINITY, l = 0.f;
+    float m = -INFINITY;      // running maximum of log2 of a weight times its value scale
+    float n = -INFINITY;      // the softmax's sum is l 2^(m - own), or l 2^n once the pages' value scales are far apart
+    float l = 0.f;
+    int own = 0;              // a value scale's (biased) exponent that the others are near
+    bool apart = false;
 #pragma unroll
     for (int c = 0; c < kOut; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
 
@@ -369,13 +379,22 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_rows_kernel(CacheAtt
       }
       // value scales as f 2^e (e at least kLeastExponent, where f may be below 1 or 0)
       float part_scale[2], exponent[2], back[2];
+      bool far = false;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        int e = (__float_as_uint(vs[i]) >> 23) & 255;
+        int e = (uniform(__float_as_int(vs[i])) >> 23) & 255;
         e = e < 127 + kLeastExponent ? 127 + kLeastExponent : (e > 253 ? 253 : e);
-        back[i] = __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
-        part_scale[i] = vs[i] * back[i];
+        part_scale[i] = vs[i] * __uint_as_float(static_cast<uint32_t>(254 - e) << 23);
         exponent[i] = static_cast<float>(e - 127);
+        const bool hole = uniform(fetched.hole[i]);
+        own = own == 0 && !hole ? e : own;
+        const int off = hole ? 0 : e - own;
+        far = far || static_cast<unsigned>(off + kNear) > 2 * kNear;
+        back[i] = __uint_as_float(static_cast<uint32_t>(127 - off) << 23);
+      }
+      if (__builtin_expect(far && !apart, 0)) {
+        apart = true;
+        n = m - static_cast<float>(own - 127);
       }
       const bool masked = at + 32 > free_until || fetched.hole[0] || fetched.hole[1];
       const auto hidden = [&](int j) { return fetched.hole[j >> 2] || at + 16 * (j >> 2) + 4 * g + (j & 3) > limit; };
@@ -391,6 +410,19 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_rows_kernel(CacheAtt
         for (int j = 0; j < 8; ++j)
           if (hidden(j)) x[j] = -INFINITY;
       }
+      if (__builtin_expect(apart, 0)) {  // the softmax's sum by exponentials of its own
+        float top = n;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (x[j] > -INFINITY) top = fmaxf(top, score[j >> 2][j & 3] * (ks[j >> 2] * factor));
+        if (top > -INFINITY) {
+          l *= exp2_fast(n - top);
+          n = top;
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            if (x[j] > -INFINITY) l += exp2_fast(score[j >> 2][j & 3] * (ks[j >> 2] * factor) - n);
+        }
+      }
       float top = m;
 #pragma unroll
       for (int j = 0; j < 8; ++j) top = fmaxf(top, x[j]);
@@ -399,7 +431,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_rows_kernel(CacheAtt
       if (__any(top > m)) {
         const float fade = exp2_fast(m - base);
         m = top;
-        l *= fade;
+        l = apart ? l : l * fade;
 #pragma unroll
         for (int c = 0; c < kOut; ++c) acc[c] *= fade;
       }
@@ -410,7 +442,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_rows_kernel(CacheAtt
         sum[j >> 2] += e;
         x[j] = e * part_scale[j >> 2];
       }
-      l += sum[0] * back[0] + sum[1] * back[1];
+      if (!apart) l += sum[0] * back[0] + sum[1] * back[1];
       if (masked) {  // nor does a scale that is not a number reach rows that do not see it
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -472,11 +504,18 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_rows_kernel(CacheAtt
         *reinterpret_cast<float2*>(dst) = make_float2(x, y);
       }
     };
+    if (apart) {
+      const float all = max_of_quarters(n);
+      l *= exp2_fast(n - (all == -INFINITY ? 0.f : all));
+      n = all;
+    } else if (m > -INFINITY) {
+      n = m - static_cast<float>(own - 127);
+    }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
     if (g == 0) {
       joined_m[wave][r] = m;
-      joined_l[wave][r] = l;
+      joined_sum[wave][r] = make_float2(n, l);
     }
     lds_barrier();
     if (r < rows) {
@@ -492,24 +531,32 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_rows_kernel(CacheAtt
     lds_barrier();
     for (int item = tid; item < rows * kPairs; item += kThreads) {
       const int row = item / kPairs, c = 2 * (item % kPairs);
-      float x = 0.f, y = 0.f, top = -INFINITY, sum = 0.f;
+      float x = 0.f, y = 0.f, top = -INFINITY, sum_top = -INFINITY, sum = 0.f;
 #pragma unroll
       for (int v = 0; v < kRowWaves; ++v) {
         const float2 f = *reinterpret_cast<const float2*>(&joined[v][row][c]);
         x += f.x;
         y += f.y;
         top = fmaxf(top, joined_m[v][row]);
+        sum_top = fmaxf(sum_top, joined_sum[v][row].x);
       }
-      const float base = top == -INFINITY ? 0.f : top;
+      const float base = sum_top == -INFINITY ? 0.f : sum_top;
 #pragma unroll
-      for (int v = 0; v < kRowWaves; ++v) sum += joined_l[v][row] * exp2_fast(joined_m[v][row] - base);
+      for (int v = 0; v < kRowWaves; ++v) sum += joined_sum[v][row].y * exp2_fast(joined_sum[v][row].x - base);
+      // x 2^(top - base) / sum, in two steps as the power may be out of range
+      const float power = exp2_fast(0.5f * (top - base));
+      const float inv = sum != 0.f ? power / sum : 0.f;
+      x = x * inv * power;
+      y = y * inv * power;
       if (whole) {
-        const float inv = sum != 0.f ? 1.f / sum : 0.f;
-        store2(row, c, x * inv, y * inv);
+        store2(row, c, x, y);
       } else {
         const int64_t to = static_cast<int64_t>(slot) * kRowTile + row;
         leave2(partial.rows + to * kDim + c, x, y);
-        if (c == 0) leave2(partial.ml + 2 * to, top, sum);
+        if (c == 0) {
+          const float2 part = part_sum(sum_top, sum);
+          leave2(partial.sums + 2 * to, part.x, part.y);
+        }
       }
     }
     lds_barrier();
@@ -526,7 +573,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_rows_kernel(CacheAtt
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
         if (tid == 0) __hip_atomic_store(partial.count + first, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         // Four channels of every row, and where they leave threads over, several threads a four's parts.
-        // The parts' maxima and sums go through LDS where it holds them.
+        // The parts' sums go through LDS where it holds them.
         const int parts = last - first + 1;
         const auto row_from = [&](int i, int row) { return static_cast<int64_t>(2 * (first + i) + (i == 0)) * kRowTile + row; };
         float2* const staged = reinterpret_cast<float2*>(&joined[0][0][0]);
@@ -534,7 +581,7 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_rows_kernel(CacheAtt
         if (fits)
           for (int i = tid; i < parts * rows; i += kThreads) {
             const int part = i / rows;
-            staged[i] = take2(partial.ml + 2 * row_from(part, i - part * rows));
+            staged[i] = take2(partial.sums + 2 * row_from(part, i - part * rows));
           }
         lds_barrier();
         constexpr int kFours = kDim / 4;
@@ -544,13 +591,13 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_rows_kernel(CacheAtt
           const int item = item0 + (teams == 1 ? tid : tid % items), team = teams == 1 ? 0 : tid / items;
           const bool busy = item < items && team < teams;
           const int row = busy ? item / kFours : 0, c = 4 * (item % kFours);
-          const auto ml_of = [&](int i) { return fits ? staged[i * rows + row] : take2(partial.ml + 2 * row_from(i, row)); };
+          const auto sum_of = [&](int i) { return fits ? staged[i * rows + row] : take2(partial.sums + 2 * row_from(i, row)); };
           f32x4 x = {0.f, 0.f, 0.f, 0.f};
           float sum = 0.f;
           if (busy) {
             float top = -INFINITY;
-            for (int i = 0; i < parts; ++i) top = fmaxf(top, ml_of(i).x);
-            const float base = top == -INFINITY ? 0.f : top;
+            for (int i = 0; i < parts; ++i) top = fmaxf(top, sum_of(i).x);
+            const float base = join_base(top, kRowsWorkers);
             constexpr int kBatch = 8;  // parts on their way at once
             for (int i0 = team; i0 < parts; i0 += kBatch * teams) {
               f32x4 v[kBatch];
@@ -562,9 +609,9 @@ __global__ __launch_bounds__(kThreads, 2) void cache_attend_rows_kernel(CacheAtt
 #pragma unroll
               for (int k = 0; k < kBatch; ++k) {
                 const int i = i0 + k * teams;
-                const float2 ml = ml_of(i < parts ? i : i0);
-                const float w = i < parts ? exp2_fast(ml.x - base) : 0.f;
-                sum += ml.y * w;
+                const float2 s = sum_of(i < parts ? i : i0);
+                const float w = i < parts ? s.y * exp2_fast(s.x - base) : 0.f;
+                sum += w;
                 x += v[k] * w;
               }
             }
@@ -609,7 +656,7 @@ static hipError_t launch_rows_as(const CacheAttendParams& p, const RowsLayout& l
   Partials partial;
   partial.count = reinterpret_cast<int*>(workspace);
   partial.rows = workspace + kCounterBytes / sizeof(float);
-  partial.ml = partial.rows + static_cast<int64_t>(2) * layout.most_workers * kRowTile * kDim;
+  partial.sums = partial.rows + static_cast<int64_t>(2) * layout.most_workers * kRowTile * kDim;
   hipLaunchKernelGGL((cache_attend_rows_kernel<T, kDim>), dim3(layout.most_workers), dim3(kThreads), 0, stream, p, layout,
                      partial);
   return hipGetLastError();

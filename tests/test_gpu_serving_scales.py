@@ -107,7 +107,7 @@ def test_wide_ranges(dtype, d, lens, held, scale):
     check(cache, table, lens, held, q, dtype, scale, prompt=prompt)
 
 
-@pytest.mark.parametrize("dtype,d,lens,held", SHAPES[4:])
+@pytest.mark.parametrize("dtype,d,lens,held", SHAPES)
 @pytest.mark.parametrize("loud", [1e6, 1e15, 1e25, 1e35])
 def test_pages_of_zeros_beside_loud_ones(dtype, d, lens, held, loud):
     cache, table, q, prompt = world(dtype, d, lens, held)
@@ -152,10 +152,11 @@ def test_many_positions_of_zeros(dtype, tokens, kv_heads, heads, zeros, ordinary
     check(cache, table, [tokens], [total - tokens], q, dtype, scale=1.0, rows=rows, prompt=tokens > 1)
 
 
-@pytest.mark.parametrize("dtype,tokens,kv_heads,heads", [("bf16", 2048, 8, 32)])
+@pytest.mark.parametrize("dtype,tokens,kv_heads,heads", [("bf16", 2048, 8, 32), ("bf16", 1, 8, 32), ("f32", 3, 2, 8)])
 @pytest.mark.parametrize("gains", [(1.0, 1e18, 1.0), (1e18, 1.0, 0.0), (0.0, 1.0, 1e-18), (1.0, 0.0, 1.0), (1e18, 1.0, 1e18)])
 def test_long_runs_of_pages_far_apart(dtype, tokens, kv_heads, heads, gains):
-    """Value scales that change every 16384 positions, as many as a workgroup of the prompts' kernel lists at once."""
+    """Value scales that change every 16384 positions, as many as a workgroup of the prompts' kernel lists at once; the
+    parts that a few rows' positions are cut into have pages of one kind and of two."""
     size, d, run = 64, 64, 16384
     total = 3 * run - 1000
     n_pages = -(-total // size)
