@@ -40,6 +40,15 @@ __device__ inline float max_of_quarters(float x) {
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return max_of_halves(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
 }
+// The largest of x over the wave.
+__device__ inline float max_of_wave(float x) {
+  const auto moved = [&](auto how) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), decltype(how)::value, 15, 15, false)); };
+  x = fmaxf(x, moved(IntC<0xb1>{}));   // lanes exchanged in pairs,
+  x = fmaxf(x, moved(IntC<0x4e>{}));   // pairs in fours,
+  x = fmaxf(x, moved(IntC<0x141>{}));  // eights mirrored,
+  x = fmaxf(x, moved(IntC<0x140>{}));  // sixteens mirrored
+  return max_of_quarters(x);
+}
 __device__ inline f32x4 mfma16(const f16x8& a, const f16x8& b, const f32x4& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }

@@ -181,10 +181,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
         scales[i] = scale;
         places[i] = page_at(p.cache, page, h, kDim) + (pos & (p.cache.page - 1)) * kDim;
       }
-      for (int o = 32; o > 0; o >>= 1) {
-        least = fminf(least, __shfl_xor(least, o));
-        most = fmaxf(most, __shfl_xor(most, o));
-      }
+      least = -max_of_wave(-least);
+      most = max_of_wave(most);
       if (lane == 0) range[wave] = make_float2(least, most);
       __syncthreads();
       for (int i = 0; i < kWaves; ++i) {
