@@ -427,7 +427,7 @@ typedef struct {
  * max_position are then not read).
  * For each page and head that new rows touch, with a = the largest magnitude of the new values:
  *   scale = max(scale, a / 127)   (the old scale counts only if the page holds earlier positions)
- *   q     = round(x / scale), ties to even, in [-127, 127]
+ *   q     = round(x / scale), ties to even, in [-127, 127]   (as x times the fp32 1 / scale)
  * and where the scale grew the page's earlier values are rounded again to the new one (so a value is
  * rounded at most once more per growth).  Scales below 2^-126 become 0 and their values 0.  A value
  * that is not finite makes the scale of its page and head NaN, and with it all the page holds of that
@@ -446,8 +446,12 @@ scd_status_t scd_cache_read(const scd_cache_t* cache, const scd_batch_t* batch, 
 /* Causal attention of the new tokens over the cache, which already holds them (append first).  For
  * query row i of request b and query head h (of KV head h / (q.n_heads / n_kv_heads)):
  *   out = sum_j p_j v_j,  p = softmax over j of softmax_scale * (q . k_j),  j in [0, pos0[b] + i]
- * One token per request and whole prompts are the same call.  Sums, the running maximum and the
- * softmax are fp32.  A row with no position to attend to (a hole at every one) is zero.
+ * One token per request and whole prompts are the same call, which one kernel takes, chosen by the mean of
+ * rows a request: a step's prompts and its single tokens are faster as two calls.  Sums, running maxima and
+ * the softmax are fp32, and positions count in it whatever their page's value scale (0, or any from 2^-126
+ * on, as scd_cache_append stores them; never negative).  Weights multiply the values with 24 bits in fp32
+ * calls and 16 or, in prompts, 11 in bf16 calls: there a weight times its value scale that is below 2^-25 of
+ * the row's largest has fewer.  A row with no position to attend to (a hole at every one) is zero.
  * q [n_tokens, n_heads, head_dim], n_heads a multiple of n_kv_heads; out alike, not overlapping q.
  * n_tokens * n_heads must be below 2^31 (else SCD_ERR_UNSUPPORTED), and cached positions from 2^31 - 64
  * on are left out.

@@ -7,7 +7,8 @@
 //    multiplies the scores, its value scale the weights, so no value is scaled one by one.
 //  - scores in fp16: a query row is multiplied by the power of two that brings its largest element to
 //    2^14 (its scores by the inverse).  bf16 rows are then exact down to 2^-28 of that element; fp32
-//    rows are split into two parts (22 bits and their sign).
+//    rows are split into two parts of 11 bits: what a third would add, 2^-22 of an element and less, is about what the fp32
+//    sums of up to 128 products leave open, at half as many matrix steps again for the scores.
 //  - a page's value scale goes into the exponent: the running maximum is that of log2 of a position's weight
 //    times its value scale, what it can add to the output, so the weights that add most to it have all their bits on the
 //    matrix cores whatever the scales; the softmax's own sum takes them divided by the scale again.
@@ -42,7 +43,9 @@ __device__ inline float max_of_quarters(float x) {
 }
 // The largest of x over the wave.
 __device__ inline float max_of_wave(float x) {
-  const auto moved = [&](auto how) { return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), decltype(how)::value, 15, 15, false)); };
+  const auto moved = [&](auto how) {
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), decltype(how)::value, 15, 15, false));
+  };
   x = fmaxf(x, moved(IntC<0xb1>{}));   // lanes exchanged in pairs,
   x = fmaxf(x, moved(IntC<0x4e>{}));   // pairs in fours,
   x = fmaxf(x, moved(IntC<0x141>{}));  // eights mirrored,
@@ -92,7 +95,8 @@ template <int kByte> __device__ inline bf16x8 byte_column_as_bf16(const uint32_t
 __device__ inline float2 part_sum(float n, float l) {
   return make_float2(n + static_cast<float>(__builtin_amdgcn_frexp_expf(l)), __builtin_amdgcn_frexp_mantf(l));
 }
-// Base of the exponents of shares, `top` the largest: shares of weights of 1 / most at most cannot exceed the largest of them.
+// Base of the exponents of up to `most` shares, `top` the largest: their weights' sum is at most 1, so what is joined is in
+// the range of what is joined from.
 __device__ inline float join_base(float top, int most) {
   return (top == -INFINITY ? 0.f : top) + static_cast<float>(32 - __builtin_clz(most - 1));
 }

@@ -22,12 +22,15 @@ static AttendPlan attend_plan(const PagedCache& c, const SeqBatch& b, int group,
   const int64_t requests = b.n_seqs < b.n_tokens ? b.n_seqs : b.n_tokens;
   // Rows of a request and KV head, on average.  From half a tile of the prompts' kernel on it takes the call, where it
   // has the type and head_dim.  New tokens of each request, 32 heads over 8 of 128, us as a few rows / as a prompt:
-  //   1 request behind  1000   8 14.0 / 18.4   16 15.8 / 19.4   32  17.0 / 21.8   64  17.3 / 27.2
-  //   1 request behind  8000                                    32  42.3 / 36.0   64  56.4 / 41.8
-  //   1 request behind 30000                                    32  81.3 / 52.8   64 127.9 / 86.8
-  //   16 requests, 1000        8 19.3 / 37.1   16 26.4 / 39.5   32  47.6 / 45.2   64  89.1 / 52.0
-  //   64 requests, 1000        8 52.7 / 68.7   16 97.1 / 70.6   32 182.1 / 86.2   64 350.5 / 118.2
-  // What a request holds already is known on the device only, so it is not part of the rule.
+  //   1 request behind  1000   8 14.7 / 19.4   16 16.0 / 20.4   32  17.2 / 22.7   64  17.4 / 28.3
+  //   1 request behind  8000                                    32  40.1 / 36.4   64  54.1 / 41.1
+  //   1 request behind 30000                                    32  74.8 / 49.7   64 122.1 / 83.6
+  //   16 requests, 1000        8 18.4 / 37.7   16 25.2 / 39.3   32  44.0 / 44.9   64  85.5 / 50.7
+  //   64 requests, 1000        8 51.3 / 69.3   16 94.8 / 71.4   32 179.4 / 82.6   64 344.1 / 111.0
+  // The two sides meet at 32 tokens (128 rows) of each of 16 requests, or of one that holds some thousands of positions;
+  // what a request holds is known on the device only, so it is not part of the rule.  It is on the slower side for 32 and 64
+  // tokens of one request behind 1000, and for 16 of each of 64 requests.  One kernel takes all of a call: 1500 tokens of one
+  // request and one of each of 63 behind 2000 take 177 us so, and 66 and 49 as two calls.
   const int64_t mean = b.n_tokens * group / requests;
   const bool prompt = bf16 && head_dim >= 64 && mean >= kPromptRows / 2;
   plan.rows = prompt ? kPromptRows : kRowTile;
@@ -35,7 +38,7 @@ static AttendPlan attend_plan(const PagedCache& c, const SeqBatch& b, int group,
   const int64_t positions = static_cast<int64_t>(c.cols) * c.page, segments = plan.tiles * c.heads;
   const size_t row = static_cast<size_t>(head_dim + 2) * sizeof(float);
   if (prompt) {
-    // Shares of at least 256 positions, as many as give the chip's 256 CUs a workgroup each.
+    // As many shares as give the chip's 256 CUs a workgroup each, but no more than one for every 256 positions.
     const int64_t most = (positions + 255) / 256, want = (256 + segments - 1) / segments;
     plan.splits = static_cast<int>(std::min<int64_t>(std::min(want, most), kMostSplits));
     if (plan.splits > 1) plan.bytes = kCounterBytes + segments * plan.splits * plan.rows * row;

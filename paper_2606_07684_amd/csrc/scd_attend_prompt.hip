@@ -35,8 +35,8 @@ __device__ inline bool tile_of(const CacheAttendParams& p, int64_t index, Locate
   set_tile<kRows>(p, at.span, at.b, at.local, t);
   return true;
 }
-// Splits of a tile that has `blocks` blocks of 32 positions, when a launch has up to `most`: at least
-// two blocks for each of a workgroup's four waves.
+// Shares of a tile that has `blocks` blocks of 32 positions, when a launch has up to `most`: one for every eight blocks
+// begun, equal to a block (nine make two shares, of four and five).
 __device__ inline int splits_of(int64_t blocks, int most) {
   const int64_t n = (blocks + 7) / 8;
   return static_cast<int>(n < 1 ? 1 : (n < most ? n : most));
@@ -52,7 +52,7 @@ __device__ inline int splits_of(int64_t blocks, int most) {
 //
 // Bound by the vector units beside the matrix cores: per 64 positions a SIMD's two waves take 2048 cycles of matrix
 // steps, about 3000 of exponentials, conversions and maxima, and the CU's LDS 2600 of reads and stores; taking turns
-// they need 5100.  2048 rows of an 8192-token prompt, 32 heads over 8 of 128, take 282 to 292 us: 820 to 850
+// they need 5100.  2048 rows of an 8192-token prompt, 32 heads over 8 of 128, take 277 to 283 us: 850 to 868
 // TFLOP/s, where a library product of 8192^3 reaches 1175.
 constexpr int kPromptLift = 11;   // the running maximum may lag by kPromptSlack: 2^15 fits fp16
 constexpr float kPromptSlack = 4.f;
@@ -87,7 +87,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
   __shared__ LocateLds locate_lds;
   __shared__ _Float16 keys[2][kPromptTokens][kPitchK];
   __shared__ _Float16 values[2][kDim][kPitchV];
-  __shared__ float4 scales[kListed];   // of keys; log2 of that of values, and its inverse to the loudest; -inf for a hole
+  __shared__ float4 scales[kListed];   // of keys; log2 of that of values, the loudest over it; 0, or -inf for a hole
   __shared__ float2 range[kWaves];
   __shared__ int64_t places[kListed];  // byte of a group's first position, in either branch's pages
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
@@ -111,7 +111,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
     const int begin = static_cast<int>(blocks * split / splits) << 5;
     const int end = static_cast<int>(blocks * (split + 1) / splits) << 5;
 
-    // queries, lifted as in the kernel above; a negative scale turns their sign
+    // queries, lifted so that the largest element is 2^kLift; a negative scale turns their sign
     f16x8 q[kSteps];
     float factor;
     int limit, free_until, wave_end;
@@ -168,12 +168,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
       for (int i = tid; i < 4 * tiles; i += kThreads) {
         const int pos = chunk + 16 * i;
         float4 scale = make_float4(0.f, -INFINITY, 0.f, -INFINITY);
-        int page = pos < chunk_end ? page_of(p.cache, t.b, pos) : -1;
+        int page = pos < chunk_end && pos < seen ? page_of(p.cache, t.b, pos) : -1;
         if (page >= 0) {
           const int64_t at = static_cast<int64_t>(page) * p.cache.heads + h;
           const float vs = p.cache.v_scale[at];
           scale = make_float4(p.cache.k_scale[at], vs < 1.17549435e-38f ? -INFINITY : __builtin_amdgcn_logf(vs), 0.f, 0.f);
-          least = scale.y > -INFINITY ? fminf(least, scale.y) : -INFINITY;  // nor is one that is not a number like others
+          least = scale.y > -INFINITY ? fminf(least, scale.y) : -INFINITY;  // also where it is not a number
           most = fmaxf(most, scale.y);
         } else {
           page = 0;
@@ -331,7 +331,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
           for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int j = 8 * (i & 1); j < 8 * (i & 1) + 8; ++j)
-              if (score[i >> 1][j] > -INFINITY) top = fmaxf(top, fmaf(score[i >> 1][j], f[i], scales[4 * tile + i].w));
+              if (score[i >> 1][j] > -INFINITY)
+                top = fmaxf(top, fmaf(score[i >> 1][j], f[i], scales[4 * tile + i].w));
           if (top > -INFINITY) {
             l *= exp2_fast(n - top);
             n = top;
@@ -339,7 +340,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cache_attend_prompt_kernel(Cac
             for (int i = 0; i < 4; ++i)
 #pragma unroll
               for (int j = 8 * (i & 1); j < 8 * (i & 1) + 8; ++j)
-                if (score[i >> 1][j] > -INFINITY) l += exp2_fast(fmaf(score[i >> 1][j], f[i], scales[4 * tile + i].w) - n);
+                if (score[i >> 1][j] > -INFINITY)
+                  l += exp2_fast(fmaf(score[i >> 1][j], f[i], scales[4 * tile + i].w) - n);
           }
         }
         float top = -INFINITY;

@@ -7,12 +7,13 @@
 // results do not depend on which is last.  Where that would cost more than it evens out, segments stay whole.
 //
 // Weights are split into two bf16 parts for bf16 output (16 bits; its own rounding has 8) and three for fp32: the
-// parts keep the whole exponent range, so a channel in which the heaviest positions are zero still has its bits.
+// parts keep fp32's exponent range, so a channel in which the heaviest positions are zero still has its bits, down to
+// 2^-110 of them.
 //
 // Bound by the pages' bytes where segments are long: one token of 16 requests of 1K to 16K positions, 32 heads over
-// 8 of 128, takes 66 us (295 MB, 4.4 TB/s; a large copy moves 5.2).  Of a wave's 430 instructions a block of 32
+// 8 of 128, takes 67 to 69 us (295 MB, 4.3 TB/s; a large copy moves 5.2).  Of a wave's 430 instructions a block of 32
 // positions some 180 turn bytes into operands, so with two waves a SIMD arithmetic alone would take about a third of
-// that.  Short contexts are latency: 333 positions of one request take 8.5 us, 2.3 to find the work and fetch
+// that.  Short contexts are latency: 333 positions of one request take 8.7 us, 2.3 to find the work and fetch
 // its first block, 2.7 for the blocks, 2 to join the waves, the rest the launch.  One request of 32K positions
 // over 4 heads takes 24 us, 7 of them the join of its 128 parts by 4 workgroups.
 #include "scd_attend.h"
@@ -131,11 +132,11 @@ __device__ inline bool share_of(const CacheAttendParams& p, const RowsLayout& la
   const int able = static_cast<int>(parts < layout.most_workers ? parts : layout.most_workers);
   if (able < 1) return false;
   // Whole segments take the longest of them (several, if a workgroup has as many); shares the mean, and what leaving
-  // and joining them costs, about two steps and one more for every 40 workgroups that do.  Tokens of requests with as
-  // many positions each, 32 heads over 8, us whole / cut:
-  //   1 of 1    600 11.3 / 9.7     1000 14.8 / 10.5               4 of 4    600 13.0 / 14.5    1000 16.8 / 16.2
-  //   16 of 16  600 12.3 / 26.6    1000 17.3 / 24.0    2000 27.0 / 28.6
-  //   8 of 16   600 13.3 / 30.6    1000 18.5 / 32.4    2000 28.8 / 39.9    4000 47.8 / 54.4
+  // and joining them costs, about two steps and one more for every 40 workgroups that do.  New tokens of each of so many
+  // requests behind as many positions, 32 heads over 8 of 128, us whole / cut:
+  //   1 of 1   behind 600 11.2 / 10.1   1000 14.7 / 10.9      4 of 4   behind 600 13.3 / 15.3   1000 16.8 / 16.5
+  //   1 of 16  behind 600 12.5 / 27.0   1000 16.9 / 24.5   2000 26.7 / 28.5   4000 45.0 / 36.6
+  //   8 of 16  behind 600 14.0 / 30.9   1000 18.6 / 32.2   2000 28.0 / 38.1   4000 46.5 / 54.5
   const int64_t whole = static_cast<int64_t>((all.x + layout.most_workers - 1) / layout.most_workers) * longest;
   const int sharers = able < all.y ? able : all.y;
   s.cut = longest > kUncutSteps && whole > all.y / sharers + 2 + sharers / kWorkersAStep;
@@ -189,7 +190,8 @@ __device__ inline float2 take2(const float* p) { return *reinterpret_cast<const 
 
 // What a workgroup leaves of a row that it does not finish: rows of two slots a worker (0: of a segment that
 // began before its share, 1: of one that goes on after it), outputs of their own positions, then their softmax's sums
-// (part_sum), then a count a worker of the parts left of the segment that begins in its share.  Counts are 0 between calls.
+// (part_sum), then a count a worker of the parts left of the segment that begins in its share.  Counts are 0 between
+// calls.
 struct Partials {
   float* rows;
   float* sums;

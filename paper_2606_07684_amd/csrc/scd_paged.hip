@@ -198,7 +198,7 @@ __device__ inline void store_item(int8_t* row, int2 at, float (&x)[16], float in
 // quantisation, the next two heads' are on their way meanwhile, and a thread's cosines and sines serve all heads.
 // Bound by HBM: rows are read once, in the model's type, and written once, in 8 bits.  8192 rows of 8 heads of 128 in
 // bf16, keys rotated, take 15 us (50 MB, 3.3 TB/s: one round of workgroups, so its start and end weigh); 111,169
-// rows 150 to 175 us (683 MB, 3.9 to 4.5 TB/s).
+// rows 160 to 180 us (683 MB, 3.8 to 4.2 TB/s).
 template <typename T, int kDim, int kThreads, TurnKind kKind>
 __device__ inline void append_page(const CacheAppendParams& p, int kv, int first_head, int last_head,
                                    const PageRows& r, uint32_t (*wave_top)[kThreads / 64], int tid) {
@@ -418,10 +418,11 @@ static hipError_t launch_append_pages(const CacheAppendParams& p, hipStream_t st
 template <typename T, int kDim, TurnKind kKind>
 static hipError_t launch_append_kind(const CacheAppendParams& p, hipStream_t stream) {
   // Few rows leave most of a page's workgroup idle, many keep a head's one wave at its page for long.  Rotated bf16
-  // rows of 8 heads of 128 in pages of 64, us as a wave a head / a workgroup a page:
-  //   1 request    16 rows 5.1 / 5.1    32 rows 5.9 / 5.1     64 rows 7.6 / 5.2
-  //   16 requests  16 rows 5.7 / 6.4    32 rows 6.8 / 7.7    128 rows 11.5 / 9.1
-  //   64 requests  16 rows 6.1 / 8.7    32 rows 8.6 / 12.0   128 rows 18.3 / 18.6
+  // rows of 8 heads of 128 in pages of 64, behind 1000, us as a wave a head / a workgroup a page:
+  //   1 request    16 rows 5.0 / 5.0    32 rows 5.9 / 5.1    64 rows  7.5 / 5.2     128 rows 10.1 / 5.3
+  //   16 requests  16 rows 5.8 / 6.6    32 rows 6.8 / 7.8    64 rows  8.5 / 8.1     128 rows 11.4 / 9.0
+  //   64 requests  16 rows 6.1 / 8.7    32 rows 8.4 / 12.2   64 rows 12.1 / 14.6    128 rows 18.0 / 18.0
+  // The rule is that of one request: of 16 and 64 a wave a head is the faster side up to 32 and 128 rows.
   const int64_t requests = p.batch.n_seqs < p.batch.n_tokens ? p.batch.n_seqs : p.batch.n_tokens;
   if (kKind == TurnKind::kOdd || p.batch.n_tokens < 32 * requests) return launch_append_few<T, kDim, kKind>(p, stream);
   if constexpr (kKind != TurnKind::kOdd) {
