@@ -331,6 +331,12 @@ def _torch_stream(stream, device) -> torch.cuda.Stream:
     return torch.cuda.ExternalStream(raw, device=device) if raw else torch.cuda.default_stream(device)
 
 
+def _made_on(stream, device):
+    """Context in which tensors that a call makes belong to the stream it runs on: memory that the
+    current stream is not done with is not taken, nor given back to it before the call has ended."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(_torch_stream(stream, device))
+
+
 def _ptr_array(tensors, n_layers: int, name: str, shapes: dict, dtype) -> ctypes.Array:
     """Host array of device pointers for one per-layer argument (None entries -> NULL)."""
     if tensors is None:
@@ -367,7 +373,8 @@ def scd_rope_table(model: Model, max_position: int, device=None, stream=None) ->
     if nbytes == 0:
         raise ValueError("invalid model or max_position for a RoPE table")
     device = device or torch.device("cuda", torch.cuda.current_device())
-    buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with _made_on(stream, device):
+        buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
     _check(lib.scd_rope_table(ctypes.byref(model._c), int(max_position), buf.data_ptr(), nbytes,
                               _stream(stream)))
     return RopeTable(buf, int(max_position), int(model.head_dim), float(model.rope_theta))
@@ -377,7 +384,8 @@ def scd_positions(batch: Batch, out: Optional[torch.Tensor] = None, stream=None)
     lib = load_library()
     if out is None:
         dev = batch.cu_seqlens.device if batch.cu_seqlens is not None else torch.device("cuda")
-        out = torch.empty(batch.n_tokens, dtype=torch.int32, device=dev)
+        with _made_on(stream, dev):
+            out = torch.empty(batch.n_tokens, dtype=torch.int32, device=dev)
     if out.dtype != torch.int32 or out.numel() != batch.n_tokens or not out.is_cuda:
         raise ValueError("out must be a CUDA int32 tensor of n_tokens entries")
     _check(lib.scd_positions(ctypes.byref(batch._c), out.data_ptr(), _stream(stream)))
@@ -809,17 +817,18 @@ def fit_reuse(model: Model, batch: Batch, rope: Optional[RopeTable], branch: int
     dev = next(t.device for t in a_in if t is not None)
     dt = model.torch_dtype
     ranks = model.rank_k if branch == FIT_KEYS else model.rank_v
-    ws = torch.empty(max(scd_fit_workspace_bytes(model, batch.n_tokens), 16), dtype=torch.uint8,
-                     device=dev)
     gram, colsum, w_enc, w_dec, mu_enc, mu_dec = ([None] * L for _ in range(6))
-    for l in R:
-        gram[l] = torch.empty((2 * w, 2 * w), dtype=torch.float32, device=dev)
-        colsum[l] = torch.empty((2 * w,), dtype=torch.float32, device=dev)
-        w_enc[l] = torch.empty((ranks[l], w), dtype=dt, device=dev)
-        w_dec[l] = torch.empty((w, ranks[l]), dtype=dt, device=dev)
-        if center:
-            mu_enc[l] = torch.empty((w,), dtype=dt, device=dev)
-            mu_dec[l] = torch.empty((w,), dtype=dt, device=dev)
+    with _made_on(stream, dev):
+        ws = torch.empty(max(scd_fit_workspace_bytes(model, batch.n_tokens), 16), dtype=torch.uint8,
+                         device=dev)
+        for l in R:
+            gram[l] = torch.empty((2 * w, 2 * w), dtype=torch.float32, device=dev)
+            colsum[l] = torch.empty((2 * w,), dtype=torch.float32, device=dev)
+            w_enc[l] = torch.empty((ranks[l], w), dtype=dt, device=dev)
+            w_dec[l] = torch.empty((w, ranks[l]), dtype=dt, device=dev)
+            if center:
+                mu_enc[l] = torch.empty((w,), dtype=dt, device=dev)
+                mu_dec[l] = torch.empty((w,), dtype=dt, device=dev)
     scd_fit_gram(model, batch, rope, branch, a_in, b_in, gram, colsum, ws, stream)
     scd_fit_solve(model, branch, batch.n_tokens * model.g, ridge_lambda, center, gram, colsum,
                   w_enc, w_dec, mu_enc if center else None, mu_dec if center else None, ws, stream)
@@ -953,7 +962,8 @@ def scd_rotary_table(rotary: Rotary, max_position: int, device=None, stream=None
         detail = lib.scd_last_error().decode()
         raise ValueError(f"invalid rotary or max_position: {detail or max_position}")
     device = device or torch.device("cuda", torch.cuda.current_device())
-    buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    with _made_on(stream, device):
+        buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
     _check(lib.scd_rotary_table(ctypes.byref(rotary._c), int(max_position), buf.data_ptr(), nbytes,
                                 _stream(stream)))
     return RotaryTable(buf, int(max_position), rotary)
@@ -1042,7 +1052,7 @@ def prepare_cache_attend(cache: PagedCache, batch: Batch, q, out, scale: Optiona
     rows = [_rows(t, n, batch.n_tokens, d, q.dtype) for t, n in ((q, "q"), (out, "out"))]
     if workspace is None:
         nbytes = scd_cache_attend_workspace_bytes(cache, batch, q.shape[1])
-        with contextlib.nullcontext() if stream is None else torch.cuda.stream(_torch_stream(stream, q.device)):
+        with _made_on(stream, q.device):
             workspace = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=q.device)
             workspace[:ATTEND_COUNTER_BYTES].zero_()
     ws, nbytes = _workspace_arg(workspace)

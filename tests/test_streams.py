@@ -3,6 +3,8 @@ import pytest
 import torch
 
 import paper_2606_07684_amd as scd
+from synth import workloads as W
+from tests import parity_util as U
 
 
 @pytest.mark.parametrize("given", [0, "default", 4096, "other"])
@@ -43,3 +45,33 @@ def test_workspace_is_cleared_on_the_default_stream(monkeypatch, as_handle):
     default.synchronize()
     assert entered == [0]
     assert bool((out == 0).all())
+
+
+@pytest.mark.gpu
+def test_tensors_belong_to_the_stream_that_fills_them(monkeypatch):
+    """Entry points that make their outputs or a workspace make them on the stream they are given: the allocator
+    neither hands them memory that the current stream still uses, nor the workspace back to it too early."""
+    from tests.test_gpu_fit import BRANCHES, _lam, _setup
+
+    wl, dev = W.FIT_POS0_KEYS, torch.device("cuda")
+    model, batch = U.model_of(wl), U.batch_of(wl, dev)
+    _, a_in, b_in, rope = _setup(wl, "k", dev)
+    calls = [lambda s: scd.scd_rope_table(model, 50, stream=s).buffer, lambda s: scd.scd_positions(batch, stream=s),
+             lambda s: scd.scd_rotary_table(scd.Rotary(64, 1e4), 50, stream=s).buffer,
+             lambda s: scd.fit_reuse(model, batch, rope, BRANCHES["k"], a_in, b_in, _lam(wl), stream=s)[0]]
+    want = [call(None) for call in calls]
+    torch.cuda.synchronize()
+    side, made, empty = torch.cuda.Stream(), [], torch.empty
+
+    def recorded(*args, **kwargs):
+        made.append(torch.cuda.current_stream().cuda_stream)
+        return empty(*args, **kwargs)
+
+    monkeypatch.setattr(torch, "empty", recorded)
+    for call, expected in zip(calls, want):
+        made.clear()
+        got = call(side)
+        assert made and set(made) == {side.cuda_stream}
+        side.synchronize()
+        for x, y in zip(*((v if isinstance(v, list) else [v]) for v in (got, expected))):
+            assert (x is None and y is None) or torch.equal(x, y)
