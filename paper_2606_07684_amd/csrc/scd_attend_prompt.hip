@@ -52,7 +52,7 @@ __device__ inline int splits_of(int64_t blocks, int most) {
 //
 // Bound by the vector units beside the matrix cores: per 64 positions a SIMD's two waves take 2048 cycles of matrix
 // steps, about 3000 of exponentials, conversions and maxima, and the CU's LDS 2600 of reads and stores; taking turns
-// they need 5100.  2048 rows of an 8192-token prompt, 32 heads over 8 of 128, take 277 to 283 us: 850 to 868
+// they need 5100.  2048 rows of an 8192-token prompt, 32 heads over 8 of 128, take 277 to 294 us: 817 to 868
 // TFLOP/s, where a library product of 8192^3 reaches 1175.
 constexpr int kPromptLift = 11;   // the running maximum may lag by kPromptSlack: 2^15 fits fp16
 constexpr float kPromptSlack = 4.f;
