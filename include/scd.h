@@ -468,6 +468,143 @@ scd_status_t scd_cache_attend(const scd_cache_t* cache, const scd_batch_t* batch
                               double softmax_scale, const scd_rows_t* q, const scd_rows_t* out,
                               void* workspace, size_t workspace_bytes, hipStream_t stream);
 
+/* ---- A latent cache: one low-rank row a token instead of keys and values ------------------------
+ * A model whose layers project every token to one latent c [latent_dim] and one key k [turned_dim] that all
+ * heads share has, for head h,
+ *   keys  [ W_k,h c | k ]  (plain_dim + turned_dim channels, k rotated to its position),
+ *   values  W_v,h c        (value_dim channels),
+ * as the codec's decoder has rows from codes.  Only (c, k) are cached, in the model's dtype: pages is
+ * [n_pages, page_tokens, latent_dim + turned_dim], page_table as of scd_cache_t, holes and positions outside
+ * the table likewise.  latent_dim a multiple of 32 up to 512, turned_dim 32 or 64, page_tokens 16, 32, 64 or
+ * 128; plain_dim and value_dim multiples of 32 up to 256.  w_k [n_heads, plain_dim, latent_dim] and
+ * w_v [n_heads, value_dim, latent_dim] are contiguous, 16-byte aligned, in the model's dtype. */
+typedef struct {
+  int32_t n_pages;
+  int32_t page_tokens;
+  int32_t latent_dim;
+  int32_t turned_dim;
+  int32_t max_pages;
+  void* pages;
+  const int32_t* page_table;
+} scd_latent_cache_t;
+
+/* Appends rows latent [n_tokens, 1, latent_dim] and turned [n_tokens, 1, turned_dim] at positions pos0[b] + i.
+ * With `rotary` (head_dim = turned_dim) the shared keys are rotated to them on the way, in fp32, rounded once;
+ * NULL: as they are.  Latents keep their bits.  Rows behind the last request are left alone, and pages that
+ * several requests name must not be appended to (scd_pages_reserve sees to it). */
+scd_status_t scd_latent_append(const scd_latent_cache_t* cache, const scd_batch_t* batch, int32_t dtype,
+                               const scd_rows_t* latent, const scd_rows_t* turned, const scd_rotary_t* rotary,
+                               const void* table, int64_t max_position, hipStream_t stream);
+
+/* Causal attention of the new tokens over the cache, which already holds them, with nothing expanded: for query
+ * row q_i,h [plain_dim + turned_dim] (its last turned_dim channels rotated: scd_rotary takes them as strided rows)
+ *   a = W_k,h^T q_i,h[:plain_dim],  s_j = softmax_scale (a . c_j + q_i,h[plain_dim:] . k_j),  j <= pos0[b] + i
+ *   out_i,h = W_v,h sum_j p_j c_j,  p = softmax(s)
+ * q [n_tokens, n_heads, plain_dim + turned_dim], out [n_tokens, n_heads, value_dim], not overlapping q.  Sums and
+ * the softmax are fp32.  In bf16 calls queries in the latents' space and the weighted latents are held as two
+ * bf16 summands, weights of the softmax are rounded to bf16 (their sum is of unrounded ones).  A row with no
+ * position to attend to is zero.  A position whose latent or key is not finite makes the rows that attend to it
+ * not finite, and no others.  One call takes one token a request or a chunk of them; for prompts of some hundred
+ * tokens scd_latent_expand and scd_rows_attend do a half to a third of the arithmetic.
+ * n_tokens up to 65535, n_tokens * n_heads below 2^27, cached positions below 2^31 - 128.
+ * `workspace` (device, 16-byte aligned, caller-owned, any contents) holds
+ * scd_latent_attend_workspace_bytes(cache, batch, dtype, n_heads) bytes, which depend on the sizes alone, so
+ * that a captured call can be replayed while lengths grow.  Calls that may overlap need one each. */
+size_t scd_latent_attend_workspace_bytes(const scd_latent_cache_t* cache, const scd_batch_t* batch, int32_t dtype,
+                                         int32_t n_heads);
+scd_status_t scd_latent_attend(const scd_latent_cache_t* cache, const scd_batch_t* batch, int32_t dtype,
+                               double softmax_scale, int32_t plain_dim, int32_t value_dim, const void* w_k,
+                               const void* w_v, const scd_rows_t* q, const scd_rows_t* out, void* workspace,
+                               size_t workspace_bytes, hipStream_t stream);
+
+/* The dense keys and values of cached positions pos0[b] + i (pos0 NULL: from the start): k_out
+ * [n_tokens, n_heads, plain_dim + turned_dim], v_out [n_tokens, n_heads, value_dim], products in fp32 and rounded
+ * once, shared keys with their bits.  A position in a hole or outside the table gives zeros, and rows behind the
+ * last request are left alone. */
+scd_status_t scd_latent_expand(const scd_latent_cache_t* cache, const scd_batch_t* batch, int32_t dtype,
+                               int32_t n_heads, int32_t plain_dim, int32_t value_dim, const void* w_k, const void* w_v,
+                               const scd_rows_t* k_out, const scd_rows_t* v_out, hipStream_t stream);
+
+/* Causal attention over dense rows: those that scd_latent_expand writes, or the caches that the codec's decode and
+ * Patch write.  `held` names the key and value rows of every request as `batch` names its query rows: row j of
+ * request b has position held.pos0[b] + j (NULL: j), row i of its queries position batch.pos0[b] + i.
+ *   out_i = sum_j p_j v_j,  p = softmax over j of softmax_scale (q_i . k_j),  position j <= position i
+ * q [batch.n_tokens, n_heads, key_dim], k [held.n_tokens, n_kv_heads, key_dim], v [.., n_kv_heads, value_dim], query
+ * head h reads KV head h / (n_heads / n_kv_heads); out [batch.n_tokens, n_heads, value_dim], overlapping no input.
+ * key_dim a multiple of 32 up to 192, value_dim up to 128.  Sums and the softmax are fp32, weights are rounded to
+ * bf16 in bf16 calls.  A row with no position to attend to is zero.  Keys and values behind a row's position do not
+ * reach it, whatever they hold; a value that is not finite makes its channel NaN in the rows that attend to it.
+ * Fastest where all rows and strides are multiples of 16 bytes.  The workspace is as of scd_latent_attend; where it is
+ * 0 bytes it may be NULL. */
+size_t scd_rows_attend_workspace_bytes(const scd_batch_t* batch, const scd_batch_t* held, int32_t dtype, int32_t n_heads,
+                                       int32_t n_kv_heads, int32_t key_dim, int32_t value_dim);
+scd_status_t scd_rows_attend(const scd_batch_t* batch, const scd_batch_t* held, int32_t dtype, double softmax_scale,
+                             int32_t key_dim, int32_t value_dim, const scd_rows_t* q, const scd_rows_t* k,
+                             const scd_rows_t* v, const scd_rows_t* out, void* workspace, size_t workspace_bytes,
+                             hipStream_t stream);
+
+/* ---- Pages of caches: given back, shared, reserved, moved -------------------------------------------
+ * One pool of pages serves the caches of all layers: page id p is page p of every layer's scd_cache_t or
+ * scd_latent_cache_t, and page_table [n_seqs, max_pages] names a request's pages for all of them.  refs [n_pages]
+ * counts the table entries that name a page (0: free), held [n_seqs] is what every request holds (its pos0 in the
+ * next batch).  All are int32 in device memory; an entry outside [0, n_pages) names nothing.  Fresh pages are the
+ * lowest free ones, to requests in their order and a request's positions in theirs, so results depend on the arguments
+ * alone.  The calls take a pool one after another: on one stream, or ordered by the caller. */
+typedef struct {
+  int32_t n_pages;
+  int32_t n_seqs;
+  int32_t max_pages;
+  int32_t page_tokens;
+  int32_t* refs;
+  int32_t* page_table;
+  int32_t* held;
+} scd_pages_t;
+
+/* Pages whose contents are to be moved, from pairs[2 k] to pairs[2 k + 1] for k < status[0], written by the two
+ * calls that say so and read by scd_pages_copy.  No page is both.  status [4] (device): the count of moves; pages in
+ * use (scd_pages_compact); pages that are missing; requests whose tokens do not fit the table.  Where one of the last
+ * two is not zero the call has changed nothing else.  Pairs past the count keep what they held. */
+typedef struct {
+  int32_t capacity;     /* pairs */
+  int32_t* pairs;       /* DEVICE [capacity, 2] */
+  int32_t* status;      /* DEVICE [4] */
+} scd_moves_t;
+
+/* Requests seqs[0 .. n) (device) give their pages back: every page they name is counted down, their table entries
+ * become -1, held 0.  A request named twice counts once; one outside [0, n_seqs) is passed over. */
+scd_status_t scd_pages_free(const scd_pages_t* pages, int32_t n, const int32_t* seqs, hipStream_t stream);
+
+/* Request dst[i] becomes a copy of src[i] without any contents moved: it names the pages that src[i] holds tokens in
+ * (the last one too, though it be begun only: scd_pages_reserve separates them once one writes), which are counted
+ * up, and holds as many tokens.  A pair is passed over where either is outside [0, n_seqs), where dst[i] holds tokens,
+ * names a page or is the target of an earlier pair, and where src[i] is the target of any pair. */
+scd_status_t scd_pages_fork(const scd_pages_t* pages, int32_t n, const int32_t* src, const int32_t* dst,
+                            hipStream_t stream);
+
+/* Makes the positions held[b] .. held[b] + n_b - 1 of every request writable, n_b its rows in `batch` (whose pos0 is
+ * not read): missing pages are taken, and pages that others name too are replaced by fresh ones, with a move
+ * where such a page holds earlier positions.  Of requests that all write to one page the last keeps it, if no other
+ * names it.  held stays: the caller counts it up with the tokens.  moves holds n_seqs pairs or more. */
+size_t scd_pages_workspace_bytes(const scd_pages_t* pages);  /* of the two calls below; any contents */
+scd_status_t scd_pages_reserve(const scd_pages_t* pages, const scd_batch_t* batch, const scd_moves_t* moves,
+                               void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* The n pages in use become pages 0 .. n - 1: the k-th of those behind moves to the k-th free page in front. Table and
+ * counts are written to `out` (NULL or equal pointers: in place; its held is not written).  moves holds n_pages / 2
+ * pairs or more. */
+scd_status_t scd_pages_compact(const scd_pages_t* pages, const scd_pages_t* out, const scd_moves_t* moves,
+                               void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Moves the contents of the listed pages in every plane: page p of a plane is page_bytes bytes (a multiple of 4) at
+ * data + p * page_bytes, data 16-byte aligned.  A scd_cache_t is four planes (k_pages, v_pages, k_scales, v_scales), a
+ * latent cache one.  A move that names a page outside [0, n_pages) is passed over. */
+typedef struct {
+  void* data;           /* DEVICE */
+  int64_t page_bytes;
+} scd_plane_t;
+scd_status_t scd_pages_copy(int32_t n_planes, const scd_plane_t* planes, int32_t n_pages, const scd_moves_t* moves,
+                            hipStream_t stream);
+
 /* ---- diagnostics ---------------------------------------------------------------------------- */
 const char* scd_status_string(scd_status_t status);
 /* Detail of the last non-OK status returned on the calling thread ("" if none). */

@@ -15,6 +15,12 @@ meaning (``include/scd.h``):
 * :func:`scd_cache_append` rows into a paged 8-bit cache, keys rotated on the way
 * :func:`scd_cache_read`   a paged cache's rows back as dense keys and values
 * :func:`scd_cache_attend` causal attention of new tokens over the paged 8-bit cache
+* :func:`scd_latent_append` latent rows and their shared keys into a paged latent cache
+* :func:`scd_latent_attend` causal attention over a latent cache, nothing expanded
+* :func:`scd_latent_expand` dense keys and values of a latent cache
+* :func:`scd_rows_attend`  causal attention over dense keys and values
+* :func:`scd_pages_free`, :func:`scd_pages_fork`, :func:`scd_pages_reserve`,
+  :func:`scd_pages_compact`, :func:`scd_pages_copy`  pages of caches given back, shared, reserved, moved
 
 If the library is missing the first call raises: there is no fallback path.
 """
@@ -41,6 +47,13 @@ __all__ = [
     "Rotary", "RotaryTable", "scd_rotary_table", "scd_rotary", "prepare_rotary", "PagedCache",
     "scd_cache_append", "prepare_cache_append", "scd_cache_read", "prepare_cache_read",
     "scd_cache_attend", "prepare_cache_attend", "scd_cache_attend_workspace_bytes",
+    "LatentCache", "scd_latent_append", "prepare_latent_append", "scd_latent_attend",
+    "prepare_latent_attend", "scd_latent_attend_workspace_bytes", "scd_latent_expand",
+    "prepare_latent_expand", "scd_rows_attend", "prepare_rows_attend",
+    "scd_rows_attend_workspace_bytes", "Pages", "Moves", "scd_pages_workspace_bytes",
+    "scd_pages_free", "prepare_pages_free", "scd_pages_fork", "prepare_pages_fork",
+    "scd_pages_reserve", "prepare_pages_reserve", "scd_pages_compact", "prepare_pages_compact",
+    "scd_pages_copy", "prepare_pages_copy",
 ]
 
 _PKG_DIR = os.path.dirname(os.path.abspath(__file__))
@@ -132,6 +145,45 @@ class _CCache(ctypes.Structure):
     ]
 
 
+class _CLatentCache(ctypes.Structure):
+    _fields_ = [
+        ("n_pages", ctypes.c_int32),
+        ("page_tokens", ctypes.c_int32),
+        ("latent_dim", ctypes.c_int32),
+        ("turned_dim", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+        ("pages", ctypes.c_void_p),
+        ("page_table", ctypes.c_void_p),
+    ]
+
+
+class _CPages(ctypes.Structure):
+    _fields_ = [
+        ("n_pages", ctypes.c_int32),
+        ("n_seqs", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+        ("page_tokens", ctypes.c_int32),
+        ("refs", ctypes.c_void_p),
+        ("page_table", ctypes.c_void_p),
+        ("held", ctypes.c_void_p),
+    ]
+
+
+class _CMoves(ctypes.Structure):
+    _fields_ = [
+        ("capacity", ctypes.c_int32),
+        ("pairs", ctypes.c_void_p),
+        ("status", ctypes.c_void_p),
+    ]
+
+
+class _CPlane(ctypes.Structure):
+    _fields_ = [
+        ("data", ctypes.c_void_p),
+        ("page_bytes", ctypes.c_int64),
+    ]
+
+
 _VP = ctypes.c_void_p
 _PP = ctypes.POINTER(ctypes.c_void_p)
 _SIGS = {
@@ -197,6 +249,35 @@ _SIGS = {
     "scd_cache_attend": (ctypes.c_int, [ctypes.POINTER(_CCache), ctypes.POINTER(_CBatch),
                                         ctypes.c_int32, ctypes.c_double, ctypes.POINTER(_CRows),
                                         ctypes.POINTER(_CRows), _VP, ctypes.c_size_t, _VP]),
+    "scd_latent_append": (ctypes.c_int, [ctypes.POINTER(_CLatentCache), ctypes.POINTER(_CBatch),
+                                         ctypes.c_int32, ctypes.POINTER(_CRows),
+                                         ctypes.POINTER(_CRows), ctypes.POINTER(_CRotary), _VP,
+                                         ctypes.c_int64, _VP]),
+    "scd_latent_attend_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(_CLatentCache),
+                                                            ctypes.POINTER(_CBatch),
+                                                            ctypes.c_int32, ctypes.c_int32]),
+    "scd_latent_attend": (ctypes.c_int, [ctypes.POINTER(_CLatentCache), ctypes.POINTER(_CBatch),
+                                         ctypes.c_int32, ctypes.c_double, ctypes.c_int32,
+                                         ctypes.c_int32, _VP, _VP, ctypes.POINTER(_CRows),
+                                         ctypes.POINTER(_CRows), _VP, ctypes.c_size_t, _VP]),
+    "scd_latent_expand": (ctypes.c_int, [ctypes.POINTER(_CLatentCache), ctypes.POINTER(_CBatch),
+                                         ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                         ctypes.c_int32, _VP, _VP, ctypes.POINTER(_CRows),
+                                         ctypes.POINTER(_CRows), _VP]),
+    "scd_rows_attend_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(_CBatch)] * 2
+                                        + [ctypes.c_int32] * 5),
+    "scd_rows_attend": (ctypes.c_int, [ctypes.POINTER(_CBatch)] * 2
+                        + [ctypes.c_int32, ctypes.c_double, ctypes.c_int32, ctypes.c_int32]
+                        + [ctypes.POINTER(_CRows)] * 4 + [_VP, ctypes.c_size_t, _VP]),
+    "scd_pages_workspace_bytes": (ctypes.c_size_t, [ctypes.POINTER(_CPages)]),
+    "scd_pages_free": (ctypes.c_int, [ctypes.POINTER(_CPages), ctypes.c_int32, _VP, _VP]),
+    "scd_pages_fork": (ctypes.c_int, [ctypes.POINTER(_CPages), ctypes.c_int32, _VP, _VP, _VP]),
+    "scd_pages_reserve": (ctypes.c_int, [ctypes.POINTER(_CPages), ctypes.POINTER(_CBatch),
+                                         ctypes.POINTER(_CMoves), _VP, ctypes.c_size_t, _VP]),
+    "scd_pages_compact": (ctypes.c_int, [ctypes.POINTER(_CPages), ctypes.POINTER(_CPages),
+                                         ctypes.POINTER(_CMoves), _VP, ctypes.c_size_t, _VP]),
+    "scd_pages_copy": (ctypes.c_int, [ctypes.c_int32, ctypes.POINTER(_CPlane), ctypes.c_int32,
+                                      ctypes.POINTER(_CMoves), _VP]),
 }
 EXPORTED_SYMBOLS = tuple(_SIGS)
 
@@ -1065,3 +1146,286 @@ def prepare_cache_attend(cache: PagedCache, batch: Batch, q, out, scale: Optiona
 def scd_cache_attend(cache: PagedCache, batch: Batch, q, out, scale: Optional[float] = None,
                      workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     prepare_cache_attend(cache, batch, q, out, scale, workspace, stream)(stream)
+
+
+# ------------------------------------------------------------------------------------------------
+# A latent cache, attention over it and over dense rows
+# ------------------------------------------------------------------------------------------------
+@dataclasses.dataclass
+class LatentCache:
+    """One layer's paged cache of latents (``scd_latent_cache_t``): ``pages`` bf16 or fp32
+    [n_pages, page_tokens, latent_dim + turned_dim], ``page_table`` int32 [n_seqs, max_pages]; the
+    first ``latent_dim`` channels of a row are the latent, the others the key that all heads share."""
+    pages: torch.Tensor
+    page_table: torch.Tensor
+    latent_dim: int
+
+    def __post_init__(self):
+        if self.pages.dim() != 3 or self.page_table.dim() != 2:
+            raise ValueError("pages must be [n_pages, page_tokens, latent_dim + turned_dim], "
+                             "page_table [n_seqs, max_pages]")
+        for name in ("pages", "page_table"):
+            t = getattr(self, name)
+            if not t.is_cuda or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous CUDA tensor")
+        _dtype_code(self.pages)
+        if self.page_table.dtype != torch.int32:
+            raise ValueError("page_table must be int32")
+        if not 0 < self.latent_dim < self.pages.shape[2]:
+            raise ValueError(f"latent_dim {self.latent_dim} of rows of {self.pages.shape[2]} channels")
+        n, size, width = self.pages.shape
+        self._c = _CLatentCache(n, size, self.latent_dim, width - self.latent_dim,
+                                self.page_table.shape[1], self.pages.data_ptr(),
+                                self.page_table.data_ptr())
+
+    @property
+    def turned_dim(self) -> int:
+        return self.pages.shape[2] - self.latent_dim
+
+
+def _one_head(t: torch.Tensor, name: str, n_tokens: int, width: int, dtype) -> _CRows:
+    """A [tokens, channels] tensor of any token stride."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 2:
+        raise ValueError(f"{name} must be a [{n_tokens}, {width}] tensor")
+    return _rows(t[:, None], name, n_tokens, width, dtype)
+
+
+def _heads_args(cache: LatentCache, w_k: torch.Tensor, w_v: torch.Tensor):
+    """Heads, plain and value channels of the heads' matrices, and their addresses."""
+    for name, w in (("w_k", w_k), ("w_v", w_v)):
+        if not isinstance(w, torch.Tensor) or not w.is_cuda or not w.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous CUDA tensor")
+        if w.dtype != cache.pages.dtype:
+            raise ValueError(f"{name} has dtype {w.dtype}, expected {cache.pages.dtype}")
+        if w.dim() != 3 or w.shape[0] != w_k.shape[0] or w.shape[2] != cache.latent_dim:
+            raise ValueError(f"{name} has shape {tuple(w.shape)}, expected "
+                             f"({w_k.shape[0]}, channels, {cache.latent_dim})")
+    return w_k.shape[0], w_k.shape[1], w_v.shape[1], w_k.data_ptr(), w_v.data_ptr()
+
+
+def prepare_latent_append(cache: LatentCache, batch: Batch, latent, turned,
+                          table: Optional[RotaryTable] = None) -> Prepared:
+    """Rows latent [n_tokens, latent_dim] and turned [n_tokens, turned_dim] into the cache at positions
+    pos0[b] + i; with a table the shared keys are rotated to them on the way."""
+    lib = load_library()
+    _cache_batch(cache, batch)
+    rows = [_one_head(t, n, batch.n_tokens, d, cache.pages.dtype)
+            for t, n, d in ((latent, "latent", cache.latent_dim), (turned, "turned", cache.turned_dim))]
+    args = (ctypes.byref(cache._c), ctypes.byref(batch._c), _dtype_code(cache.pages),
+            *[ctypes.byref(r) for r in rows], *((None, None, 0) if table is None else _turns_args(table)))
+    return Prepared(lib.scd_latent_append, args, (cache, batch, table, rows, latent, turned))
+
+
+def scd_latent_append(cache: LatentCache, batch: Batch, latent, turned,
+                      table: Optional[RotaryTable] = None, stream=None) -> None:
+    prepare_latent_append(cache, batch, latent, turned, table)(stream)
+
+
+def scd_latent_attend_workspace_bytes(cache: LatentCache, batch: Batch, n_heads: int) -> int:
+    return int(load_library().scd_latent_attend_workspace_bytes(
+        ctypes.byref(cache._c), ctypes.byref(batch._c), _dtype_code(cache.pages), int(n_heads)))
+
+
+def _workspace_of(workspace, nbytes: int, device, stream) -> torch.Tensor:
+    """The caller's workspace, or one made for a call that belongs to ``stream`` (or the current one)."""
+    if workspace is None:
+        with _made_on(stream, device):
+            workspace = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=device)
+    return workspace
+
+
+def prepare_latent_attend(cache: LatentCache, batch: Batch, q, w_k, w_v, out,
+                          scale: Optional[float] = None, workspace: Optional[torch.Tensor] = None,
+                          stream=None) -> Prepared:
+    """Causal attention of rows q [n_tokens, heads, plain + turned_dim] (their last turned_dim channels
+    rotated) over the cache, which holds them already, into out [n_tokens, heads, value]; w_k
+    [heads, plain, latent_dim], w_v [heads, value, latent_dim].  ``scale`` None:
+    (plain + turned_dim)^-1/2.  ``workspace`` None: one of
+    :func:`scd_latent_attend_workspace_bytes` is made on ``stream`` (or the current one), which the
+    calls then belong to, and kept with the call."""
+    lib = load_library()
+    _cache_batch(cache, batch)
+    heads, plain, value, wk, wv = _heads_args(cache, w_k, w_v)
+    dt = cache.pages.dtype
+    rows = [_rows(q, "q", batch.n_tokens, plain + cache.turned_dim, dt), _rows(out, "out", batch.n_tokens, value, dt)]
+    if q.shape[1] != heads:
+        raise ValueError(f"q has {q.shape[1]} heads, w_k {heads}")
+    workspace = _workspace_of(workspace, scd_latent_attend_workspace_bytes(cache, batch, heads), q.device, stream)
+    args = (ctypes.byref(cache._c), ctypes.byref(batch._c), _dtype_code(q),
+            float((plain + cache.turned_dim) ** -0.5 if scale is None else scale), plain, value, wk, wv,
+            *[ctypes.byref(r) for r in rows], *_workspace_arg(workspace))
+    return Prepared(lib.scd_latent_attend, args, (cache, batch, rows, q, w_k, w_v, out, workspace))
+
+
+def scd_latent_attend(cache: LatentCache, batch: Batch, q, w_k, w_v, out, scale: Optional[float] = None,
+                      workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    prepare_latent_attend(cache, batch, q, w_k, w_v, out, scale, workspace, stream)(stream)
+
+
+def prepare_latent_expand(cache: LatentCache, batch: Batch, w_k, w_v, k_out, v_out) -> Prepared:
+    """Dense keys [n_tokens, heads, plain + turned_dim] and values [n_tokens, heads, value] of the
+    cached positions pos0[b] + i."""
+    lib = load_library()
+    _cache_batch(cache, batch)
+    heads, plain, value, wk, wv = _heads_args(cache, w_k, w_v)
+    dt = cache.pages.dtype
+    rows = [_rows(k_out, "k_out", batch.n_tokens, plain + cache.turned_dim, dt),
+            _rows(v_out, "v_out", batch.n_tokens, value, dt)]
+    args = (ctypes.byref(cache._c), ctypes.byref(batch._c), _dtype_code(k_out), heads, plain, value, wk, wv,
+            *[ctypes.byref(r) for r in rows])
+    return Prepared(lib.scd_latent_expand, args, (cache, batch, rows, w_k, w_v, k_out, v_out))
+
+
+def scd_latent_expand(cache: LatentCache, batch: Batch, w_k, w_v, k_out, v_out, stream=None) -> None:
+    prepare_latent_expand(cache, batch, w_k, w_v, k_out, v_out)(stream)
+
+
+def scd_rows_attend_workspace_bytes(batch: Batch, held: Batch, dtype, n_heads: int, n_kv_heads: int,
+                                    key_dim: int, value_dim: int) -> int:
+    code = SCD_BF16 if dtype == torch.bfloat16 else SCD_F32
+    return int(load_library().scd_rows_attend_workspace_bytes(
+        ctypes.byref(batch._c), ctypes.byref(held._c), code, int(n_heads), int(n_kv_heads), int(key_dim),
+        int(value_dim)))
+
+
+def prepare_rows_attend(batch: Batch, held: Batch, q, k, v, out, scale: Optional[float] = None,
+                        workspace: Optional[torch.Tensor] = None, stream=None) -> Prepared:
+    """Causal attention of rows q [n_tokens, heads, key_dim] (``batch``) over dense rows k
+    [held tokens, kv_heads, key_dim], v [held tokens, kv_heads, value_dim] (``held``: the same requests, row
+    j of one at position held.pos0[b] + j) into out [n_tokens, heads, value_dim].  ``scale`` None:
+    key_dim^-1/2.  ``workspace`` as of :func:`prepare_latent_attend`."""
+    lib = load_library()
+    if batch.n_seqs != held.n_seqs:
+        raise ValueError(f"the batch has {batch.n_seqs} requests, held {held.n_seqs}")
+    for t, name in ((q, "q"), (k, "k"), (v, "v"), (out, "out")):
+        if not isinstance(t, torch.Tensor) or t.dim() != 3:
+            raise ValueError(f"{name} must be a [tokens, heads, channels] tensor")
+    key, value = q.shape[2], v.shape[2]
+    rows = [_rows(t, n, b.n_tokens, d, q.dtype) for t, n, b, d in (
+        (q, "q", batch, key), (k, "k", held, key), (v, "v", held, value), (out, "out", batch, value))]
+    nbytes = 0
+    if k.shape[1] > 0 and q.shape[1] % k.shape[1] == 0:
+        nbytes = scd_rows_attend_workspace_bytes(batch, held, q.dtype, q.shape[1], k.shape[1], key, value)
+    workspace = _workspace_of(workspace, nbytes, q.device, stream)
+    args = (ctypes.byref(batch._c), ctypes.byref(held._c), _dtype_code(q),
+            float(key ** -0.5 if scale is None else scale), key, value, *[ctypes.byref(r) for r in rows],
+            *_workspace_arg(workspace))
+    return Prepared(lib.scd_rows_attend, args, (batch, held, rows, q, k, v, out, workspace))
+
+
+def scd_rows_attend(batch: Batch, held: Batch, q, k, v, out, scale: Optional[float] = None,
+                    workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    prepare_rows_attend(batch, held, q, k, v, out, scale, workspace, stream)(stream)
+
+
+# ------------------------------------------------------------------------------------------------
+# Pages of caches
+# ------------------------------------------------------------------------------------------------
+def _entries(t: torch.Tensor, name: str, shape) -> int:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype != torch.int32 or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 CUDA tensor")
+    if any(want is not None and got != want for got, want in zip(t.shape, shape)) or t.dim() != len(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    return t.data_ptr()
+
+
+@dataclasses.dataclass
+class Pages:
+    """A pool of pages that the caches of all layers share (``scd_pages_t``): ``page_table`` int32
+    [n_seqs, max_pages], ``refs`` int32 [n_pages] table entries that name a page, ``held`` int32
+    [n_seqs] tokens that requests hold."""
+    page_table: torch.Tensor
+    refs: torch.Tensor
+    held: torch.Tensor
+    page_tokens: int
+
+    def __post_init__(self):
+        table = _entries(self.page_table, "page_table", (None, None))
+        n, cols = self.page_table.shape
+        self._c = _CPages(self.refs.numel(), n, cols, int(self.page_tokens),
+                          _entries(self.refs, "refs", (None,)), table, _entries(self.held, "held", (n,)))
+
+
+@dataclasses.dataclass
+class Moves:
+    """Pages to be moved (``scd_moves_t``): ``pairs`` int32 [capacity, 2] (from, to), ``status`` int32 [4]:
+    the count of pairs, pages in use, pages missing, requests that do not fit the table."""
+    pairs: torch.Tensor
+    status: torch.Tensor
+
+    def __post_init__(self):
+        pairs = _entries(self.pairs, "pairs", (None, 2))
+        self._c = _CMoves(self.pairs.shape[0], pairs, _entries(self.status, "status", (4,)))
+
+
+def scd_pages_workspace_bytes(pages: Pages) -> int:
+    return int(load_library().scd_pages_workspace_bytes(ctypes.byref(pages._c)))
+
+
+def prepare_pages_free(pages: Pages, seqs) -> Prepared:
+    """Requests seqs (int32, device) give their pages back."""
+    return Prepared(load_library().scd_pages_free,
+                    (ctypes.byref(pages._c), seqs.numel(), _entries(seqs, "seqs", (None,))), (pages, seqs))
+
+
+def scd_pages_free(pages: Pages, seqs, stream=None) -> None:
+    prepare_pages_free(pages, seqs)(stream)
+
+
+def prepare_pages_fork(pages: Pages, src, dst) -> Prepared:
+    """Request dst[i] becomes a copy of src[i] that shares its pages (int32, device)."""
+    args = (ctypes.byref(pages._c), src.numel(), _entries(src, "src", (None,)), _entries(dst, "dst", (src.numel(),)))
+    return Prepared(load_library().scd_pages_fork, args, (pages, src, dst))
+
+
+def scd_pages_fork(pages: Pages, src, dst, stream=None) -> None:
+    prepare_pages_fork(pages, src, dst)(stream)
+
+
+def prepare_pages_reserve(pages: Pages, batch: Batch, moves: Moves, workspace: Optional[torch.Tensor] = None,
+                          stream=None) -> Prepared:
+    """Pages for every request's new tokens: missing ones, and fresh ones in place of shared ones, whose
+    contents ``moves`` lists for :func:`scd_pages_copy`.  ``workspace`` None: one is made on ``stream``
+    (or the current one) and kept with the call."""
+    workspace = _workspace_of(workspace, scd_pages_workspace_bytes(pages), pages.refs.device, stream)
+    args = (ctypes.byref(pages._c), ctypes.byref(batch._c), ctypes.byref(moves._c), *_workspace_arg(workspace))
+    return Prepared(load_library().scd_pages_reserve, args, (pages, batch, moves, workspace))
+
+
+def scd_pages_reserve(pages: Pages, batch: Batch, moves: Moves, workspace: Optional[torch.Tensor] = None,
+                      stream=None) -> None:
+    prepare_pages_reserve(pages, batch, moves, workspace, stream)(stream)
+
+
+def prepare_pages_compact(pages: Pages, moves: Moves, out: Optional[Pages] = None,
+                          workspace: Optional[torch.Tensor] = None, stream=None) -> Prepared:
+    """The pages in use become the pool's first ones; table and counts go to ``out`` (None: in place), whose
+    ``held`` is not written, and the moves to ``moves``."""
+    workspace = _workspace_of(workspace, scd_pages_workspace_bytes(pages), pages.refs.device, stream)
+    args = (ctypes.byref(pages._c), None if out is None else ctypes.byref(out._c), ctypes.byref(moves._c),
+            *_workspace_arg(workspace))
+    return Prepared(load_library().scd_pages_compact, args, (pages, moves, out, workspace))
+
+
+def scd_pages_compact(pages: Pages, moves: Moves, out: Optional[Pages] = None,
+                      workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    prepare_pages_compact(pages, moves, out, workspace, stream)(stream)
+
+
+def prepare_pages_copy(caches, moves: Moves) -> Prepared:
+    """Contents of the listed pages, in every cache (:class:`PagedCache` or :class:`LatentCache`, all of
+    the same number of pages)."""
+    tensors = []
+    for c in caches:
+        tensors += [c.pages] if isinstance(c, LatentCache) else [c.k_pages, c.v_pages, c.k_scales, c.v_scales]
+    if not tensors:
+        raise ValueError("caches must name one cache at least")
+    if any(t.shape[0] != tensors[0].shape[0] for t in tensors):
+        raise ValueError("the caches differ in their number of pages")
+    planes = (_CPlane * len(tensors))(*[_CPlane(t.data_ptr(), t[0].numel() * t.element_size()) for t in tensors])
+    args = (len(tensors), planes, tensors[0].shape[0], ctypes.byref(moves._c))
+    return Prepared(load_library().scd_pages_copy, args, (tensors, planes, moves))
+
+
+def scd_pages_copy(caches, moves: Moves, stream=None) -> None:
+    prepare_pages_copy(caches, moves)(stream)

@@ -1,0 +1,376 @@
+// The step that attention over latents and over dense rows share (gfx950): the scores of 16 query rows a
+// wave (or two times 16) against a step of positions that lie in LDS, the softmax's running maximum and
+// sum, and the weighted sum of the values.
+//
+//   s_j = q . k_j,  m = max_j s_j,  l = sum_j 2^(s_j - m),  o = sum_j 2^(s_j - m) v_j
+//
+// in powers of two: q or the scores carry log2(e).  Scores are formed transposed, positions as matrix rows
+// and query rows as columns, so that a lane's scores belong to one query row and are, as they stand, the
+// right operand of the second product: weights never leave the registers.  That product's contraction runs
+// over the positions in the order the lanes hold them, which the transposing LDS reads of the values follow.
+#pragma once
+
+#include "scd_serve_device.h"
+#include "scd_latent.h"
+
+namespace scd {
+namespace dev {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* lds_s16x4_t;
+
+// kStep positions a wave takes at once, kVec channels of a 16-byte piece.
+template <typename T> struct Elem;
+template <> struct Elem<uint16_t> {
+  static constexpr int kStep = 32, kVec = 8;
+  typedef bf16x8 Frag;
+};
+template <> struct Elem<float> {
+  static constexpr int kStep = 16, kVec = 4;
+  typedef f32x4 Frag;
+};
+
+__device__ inline f32x4 mma(const bf16x8& a, const bf16x8& b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+// 16 channels: contraction step j takes channel 4 g + j of lane group g.
+__device__ inline f32x4 mma(const f32x4& a, const f32x4& b, f32x4 c) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+  return c;
+}
+
+// Whether one of the 16-byte piece's values is not finite.
+__device__ inline bool odd_piece(const uint16_t* p) {
+  const uint4 v = *reinterpret_cast<const uint4*>(p);
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    bad |= (w[i] & 0x7f800000u) == 0x7f800000u || (w[i] & 0x7f80u) == 0x7f80u;
+  return bad;
+}
+__device__ inline bool odd_piece(const float* p) {
+  const uint4 v = *reinterpret_cast<const uint4*>(p);
+  return (v.x & 0x7f800000u) == 0x7f800000u || (v.y & 0x7f800000u) == 0x7f800000u ||
+         (v.z & 0x7f800000u) == 0x7f800000u || (v.w & 0x7f800000u) == 0x7f800000u;
+}
+
+// kFrags pieces of 4 kVec channels that a score contracts at most (the first kFixed always), kTiles tiles of
+// 16 value channels (the first kFixedTiles always), NT tiles of 16 query rows, a query as kParts summands;
+// kKeyRow, kValueRow elements between LDS rows.
+template <typename T, int kFrags, int kFixed, int kTiles, int kFixedTiles, int NT, int kParts, int kKeyRow,
+          int kValueRow>
+struct AttendCore {
+  typedef typename Elem<T>::Frag Frag;
+  static constexpr int kStep = Elem<T>::kStep, kVec = Elem<T>::kVec, kSub = kStep / 16;
+
+  Frag q[NT][kParts][kFrags];
+  f32x4 o[NT][kTiles];
+  float m[NT], l[NT];  // l: this lane's positions only
+  int limit[NT];       // last position the lane's row attends to
+
+  __device__ void clear() {
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      m[n] = -INFINITY;
+      l[n] = 0.f;
+#pragma unroll
+      for (int c = 0; c < kTiles; ++c) o[n][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+  }
+
+  // Positions pos .. pos + kStep - 1 at LDS rows k, v.  kCareful: some row leaves some of them out (behind its
+  // limit, or in a hole: bit t of `holes` for positions 16 t on); weights there are zero and values that are
+  // not finite do not count.  A value that is not finite makes its channel NaN for the rows that attend to it.
+  template <bool kCareful>
+  __device__ void step(const T* k, const T* v, int frags, int tiles, float scale, int pos, int holes, int lane) {
+    const int lr = lane & 15, g = lane >> 4;
+    f32x4 s[kSub][NT];
+#pragma unroll
+    for (int t = 0; t < kSub; ++t)
+#pragma unroll
+      for (int n = 0; n < NT; ++n) s[t][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int f = 0; f < kFrags; ++f) {
+      if (f < kFixed || f < frags) {
+#pragma unroll
+        for (int t = 0; t < kSub; ++t) {
+          const Frag a = *reinterpret_cast<const Frag*>(k + (16 * t + lr) * kKeyRow + 4 * kVec * f + kVec * g);
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < kParts; ++i) s[t][n] = mma(a, q[n][i][f], s[t][n]);
+        }
+      }
+    }
+    bool odd = false;
+    if constexpr (kCareful) {
+      for (int i = lane; i < kStep * 16 * tiles / kVec; i += 64) {
+        const int row = i / (16 / kVec * tiles), c = i - row * (16 / kVec * tiles);
+        odd |= odd_piece(v + row * kValueRow + kVec * c);
+      }
+      odd = __any(odd);
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < kSub; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float x = s[t][n][i] * scale;
+          if constexpr (kCareful) x = seen(n, t, i, pos, holes, g) ? x : -INFINITY;
+          s[t][n][i] = x;
+          top = fmaxf(top, x);
+        }
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      if (__any(top > m[n])) {
+        const float now = fmaxf(top, m[n]);
+        const float by = __builtin_amdgcn_exp2f(m[n] - (now == -INFINITY ? 0.f : now));
+        m[n] = now;
+        l[n] *= by;
+#pragma unroll
+        for (int c = 0; c < kTiles; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[n][c][i] *= by;
+      }
+      const float base = m[n] == -INFINITY ? 0.f : m[n];
+#pragma unroll
+      for (int t = 0; t < kSub; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[t][n][i] = __builtin_amdgcn_exp2f(s[t][n][i] - base);
+          l[n] += s[t][n][i];
+        }
+    }
+    if (kCareful && odd) {
+      weigh<true>(v, s, tiles, pos, holes, lr, g);
+    } else {
+      weigh<false>(v, s, tiles, pos, holes, lr, g);
+    }
+  }
+
+  // The row's sum over the lanes that hold its positions.
+  __device__ float sum(int n) const {
+    float x = l[n];
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+  }
+
+ private:
+  __device__ bool seen(int n, int t, int i, int pos, int holes, int g) const {
+    return pos + 16 * t + 4 * g + i <= limit[n] && !(holes >> t & 1);
+  }
+
+  template <bool kOdd>
+  __device__ void weigh(const T* v, const f32x4 (&s)[kSub][NT], int tiles, int pos, int holes, int lr, int g) {
+    if constexpr (sizeof(T) == 2) {
+      bf16x8 w[NT], ones[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          // one rounding of a weight to bf16, 8 bits: over many positions it averages out, and the heaviest
+          // position of a row that one position dominates has a weight of 1, which is exact
+          w[n][e] = static_cast<__bf16>(s[e >> 2][n][e & 3]);
+          if constexpr (kOdd) ones[n][e] = static_cast<__bf16>(seen(n, e >> 2, e & 3, pos, holes, g) ? 1.f : 0.f);
+        }
+#pragma unroll
+      for (int c = 0; c < kTiles; ++c) {
+        if (c < kFixedTiles || c < tiles) {
+          union { s16x4 h[2]; bf16x8 v; uint16_t u[8]; } a;
+          const T* at = v + (4 * g + (lr >> 2)) * kValueRow + 16 * c + 4 * (lr & 3);
+          a.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(at));
+          a.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(at + 16 * kValueRow));
+          if constexpr (kOdd) {
+            union { bf16x8 v; uint16_t u[8]; } flag;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const bool bad = (a.u[e] & 0x7f80) == 0x7f80;
+              flag.u[e] = bad ? 0x3f80 : 0;
+              if (bad) a.u[e] = 0;
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+              const f32x4 x = mma(flag.v, ones[n], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (x[i] > 0.f) o[n][c][i] = __builtin_nanf("");
+            }
+          }
+#pragma unroll
+          for (int n = 0; n < NT; ++n) o[n][c] = mma(a.v, w[n], o[n][c]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int c = 0; c < kTiles; ++c) {
+        if (c < kFixedTiles || c < tiles) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float a = v[(4 * g + i) * kValueRow + 16 * c + lr];
+            if constexpr (kOdd) {
+              const bool bad = (__float_as_uint(a) & 0x7f800000u) == 0x7f800000u;
+              if (bad) a = 0.f;
+#pragma unroll
+              for (int n = 0; n < NT; ++n) {
+                const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                    bad ? 1.f : 0.f, seen(n, 0, i, pos, holes, g) ? 1.f : 0.f, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  if (x[e] > 0.f) o[n][c][e] = __builtin_nanf("");
+              }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+              o[n][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, s[0][n][i], o[n][c], 0, 0, 0);
+          }
+        }
+      }
+    }
+  }
+};
+
+// 16 bytes a lane from memory into LDS, `to` the wave's first byte.
+__device__ inline void copy16(const void* from, char* to) {
+  __builtin_amdgcn_global_load_lds(from, (lds_void_t)to, 16, 0, 0);
+}
+
+// s_waitcnt vmcnt(n), the other counters left alone.
+template <int n>
+__device__ inline void wait_copies() {
+  static_assert(n >= 0 && n < 64, "counter range");
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (n & 15) | (n >> 4) << 14);
+}
+
+// ---- shares ------------------------------------------------------------------------------------------
+// A request's query rows make tiles, its positions blocks of kBlock.  While there are fewer tiles than twice what
+// fills the chip, every tile's positions are cut into shares of at most `chunk` blocks, so that the shares of all
+// tiles are no more than the goal:  sum ceil(blocks / chunk) <= sum blocks / chunk + tiles <= goal.
+struct Share {
+  Span span;
+  int64_t len;     // positions of the request
+  int b, head, tile, tiles, part, parts;
+  int64_t first;   // unit of the tile's first share; share s is unit first + s * tiles
+};
+struct ShareLds {
+  int64_t wave[2][16];
+  LocateLds found;
+};
+
+template <typename Length>
+struct Tiles {
+  const SharePlan& p;
+  Length length;   // positions of request b with this span
+  int block;
+  __device__ int64_t tiles(const Span& s) const {
+    return ((s.end - s.begin) * p.per_token + p.rows - 1) / p.rows;
+  }
+  __device__ int64_t blocks(const Span& s, int b) const { return (length(s, b) + block - 1) / block; }
+};
+
+// The share that is work unit `unit`; false past the last.  Every thread calls it and gets the answer.
+template <int kThreads, typename Length>
+__device__ inline bool find_share(const SeqBatch& s, const SharePlan& p, int block, int least, int64_t unit,
+                                  ShareLds& lds, int tid, Length length, Share& out) {
+  const Tiles<Length> of{p, length, block};
+  int64_t chunk = int64_t{1} << 40;
+  if (p.cut) {
+    // all tiles, and all blocks of all tiles
+    int64_t tiles = 0, work = 0;
+    if (s.n_seqs == 1) {
+      const Span span = span_of(s, 0);
+      tiles = of.tiles(span);
+      work = tiles * of.blocks(span, 0);
+    } else {
+      for (int b = tid; b < s.n_seqs; b += kThreads) {
+        const Span span = span_of(s, b);
+        const int64_t n = of.tiles(span);
+        tiles += n;
+        work += n * of.blocks(span, b);
+      }
+      for (int o = 32; o > 0; o >>= 1) {
+        tiles += __shfl_xor(tiles, o);
+        work += __shfl_xor(work, o);
+      }
+      if ((tid & 63) == 0) {
+        lds.wave[0][tid >> 6] = tiles;
+        lds.wave[1][tid >> 6] = work;
+      }
+      __syncthreads();
+      tiles = work = 0;
+      for (int w = 0; w < kThreads / 64; ++w) {
+        tiles += lds.wave[0][w];
+        work += lds.wave[1][w];
+      }
+    }
+    tiles *= p.heads;
+    work *= p.heads;
+    if (tiles < 2 * p.target) {
+      const int64_t room = share_goal(tiles, p.target) - tiles;
+      chunk = room > 0 ? (work + room - 1) / room : chunk;
+      chunk = chunk < least ? least : chunk;
+    }
+  }
+  // heads one after another, each with all requests' shares; a head's number of shares is the same
+  const auto parts_of = [&](const Span& span, int b) {
+    const int64_t n = of.blocks(span, b);
+    return n <= chunk ? int64_t{1} : (n + chunk - 1) / chunk;
+  };
+  Located at;
+  int b_of = 0;
+  int64_t per_head = 0;
+  if (s.n_seqs == 1) {
+    const Span span = span_of(s, 0);
+    per_head = of.tiles(span) * parts_of(span, 0);
+    if (per_head == 0 || unit >= per_head * p.heads) return false;
+    out.head = static_cast<int>(unit / per_head);
+    at.b = 0;
+    at.span = span;
+    at.local = unit - out.head * per_head;
+    out.first = out.head * per_head;
+  } else {
+    out.head = 0;
+    out.first = 0;
+    int64_t left = unit;
+    if (p.heads > 1) {
+      int64_t n = 0;
+      for (int b = tid; b < s.n_seqs; b += kThreads) {
+        const Span span = span_of(s, b);
+        n += of.tiles(span) * parts_of(span, b);
+      }
+      for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
+      __syncthreads();
+      if ((tid & 63) == 0) lds.wave[0][tid >> 6] = n;
+      __syncthreads();
+      for (int w = 0; w < kThreads / 64; ++w) per_head += lds.wave[0][w];
+      if (per_head == 0 || unit >= per_head * p.heads) return false;
+      out.head = static_cast<int>(unit / per_head);
+      left = unit - out.head * per_head;
+    }
+    // locate() calls the count once for every request of this thread, in order
+    int next = tid;
+    const auto count = [&](const Span& span) {
+      const int b = next;
+      next += kThreads;
+      return b < s.n_seqs ? of.tiles(span) * parts_of(span, b) : int64_t{0};
+    };
+    if (!locate<kThreads>(s, left, lds.found, tid, count, at)) return false;
+    out.first = unit - at.local;
+  }
+  b_of = at.b;
+  out.b = b_of;
+  out.span = at.span;
+  out.len = length(at.span, b_of);
+  out.tiles = static_cast<int>(of.tiles(at.span));
+  out.parts = static_cast<int>(parts_of(at.span, b_of));
+  out.part = static_cast<int>(at.local / out.tiles);
+  out.tile = static_cast<int>(at.local - static_cast<int64_t>(out.part) * out.tiles);
+  out.first += out.tile;
+  return true;
+}
+
+}  // namespace dev
+}  // namespace scd

@@ -1,0 +1,370 @@
+// Pages of caches given back, shared, reserved and moved to the front (gfx950).
+//
+// A page is in use while table entries name it; refs counts them.  What a call hands out is decided by
+// numbers alone: the lowest free pages, to requests in their order and a request's positions in theirs.  All
+// of it is integers, a few hundred to some ten thousand, so the calls are chains of dependent memory accesses
+// of one workgroup (a workgroup a request where requests are on their own); the contents are moved by
+// pages_copy_kernel, which HBM bounds.
+#include <algorithm>
+
+#include "scd_pages.h"
+#include "scd_serve_device.h"
+
+namespace scd {
+using namespace dev;
+
+constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
+
+// Whether value v is among list[0 .. n).
+template <int kThreads>
+__device__ inline bool listed(const int32_t* list, int n, int v, int tid) {
+  int found = 0;
+  for (int i = tid; i < n; i += kThreads) found |= list[i] == v;
+  return __syncthreads_or(found) != 0;
+}
+
+// Workgroup i takes request seqs[i] out of its pages; one named before it in the list is left to that one.
+__global__ __launch_bounds__(256) void pages_free_kernel(PagePool p, const int32_t* seqs) {
+  const int tid = threadIdx.x, i = blockIdx.x, b = seqs[i];
+  if (b < 0 || b >= p.n_seqs || listed<256>(seqs, i, b, tid)) return;
+  int32_t* row = p.table + static_cast<int64_t>(b) * p.cols;
+  for (int j = tid; j < p.cols; j += 256) {
+    const int id = row[j];
+    // a count that is zero already stays zero
+    if (id >= 0 && id < p.n_pages && atomicSub(p.refs + id, 1) <= 0) atomicAdd(p.refs + id, 1);
+    row[j] = -1;
+  }
+  if (tid == 0) p.held[b] = 0;
+}
+
+// Workgroup i gives request dst[i] the pages of what src[i] holds.
+__global__ __launch_bounds__(256) void pages_fork_kernel(PagePool p, int n, const int32_t* src, const int32_t* dst) {
+  const int tid = threadIdx.x, i = blockIdx.x, from = src[i], to = dst[i];
+  if (from < 0 || from >= p.n_seqs || to < 0 || to >= p.n_seqs) return;
+  // A row that is written is written by one workgroup and read by no other: the first pair that names it,
+  // and no pair that takes it for a source.
+  if (listed<256>(dst, i, to, tid) || listed<256>(dst, n, from, tid)) return;
+  int32_t* row = p.table + static_cast<int64_t>(to) * p.cols;
+  const int32_t* old = p.table + static_cast<int64_t>(from) * p.cols;
+  int any = p.held[to] != 0;
+  for (int j = tid; j < p.cols; j += 256) any |= row[j] >= 0 && row[j] < p.n_pages;
+  if (__syncthreads_or(any)) return;
+  const int64_t held = p.held[from];
+  for (int j = tid; j < p.cols; j += 256) {
+    int id = static_cast<int64_t>(j) * p.page < held ? old[j] : -1;
+    id = id >= 0 && id < p.n_pages ? id : -1;
+    row[j] = id;
+    if (id >= 0) atomicAdd(p.refs + id, 1);
+  }
+  if (tid == 0) p.held[to] = static_cast<int32_t>(held);
+}
+
+// Sum over the workgroup of x, and of the threads before this one.
+struct PlanLds {
+  int wave[kPlanWaves];
+};
+__device__ inline int plan_scan(int x, PlanLds& lds, int tid, int& total) {
+  const int lane = tid & 63, wave = tid >> 6;
+  int sum = x;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int other = __shfl_up(sum, o);
+    if (lane >= o) sum += other;
+  }
+  __syncthreads();  // the last scan's readers are done
+  if (lane == 63) lds.wave[wave] = sum;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanWaves; ++w) {
+    const int v = lds.wave[w];
+    if (w < wave) before += v;
+    total += v;
+  }
+  return before + sum - x;
+}
+
+// Pages that the new tokens of every request go to, one workgroup for all.  A missing page is taken, and so
+// is one in place of a page that others name too; where that holds earlier positions its contents are to be
+// moved (a move is listed).  If all that name a page are to write to it, the last of them keeps it.
+__global__ __launch_bounds__(kPlanThreads) void pages_reserve_kernel(PagePool p, SeqBatch batch, PageMoves m, int32_t* ws) {
+  __shared__ PlanLds lds;
+  __shared__ int refused;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int32_t* writers = ws;                        // [n_pages] requests that write to a shared page
+  int32_t* keeper = writers + p.n_pages;        // [n_pages] the last of them
+  int32_t* free = keeper + p.n_pages;           // [n_pages] free pages, lowest first
+  int32_t* takes = free + p.n_pages;            // [n_seqs] pages that a request takes, then where its begin
+  int32_t* copies = takes + p.n_seqs;           // [n_seqs] likewise of its moves
+  if (tid == 0) refused = 0;
+  __syncthreads();
+
+  // a request's columns lo .. hi - 1 are written
+  struct Range { int64_t lo, hi, held; };
+  const auto range = [&](int b) {
+    const Span s = span_of(batch, b);
+    const int64_t n = s.end - s.begin, held = p.held[b];
+    Range r{0, 0, held};
+    if (n <= 0) return r;
+    r.lo = held / p.page;
+    r.hi = (held + n + p.page - 1) / p.page;
+    if (held < 0 || r.hi > p.cols) {
+      r.lo = r.hi = 0;
+      if (lane == 0) atomicAdd(&refused, 1);
+    }
+    return r;
+  };
+  const auto load = [](const int32_t* at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+  const auto store = [](int32_t* at, int v) { __hip_atomic_store(at, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };
+  // every page that is named in the requests' ranges
+  const auto each = [&](auto&& visit) {
+    for (int b = wave; b < p.n_seqs; b += kPlanWaves) {
+      const Range r = range(b);
+      for (int64_t j = r.lo + lane; j < r.hi; j += 64) {
+        const int id = p.table[static_cast<int64_t>(b) * p.cols + j];
+        if (id >= 0 && id < p.n_pages) visit(b, id);
+      }
+    }
+    __threadfence();
+    __syncthreads();
+  };
+  // A page's keeper writes to it, the others take pages of their own: its only owner; of several the last,
+  // and none if requests that do not write name it too.
+  each([&](int b, int id) {
+    const bool shared = p.refs[id] > 1;
+    store(writers + id, 0);
+    store(keeper + id, shared ? -1 : b);
+  });
+  const int wrong = refused;
+  __syncthreads();
+  if (wrong > 0) {
+    if (tid < 4) m.status[tid] = tid == 3 ? wrong : 0;
+    return;
+  }
+  each([&](int b, int id) {
+    if (p.refs[id] <= 1) return;
+    atomicAdd(writers + id, 1);
+    atomicMax(keeper + id, b);
+  });
+  each([&](int b, int id) {
+    if (p.refs[id] > 1 && load(keeper + id) == b && p.refs[id] > load(writers + id)) store(keeper + id, -1);
+  });
+  for (int b = wave; b < p.n_seqs; b += kPlanWaves) {
+    const Range r = range(b);
+    int taken = 0, moved = 0;
+    for (int64_t j = r.lo + lane; j < r.hi; j += 64) {
+      const int id = p.table[static_cast<int64_t>(b) * p.cols + j];
+      const bool missing = id < 0 || id >= p.n_pages, left = !missing && load(keeper + id) != b;
+      taken += missing || left;
+      moved += left && j * p.page < r.held;
+    }
+    for (int o = 32; o > 0; o >>= 1) {
+      taken += __shfl_xor(taken, o);
+      moved += __shfl_xor(moved, o);
+    }
+    if (lane == 0) {
+      takes[b] = taken;
+      copies[b] = moved;
+    }
+  }
+  __threadfence();
+  __syncthreads();
+  int wanted = 0, moves = 0;
+  for (int b0 = 0; b0 < p.n_seqs; b0 += kPlanThreads) {
+    const int b = b0 + tid;
+    const int x = b < p.n_seqs ? takes[b] : 0, y = b < p.n_seqs ? copies[b] : 0;
+    int total;
+    const int at = plan_scan(x, lds, tid, total);
+    if (b < p.n_seqs) takes[b] = wanted + at;
+    wanted += total;
+    const int to = plan_scan(y, lds, tid, total);
+    if (b < p.n_seqs) copies[b] = moves + to;
+    moves += total;
+  }
+  int found = 0;
+  for (int id0 = 0; id0 < p.n_pages && found < wanted; id0 += 4 * kPlanThreads) {
+    const int id = id0 + 4 * tid;
+    bool open[4];
+    int n = 0, total;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      open[e] = id + e < p.n_pages && p.refs[id + e] <= 0;
+      n += open[e];
+    }
+    int at = found + plan_scan(n, lds, tid, total);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (open[e]) free[at++] = id + e;
+    found += total;
+  }
+  if (found < wanted || moves > m.capacity) {
+    if (tid < 4) m.status[tid] = tid == 2 ? std::max(wanted - found, 1) : 0;
+    return;
+  }
+  __threadfence();
+  __syncthreads();
+  // All is decided, by keepers alone: from here on tables and counts are written.
+  for (int b = wave; b < p.n_seqs; b += kPlanWaves) {
+    const Range r = range(b);
+    int take = takes[b], move = copies[b];
+    for (int64_t j0 = r.lo; j0 < r.hi; j0 += 64) {
+      const int64_t j = j0 + lane, at = static_cast<int64_t>(b) * p.cols + j;
+      const int id = j < r.hi ? p.table[at] : 0;
+      const bool missing = j < r.hi && (id < 0 || id >= p.n_pages);
+      const bool left = j < r.hi && !missing && load(keeper + id) != b;
+      const bool moved = left && j * p.page < r.held;
+      const uint64_t taking = __ballot(missing || left), moving = __ballot(moved);
+      const uint64_t below = (uint64_t{1} << lane) - 1;
+      if (missing || left) {
+        const int to = free[take + __popcll(taking & below)];
+        p.table[at] = to;
+        p.refs[to] = 1;
+        if (left) atomicSub(p.refs + id, 1);
+        if (moved) {
+          const int64_t k = 2 * static_cast<int64_t>(move + __popcll(moving & below));
+          m.pairs[k] = id;
+          m.pairs[k + 1] = to;
+        }
+      }
+      take += __popcll(taking);
+      move += __popcll(moving);
+    }
+  }
+  if (tid < 4) m.status[tid] = tid == 0 ? moves : 0;
+}
+
+// The pages in use become pages 0 .. n - 1: the k-th of those behind goes to the k-th free one in front.
+__global__ __launch_bounds__(kPlanThreads) void pages_compact_kernel(PagePool p, int32_t* refs_out, PageMoves m,
+                                                                     int32_t* ws) {
+  __shared__ PlanLds lds;
+  const int tid = threadIdx.x;
+  int32_t* to = ws;                 // [n_pages] where a page goes
+  int32_t* high = to + p.n_pages;   // [n_pages] pages that move, counts with them
+  int32_t* hole = high + p.n_pages;
+  int mine = 0, used;
+  for (int id = tid; id < p.n_pages; id += kPlanThreads) mine += p.refs[id] > 0;
+  plan_scan(mine, lds, tid, used);
+  int highs = 0, holes = 0;
+  for (int id0 = 0; id0 < p.n_pages; id0 += 4 * kPlanThreads) {
+    const int id = id0 + 4 * tid;
+    int refs[4], n = 0, k = 0, total;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      refs[e] = id + e < p.n_pages ? p.refs[id + e] : 0;
+      n += refs[e] > 0 && id + e >= used;
+      k += id + e < used && refs[e] <= 0;
+    }
+    int at = highs + plan_scan(n, lds, tid, total);
+    highs += total;
+    int gap = holes + plan_scan(k, lds, tid, total);
+    holes += total;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (id + e >= p.n_pages) continue;
+      to[id + e] = id + e;
+      if (refs[e] > 0 && id + e >= used) high[at++] = id + e;
+      if (id + e < used && refs[e] <= 0) hole[gap++] = id + e;
+      refs_out[id + e] = refs[e] > 0 ? refs[e] : 0;
+    }
+  }
+  __threadfence();
+  __syncthreads();
+  // as many holes in front as pages behind; no more than half of the pool, which the list holds
+  for (int k = tid; k < highs; k += kPlanThreads) {
+    const int from = high[k], gap = hole[k];
+    to[from] = gap;
+    refs_out[gap] = refs_out[from];
+    refs_out[from] = 0;
+    m.pairs[2 * static_cast<int64_t>(k)] = from;
+    m.pairs[2 * static_cast<int64_t>(k) + 1] = gap;
+  }
+  if (tid < 4) m.status[tid] = tid == 0 ? highs : tid == 1 ? used : 0;
+}
+
+__global__ __launch_bounds__(256) void pages_rename_kernel(PagePool p, int32_t* table_out, const int32_t* to, int64_t n) {
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < n; i += static_cast<int64_t>(gridDim.x) * 256) {
+    const int id = p.table[i];
+    table_out[i] = id >= 0 && id < p.n_pages ? to[id] : -1;
+  }
+}
+
+// Units of kPiece bytes of one move of one plane, dealt to as many workgroups as the chip holds: the count of
+// moves is read on the device.  Four 16-byte loads a thread are under way before the first store.
+constexpr int kPiece = 16384;
+__global__ __launch_bounds__(256) void pages_copy_kernel(PagesCopyParams p, int64_t pieces) {
+  const int tid = threadIdx.x;
+  int n = p.moves.status[0];
+  n = n < 0 ? 0 : (n > p.moves.capacity ? p.moves.capacity : n);
+  const int64_t units = pieces * n;  // pieces: of a page in all planes
+  for (int64_t unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    // a move's pieces lie in different planes: neighbours take the same piece of neighbouring moves
+    const int64_t piece = unit / n;
+    const int k = static_cast<int>(unit - piece * n);
+    int64_t left = piece;
+    int plane = 0;
+    for (;; ++plane) {
+      const int64_t of = (p.planes[plane].page_bytes + kPiece - 1) / kPiece;
+      if (left < of) break;
+      left -= of;
+    }
+    const int from = p.moves.pairs[2 * static_cast<int64_t>(k)], to = p.moves.pairs[2 * static_cast<int64_t>(k) + 1];
+    if (from < 0 || from >= p.n_pages || to < 0 || to >= p.n_pages) continue;
+    const int64_t bytes = p.planes[plane].page_bytes, at = left * kPiece;
+    const char* src = p.planes[plane].data + from * bytes + at;
+    char* dst = p.planes[plane].data + to * bytes + at;
+    const int size = static_cast<int>(bytes - at < kPiece ? bytes - at : kPiece);
+    if (bytes % 16 == 0) {
+      u32x4 x[kPiece / 4096];
+#pragma unroll
+      for (int j = 0; j < kPiece / 4096; ++j)
+        if (16 * tid + 4096 * j < size) x[j] = *reinterpret_cast<const u32x4*>(src + 16 * tid + 4096 * j);
+#pragma unroll
+      for (int j = 0; j < kPiece / 4096; ++j)
+        if (16 * tid + 4096 * j < size) *reinterpret_cast<u32x4*>(dst + 16 * tid + 4096 * j) = x[j];
+    } else {
+      for (int i = 4 * tid; i < size; i += 1024)
+        *reinterpret_cast<uint32_t*>(dst + i) = *reinterpret_cast<const uint32_t*>(src + i);
+    }
+  }
+}
+
+size_t pages_workspace(int64_t n_pages, int64_t n_seqs) {
+  return static_cast<size_t>(3 * n_pages + 2 * n_seqs) * sizeof(int32_t);
+}
+
+hipError_t launch_pages_free(const PagePool& p, int n, const int32_t* seqs, hipStream_t stream) {
+  hipLaunchKernelGGL(pages_free_kernel, dim3(n), dim3(256), 0, stream, p, seqs);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_fork(const PagePool& p, int n, const int32_t* src, const int32_t* dst, hipStream_t stream) {
+  hipLaunchKernelGGL(pages_fork_kernel, dim3(n), dim3(256), 0, stream, p, n, src, dst);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_reserve(const PagePool& p, const SeqBatch& b, const PageMoves& m, int32_t* ws,
+                                hipStream_t stream) {
+  hipLaunchKernelGGL(pages_reserve_kernel, dim3(1), dim3(kPlanThreads), 0, stream, p, b, m, ws);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_compact(const PagePool& p, const PagePool& out, const PageMoves& m, int32_t* ws,
+                                hipStream_t stream) {
+  hipLaunchKernelGGL(pages_compact_kernel, dim3(1), dim3(kPlanThreads), 0, stream, p, out.refs, m, ws);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const int64_t n = static_cast<int64_t>(p.n_seqs) * p.cols;
+  hipLaunchKernelGGL(pages_rename_kernel, dim3(static_cast<unsigned>(std::min<int64_t>((n + 255) / 256, 2048))), dim3(256),
+                     0, stream, p, out.table, ws, n);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_copy(const PagesCopyParams& p, hipStream_t stream) {
+  int64_t pieces = 0;
+  for (int i = 0; i < p.n_planes; ++i) pieces += (p.planes[i].page_bytes + kPiece - 1) / kPiece;
+  const int64_t blocks = std::min<int64_t>(2048, pieces * p.moves.capacity);
+  hipLaunchKernelGGL(pages_copy_kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream, p, pieces);
+  return hipGetLastError();
+}
+
+}  // namespace scd

@@ -1,0 +1,264 @@
+// Causal attention over dense keys and values (gfx950), key and value rows of different widths, grouped heads.
+//
+// A workgroup takes a tile of query rows of one KV head (its group's heads side by side) and goes through the
+// positions in blocks that four waves fetch into LDS ahead of the arithmetic.  With 128 rows the matrix cores
+// and the LDS reads of the right operands take the same time, and the softmax's exponentials and maxima run
+// beside them in the other workgroup of the CU.
+#pragma once
+
+#include "scd_attend_core.h"
+
+namespace scd {
+using namespace dev;
+
+template <typename T, int kKey, int kValue, int NT>
+struct RowsShape {
+  static constexpr int kVec = Elem<T>::kVec;
+  static constexpr int kBlock = 2 * Elem<T>::kStep;
+  static constexpr int kKeyPieces = kKey / kVec + 1, kValuePieces = kValue / kVec + 1;  // odd
+  static constexpr int kBlockBytes = kBlock * (kKeyPieces + kValuePieces) * 16;
+  static constexpr int kRing = kBlockBytes * 6 <= 156 * 1024 ? 3 : kBlockBytes * 4 <= 156 * 1024 ? 2 :
+                               kBlockBytes * 3 <= 156 * 1024 ? 3 : 2;
+  static constexpr int kFrags = kKey / (4 * kVec), kTiles = kValue / 16;
+  static constexpr int kFixed = (kKey == 64 ? 32 : kKey - 32) / (4 * kVec);
+  static constexpr int kFixedTiles = (kValue == 64 ? 32 : kValue - 32) / 16;
+  typedef AttendCore<T, kFrags, kFixed, kTiles, kFixedTiles, NT, 1, kKeyPieces * kVec, kValuePieces * kVec> Core;
+};
+
+// Rows pos0 .. pos0 + kBlock - 1 (the last one seen in place of those behind it) into LDS rows of kPieces 16-byte
+// pieces, `pieces` of them filled: straight from memory, or, where rows do not start on 16 bytes, element by element.
+template <typename T, int kBlock, int kPieces>
+__device__ inline void fetch_rows(const T* from, int64_t stride, bool wide, int pieces, int64_t pos0, int64_t seen,
+                                  char* to, int wave, int lane) {
+  constexpr int kVec = Elem<T>::kVec, kCopies = (kBlock * kPieces + 63) / 64;
+#pragma unroll
+  for (int j = 0; j < (kCopies + 3) / 4; ++j) {
+    if (4 * j + 3 < kCopies || wave + 4 * j < kCopies) {
+      const int i = (wave + 4 * j) * 64 + lane, row = i / kPieces, piece = i - row * kPieces;
+      if (row < kBlock && piece < pieces) {
+        const int64_t pos = pos0 + row < seen ? pos0 + row : seen - 1;
+        const T* src = from + pos * stride + kVec * piece;
+        if (wide) {
+          copy16(src, to + (wave + 4 * j) * 1024);
+        } else {
+          union { T t[kVec]; u32x4 v; } x;
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) x.t[e] = src[e];
+          *reinterpret_cast<u32x4*>(to + 16 * i) = x.v;
+        }
+      }
+    }
+  }
+}
+
+template <typename T, int kKey, int kValue, int NT>
+__global__ __launch_bounds__(256) void rows_attend_kernel(RowsAttendParams p) {
+  typedef RowsShape<T, kKey, kValue, NT> S;
+  typedef typename S::Core Core;
+  constexpr int kStep = Elem<T>::kStep, kVec = S::kVec;
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  __shared__ ShareLds lds;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lr = lane & 15, g = lane >> 4;
+
+  // positions that a request's rows can attend to: those its dense rows hold, up to its last query's
+  const auto length = [&](const Span& s, int b) {
+    const Span held = span_of(p.held, b);
+    const int64_t rows = held.end - held.begin, upto = s.pos0 + (s.end - s.begin) - held.pos0;
+    return upto < 0 ? int64_t{0} : (upto < rows ? upto : rows);
+  };
+  Share sh;
+  if (!find_share<256>(p.batch, p.plan, S::kBlock, 2, xcd_remap(blockIdx.x, gridDim.x), lds, tid, length, sh)) return;
+  const Span held = span_of(p.held, sh.b);
+  // the tiles that see most come first
+  const int tile = sh.tiles - 1 - sh.tile;
+
+  const int group = p.plan.per_token;
+  const int n_rows = static_cast<int>(sh.span.end - sh.span.begin) * group;
+  const int row0 = tile * p.plan.rows;
+  const int tile_rows = n_rows - row0 < p.plan.rows ? n_rows - row0 : p.plan.rows;
+  const int64_t base = sh.span.pos0 - held.pos0;  // the first query's place among the dense rows
+  int64_t seen = base + (row0 + tile_rows - 1) / group + 1;
+  seen = seen < 0 ? 0 : (seen > sh.len ? sh.len : seen);
+  const int blocks = static_cast<int>((seen + S::kBlock - 1) / S::kBlock);
+  const int first = static_cast<int>(static_cast<int64_t>(blocks) * sh.part / sh.parts);
+  const int last = static_cast<int>(static_cast<int64_t>(blocks) * (sh.part + 1) / sh.parts);
+  const int64_t unit = sh.first + static_cast<int64_t>(sh.part) * sh.tiles;
+  if (p.parts != nullptr && sh.part == 0 && tid < tile_rows) {
+    const int row = row0 + tid;
+    p.parts[(sh.span.begin + row / group) * p.q.n_heads + sh.head * group + row % group] =
+        RowParts{static_cast<int>(sh.first), sh.tiles, sh.parts, tid};
+  }
+
+  const int wr = wave % p.plan.row_groups, wp = wave / p.plan.row_groups;
+  const bool both = p.plan.row_groups == 4;
+  const bool works = both || wp < 2;
+
+  Core core;
+  core.clear();
+  int lowest = 0;
+  {
+    const int64_t low = base + row0 / group;
+    lowest = low < -1 ? -1 : (low >= seen ? static_cast<int>(seen) - 1 : static_cast<int>(low));
+  }
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    int row = (wr * NT + n) * 16 + lr;
+    row = row0 + (row < tile_rows ? row : tile_rows - 1);
+    const int64_t at = base + row / group;
+    core.limit[n] = at < 0 ? -1 : (at >= sh.len ? static_cast<int>(sh.len) - 1 : static_cast<int>(at));
+    const T* q = reinterpret_cast<const T*>(p.q.data) + (sh.span.begin + row / group) * p.q.token +
+                 (sh.head * group + row % group) * p.q.head;
+#pragma unroll
+    for (int f = 0; f < S::kFrags; ++f)
+      if (works && 4 * kVec * f < p.key) {
+        const T* from = q + 4 * kVec * f + kVec * g;
+        if (p.q.wide) {
+          core.q[n][0][f] = *reinterpret_cast<const typename Core::Frag*>(from);
+        } else {
+          union { T t[kVec]; typename Core::Frag v; } x;
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) x.t[e] = from[e];
+          core.q[n][0][f] = x.v;
+        }
+      }
+  }
+
+  if (first < last) {
+    constexpr int kKeyCopies = (S::kBlock * S::kKeyPieces + 63) / 64, kValueCopies = (S::kBlock * S::kValuePieces + 63) / 64;
+    constexpr int kMine = kKeyCopies / 4 + kValueCopies / 4;  // of a wave, at least
+    const T* keys = reinterpret_cast<const T*>(p.k.data) + held.begin * p.k.token + sh.head * p.k.head;
+    const T* vals = reinterpret_cast<const T*>(p.v.data) + held.begin * p.v.token + sh.head * p.v.head;
+    const auto fetch = [&](int block, int slot) {
+      char* to = smem + slot * S::kBlockBytes;
+      const int64_t pos0 = static_cast<int64_t>(block) * S::kBlock;
+      fetch_rows<T, S::kBlock, S::kKeyPieces>(keys, p.k.token, p.k.wide, p.key / kVec, pos0, seen, to, wave, lane);
+      fetch_rows<T, S::kBlock, S::kValuePieces>(vals, p.v.token, p.v.wide, p.value / kVec, pos0, seen,
+                                                to + S::kBlock * S::kKeyPieces * 16, wave, lane);
+    };
+    constexpr int kAhead = S::kRing - 1;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) fetch(first + i < last ? first + i : last - 1, i);
+    int slot = 0;
+    for (int block = first; block < last; ++block) {
+      wait_copies<(kAhead - 1) * kMine>();
+      lds_barrier();
+      fetch(block + kAhead < last ? block + kAhead : last - 1, slot == 0 ? S::kRing - 1 : slot - 1);
+      if (works) {
+        const int pos = block * S::kBlock;
+        const char* at = smem + slot * S::kBlockBytes;
+        const T* k = reinterpret_cast<const T*>(at);
+        const T* v = reinterpret_cast<const T*>(at + S::kBlock * S::kKeyPieces * 16);
+        const bool careful = pos + S::kBlock - 1 > lowest;
+        for (int st = both ? 0 : wp; st < (both ? 2 : wp + 1); ++st) {
+          const T* ks = k + st * kStep * (S::kKeyPieces * kVec);
+          const T* vs = v + st * kStep * (S::kValuePieces * kVec);
+          if (careful) {
+            core.template step<true>(ks, vs, p.key / (4 * kVec), p.value / 16, p.scale, pos + st * kStep, 0, lane);
+          } else {
+            core.template step<false>(ks, vs, p.key / (4 * kVec), p.value / 16, p.scale, pos + st * kStep, 0, lane);
+          }
+        }
+      }
+      slot = slot + 1 == S::kRing ? 0 : slot + 1;
+    }
+    wait_copies<0>();
+  }
+
+  constexpr int kLine = kValue + 4;
+  if (!both) {
+    float* rest = reinterpret_cast<float*>(smem);
+    lds_barrier();
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      float* row = rest + ((wr * NT + n) * 16 + lr) * kLine;
+      if (wp == 1) {
+        const float total = core.sum(n);
+        if (g == 0) {
+          row[kValue] = core.m[n];
+          row[kValue + 1] = total;
+        }
+#pragma unroll
+        for (int c = 0; c < S::kTiles; ++c) *reinterpret_cast<f32x4*>(row + 16 * c + 4 * g) = core.o[n][c];
+      }
+    }
+    lds_barrier();
+    if (wp != 0) return;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const float* row = rest + ((wr * NT + n) * 16 + lr) * kLine;
+      const float other = row[kValue], now = fmaxf(core.m[n], other), zero = now == -INFINITY ? 0.f : now;
+      const float mine = __builtin_amdgcn_exp2f(core.m[n] - zero), its = __builtin_amdgcn_exp2f(other - zero);
+      core.l[n] = core.sum(n) * mine + row[kValue + 1] * its;
+      core.m[n] = now;
+#pragma unroll
+      for (int c = 0; c < S::kTiles; ++c) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(row + 16 * c + 4 * g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) core.o[n][c][i] = core.o[n][c][i] * mine + x[i] * its;
+      }
+    }
+  }
+  const int line = p.value + 2;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int in_tile = (wr * NT + n) * 16 + lr, row = row0 + in_tile;
+    const float total = both ? core.sum(n) : core.l[n];
+    if (in_tile >= tile_rows) continue;
+    if (sh.parts > 1) {
+      float* out = p.slots + (unit * p.plan.rows + in_tile) * line;
+      if (g == 0) *reinterpret_cast<float2*>(out) = make_float2(core.m[n], total);
+#pragma unroll
+      for (int c = 0; c < S::kTiles; ++c)
+        if (c < S::kFixedTiles || 16 * c < p.value) {
+          float2* to = reinterpret_cast<float2*>(out + 2 + 16 * c + 4 * g);
+          to[0] = make_float2(core.o[n][c][0], core.o[n][c][1]);
+          to[1] = make_float2(core.o[n][c][2], core.o[n][c][3]);
+        }
+      continue;
+    }
+    const float by = total == 0.f ? 0.f : 1.f / total;
+    T* out = reinterpret_cast<T*>(p.out.data) + (sh.span.begin + row / group) * p.out.token +
+             (sh.head * group + row % group) * p.out.head + 4 * g;
+#pragma unroll
+    for (int c = 0; c < S::kTiles; ++c)
+      if (c < S::kFixedTiles || 16 * c < p.value) {
+        const f32x4 x = core.o[n][c] * by;
+        if (p.out.wide) {
+          if constexpr (sizeof(T) == 2) {
+            *reinterpret_cast<uint2*>(out + 16 * c) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+          } else {
+            *reinterpret_cast<f32x4*>(out + 16 * c) = x;
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) store1(out + 16 * c + i, x[i]);
+        }
+      }
+  }
+}
+
+template <typename T, int kKey, int kValue, int NT>
+hipError_t launch_rows_shape(const RowsAttendParams& p, hipStream_t stream) {
+  typedef RowsShape<T, kKey, kValue, NT> S;
+  static_assert(32 * NT * (kValue + 4) * 4 <= S::kRing * S::kBlockBytes, "the halves' join fits the ring");
+  hipLaunchKernelGGL((rows_attend_kernel<T, kKey, kValue, NT>), dim3(static_cast<unsigned>(p.plan.grid)), dim3(256),
+                     S::kRing * S::kBlockBytes, stream, p);
+  return hipGetLastError();
+}
+template <typename T, int NT>
+hipError_t launch_rows_as(const RowsAttendParams& p, hipStream_t stream) {
+  if (p.value <= 64) {
+    if (p.key <= 64) return launch_rows_shape<T, 64, 64, NT>(p, stream);
+    if (p.key <= 128) return launch_rows_shape<T, 128, 64, NT>(p, stream);
+    return launch_rows_shape<T, 192, 64, NT>(p, stream);
+  }
+  if (p.key <= 64) return launch_rows_shape<T, 64, 128, NT>(p, stream);
+  if (p.key <= 128) return launch_rows_shape<T, 128, 128, NT>(p, stream);
+  return launch_rows_shape<T, 192, 128, NT>(p, stream);
+}
+
+hipError_t launch_rows_bf16(const RowsAttendParams& p, hipStream_t stream);
+hipError_t launch_rows_f32(const RowsAttendParams& p, hipStream_t stream);
+
+}  // namespace scd

@@ -2,15 +2,9 @@
 // before the first launch; nothing allocates, synchronises or keeps state.
 #include <cmath>
 
-#include "scd_host.h"
-#include "scd_serve.h"
+#include "scd_serve_host.h"
 
-namespace {
-
-using scd::aligned16;
-using scd::check_batch;
-using scd::fail;
-using scd::ok;
+namespace scd {
 
 scd_status_t check_dtype(int32_t dtype) {
   if (dtype != SCD_F32 && dtype != SCD_BF16) return fail(SCD_ERR_SHAPE, "dtype %d unknown", dtype);
@@ -54,8 +48,6 @@ scd_status_t check_table(const void* table, int64_t max_position) {
   return SCD_OK;
 }
 
-// Strided rows of `heads` heads (0: any positive number).  `written`: no two elements may share an
-// address.
 scd_status_t check_rows(const scd_rows_t* r, const char* name, int32_t heads, int32_t head_dim,
                         int32_t dtype, int64_t n_tokens, bool written) {
   if (r == nullptr) return fail(SCD_ERR_NULL, "%s is NULL", name);
@@ -92,6 +84,28 @@ scd::Turn turn_of(const scd_rotary_t* r, const void* table, int64_t max_position
           r->layout == SCD_ROTARY_INTERLEAVED};
 }
 
+scd_status_t launched(hipError_t e, const char* what) {
+  if (e != hipSuccess) return fail(SCD_ERR_HIP, "%s launch failed: %s", what, hipGetErrorString(e));
+  return ok();
+}
+
+}  // namespace scd
+
+namespace {
+
+using scd::aligned16;
+using scd::batch_of;
+using scd::check_batch;
+using scd::check_dtype;
+using scd::check_rotary;
+using scd::check_rows;
+using scd::check_table;
+using scd::fail;
+using scd::launched;
+using scd::ok;
+using scd::rows_of;
+using scd::turn_of;
+
 scd_status_t check_cache_shape(const scd_cache_t* c) {
   if (c == nullptr) return fail(SCD_ERR_NULL, "cache is NULL");
   if (c->n_pages < 1 || c->n_kv_heads < 1 || c->max_pages < 1)
@@ -127,11 +141,6 @@ scd::PagedCache cache_of(const scd_cache_t* c) {
   while ((1 << lg) < c->page_tokens) ++lg;
   return {c->k_pages, c->v_pages, c->k_scales, c->v_scales, c->page_table,
           c->n_pages, c->n_kv_heads, c->max_pages, c->page_tokens, lg};
-}
-
-scd_status_t launched(hipError_t e, const char* what) {
-  if (e != hipSuccess) return fail(SCD_ERR_HIP, "%s launch failed: %s", what, hipGetErrorString(e));
-  return ok();
 }
 
 }  // namespace
