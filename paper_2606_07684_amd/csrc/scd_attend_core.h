@@ -56,14 +56,23 @@ __device__ inline bool odd_piece(const float* p) {
          (v.z & 0x7f800000u) == 0x7f800000u || (v.w & 0x7f800000u) == 0x7f800000u;
 }
 
-// kFrags pieces of 4 kVec channels that a score contracts at most (the first kFixed always), kTiles tiles of
-// 16 value channels (the first kFixedTiles always), NT tiles of 16 query rows, a query as kParts summands;
-// kKeyRow, kValueRow elements between LDS rows.
-template <typename T, int kFrags, int kFixed, int kTiles, int kFixedTiles, int NT, int kParts, int kKeyRow,
-          int kValueRow>
+// The largest value of the four lanes that hold a query row's positions (16 lanes apart).
+__device__ inline float row_top(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// kFrags pieces of 4 kVec channels that a score contracts, kTiles tiles of 16 value channels, NT tiles of 16
+// query rows, a query as kParts summands; kKeyRow, kValueRow elements between LDS rows.
+template <typename T, int kFrags, int kTiles, int NT, int kParts, int kKeyRow, int kValueRow>
 struct AttendCore {
   typedef typename Elem<T>::Frag Frag;
   static constexpr int kStep = Elem<T>::kStep, kVec = Elem<T>::kVec, kSub = kStep / 16;
+  // A row's base m follows its largest score once that is ahead by more than this: weights stay below 2^8, and
+  // most steps neither compare scores across lanes nor scale what they have.
+  static constexpr float kSlack = 8.f;
 
   Frag q[NT][kParts][kFrags];
   f32x4 o[NT][kTiles];
@@ -80,54 +89,57 @@ struct AttendCore {
     }
   }
 
-  // Positions pos .. pos + kStep - 1 at LDS rows k, v.  kCareful: some row leaves some of them out (behind its
-  // limit, or in a hole: bit t of `holes` for positions 16 t on); weights there are zero and values that are
-  // not finite do not count.  A value that is not finite makes its channel NaN for the rows that attend to it.
+  // Positions pos .. pos + kStep - 1 at LDS rows k, v; scale >= 0.  kCareful: some row leaves some of them out
+  // (behind its limit, or in a hole: bit t of `holes` for positions 16 t on); weights there are zero and values
+  // that are not finite do not count.  A value that is not finite makes its channel NaN for the rows that attend
+  // to it.
   template <bool kCareful>
-  __device__ void step(const T* k, const T* v, int frags, int tiles, float scale, int pos, int holes, int lane) {
+  __device__ void step(const T* k, const T* v, float scale, int pos, int holes, int lane) {
     const int lr = lane & 15, g = lane >> 4;
     f32x4 s[kSub][NT];
 #pragma unroll
     for (int t = 0; t < kSub; ++t)
 #pragma unroll
       for (int n = 0; n < NT; ++n) s[t][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const T* row = k + lr * kKeyRow + kVec * g;
 #pragma unroll
-    for (int f = 0; f < kFrags; ++f) {
-      if (f < kFixed || f < frags) {
+    for (int f = 0; f < kFrags; ++f)
 #pragma unroll
-        for (int t = 0; t < kSub; ++t) {
-          const Frag a = *reinterpret_cast<const Frag*>(k + (16 * t + lr) * kKeyRow + 4 * kVec * f + kVec * g);
+      for (int t = 0; t < kSub; ++t) {
+        const Frag a = *reinterpret_cast<const Frag*>(row + 16 * t * kKeyRow + 4 * kVec * f);
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
+        for (int i = 0; i < kParts; ++i)
 #pragma unroll
-            for (int i = 0; i < kParts; ++i) s[t][n] = mma(a, q[n][i][f], s[t][n]);
-        }
+          for (int n = 0; n < NT; ++n) s[t][n] = mma(a, q[n][i][f], s[t][n]);
       }
-    }
     bool odd = false;
     if constexpr (kCareful) {
-      for (int i = lane; i < kStep * 16 * tiles / kVec; i += 64) {
-        const int row = i / (16 / kVec * tiles), c = i - row * (16 / kVec * tiles);
-        odd |= odd_piece(v + row * kValueRow + kVec * c);
+      constexpr int kRowPieces = 16 / kVec * kTiles;
+      for (int i = lane; i < kStep * kRowPieces; i += 64) {
+        const int r = i / kRowPieces, c = i - r * kRowPieces;
+        odd |= odd_piece(v + r * kValueRow + kVec * c);
       }
       odd = __any(odd);
     }
+    float top[NT];
+    bool ahead = false;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      float top = -INFINITY;
+      top[n] = -INFINITY;
 #pragma unroll
       for (int t = 0; t < kSub; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float x = s[t][n][i] * scale;
-          if constexpr (kCareful) x = seen(n, t, i, pos, holes, g) ? x : -INFINITY;
-          s[t][n][i] = x;
-          top = fmaxf(top, x);
-        }
-      top = fmaxf(top, __shfl_xor(top, 16));
-      top = fmaxf(top, __shfl_xor(top, 32));
-      if (__any(top > m[n])) {
-        const float now = fmaxf(top, m[n]);
+        for (int i = 0; i < 4; ++i)
+          if (!kCareful || seen(n, t, i, pos, holes, g)) top[n] = fmaxf(top[n], s[t][n][i]);
+      // where nothing is seen, a scale of 0 must not make it something
+      if (!kCareful || top[n] != -INFINITY) top[n] *= scale;
+      ahead |= top[n] > m[n] + kSlack;
+    }
+    if (__any(ahead)) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        // by the row's own scores alone, so that a row's result does not depend on the rows beside it
+        const float most = row_top(top[n]), now = most > m[n] + kSlack ? most : m[n];
         const float by = __builtin_amdgcn_exp2f(m[n] - (now == -INFINITY ? 0.f : now));
         m[n] = now;
         l[n] *= by;
@@ -136,19 +148,24 @@ struct AttendCore {
 #pragma unroll
           for (int i = 0; i < 4; ++i) o[n][c][i] *= by;
       }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
       const float base = m[n] == -INFINITY ? 0.f : m[n];
 #pragma unroll
       for (int t = 0; t < kSub; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          s[t][n][i] = __builtin_amdgcn_exp2f(s[t][n][i] - base);
-          l[n] += s[t][n][i];
+          float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][n][i], scale, -base));
+          if constexpr (kCareful) w = seen(n, t, i, pos, holes, g) ? w : 0.f;
+          s[t][n][i] = w;
+          l[n] += w;
         }
     }
     if (kCareful && odd) {
-      weigh<true>(v, s, tiles, pos, holes, lr, g);
+      weigh<true>(v, s, pos, holes, lr, g);
     } else {
-      weigh<false>(v, s, tiles, pos, holes, lr, g);
+      weigh<false>(v, s, pos, holes, lr, g);
     }
   }
 
@@ -165,70 +182,66 @@ struct AttendCore {
   }
 
   template <bool kOdd>
-  __device__ void weigh(const T* v, const f32x4 (&s)[kSub][NT], int tiles, int pos, int holes, int lr, int g) {
+  __device__ void weigh(const T* v, const f32x4 (&s)[kSub][NT], int pos, int holes, int lr, int g) {
     if constexpr (sizeof(T) == 2) {
       bf16x8 w[NT], ones[NT];
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          // one rounding of a weight to bf16, 8 bits: over many positions it averages out, and the heaviest
-          // position of a row that one position dominates has a weight of 1, which is exact
+          // one rounding of a weight to bf16, 8 bits: over many positions it averages out, and the sum that
+          // divides is of unrounded weights
           w[n][e] = static_cast<__bf16>(s[e >> 2][n][e & 3]);
           if constexpr (kOdd) ones[n][e] = static_cast<__bf16>(seen(n, e >> 2, e & 3, pos, holes, g) ? 1.f : 0.f);
         }
+      const T* at = v + (4 * g + (lr >> 2)) * kValueRow + 4 * (lr & 3);
 #pragma unroll
       for (int c = 0; c < kTiles; ++c) {
-        if (c < kFixedTiles || c < tiles) {
-          union { s16x4 h[2]; bf16x8 v; uint16_t u[8]; } a;
-          const T* at = v + (4 * g + (lr >> 2)) * kValueRow + 16 * c + 4 * (lr & 3);
-          a.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(at));
-          a.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(at + 16 * kValueRow));
-          if constexpr (kOdd) {
-            union { bf16x8 v; uint16_t u[8]; } flag;
+        union { s16x4 h[2]; bf16x8 v; uint16_t u[8]; } a;
+        a.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(at + 16 * c));
+        a.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(at + 16 * c + 16 * kValueRow));
+        if constexpr (kOdd) {
+          union { bf16x8 v; uint16_t u[8]; } flag;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const bool bad = (a.u[e] & 0x7f80) == 0x7f80;
-              flag.u[e] = bad ? 0x3f80 : 0;
-              if (bad) a.u[e] = 0;
-            }
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-              const f32x4 x = mma(flag.v, ones[n], f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (x[i] > 0.f) o[n][c][i] = __builtin_nanf("");
-            }
+          for (int e = 0; e < 8; ++e) {
+            const bool bad = (a.u[e] & 0x7f80) == 0x7f80;
+            flag.u[e] = bad ? 0x3f80 : 0;
+            if (bad) a.u[e] = 0;
           }
 #pragma unroll
-          for (int n = 0; n < NT; ++n) o[n][c] = mma(a.v, w[n], o[n][c]);
+          for (int n = 0; n < NT; ++n) {
+            const f32x4 x = mma(flag.v, ones[n], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (x[i] > 0.f) o[n][c][i] = __builtin_nanf("");
+          }
         }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) o[n][c] = mma(a.v, w[n], o[n][c]);
       }
     } else {
+      const T* at = v + 4 * g * kValueRow + lr;
 #pragma unroll
-      for (int c = 0; c < kTiles; ++c) {
-        if (c < kFixedTiles || c < tiles) {
+      for (int c = 0; c < kTiles; ++c)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float a = v[(4 * g + i) * kValueRow + 16 * c + lr];
-            if constexpr (kOdd) {
-              const bool bad = (__float_as_uint(a) & 0x7f800000u) == 0x7f800000u;
-              if (bad) a = 0.f;
+        for (int i = 0; i < 4; ++i) {
+          float a = at[i * kValueRow + 16 * c];
+          if constexpr (kOdd) {
+            const bool bad = (__float_as_uint(a) & 0x7f800000u) == 0x7f800000u;
+            if (bad) a = 0.f;
 #pragma unroll
-              for (int n = 0; n < NT; ++n) {
-                const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x4f32(
-                    bad ? 1.f : 0.f, seen(n, 0, i, pos, holes, g) ? 1.f : 0.f, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+            for (int n = 0; n < NT; ++n) {
+              const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x4f32(
+                  bad ? 1.f : 0.f, seen(n, 0, i, pos, holes, g) ? 1.f : 0.f, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  if (x[e] > 0.f) o[n][c][e] = __builtin_nanf("");
-              }
+              for (int e = 0; e < 4; ++e)
+                if (x[e] > 0.f) o[n][c][e] = __builtin_nanf("");
             }
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-              o[n][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, s[0][n][i], o[n][c], 0, 0, 0);
           }
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+            o[n][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(a, s[0][n][i], o[n][c], 0, 0, 0);
         }
-      }
     }
   }
 };
@@ -238,12 +251,37 @@ __device__ inline void copy16(const void* from, char* to) {
   __builtin_amdgcn_global_load_lds(from, (lds_void_t)to, 16, 0, 0);
 }
 
+// The 64-lane copies that bring a block of kRows rows of `pieces` 16-byte pieces into LDS rows of kPieces, dealt to
+// the four waves: copy j of a wave fills kilobyte index(wave, j) of the block's region of kBytes bytes.  Every wave
+// issues kMine of them, the last ones twice where they do not come out even, so that one count of copies under way
+// holds for all; LDS pieces that a row does not have get its last one again.
+template <int kRows, int kPieces>
+struct Copies {
+  static constexpr int kAll = (kRows * kPieces + 63) / 64, kMine = (kAll + 3) / 4, kBytes = kAll * 1024;
+  static __device__ int index(int wave, int j) { return wave + 4 * j < kAll ? wave + 4 * j : kAll - 1; }
+  static __device__ int row(int wave, int j, int lane) {
+    const int r = (index(wave, j) * 64 + lane) / kPieces;
+    return r < kRows ? r : kRows - 1;
+  }
+  static __device__ int piece(int wave, int j, int lane, int pieces) {
+    const int c = (index(wave, j) * 64 + lane) % kPieces;
+    return c < pieces ? c : pieces - 1;
+  }
+};
+
 // s_waitcnt vmcnt(n), the other counters left alone.
 template <int n>
 __device__ inline void wait_copies() {
   static_assert(n >= 0 && n < 64, "counter range");
   __builtin_amdgcn_s_waitcnt(0x0F70 | (n & 15) | (n >> 4) << 14);
 }
+
+// a / b for a >= 0, b > 0; in 32 bits where both fit, which takes a tenth of the time.
+__device__ inline int64_t div_up_to(int64_t a, int64_t b) {
+  if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+  return a / b;
+}
+__device__ inline int64_t div_ceil(int64_t a, int64_t b) { return div_up_to(a + b - 1, b); }
 
 // ---- shares ------------------------------------------------------------------------------------------
 // A request's query rows make tiles, its positions blocks of kBlock.  While there are fewer tiles than twice what
@@ -264,11 +302,11 @@ template <typename Length>
 struct Tiles {
   const SharePlan& p;
   Length length;   // positions of request b with this span
-  int block;
+  int block;       // a power of two
   __device__ int64_t tiles(const Span& s) const {
-    return ((s.end - s.begin) * p.per_token + p.rows - 1) / p.rows;
+    return div_ceil((s.end - s.begin) * p.per_token, p.rows);
   }
-  __device__ int64_t blocks(const Span& s, int b) const { return (length(s, b) + block - 1) / block; }
+  __device__ int64_t blocks(const Span& s, int b) const { return (length(s, b) + block - 1) >> (31 - __builtin_clz(block)); }
 };
 
 // The share that is work unit `unit`; false past the last.  Every thread calls it and gets the answer.
@@ -308,16 +346,16 @@ __device__ inline bool find_share(const SeqBatch& s, const SharePlan& p, int blo
     }
     tiles *= p.heads;
     work *= p.heads;
-    if (tiles < 2 * p.target) {
-      const int64_t room = share_goal(tiles, p.target) - tiles;
-      chunk = room > 0 ? (work + room - 1) / room : chunk;
+    if (tiles < 2 * kFill) {
+      const int64_t room = share_goal(tiles) - tiles;
+      chunk = room > 0 ? div_ceil(work, room) : chunk;
       chunk = chunk < least ? least : chunk;
     }
   }
   // heads one after another, each with all requests' shares; a head's number of shares is the same
   const auto parts_of = [&](const Span& span, int b) {
     const int64_t n = of.blocks(span, b);
-    return n <= chunk ? int64_t{1} : (n + chunk - 1) / chunk;
+    return n <= chunk ? int64_t{1} : div_ceil(n, chunk);
   };
   Located at;
   int b_of = 0;
@@ -326,7 +364,7 @@ __device__ inline bool find_share(const SeqBatch& s, const SharePlan& p, int blo
     const Span span = span_of(s, 0);
     per_head = of.tiles(span) * parts_of(span, 0);
     if (per_head == 0 || unit >= per_head * p.heads) return false;
-    out.head = static_cast<int>(unit / per_head);
+    out.head = static_cast<int>(div_up_to(unit, per_head));
     at.b = 0;
     at.span = span;
     at.local = unit - out.head * per_head;
@@ -347,7 +385,7 @@ __device__ inline bool find_share(const SeqBatch& s, const SharePlan& p, int blo
       __syncthreads();
       for (int w = 0; w < kThreads / 64; ++w) per_head += lds.wave[0][w];
       if (per_head == 0 || unit >= per_head * p.heads) return false;
-      out.head = static_cast<int>(unit / per_head);
+      out.head = static_cast<int>(div_up_to(unit, per_head));
       left = unit - out.head * per_head;
     }
     // locate() calls the count once for every request of this thread, in order
@@ -366,7 +404,7 @@ __device__ inline bool find_share(const SeqBatch& s, const SharePlan& p, int blo
   out.len = length(at.span, b_of);
   out.tiles = static_cast<int>(of.tiles(at.span));
   out.parts = static_cast<int>(parts_of(at.span, b_of));
-  out.part = static_cast<int>(at.local / out.tiles);
+  out.part = static_cast<int>(div_up_to(at.local, out.tiles));
   out.tile = static_cast<int>(at.local - static_cast<int64_t>(out.part) * out.tiles);
   out.first += out.tile;
   return true;

@@ -37,14 +37,15 @@ struct SharePlan {
   int32_t heads;        // KV heads, each with tiles of its own
   int32_t per_token;    // query rows a token has in a tile's head
   int32_t cut;          // whether tiles are cut at all
-  int32_t target;       // workgroups that fill the chip
   int64_t cap;          // positions a request can hold
   int64_t grid;         // workgroups launched: a bound on the shares
 };
 
-// Shares that a call's tiles may be cut into; all of them one after another from twice what fills the chip on.
-__host__ __device__ inline int64_t share_goal(int64_t tiles, int target) {
-  return tiles >= 2 * target ? tiles : target * ((2 * tiles + target - 1) / target);
+// Shares that a call's tiles may be cut into, a multiple of the workgroups that fill the chip, one a CU; all tiles
+// one after another from twice that many on.
+constexpr int kFill = 256;
+__host__ __device__ inline int64_t share_goal(int64_t tiles) {
+  return tiles >= 2 * kFill ? tiles : (2 * tiles + kFill - 1) / kFill * kFill;
 }
 
 // A query row's shares in the workspace, left by the first of them: share s is slot first + s * step.
@@ -94,7 +95,11 @@ struct RowsSizes {
   size_t parts, slots;
   size_t total() const { return parts + slots; }
 };
-RowsSizes rows_sizes(bool bf16, const SeqBatch& b, int64_t held_rows, int heads, int kv_heads, int key, int value);
+// Rows that are fetched 16 bytes at a time, a block's from its first one on in 32 bits.
+inline bool rows_wide(const Rows& k, const Rows& v) {
+  return k.wide && v.wide && k.token < (int64_t{1} << 22) && v.token < (int64_t{1} << 22);
+}
+RowsSizes rows_sizes(bool bf16, bool wide, const SeqBatch& b, int64_t held_rows, int heads, int kv_heads, int value);
 hipError_t launch_rows_attend(bool bf16, const RowsAttendParams& p, hipStream_t stream);
 
 }  // namespace scd

@@ -272,23 +272,20 @@ __global__ __launch_bounds__(256) void latent_out_kernel(LatentAttendParams p, i
 }
 
 // ---- plan and launches -----------------------------------------------------------------------------------
-static constexpr int kFill = 256;  // workgroups that fill the chip: one a CU
-
 LatentSizes latent_sizes(bool bf16, const LatentPages& c, const SeqBatch& b, int heads) {
   LatentSizes z{};
   SharePlan& plan = z.plan;
   const int64_t requests = std::min<int64_t>(b.n_seqs, b.n_tokens), rows = b.n_tokens * heads;
   const int64_t mean = (rows + requests - 1) / requests;
-  const bool two = bf16 && c.latent <= 256;
+  const bool two = bf16 && c.latent <= 128;
   plan.rows = mean <= 16 ? 16 : mean <= 32 ? 32 : mean <= 64 || !two ? 64 : 128;
   plan.row_groups = plan.rows >= 64 ? 4 : plan.rows / 16;
   plan.heads = 1;
   plan.per_token = heads;
   plan.cut = 1;
-  plan.target = kFill;
   plan.cap = std::min<int64_t>(static_cast<int64_t>(c.cols) * c.page, (int64_t{1} << 31) - 128);
   const int64_t tiles = rows / plan.rows + requests;
-  const int64_t goal = std::max(tiles, share_goal(std::min<int64_t>(tiles, 2 * kFill - 1), kFill));
+  const int64_t goal = std::max(tiles, share_goal(std::min<int64_t>(tiles, 2 * kFill - 1)));
   const int block = bf16 ? 64 : 32;
   const int64_t most = std::max<int64_t>(1, ((plan.cap + block - 1) / block + 1) / 2);  // shares of two blocks each
   plan.grid = tiles > goal / most ? goal : tiles * most;

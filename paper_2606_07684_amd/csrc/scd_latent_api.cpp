@@ -186,7 +186,11 @@ size_t scd_rows_attend_workspace_bytes(const scd_batch_t* batch, const scd_batch
       n_heads % n_kv_heads != 0 || batch->n_tokens == 0 || key_dim < 32 || value_dim < 32 || key_dim > 192 ||
       value_dim > 128)
     return 0;
-  return rows_sizes(dtype == SCD_BF16, batch_of(batch), held->n_tokens, n_heads, n_kv_heads, key_dim, value_dim).total();
+  // rows that start on 16 bytes or not: enough for both
+  const auto size = [&](bool wide) {
+    return rows_sizes(dtype == SCD_BF16, wide, batch_of(batch), held->n_tokens, n_heads, n_kv_heads, value_dim).total();
+  };
+  return size(true) > size(false) ? size(true) : size(false);
 }
 
 scd_status_t scd_rows_attend(const scd_batch_t* batch, const scd_batch_t* held, int32_t dtype, double softmax_scale,
@@ -210,15 +214,17 @@ scd_status_t scd_rows_attend(const scd_batch_t* batch, const scd_batch_t* held, 
     return fail(SCD_ERR_UNSUPPORTED, "n_tokens * n_heads reaches 2^31");
   SCD_TRY(check_rows(out, "out", q->n_heads, value_dim, dtype, batch->n_tokens, true));
   if (batch->n_tokens == 0) return ok();
-  const RowsSizes z = rows_sizes(dtype == SCD_BF16, batch_of(batch), held->n_tokens, q->n_heads, k->n_heads, key_dim, value_dim);
-  SCD_TRY(check_workspace(workspace, workspace_bytes, z.total()));
   RowsAttendParams p{};
+  p.k = rows_of(k, dtype);
+  p.v = rows_of(v, dtype);
+  const RowsSizes z = rows_sizes(dtype == SCD_BF16, rows_wide(p.k, p.v), batch_of(batch), held->n_tokens, q->n_heads,
+                                 k->n_heads, value_dim);
+  SCD_TRY(check_workspace(workspace, workspace_bytes, scd_rows_attend_workspace_bytes(batch, held, dtype, q->n_heads,
+                                                                                      k->n_heads, key_dim, value_dim)));
   p.batch = batch_of(batch);
   p.held = batch_of(held);
   p.plan = z.plan;
   p.q = rows_of(q, dtype);
-  p.k = rows_of(k, dtype);
-  p.v = rows_of(v, dtype);
   p.out = rows_of(out, dtype);
   p.key = key_dim;
   p.value = value_dim;

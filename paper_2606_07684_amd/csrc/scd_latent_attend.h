@@ -22,23 +22,18 @@ struct LatentShape {
   static constexpr int kBlock = 2 * Elem<T>::kStep;             // positions of an LDS block
   // 16-byte pieces of an LDS row: an odd number, so that a column's pieces lie in different banks
   static constexpr int kPieces = (kWide + kMostTurned) / kVec + 1;
+  typedef dev::Copies<kBlock, kPieces> Copies;
   static constexpr int kRow = kPieces * kVec;                   // elements
-  static constexpr int kBlockBytes = kBlock * kPieces * 16;
+  static constexpr int kBlockBytes = Copies::kBytes;
   static constexpr int kRing = kBlockBytes * 4 <= 110 * 1024 ? 4 : kBlockBytes * 3 <= 150 * 1024 ? 3 : 2;
-  static constexpr int kCopies = (kBlock * kPieces + 63) / 64;  // 64-lane copies of a block
-  static constexpr int kMineMin = kCopies / 4;                  // of a wave, at least
-  static constexpr int kMineMax = (kCopies + 3) / 4;
-  static constexpr int kFrags = (kWide + kMostTurned) / (4 * kVec);
-  static constexpr int kFixed = (kWide == 128 ? 32 : kWide / 2) / (4 * kVec);
-  static constexpr int kTiles = kWide / 16;
-  static constexpr int kFixedTiles = (kWide == 128 ? 32 : kWide / 2) / 16;
   static constexpr int kIds = 1024;
-  typedef AttendCore<T, kFrags, kFixed, kTiles, kFixedTiles, NT, kParts, kRow, kRow> Core;
+  static constexpr int kFrags = (kWide + kMostTurned) / (4 * kVec), kTiles = kWide / 16;
+  typedef AttendCore<T, kFrags, kTiles, NT, kParts, kRow, kRow> Core;
   static constexpr int kLds = kRing * kBlockBytes + kIds * 4;
 };
 
 template <typename T, int kWide, int NT>
-__global__ __launch_bounds__(256, 1) void latent_attend_kernel(LatentAttendParams p) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void latent_attend_kernel(LatentAttendParams p) {
   typedef LatentShape<T, kWide, NT> S;
   typedef typename S::Core Core;
   constexpr int kStep = Elem<T>::kStep, kVec = S::kVec;
@@ -93,9 +88,12 @@ __global__ __launch_bounds__(256, 1) void latent_attend_kernel(LatentAttendParam
 #pragma unroll
     for (int i = 0; i < S::kParts; ++i)
 #pragma unroll
-      for (int f = 0; f < S::kFrags; ++f)
-        if (works && 4 * kVec * f < width)
-          core.q[n][i][f] = *reinterpret_cast<const typename Core::Frag*>(q + i * width + 4 * kVec * f + kVec * g);
+      for (int f = 0; f < S::kFrags; ++f) {
+        union { u32x4 u; typename Core::Frag v; } x;
+        x.u = u32x4{0, 0, 0, 0};
+        if (works && 4 * kVec * f < width) x.u = *reinterpret_cast<const u32x4*>(q + i * width + 4 * kVec * f + kVec * g);
+        core.q[n][i][f] = x.v;
+      }
   }
 
   if (first < last) {
@@ -114,30 +112,35 @@ __global__ __launch_bounds__(256, 1) void latent_attend_kernel(LatentAttendParam
     fill();
     __syncthreads();
 
-    // a copy's lanes: which row and piece of the block they fetch
-    int where[S::kMineMax];
-#pragma unroll
-    for (int j = 0; j < S::kMineMax; ++j) {
-      const int slot = (wave + 4 * j) * 64 + lane;
-      const int row = slot / S::kPieces;
-      where[j] = row << 8 | (slot - row * S::kPieces);
-    }
+    // a lane's pieces: the page of their row among the block's, their place in it, the column among the window's
     const int pieces = width / kVec;
-    const int64_t row_bytes = static_cast<int64_t>(width) * sizeof(T);
+    const uint32_t row_bytes = static_cast<uint32_t>(width * sizeof(T));
+    const uint64_t page_bytes = static_cast<uint64_t>(row_bytes) << lg;
     const int mask = (1 << lg) - 1;
-    const auto fetch = [&](int block, int slot) {
+    uint32_t place[S::Copies::kMine];
+    int page[S::Copies::kMine];
 #pragma unroll
-      for (int j = 0; j < S::kMineMax; ++j) {
-        if (j < S::kMineMin || wave + 4 * j < S::kCopies) {
-          const int row = where[j] >> 8, piece = where[j] & 255;
-          if (piece < pieces && row < S::kBlock) {
-            int64_t pos = static_cast<int64_t>(block) * S::kBlock + row;
-            pos = pos < seen ? pos : seen - 1;
-            const int id = ids[static_cast<int>(pos >> lg) - window];
-            const int64_t at = (static_cast<int64_t>(id < 0 ? 0 : id) << lg) + (static_cast<int>(pos) & mask);
-            copy16(p.cache.pages + at * row_bytes + 16 * piece, smem + slot * S::kBlockBytes + (wave + 4 * j) * 1024);
-          }
-        }
+    for (int j = 0; j < S::Copies::kMine; ++j) {
+      const int row = S::Copies::row(wave, j, lane);
+      page[j] = row >> lg;
+      place[j] = (row & mask) * row_bytes + 16 * S::Copies::piece(wave, j, lane, pieces);
+    }
+    const int last_column = static_cast<int>((seen - 1) >> lg);
+    const auto fetch = [&](int block, int slot) {
+      const int pos0 = block * S::kBlock, col0 = pos0 >> lg;
+      const uint32_t in_page = (pos0 & mask) * row_bytes;  // a page of more than a block
+      int id[S::Copies::kMine];
+#pragma unroll
+      for (int j = 0; j < S::Copies::kMine; ++j) {
+        // columns behind the last one that is seen are its page again
+        const int col = col0 + page[j];
+        id[j] = ids[(col < last_column ? col : last_column) - window];
+      }
+#pragma unroll
+      for (int j = 0; j < S::Copies::kMine; ++j) {
+        const uint32_t p0 = id[j] < 0 ? 0 : id[j];  // a hole's rows are left out: any page will do
+        copy16(p.cache.pages + (p0 * page_bytes + (in_page + place[j])),
+               smem + slot * S::kBlockBytes + S::Copies::index(wave, j) * 1024);
       }
     };
     constexpr int kAhead = S::kRing - 1;
@@ -149,7 +152,7 @@ __global__ __launch_bounds__(256, 1) void latent_attend_kernel(LatentAttendParam
     for (int i = 0; i < kAhead; ++i) fetch(first + i < last ? first + i : last - 1, i);
     int slot = 0;
     for (int block = first; block < last; ++block) {
-      wait_copies<(kAhead - 1) * S::kMineMin>();
+      wait_copies<(kAhead - 1) * S::Copies::kMine>();
       lds_barrier();
       const int next = block + kAhead < last ? block + kAhead : last - 1;
       if (!covered(next)) {
@@ -170,9 +173,9 @@ __global__ __launch_bounds__(256, 1) void latent_attend_kernel(LatentAttendParam
           const T* at = rows + st * kStep * S::kRow;
           const int bits = holes >> (st * (kStep / 16));
           if (careful) {
-            core.template step<true>(at, at, width / (4 * kVec), p.cache.latent / 16, 1.f, pos + st * kStep, bits, lane);
+            core.template step<true>(at, at, 1.f, pos + st * kStep, bits, lane);
           } else {
-            core.template step<false>(at, at, width / (4 * kVec), p.cache.latent / 16, 1.f, pos + st * kStep, bits, lane);
+            core.template step<false>(at, at, 1.f, pos + st * kStep, bits, lane);
           }
         }
       }
@@ -227,7 +230,7 @@ __global__ __launch_bounds__(256, 1) void latent_attend_kernel(LatentAttendParam
       if (g == 0) *reinterpret_cast<float2*>(out) = make_float2(core.m[n], total);
 #pragma unroll
       for (int c = 0; c < S::kTiles; ++c)
-        if (c < S::kFixedTiles || 16 * c < p.cache.latent) {
+        if (16 * c < p.cache.latent) {
           float2* to = reinterpret_cast<float2*>(out + 2 + 16 * c + 4 * g);
           to[0] = make_float2(core.o[n][c][0], core.o[n][c][1]);
           to[1] = make_float2(core.o[n][c][2], core.o[n][c][3]);

@@ -48,27 +48,24 @@ __global__ __launch_bounds__(256) void rows_join_kernel(RowsAttendParams p, int6
   }
 }
 
-static constexpr int kFill = 256;  // workgroups that fill the chip
-
-RowsSizes rows_sizes(bool bf16, const SeqBatch& b, int64_t held_rows, int heads, int kv_heads, int key, int value) {
+RowsSizes rows_sizes(bool bf16, bool wide, const SeqBatch& b, int64_t held_rows, int heads, int kv_heads, int value) {
   RowsSizes z{};
   SharePlan& plan = z.plan;
   const int group = heads / kv_heads;
   const int64_t requests = std::min<int64_t>(b.n_seqs, b.n_tokens), rows = b.n_tokens * group;
   const int64_t mean = (rows + requests - 1) / requests;
-  plan.rows = mean <= 16 ? 16 : mean <= 32 ? 32 : mean <= 64 || !bf16 ? 64 : 128;
+  plan.rows = mean <= 16 ? 16 : mean <= 32 ? 32 : mean <= 64 || !bf16 || !wide ? 64 : 128;
   plan.row_groups = plan.rows >= 64 ? 4 : plan.rows / 16;
   plan.heads = kv_heads;
   plan.per_token = group;
-  plan.target = kFill;
   plan.cap = held_rows;
   const int64_t least = ((rows + plan.rows - 1) / plan.rows) * kv_heads;
   const int64_t tiles = (rows / plan.rows + requests) * kv_heads;
   plan.cut = least < 2 * kFill;
   plan.grid = tiles;
   if (!plan.cut) return z;
-  const int block = bf16 ? 64 : 32;
-  const int64_t goal = std::max(tiles, share_goal(std::min<int64_t>(tiles, 2 * kFill - 1), kFill));
+  const int block = plan.rows == 128 || !bf16 ? 32 : 64;
+  const int64_t goal = std::max(tiles, share_goal(std::min<int64_t>(tiles, 2 * kFill - 1)));
   const int64_t most = std::max<int64_t>(1, ((held_rows + block - 1) / block + 1) / 2);  // shares of two blocks each
   plan.grid = tiles > goal / most ? goal : tiles * most;
   if (most == 1) {
@@ -82,7 +79,9 @@ RowsSizes rows_sizes(bool bf16, const SeqBatch& b, int64_t held_rows, int heads,
 }
 
 hipError_t launch_rows_attend(bool bf16, const RowsAttendParams& p, hipStream_t stream) {
-  const hipError_t e = bf16 ? launch_rows_bf16(p, stream) : launch_rows_f32(p, stream);
+  const hipError_t e = !rows_wide(p.k, p.v) ? launch_odd_rows(bf16, p, stream)
+                       : bf16             ? launch_rows_bf16(p, stream)
+                                          : launch_rows_f32(p, stream);
   if (e != hipSuccess || !p.plan.cut) return e;
   const int64_t rows = p.batch.n_tokens * p.q.n_heads;
   const unsigned blocks = static_cast<unsigned>(std::min<int64_t>((rows + 3) / 4, kMaxGrid));

@@ -11,51 +11,45 @@
 namespace scd {
 using namespace dev;
 
-template <typename T, int kKey, int kValue, int NT>
+// kWide: all rows of keys and values start on 16 bytes.
+template <typename T, int kKey, int kValue, int NT, bool kWide>
 struct RowsShape {
-  static constexpr int kVec = Elem<T>::kVec;
-  static constexpr int kBlock = 2 * Elem<T>::kStep;
+  static constexpr int kVec = Elem<T>::kVec, kStep = Elem<T>::kStep;
+  // With 128 rows a wave has work enough for a step of positions between two barriers, and blocks of one leave room
+  // for a second workgroup on the CU; tiles of fewer rows have two waves take a step each.
+  static constexpr int kBlock = NT == 2 ? kStep : 2 * kStep;
   static constexpr int kKeyPieces = kKey / kVec + 1, kValuePieces = kValue / kVec + 1;  // odd
-  static constexpr int kBlockBytes = kBlock * (kKeyPieces + kValuePieces) * 16;
-  static constexpr int kRing = kBlockBytes * 6 <= 156 * 1024 ? 3 : kBlockBytes * 4 <= 156 * 1024 ? 2 :
+  typedef Copies<kBlock, kKeyPieces> KeyCopies;
+  typedef Copies<kBlock, kValuePieces> ValueCopies;
+  static constexpr int kBlockBytes = KeyCopies::kBytes + ValueCopies::kBytes;
+  static constexpr int kRing = kBlockBytes * 3 <= 80 * 1024 ? 3 : kBlockBytes * 2 <= 80 * 1024 ? 2 :
                                kBlockBytes * 3 <= 156 * 1024 ? 3 : 2;
-  static constexpr int kFrags = kKey / (4 * kVec), kTiles = kValue / 16;
-  static constexpr int kFixed = (kKey == 64 ? 32 : kKey - 32) / (4 * kVec);
-  static constexpr int kFixedTiles = (kValue == 64 ? 32 : kValue - 32) / 16;
-  typedef AttendCore<T, kFrags, kFixed, kTiles, kFixedTiles, NT, 1, kKeyPieces * kVec, kValuePieces * kVec> Core;
+  static constexpr int kMine = KeyCopies::kMine + ValueCopies::kMine;
+  typedef AttendCore<T, kKey / (4 * kVec), kValue / 16, NT, 1, kKeyPieces * kVec, kValuePieces * kVec> Core;
 };
 
-// Rows pos0 .. pos0 + kBlock - 1 (the last one seen in place of those behind it) into LDS rows of kPieces 16-byte
-// pieces, `pieces` of them filled: straight from memory, or, where rows do not start on 16 bytes, element by element.
+// Rows that do not start on 16 bytes, element by element.
 template <typename T, int kBlock, int kPieces>
-__device__ inline void fetch_rows(const T* from, int64_t stride, bool wide, int pieces, int64_t pos0, int64_t seen,
-                                  char* to, int wave, int lane) {
-  constexpr int kVec = Elem<T>::kVec, kCopies = (kBlock * kPieces + 63) / 64;
+__device__ inline void fetch_odd_rows(const T* from, int64_t stride, int pieces, int pos0, int seen, char* to, int wave,
+                                      int lane) {
+  constexpr int kVec = Elem<T>::kVec;
+  typedef Copies<kBlock, kPieces> C;
+#pragma unroll 1
+  for (int j = 0; j < C::kMine; ++j) {
+    const int row = C::row(wave, j, lane), pos = pos0 + row < seen ? pos0 + row : seen - 1;
+    const T* src = from + pos * stride + kVec * C::piece(wave, j, lane, pieces);
+    union { T t[kVec]; u32x4 v; } x;
 #pragma unroll
-  for (int j = 0; j < (kCopies + 3) / 4; ++j) {
-    if (4 * j + 3 < kCopies || wave + 4 * j < kCopies) {
-      const int i = (wave + 4 * j) * 64 + lane, row = i / kPieces, piece = i - row * kPieces;
-      if (row < kBlock && piece < pieces) {
-        const int64_t pos = pos0 + row < seen ? pos0 + row : seen - 1;
-        const T* src = from + pos * stride + kVec * piece;
-        if (wide) {
-          copy16(src, to + (wave + 4 * j) * 1024);
-        } else {
-          union { T t[kVec]; u32x4 v; } x;
-#pragma unroll
-          for (int e = 0; e < kVec; ++e) x.t[e] = src[e];
-          *reinterpret_cast<u32x4*>(to + 16 * i) = x.v;
-        }
-      }
-    }
+    for (int e = 0; e < kVec; ++e) x.t[e] = src[e];
+    *reinterpret_cast<u32x4*>(to + C::index(wave, j) * 1024 + 16 * lane) = x.v;
   }
 }
 
-template <typename T, int kKey, int kValue, int NT>
-__global__ __launch_bounds__(256) void rows_attend_kernel(RowsAttendParams p) {
-  typedef RowsShape<T, kKey, kValue, NT> S;
+template <typename T, int kKey, int kValue, int NT, bool kWide>
+__global__ __launch_bounds__(256, 2) void rows_attend_kernel(RowsAttendParams p) {
+  typedef RowsShape<T, kKey, kValue, NT, kWide> S;
   typedef typename S::Core Core;
-  constexpr int kStep = Elem<T>::kStep, kVec = S::kVec;
+  constexpr int kStep = S::kStep, kVec = S::kVec, kKeyBytes = S::KeyCopies::kBytes;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   __shared__ ShareLds lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -110,53 +104,95 @@ __global__ __launch_bounds__(256) void rows_attend_kernel(RowsAttendParams p) {
     const T* q = reinterpret_cast<const T*>(p.q.data) + (sh.span.begin + row / group) * p.q.token +
                  (sh.head * group + row % group) * p.q.head;
 #pragma unroll
-    for (int f = 0; f < S::kFrags; ++f)
+    for (int f = 0; f < kKey / (4 * kVec); ++f) {
+      union { T t[kVec]; u32x4 u; typename Core::Frag v; } x;
+      x.u = u32x4{0, 0, 0, 0};
       if (works && 4 * kVec * f < p.key) {
         const T* from = q + 4 * kVec * f + kVec * g;
         if (p.q.wide) {
-          core.q[n][0][f] = *reinterpret_cast<const typename Core::Frag*>(from);
+          x.u = *reinterpret_cast<const u32x4*>(from);
         } else {
-          union { T t[kVec]; typename Core::Frag v; } x;
 #pragma unroll
           for (int e = 0; e < kVec; ++e) x.t[e] = from[e];
-          core.q[n][0][f] = x.v;
         }
+        // a negative scale is its magnitude and queries of the other sign
+        if (p.scale < 0.f) x.u ^= sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
       }
+      core.q[n][0][f] = x.v;
+    }
   }
 
   if (first < last) {
-    constexpr int kKeyCopies = (S::kBlock * S::kKeyPieces + 63) / 64, kValueCopies = (S::kBlock * S::kValuePieces + 63) / 64;
-    constexpr int kMine = kKeyCopies / 4 + kValueCopies / 4;  // of a wave, at least
+    const float scale = fabsf(p.scale);
     const T* keys = reinterpret_cast<const T*>(p.k.data) + held.begin * p.k.token + sh.head * p.k.head;
     const T* vals = reinterpret_cast<const T*>(p.v.data) + held.begin * p.v.token + sh.head * p.v.head;
+    // where a lane's pieces lie from the block's first row on
+    const int key_pieces = p.key / kVec, value_pieces = p.value / kVec;
+    const uint32_t key_stride = static_cast<uint32_t>(p.k.token * sizeof(T)), value_stride = static_cast<uint32_t>(p.v.token * sizeof(T));
+    uint32_t key_at[S::KeyCopies::kMine], value_at[S::ValueCopies::kMine];
+    if constexpr (kWide) {
+#pragma unroll
+      for (int j = 0; j < S::KeyCopies::kMine; ++j)
+        key_at[j] = S::KeyCopies::row(wave, j, lane) * key_stride + 16 * S::KeyCopies::piece(wave, j, lane, key_pieces);
+#pragma unroll
+      for (int j = 0; j < S::ValueCopies::kMine; ++j)
+        value_at[j] = S::ValueCopies::row(wave, j, lane) * value_stride + 16 * S::ValueCopies::piece(wave, j, lane, value_pieces);
+    }
+    const int end = static_cast<int>(seen);
     const auto fetch = [&](int block, int slot) {
       char* to = smem + slot * S::kBlockBytes;
-      const int64_t pos0 = static_cast<int64_t>(block) * S::kBlock;
-      fetch_rows<T, S::kBlock, S::kKeyPieces>(keys, p.k.token, p.k.wide, p.key / kVec, pos0, seen, to, wave, lane);
-      fetch_rows<T, S::kBlock, S::kValuePieces>(vals, p.v.token, p.v.wide, p.value / kVec, pos0, seen,
-                                                to + S::kBlock * S::kKeyPieces * 16, wave, lane);
+      const int pos0 = block * S::kBlock;
+      if constexpr (kWide) {
+        const char* kb = reinterpret_cast<const char*>(keys + static_cast<int64_t>(pos0) * p.k.token);
+        const char* vb = reinterpret_cast<const char*>(vals + static_cast<int64_t>(pos0) * p.v.token);
+        if (pos0 + S::kBlock <= end) {
+#pragma unroll
+          for (int j = 0; j < S::KeyCopies::kMine; ++j) copy16(kb + key_at[j], to + S::KeyCopies::index(wave, j) * 1024);
+#pragma unroll
+          for (int j = 0; j < S::ValueCopies::kMine; ++j)
+            copy16(vb + value_at[j], to + kKeyBytes + S::ValueCopies::index(wave, j) * 1024);
+        } else {
+          // the last row that is seen in place of those behind it
+          const int most = end - 1 - pos0;
+#pragma unroll
+          for (int j = 0; j < S::KeyCopies::kMine; ++j) {
+            const int row = S::KeyCopies::row(wave, j, lane);
+            copy16(kb + key_at[j] - (row > most ? (row - most) * key_stride : 0), to + S::KeyCopies::index(wave, j) * 1024);
+          }
+#pragma unroll
+          for (int j = 0; j < S::ValueCopies::kMine; ++j) {
+            const int row = S::ValueCopies::row(wave, j, lane);
+            copy16(vb + value_at[j] - (row > most ? (row - most) * value_stride : 0),
+                   to + kKeyBytes + S::ValueCopies::index(wave, j) * 1024);
+          }
+        }
+      } else {
+        fetch_odd_rows<T, S::kBlock, S::kKeyPieces>(keys, p.k.token, key_pieces, pos0, end, to, wave, lane);
+        fetch_odd_rows<T, S::kBlock, S::kValuePieces>(vals, p.v.token, value_pieces, pos0, end, to + kKeyBytes, wave, lane);
+      }
     };
     constexpr int kAhead = S::kRing - 1;
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) fetch(first + i < last ? first + i : last - 1, i);
     int slot = 0;
     for (int block = first; block < last; ++block) {
-      wait_copies<(kAhead - 1) * kMine>();
+      wait_copies<(kAhead - 1) * S::kMine>();
       lds_barrier();
       fetch(block + kAhead < last ? block + kAhead : last - 1, slot == 0 ? S::kRing - 1 : slot - 1);
       if (works) {
-        const int pos = block * S::kBlock;
         const char* at = smem + slot * S::kBlockBytes;
         const T* k = reinterpret_cast<const T*>(at);
-        const T* v = reinterpret_cast<const T*>(at + S::kBlock * S::kKeyPieces * 16);
-        const bool careful = pos + S::kBlock - 1 > lowest;
-        for (int st = both ? 0 : wp; st < (both ? 2 : wp + 1); ++st) {
+        const T* v = reinterpret_cast<const T*>(at + kKeyBytes);
+        const bool careful = (block + 1) * S::kBlock - 1 > lowest;
+        constexpr int kSteps = S::kBlock / kStep;
+        for (int st = both ? 0 : wp; st < (both ? kSteps : wp + 1); ++st) {
           const T* ks = k + st * kStep * (S::kKeyPieces * kVec);
           const T* vs = v + st * kStep * (S::kValuePieces * kVec);
+          const int pos = block * S::kBlock + st * kStep;
           if (careful) {
-            core.template step<true>(ks, vs, p.key / (4 * kVec), p.value / 16, p.scale, pos + st * kStep, 0, lane);
+            core.template step<true>(ks, vs, scale, pos, 0, lane);
           } else {
-            core.template step<false>(ks, vs, p.key / (4 * kVec), p.value / 16, p.scale, pos + st * kStep, 0, lane);
+            core.template step<false>(ks, vs, scale, pos, 0, lane);
           }
         }
       }
@@ -179,7 +215,7 @@ __global__ __launch_bounds__(256) void rows_attend_kernel(RowsAttendParams p) {
           row[kValue + 1] = total;
         }
 #pragma unroll
-        for (int c = 0; c < S::kTiles; ++c) *reinterpret_cast<f32x4*>(row + 16 * c + 4 * g) = core.o[n][c];
+        for (int c = 0; c < kValue / 16; ++c) *reinterpret_cast<f32x4*>(row + 16 * c + 4 * g) = core.o[n][c];
       }
     }
     lds_barrier();
@@ -192,7 +228,7 @@ __global__ __launch_bounds__(256) void rows_attend_kernel(RowsAttendParams p) {
       core.l[n] = core.sum(n) * mine + row[kValue + 1] * its;
       core.m[n] = now;
 #pragma unroll
-      for (int c = 0; c < S::kTiles; ++c) {
+      for (int c = 0; c < kValue / 16; ++c) {
         const f32x4 x = *reinterpret_cast<const f32x4*>(row + 16 * c + 4 * g);
 #pragma unroll
         for (int i = 0; i < 4; ++i) core.o[n][c][i] = core.o[n][c][i] * mine + x[i] * its;
@@ -209,8 +245,8 @@ __global__ __launch_bounds__(256) void rows_attend_kernel(RowsAttendParams p) {
       float* out = p.slots + (unit * p.plan.rows + in_tile) * line;
       if (g == 0) *reinterpret_cast<float2*>(out) = make_float2(core.m[n], total);
 #pragma unroll
-      for (int c = 0; c < S::kTiles; ++c)
-        if (c < S::kFixedTiles || 16 * c < p.value) {
+      for (int c = 0; c < kValue / 16; ++c)
+        if (16 * c < p.value) {
           float2* to = reinterpret_cast<float2*>(out + 2 + 16 * c + 4 * g);
           to[0] = make_float2(core.o[n][c][0], core.o[n][c][1]);
           to[1] = make_float2(core.o[n][c][2], core.o[n][c][3]);
@@ -221,8 +257,8 @@ __global__ __launch_bounds__(256) void rows_attend_kernel(RowsAttendParams p) {
     T* out = reinterpret_cast<T*>(p.out.data) + (sh.span.begin + row / group) * p.out.token +
              (sh.head * group + row % group) * p.out.head + 4 * g;
 #pragma unroll
-    for (int c = 0; c < S::kTiles; ++c)
-      if (c < S::kFixedTiles || 16 * c < p.value) {
+    for (int c = 0; c < kValue / 16; ++c)
+      if (16 * c < p.value) {
         const f32x4 x = core.o[n][c] * by;
         if (p.out.wide) {
           if constexpr (sizeof(T) == 2) {
@@ -238,27 +274,28 @@ __global__ __launch_bounds__(256) void rows_attend_kernel(RowsAttendParams p) {
   }
 }
 
-template <typename T, int kKey, int kValue, int NT>
+template <typename T, int kKey, int kValue, int NT, bool kWide>
 hipError_t launch_rows_shape(const RowsAttendParams& p, hipStream_t stream) {
-  typedef RowsShape<T, kKey, kValue, NT> S;
-  static_assert(32 * NT * (kValue + 4) * 4 <= S::kRing * S::kBlockBytes, "the halves' join fits the ring");
-  hipLaunchKernelGGL((rows_attend_kernel<T, kKey, kValue, NT>), dim3(static_cast<unsigned>(p.plan.grid)), dim3(256),
+  typedef RowsShape<T, kKey, kValue, NT, kWide> S;
+  static_assert(NT == 2 || 32 * (kValue + 4) * 4 <= S::kRing * S::kBlockBytes, "the halves' join fits the ring");
+  hipLaunchKernelGGL((rows_attend_kernel<T, kKey, kValue, NT, kWide>), dim3(static_cast<unsigned>(p.plan.grid)), dim3(256),
                      S::kRing * S::kBlockBytes, stream, p);
   return hipGetLastError();
 }
-template <typename T, int NT>
+template <typename T, int NT, bool kWide>
 hipError_t launch_rows_as(const RowsAttendParams& p, hipStream_t stream) {
   if (p.value <= 64) {
-    if (p.key <= 64) return launch_rows_shape<T, 64, 64, NT>(p, stream);
-    if (p.key <= 128) return launch_rows_shape<T, 128, 64, NT>(p, stream);
-    return launch_rows_shape<T, 192, 64, NT>(p, stream);
+    if (p.key <= 64) return launch_rows_shape<T, 64, 64, NT, kWide>(p, stream);
+    if (p.key <= 128) return launch_rows_shape<T, 128, 64, NT, kWide>(p, stream);
+    return launch_rows_shape<T, 192, 64, NT, kWide>(p, stream);
   }
-  if (p.key <= 64) return launch_rows_shape<T, 64, 128, NT>(p, stream);
-  if (p.key <= 128) return launch_rows_shape<T, 128, 128, NT>(p, stream);
-  return launch_rows_shape<T, 192, 128, NT>(p, stream);
+  if (p.key <= 64) return launch_rows_shape<T, 64, 128, NT, kWide>(p, stream);
+  if (p.key <= 128) return launch_rows_shape<T, 128, 128, NT, kWide>(p, stream);
+  return launch_rows_shape<T, 192, 128, NT, kWide>(p, stream);
 }
 
 hipError_t launch_rows_bf16(const RowsAttendParams& p, hipStream_t stream);
 hipError_t launch_rows_f32(const RowsAttendParams& p, hipStream_t stream);
+hipError_t launch_odd_rows(bool bf16, const RowsAttendParams& p, hipStream_t stream);
 
 }  // namespace scd
