@@ -40,6 +40,28 @@ __device__ inline f32x4 mma(const f32x4& a, const f32x4& b, f32x4 c) {
   return c;
 }
 
+// kCount tiles of 16 value channels, transposed on the way out of LDS: half 0 of tile c holds, of the lane's channel,
+// the positions 4 g .. 4 g + 3 and half 1 the same 16 positions on, kHalf bytes behind.  The reads and the wait for
+// them are one piece of assembly: the compiler takes a transposing read for one that waits for every copy under way
+// into LDS, which would empty the ring of blocks at every step.
+template <int kFirst, int kHalf>
+__device__ inline void read_values4(uint32_t at, s16x4 (&h)[8]) {
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %8 offset:%9\n\t"
+      "ds_read_b64_tr_b16 %1, %8 offset:%10\n\t"
+      "ds_read_b64_tr_b16 %2, %8 offset:%11\n\t"
+      "ds_read_b64_tr_b16 %3, %8 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %4, %8 offset:%13\n\t"
+      "ds_read_b64_tr_b16 %5, %8 offset:%14\n\t"
+      "ds_read_b64_tr_b16 %6, %8 offset:%15\n\t"
+      "ds_read_b64_tr_b16 %7, %8 offset:%16\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(h[0]), "=&v"(h[1]), "=&v"(h[2]), "=&v"(h[3]), "=&v"(h[4]), "=&v"(h[5]), "=&v"(h[6]), "=&v"(h[7])
+      : "v"(at), "n"(kFirst), "n"(kFirst + kHalf), "n"(kFirst + 32), "n"(kFirst + 32 + kHalf), "n"(kFirst + 64),
+        "n"(kFirst + 64 + kHalf), "n"(kFirst + 96), "n"(kFirst + 96 + kHalf)
+      : "memory");
+}
+
 // Whether one of the 16-byte piece's values is not finite.
 __device__ inline bool odd_piece(const uint16_t* p) {
   const uint4 v = *reinterpret_cast<const uint4*>(p);
@@ -181,25 +203,17 @@ struct AttendCore {
     return pos + 16 * t + 4 * g + i <= limit[n] && !(holes >> t & 1);
   }
 
-  template <bool kOdd>
-  __device__ void weigh(const T* v, const f32x4 (&s)[kSub][NT], int pos, int holes, int lr, int g) {
-    if constexpr (sizeof(T) == 2) {
-      bf16x8 w[NT], ones[NT];
+  // Tiles kTile .. kTile + 3 and those behind them.
+  template <int kTile, bool kOdd>
+  __device__ void weigh_tiles(uint32_t at, const bf16x8 (&w)[NT], const bf16x8 (&ones)[NT]) {
+    if constexpr (kTile < kTiles) {
+      s16x4 h[8];
+      read_values4<32 * kTile, 32 * kValueRow>(at, h);
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          // one rounding of a weight to bf16, 8 bits: over many positions it averages out, and the sum that
-          // divides is of unrounded weights
-          w[n][e] = static_cast<__bf16>(s[e >> 2][n][e & 3]);
-          if constexpr (kOdd) ones[n][e] = static_cast<__bf16>(seen(n, e >> 2, e & 3, pos, holes, g) ? 1.f : 0.f);
-        }
-      const T* at = v + (4 * g + (lr >> 2)) * kValueRow + 4 * (lr & 3);
-#pragma unroll
-      for (int c = 0; c < kTiles; ++c) {
+      for (int c = 0; c < 4; ++c) {
         union { s16x4 h[2]; bf16x8 v; uint16_t u[8]; } a;
-        a.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(at + 16 * c));
-        a.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t)(at + 16 * c + 16 * kValueRow));
+        a.h[0] = h[2 * c];
+        a.h[1] = h[2 * c + 1];
         if constexpr (kOdd) {
           union { bf16x8 v; uint16_t u[8]; } flag;
 #pragma unroll
@@ -213,12 +227,32 @@ struct AttendCore {
             const f32x4 x = mma(flag.v, ones[n], f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              if (x[i] > 0.f) o[n][c][i] = __builtin_nanf("");
+              if (x[i] > 0.f) o[n][kTile + c][i] = __builtin_nanf("");
           }
         }
 #pragma unroll
-        for (int n = 0; n < NT; ++n) o[n][c] = mma(a.v, w[n], o[n][c]);
+        for (int n = 0; n < NT; ++n) o[n][kTile + c] = mma(a.v, w[n], o[n][kTile + c]);
       }
+      weigh_tiles<kTile + 4, kOdd>(at, w, ones);
+    }
+  }
+
+  template <bool kOdd>
+  __device__ void weigh(const T* v, const f32x4 (&s)[kSub][NT], int pos, int holes, int lr, int g) {
+    if constexpr (sizeof(T) == 2) {
+      bf16x8 w[NT], ones[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          // one rounding of a weight to bf16, 8 bits: over many positions it averages out, and the sum that
+          // divides is of unrounded weights
+          w[n][e] = static_cast<__bf16>(s[e >> 2][n][e & 3]);
+          if constexpr (kOdd) ones[n][e] = static_cast<__bf16>(seen(n, e >> 2, e & 3, pos, holes, g) ? 1.f : 0.f);
+        }
+      const uint32_t at = static_cast<uint32_t>(
+          reinterpret_cast<uintptr_t>((lds_s16x4_t)(v + (4 * g + (lr >> 2)) * kValueRow + 4 * (lr & 3))));
+      weigh_tiles<0, kOdd>(at, w, ones);
     } else {
       const T* at = v + 4 * g * kValueRow + lr;
 #pragma unroll
@@ -246,9 +280,27 @@ struct AttendCore {
   }
 };
 
+// A value that all lanes hold, in a scalar register.
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ inline int64_t uniform(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<int>(x));
+  const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<int>(x >> 32));
+  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+__device__ inline Span uniform(const Span& s) { return Span{uniform(s.begin), uniform(s.end), uniform(s.pos0)}; }
+
 // 16 bytes a lane from memory into LDS, `to` the wave's first byte.
 __device__ inline void copy16(const void* from, char* to) {
   __builtin_amdgcn_global_load_lds(from, (lds_void_t)to, 16, 0, 0);
+}
+
+// A lane's 16 bytes at `at` of a region (the same for all lanes) of `bytes` bytes; zeros behind its end.
+constexpr int kRegionFlags = 0x00020000;
+__device__ inline void copy16(const void* region, int64_t bytes, uint32_t at, char* to) {
+  const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(
+      reinterpret_cast<void*>(uniform(reinterpret_cast<int64_t>(region))), 0,
+      uniform(static_cast<int>(bytes < 0x7fffffff ? bytes : 0x7fffffff)), kRegionFlags);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t)to, 16, at, 0, 0, 0);
 }
 
 // The 64-lane copies that bring a block of kRows rows of `pieces` 16-byte pieces into LDS rows of kPieces, dealt to
@@ -358,7 +410,6 @@ __device__ inline bool find_share(const SeqBatch& s, const SharePlan& p, int blo
     return n <= chunk ? int64_t{1} : div_ceil(n, chunk);
   };
   Located at;
-  int b_of = 0;
   int64_t per_head = 0;
   if (s.n_seqs == 1) {
     const Span span = span_of(s, 0);
@@ -398,14 +449,16 @@ __device__ inline bool find_share(const SeqBatch& s, const SharePlan& p, int blo
     if (!locate<kThreads>(s, left, lds.found, tid, count, at)) return false;
     out.first = unit - at.local;
   }
-  b_of = at.b;
-  out.b = b_of;
-  out.span = at.span;
-  out.len = length(at.span, b_of);
-  out.tiles = static_cast<int>(of.tiles(at.span));
-  out.parts = static_cast<int>(parts_of(at.span, b_of));
-  out.part = static_cast<int>(div_up_to(at.local, out.tiles));
-  out.tile = static_cast<int>(at.local - static_cast<int64_t>(out.part) * out.tiles);
+  out.b = uniform(at.b);
+  out.span = uniform(at.span);
+  out.head = uniform(out.head);
+  out.first = uniform(out.first);
+  const int64_t local = uniform(at.local);
+  out.len = length(out.span, out.b);
+  out.tiles = static_cast<int>(of.tiles(out.span));
+  out.parts = uniform(static_cast<int>(parts_of(out.span, out.b)));
+  out.part = static_cast<int>(div_up_to(local, out.tiles));
+  out.tile = static_cast<int>(local - static_cast<int64_t>(out.part) * out.tiles);
   out.first += out.tile;
   return true;
 }

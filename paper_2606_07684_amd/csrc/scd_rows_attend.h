@@ -63,7 +63,8 @@ __global__ __launch_bounds__(256, 2) void rows_attend_kernel(RowsAttendParams p)
   };
   Share sh;
   if (!find_share<256>(p.batch, p.plan, S::kBlock, 2, xcd_remap(blockIdx.x, gridDim.x), lds, tid, length, sh)) return;
-  const Span held = span_of(p.held, sh.b);
+  const Span held = uniform(span_of(p.held, sh.b));
+  sh.len = uniform(sh.len);
   // the tiles that see most come first
   const int tile = sh.tiles - 1 - sh.tile;
 
@@ -145,27 +146,14 @@ __global__ __launch_bounds__(256, 2) void rows_attend_kernel(RowsAttendParams p)
       if constexpr (kWide) {
         const char* kb = reinterpret_cast<const char*>(keys + static_cast<int64_t>(pos0) * p.k.token);
         const char* vb = reinterpret_cast<const char*>(vals + static_cast<int64_t>(pos0) * p.v.token);
-        if (pos0 + S::kBlock <= end) {
+        // rows from `end` on are behind the region: zeros
+        const int64_t rows = end - pos0 - 1;
+        const int64_t key_bytes = rows * key_stride + 16 * key_pieces, value_bytes = rows * value_stride + 16 * value_pieces;
 #pragma unroll
-          for (int j = 0; j < S::KeyCopies::kMine; ++j) copy16(kb + key_at[j], to + S::KeyCopies::index(wave, j) * 1024);
+        for (int j = 0; j < S::KeyCopies::kMine; ++j) copy16(kb, key_bytes, key_at[j], to + S::KeyCopies::index(wave, j) * 1024);
 #pragma unroll
-          for (int j = 0; j < S::ValueCopies::kMine; ++j)
-            copy16(vb + value_at[j], to + kKeyBytes + S::ValueCopies::index(wave, j) * 1024);
-        } else {
-          // the last row that is seen in place of those behind it
-          const int most = end - 1 - pos0;
-#pragma unroll
-          for (int j = 0; j < S::KeyCopies::kMine; ++j) {
-            const int row = S::KeyCopies::row(wave, j, lane);
-            copy16(kb + key_at[j] - (row > most ? (row - most) * key_stride : 0), to + S::KeyCopies::index(wave, j) * 1024);
-          }
-#pragma unroll
-          for (int j = 0; j < S::ValueCopies::kMine; ++j) {
-            const int row = S::ValueCopies::row(wave, j, lane);
-            copy16(vb + value_at[j] - (row > most ? (row - most) * value_stride : 0),
-                   to + kKeyBytes + S::ValueCopies::index(wave, j) * 1024);
-          }
-        }
+        for (int j = 0; j < S::ValueCopies::kMine; ++j)
+          copy16(vb, value_bytes, value_at[j], to + kKeyBytes + S::ValueCopies::index(wave, j) * 1024);
       } else {
         fetch_odd_rows<T, S::kBlock, S::kKeyPieces>(keys, p.k.token, key_pieces, pos0, end, to, wave, lane);
         fetch_odd_rows<T, S::kBlock, S::kValuePieces>(vals, p.v.token, value_pieces, pos0, end, to + kKeyBytes, wave, lane);
@@ -174,8 +162,10 @@ __global__ __launch_bounds__(256, 2) void rows_attend_kernel(RowsAttendParams p)
     constexpr int kAhead = S::kRing - 1;
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) fetch(first + i < last ? first + i : last - 1, i);
+    // blocks that all rows of the tile see whole, then those that some leave a part of out
     int slot = 0;
-    for (int block = first; block < last; ++block) {
+    const int whole = (lowest + 1) / S::kBlock;
+    const auto run = [&](int block, auto careful) {
       wait_copies<(kAhead - 1) * S::kMine>();
       lds_barrier();
       fetch(block + kAhead < last ? block + kAhead : last - 1, slot == 0 ? S::kRing - 1 : slot - 1);
@@ -183,21 +173,17 @@ __global__ __launch_bounds__(256, 2) void rows_attend_kernel(RowsAttendParams p)
         const char* at = smem + slot * S::kBlockBytes;
         const T* k = reinterpret_cast<const T*>(at);
         const T* v = reinterpret_cast<const T*>(at + kKeyBytes);
-        const bool careful = (block + 1) * S::kBlock - 1 > lowest;
         constexpr int kSteps = S::kBlock / kStep;
-        for (int st = both ? 0 : wp; st < (both ? kSteps : wp + 1); ++st) {
-          const T* ks = k + st * kStep * (S::kKeyPieces * kVec);
-          const T* vs = v + st * kStep * (S::kValuePieces * kVec);
-          const int pos = block * S::kBlock + st * kStep;
-          if (careful) {
-            core.template step<true>(ks, vs, scale, pos, 0, lane);
-          } else {
-            core.template step<false>(ks, vs, scale, pos, 0, lane);
-          }
-        }
+        for (int st = both ? 0 : wp; st < (both ? kSteps : wp + 1); ++st)
+          core.template step<decltype(careful)::value != 0>(k + st * kStep * (S::kKeyPieces * kVec),
+                                                            v + st * kStep * (S::kValuePieces * kVec), scale,
+                                                            block * S::kBlock + st * kStep, 0, lane);
       }
       slot = slot + 1 == S::kRing ? 0 : slot + 1;
-    }
+    };
+    int block = first;
+    for (; block < last && block < whole; ++block) run(block, IntC<0>{});
+    for (; block < last; ++block) run(block, IntC<1>{});
     wait_copies<0>();
   }
 
