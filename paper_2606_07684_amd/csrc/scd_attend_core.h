@@ -361,84 +361,68 @@ struct Tiles {
   __device__ int64_t blocks(const Span& s, int b) const { return (length(s, b) + block - 1) >> (31 - __builtin_clz(block)); }
 };
 
-// The share that is work unit `unit`; false past the last.  Every thread calls it and gets the answer.
+// The share that workgroup `block` takes; false past the last.  Every thread calls it and gets the answer.
+// Shares are dealt to the XCDs in contiguous ranges, of the shares there are (a launch may have more workgroups), so
+// that those that read the same rows share an L2 and every XCD gets as many.
 template <int kThreads, typename Length>
-__device__ inline bool find_share(const SeqBatch& s, const SharePlan& p, int block, int least, int64_t unit,
+__device__ inline bool find_share(const SeqBatch& s, const SharePlan& p, int block, int least, int workgroup,
                                   ShareLds& lds, int tid, Length length, Share& out) {
   const Tiles<Length> of{p, length, block};
-  int64_t chunk = int64_t{1} << 40;
+  const auto all = [&](auto count, int64_t (&total)[2]) {
+    total[0] = total[1] = 0;
+    if (s.n_seqs == 1) {
+      count(span_of(s, 0), 0, total);
+      return;
+    }
+    for (int b = tid; b < s.n_seqs; b += kThreads) count(span_of(s, b), b, total);
+    for (int o = 32; o > 0; o >>= 1) {
+      total[0] += __shfl_xor(total[0], o);
+      total[1] += __shfl_xor(total[1], o);
+    }
+    __syncthreads();  // the last sum's readers are done
+    if ((tid & 63) == 0) {
+      lds.wave[0][tid >> 6] = total[0];
+      lds.wave[1][tid >> 6] = total[1];
+    }
+    __syncthreads();
+    total[0] = total[1] = 0;
+    for (int w = 0; w < kThreads / 64; ++w) {
+      total[0] += lds.wave[0][w];
+      total[1] += lds.wave[1][w];
+    }
+  };
+  int64_t chunk = int64_t{1} << 40, total[2];
   if (p.cut) {
     // all tiles, and all blocks of all tiles
-    int64_t tiles = 0, work = 0;
-    if (s.n_seqs == 1) {
-      const Span span = span_of(s, 0);
-      tiles = of.tiles(span);
-      work = tiles * of.blocks(span, 0);
-    } else {
-      for (int b = tid; b < s.n_seqs; b += kThreads) {
-        const Span span = span_of(s, b);
-        const int64_t n = of.tiles(span);
-        tiles += n;
-        work += n * of.blocks(span, b);
-      }
-      for (int o = 32; o > 0; o >>= 1) {
-        tiles += __shfl_xor(tiles, o);
-        work += __shfl_xor(work, o);
-      }
-      if ((tid & 63) == 0) {
-        lds.wave[0][tid >> 6] = tiles;
-        lds.wave[1][tid >> 6] = work;
-      }
-      __syncthreads();
-      tiles = work = 0;
-      for (int w = 0; w < kThreads / 64; ++w) {
-        tiles += lds.wave[0][w];
-        work += lds.wave[1][w];
-      }
-    }
-    tiles *= p.heads;
-    work *= p.heads;
+    all([&](const Span& span, int b, int64_t (&t)[2]) {
+      const int64_t n = of.tiles(span);
+      t[0] += n;
+      t[1] += n * of.blocks(span, b);
+    }, total);
+    const int64_t tiles = total[0] * p.heads, work = total[1] * p.heads;
     if (tiles < 2 * kFill) {
       const int64_t room = share_goal(tiles) - tiles;
       chunk = room > 0 ? div_ceil(work, room) : chunk;
       chunk = chunk < least ? least : chunk;
     }
   }
-  // heads one after another, each with all requests' shares; a head's number of shares is the same
   const auto parts_of = [&](const Span& span, int b) {
     const int64_t n = of.blocks(span, b);
     return n <= chunk ? int64_t{1} : div_ceil(n, chunk);
   };
+  // heads one after another, each with all requests' shares; every head has as many
+  all([&](const Span& span, int b, int64_t (&t)[2]) { t[0] += of.tiles(span) * parts_of(span, b); }, total);
+  const int64_t per_head = total[0];
+  if (per_head == 0 || workgroup >= per_head * p.heads) return false;
+  const int64_t unit = xcd_remap(workgroup, static_cast<int>(per_head * p.heads));
+  out.head = static_cast<int>(div_up_to(unit, per_head));
+  const int64_t left = unit - out.head * per_head;
   Located at;
-  int64_t per_head = 0;
   if (s.n_seqs == 1) {
-    const Span span = span_of(s, 0);
-    per_head = of.tiles(span) * parts_of(span, 0);
-    if (per_head == 0 || unit >= per_head * p.heads) return false;
-    out.head = static_cast<int>(div_up_to(unit, per_head));
     at.b = 0;
-    at.span = span;
-    at.local = unit - out.head * per_head;
-    out.first = out.head * per_head;
+    at.span = span_of(s, 0);
+    at.local = left;
   } else {
-    out.head = 0;
-    out.first = 0;
-    int64_t left = unit;
-    if (p.heads > 1) {
-      int64_t n = 0;
-      for (int b = tid; b < s.n_seqs; b += kThreads) {
-        const Span span = span_of(s, b);
-        n += of.tiles(span) * parts_of(span, b);
-      }
-      for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
-      __syncthreads();
-      if ((tid & 63) == 0) lds.wave[0][tid >> 6] = n;
-      __syncthreads();
-      for (int w = 0; w < kThreads / 64; ++w) per_head += lds.wave[0][w];
-      if (per_head == 0 || unit >= per_head * p.heads) return false;
-      out.head = static_cast<int>(div_up_to(unit, per_head));
-      left = unit - out.head * per_head;
-    }
     // locate() calls the count once for every request of this thread, in order
     int next = tid;
     const auto count = [&](const Span& span) {
@@ -447,8 +431,8 @@ __device__ inline bool find_share(const SeqBatch& s, const SharePlan& p, int blo
       return b < s.n_seqs ? of.tiles(span) * parts_of(span, b) : int64_t{0};
     };
     if (!locate<kThreads>(s, left, lds.found, tid, count, at)) return false;
-    out.first = unit - at.local;
   }
+  out.first = unit - at.local;
   out.b = uniform(at.b);
   out.span = uniform(at.span);
   out.head = uniform(out.head);

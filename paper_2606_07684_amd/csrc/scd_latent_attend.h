@@ -49,7 +49,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     return n < 0 ? int64_t{0} : (n > cap ? cap : n);
   };
   Share sh;
-  if (!find_share<256>(p.batch, p.plan, S::kBlock, 2, xcd_remap(blockIdx.x, gridDim.x), lds, tid, length, sh)) return;
+  if (!find_share<256>(p.batch, p.plan, S::kBlock, 2, blockIdx.x, lds, tid, length, sh)) return;
   sh.len = uniform(sh.len);
 
   const int width = p.cache.latent + p.cache.turned;

@@ -18,7 +18,9 @@ struct RowsShape {
   // With 128 rows a wave has work enough for a step of positions between two barriers, and blocks of one leave room
   // for a second workgroup on the CU; tiles of fewer rows have two waves take a step each.
   static constexpr int kBlock = NT == 2 ? kStep : 2 * kStep;
-  static constexpr int kKeyPieces = kKey / kVec + 1, kValuePieces = kValue / kVec + 1;  // odd
+  static constexpr int kKeyPieces = kKey / kVec + 1;
+  // a column of keys takes 16 rows by 16 bytes; of values, transposed, 8 rows by 32 bytes or 4 by 64: each in its own banks
+  static constexpr int kValuePieces = kValue / kVec + (sizeof(T) == 2 ? 2 : 1);
   typedef Copies<kBlock, kKeyPieces> KeyCopies;
   typedef Copies<kBlock, kValuePieces> ValueCopies;
   static constexpr int kBlockBytes = KeyCopies::kBytes + ValueCopies::kBytes;
@@ -62,7 +64,7 @@ __global__ __launch_bounds__(256, 2) void rows_attend_kernel(RowsAttendParams p)
     return upto < 0 ? int64_t{0} : (upto < rows ? upto : rows);
   };
   Share sh;
-  if (!find_share<256>(p.batch, p.plan, S::kBlock, 2, xcd_remap(blockIdx.x, gridDim.x), lds, tid, length, sh)) return;
+  if (!find_share<256>(p.batch, p.plan, S::kBlock, 2, blockIdx.x, lds, tid, length, sh)) return;
   const Span held = uniform(span_of(p.held, sh.b));
   sh.len = uniform(sh.len);
   // the tiles that see most come first
