@@ -304,13 +304,13 @@ __device__ inline void copy16(const void* region, int64_t bytes, uint32_t at, ch
 }
 
 // The 64-lane copies that bring a block of kRows rows of `pieces` 16-byte pieces into LDS rows of kPieces, dealt to
-// the four waves: copy j of a wave fills kilobyte index(wave, j) of the block's region of kBytes bytes.  Every wave
+// kWaves waves: copy j of a wave fills kilobyte index(wave, j) of the block's region of kBytes bytes.  Every wave
 // issues kMine of them, the last ones twice where they do not come out even, so that one count of copies under way
 // holds for all; LDS pieces that a row does not have get its last one again.
-template <int kRows, int kPieces>
+template <int kRows, int kPieces, int kWaves = 4>
 struct Copies {
-  static constexpr int kAll = (kRows * kPieces + 63) / 64, kMine = (kAll + 3) / 4, kBytes = kAll * 1024;
-  static __device__ int index(int wave, int j) { return wave + 4 * j < kAll ? wave + 4 * j : kAll - 1; }
+  static constexpr int kAll = (kRows * kPieces + 63) / 64, kMine = (kAll + kWaves - 1) / kWaves, kBytes = kAll * 1024;
+  static __device__ int index(int wave, int j) { return wave + kWaves * j < kAll ? wave + kWaves * j : kAll - 1; }
   static __device__ int row(int wave, int j, int lane) {
     const int r = (index(wave, j) * 64 + lane) / kPieces;
     return r < kRows ? r : kRows - 1;

@@ -53,6 +53,15 @@ struct RowParts {
   int32_t first, step, count, row;
 };
 
+// What a workgroup of attention over latents takes: a tile of a request's query rows and a share of its positions.
+struct LatentShare {
+  int32_t b, tokens;    // request (-1: nothing), its new tokens
+  int32_t tile, tiles, part, parts;
+  int32_t first;        // slot of the tile's first share
+  int32_t pad;
+  int64_t begin, held;  // first packed row, tokens held before
+};
+
 struct LatentAttendParams {
   LatentPages cache;
   SeqBatch batch;
@@ -63,6 +72,7 @@ struct LatentAttendParams {
   int32_t heads, plain, value;
   float scale;          // of the scores, times log2(e)
   char* absorbed;       // [n_tokens * heads][parts of q][latent + turned]
+  LatentShare* shares;  // [grid]
   RowParts* parts;      // [n_tokens * heads]
   float* slots;         // [grid][rows][latent + 2]
 };
@@ -80,11 +90,14 @@ struct RowsAttendParams {
 hipError_t launch_latent_append(bool bf16, const LatentAppendParams& p, hipStream_t stream);
 hipError_t launch_latent_expand(bool bf16, const LatentExpandParams& p, hipStream_t stream);
 
+// Positions of a block of attention over latents.
+__host__ __device__ constexpr int latent_block(bool bf16) { return bf16 ? 64 : 32; }
+
 // Absorbed queries, attention over the latents, the shares' join with the value matrices applied.
 struct LatentSizes {
   SharePlan plan;
-  size_t absorbed, parts, slots;  // bytes of the workspace
-  size_t total() const { return absorbed + parts + slots; }
+  size_t absorbed, shares, parts, slots;  // bytes of the workspace
+  size_t total() const { return absorbed + shares + parts + slots; }
 };
 LatentSizes latent_sizes(bool bf16, const LatentPages& c, const SeqBatch& b, int heads);
 hipError_t launch_latent_attend(bool bf16, const LatentAttendParams& p, hipStream_t stream);

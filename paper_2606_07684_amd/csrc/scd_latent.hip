@@ -89,69 +89,198 @@ __device__ inline void put_query(uint16_t* row, int width, int i, float x) {
 }
 __device__ inline void put_query(float* row, int, int i, float x) { row[i] = x; }
 
-__device__ inline f32x4 load4(const uint16_t* p) {
-  const uint2 v = *reinterpret_cast<const uint2*>(p);
-  return f32x4{bf16_lo(v.x), bf16_hi(v.x), bf16_lo(v.y), bf16_hi(v.y)};
+// What every workgroup of the attention takes, by one workgroup beside those of the queries: there it costs
+// nothing, and the attention, whose start is a chain of memory accesses, finds it with one.
+__device__ inline void plan_shares(const LatentAttendParams& p, int block, int tid) {
+  __shared__ int64_t sums[2][4];
+  __shared__ int64_t before[256];
+  const int lane = tid & 63, wave = tid >> 6;
+  const auto span = [&](int b) { return span_of(p.batch, b); };
+  const auto tiles_of = [&](const Span& s) { return div_ceil((s.end - s.begin) * p.heads, p.plan.rows); };
+  const auto blocks_of = [&](const Span& s) {
+    int64_t n = s.pos0 + (s.end - s.begin);
+    n = n < 0 ? 0 : (n > p.plan.cap ? p.plan.cap : n);
+    return (n + block - 1) >> (31 - __builtin_clz(block));
+  };
+  int64_t tiles = 0, work = 0;
+  for (int b = tid; b < p.batch.n_seqs; b += 256) {
+    const Span s = span(b);
+    const int64_t n = tiles_of(s);
+    tiles += n;
+    work += n * blocks_of(s);
+  }
+  for (int o = 32; o > 0; o >>= 1) {
+    tiles += __shfl_xor(tiles, o);
+    work += __shfl_xor(work, o);
+  }
+  if (lane == 0) {
+    sums[0][wave] = tiles;
+    sums[1][wave] = work;
+  }
+  __syncthreads();
+  tiles = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
+  work = sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
+  int64_t chunk = int64_t{1} << 40;
+  if (tiles < 2 * kFill) {
+    const int64_t room = share_goal(tiles) - tiles;
+    chunk = room > 0 ? div_ceil(work, room) : chunk;
+    chunk = chunk < 1 ? 1 : chunk;
+  }
+  const auto shares_of = [&](const Span& s) {
+    const int64_t n = blocks_of(s);
+    return tiles_of(s) * (n <= chunk ? 1 : div_ceil(n, chunk));
+  };
+  int64_t total = 0;
+  for (int b = tid; b < p.batch.n_seqs; b += 256) total += shares_of(span(b));
+  for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
+  __syncthreads();
+  if (lane == 0) sums[0][wave] = total;
+  __syncthreads();
+  total = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
+  total = total < p.plan.grid ? total : p.plan.grid;
+  for (int64_t w = total + tid; w < p.plan.grid; w += 256) p.shares[w].b = -1;
+  // 256 requests after another: where their shares begin, then the workgroups that take them
+  int64_t first = 0;
+  for (int b0 = 0; b0 < p.batch.n_seqs; b0 += 256) {
+    const int64_t mine = b0 + tid < p.batch.n_seqs ? shares_of(span(b0 + tid)) : 0;
+    int64_t sum = mine;
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t other = __shfl_up(sum, o);
+      if (lane >= o) sum += other;
+    }
+    __syncthreads();
+    if (lane == 63) sums[1][wave] = sum;
+    __syncthreads();
+    int64_t ahead = first;
+    for (int w = 0; w < wave; ++w) ahead += sums[1][w];
+    before[tid] = ahead + sum - mine;
+    const int64_t next = first + sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
+    __syncthreads();
+    for (int64_t w = tid; w < total; w += 256) {
+      const int64_t unit = xcd_remap(static_cast<int>(w), static_cast<int>(total));
+      if (unit < first || unit >= next) continue;
+      int lo = 0, hi = 255;  // the last request whose shares begin at or before the unit
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (before[mid] <= unit) lo = mid; else hi = mid - 1;
+      }
+      const int b = b0 + lo;
+      const Span s = span(b);
+      const int64_t local = unit - before[lo], n = tiles_of(s), blocks = blocks_of(s);
+      LatentShare out;
+      out.b = b;
+      out.tokens = static_cast<int>(s.end - s.begin);
+      out.tiles = static_cast<int>(n);
+      out.part = static_cast<int>(div_up_to(local, n));
+      out.tile = static_cast<int>(local - out.part * n);
+      out.parts = static_cast<int>(blocks <= chunk ? 1 : div_ceil(blocks, chunk));
+      out.first = static_cast<int>(before[lo] + out.tile);
+      out.pad = 0;
+      out.begin = s.begin;
+      out.held = s.pos0;
+      p.shares[w] = out;
+    }
+    first = next;
+    __syncthreads();
+  }
 }
-__device__ inline f32x4 load4(const float* p) { return *reinterpret_cast<const f32x4*>(p); }
 
-// absorbed_h = scale [ q_h[:plain] W_k,h | q_h[plain:] ]: workgroup (h, a few tokens), four latent channels a
+// absorbed_h = scale [ q_h[:plain] W_k,h | q_h[plain:] ]: workgroup (h, a few tokens), eight latent channels a
 // thread, the matrix's rows dealt to groups of threads whose sums meet in LDS.  The matrix is read once for
 // kTokens tokens; with few tokens that read is the call.
 template <typename T, int kTokens>
 __global__ __launch_bounds__(256) void latent_query_kernel(LatentAttendParams p) {
+  constexpr int kAhead = 16;  // rows of the matrix under way for a thread
   __shared__ float q[kTokens][256 + 64];
-  __shared__ __attribute__((aligned(16))) float sums[kTokens * 1024];
-  const int tid = threadIdx.x, h = blockIdx.x;
+  __shared__ __attribute__((aligned(16))) float sums[kTokens * 2048];
+  const int tid = threadIdx.x, h = static_cast<int>(blockIdx.x) - 1;
+  if (h < 0) {
+    if (blockIdx.y == 0) plan_shares(p, latent_block(sizeof(T) == 2), tid);
+    return;
+  }
   const int64_t t0 = static_cast<int64_t>(blockIdx.y) * kTokens;
   const int n = static_cast<int>(p.batch.n_tokens - t0 < kTokens ? p.batch.n_tokens - t0 : kTokens);
   const int latent = p.cache.latent, turned = p.cache.turned, width = latent + turned;
   const int wide = p.plain + turned;
+  const int eights = latent / 8, groups = 256 / eights;
+  const int group = tid / eights, eight = tid - group * eights;
+  const bool works = group < groups;
+  const T* w = reinterpret_cast<const T*>(p.w_k) + static_cast<int64_t>(h) * p.plain * latent + 8 * eight;
+  // the first rows are on their way while the queries are
+  constexpr int kWords = sizeof(T) / 2;
+  u32x4 x[kAhead][kWords];
+  const auto rows = [&](int d0) {
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+#pragma unroll
+      for (int i = 0; i < kWords; ++i)
+        if (works && d0 + j * groups < p.plain)
+          x[j][i] = reinterpret_cast<const u32x4*>(w + static_cast<int64_t>(d0 + j * groups) * latent)[i];
+  };
+  rows(group);
   for (int i = tid; i < kTokens * wide; i += 256) {
     const int t = i / wide, c = i - t * wide;
-    float x = 0.f;
-    if (t < n) x = load1(reinterpret_cast<const T*>(p.q.data) + (t0 + t) * p.q.token + h * p.q.head + c);
-    q[t][c] = x * p.scale;
+    float y = 0.f;
+    if (t < n) y = load1(reinterpret_cast<const T*>(p.q.data) + (t0 + t) * p.q.token + h * p.q.head + c);
+    q[t][c] = y * p.scale;
   }
   __syncthreads();
-  const int quads = latent / 4, groups = 256 / quads;
-  const int group = tid / quads, quad = tid - group * quads;
-  f32x4 acc[kTokens];
+  float acc[kTokens][8];
 #pragma unroll
-  for (int t = 0; t < kTokens; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (group < groups) {
-    const T* w = reinterpret_cast<const T*>(p.w_k) + static_cast<int64_t>(h) * p.plain * latent + 4 * quad;
-#pragma unroll 8
-    for (int d = group; d < p.plain; d += groups) {
-      const f32x4 x = load4(w + static_cast<int64_t>(d) * latent);
+  for (int t = 0; t < kTokens; ++t)
 #pragma unroll
-      for (int t = 0; t < kTokens; ++t) {
-        const float y = q[t][d];
+    for (int i = 0; i < 8; ++i) acc[t][i] = 0.f;
+  for (int d0 = group; d0 < p.plain; d0 += kAhead * groups) {
+    if (d0 != group) rows(d0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[t][i] += x[i] * y;
+    for (int j = 0; j < kAhead; ++j) {
+      const int d = d0 + j * groups;
+      if (works && d < p.plain) {
+        float f[8];
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            f[2 * i] = bf16_lo(x[j][0][i]);
+            f[2 * i + 1] = bf16_hi(x[j][0][i]);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(x[j][i >> 2][i & 3]);
+        }
+#pragma unroll
+        for (int t = 0; t < kTokens; ++t) {
+          const float y = q[t][d];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) acc[t][i] += f[i] * y;
+        }
       }
     }
+  }
+  if (works) {
 #pragma unroll
-    for (int t = 0; t < kTokens; ++t)
-      *reinterpret_cast<f32x4*>(&sums[(group * kTokens + t) * latent + 4 * quad]) = acc[t];
+    for (int t = 0; t < kTokens; ++t) {
+      float* to = &sums[(group * kTokens + t) * latent + 8 * eight];
+      *reinterpret_cast<f32x4*>(to) = f32x4{acc[t][0], acc[t][1], acc[t][2], acc[t][3]};
+      *reinterpret_cast<f32x4*>(to + 4) = f32x4{acc[t][4], acc[t][5], acc[t][6], acc[t][7]};
+    }
   }
   __syncthreads();
   constexpr int kParts = sizeof(T) == 2 ? 2 : 1;
   for (int i = tid; i < n * width; i += 256) {
     const int t = i / width, c = i - t * width;
-    float x = 0.f;
+    float y = 0.f;
     if (c < latent) {
-      for (int g = 0; g < groups; ++g) x += sums[(g * kTokens + t) * latent + c];
+      for (int g = 0; g < groups; ++g) y += sums[(g * kTokens + t) * latent + c];
     } else {
-      x = q[t][p.plain + c - latent];
+      y = q[t][p.plain + c - latent];
     }
-    put_query(reinterpret_cast<T*>(p.absorbed) + ((t0 + t) * p.heads + h) * (kParts * width), width, c, x);
+    put_query(reinterpret_cast<T*>(p.absorbed) + ((t0 + t) * p.heads + h) * (kParts * width), width, c, y);
   }
 }
 
 // ---- shares joined, results out of the latents' space ----------------------------------------------------
 // out_h = W_v,h (sum_s 2^(m_s - m) o_s) / (sum_s 2^(m_s - m) l_s) over a row's shares s: workgroup (h, tokens
-// of it).  One token's shares are dealt to the four waves, several tokens are dealt as they are.  The joined
+// of it).  One or two tokens' shares are dealt to the four waves, more tokens are dealt as they are.  The joined
 // rows, as two bf16 summands, are the right operands of the product with W_v,h, whose rows come from memory
 // as they lie.
 template <typename T>
@@ -181,48 +310,85 @@ __global__ __launch_bounds__(256) void latent_out_kernel(LatentAttendParams p, i
     const RowParts r = p.parts[t * p.heads + h];
     const int64_t last = r.first + static_cast<int64_t>(r.count - 1) * r.step;
     const bool fits = r.first >= 0 && r.step >= 0 && r.row >= 0 && r.row < p.plan.rows && last < p.plan.grid;
-    const int count = fits ? r.count : 0;
+    const int count = uniform(fits ? r.count : 0);
+    const float* row = p.slots + (static_cast<int64_t>(uniform(r.first)) * p.plan.rows + uniform(r.row)) * line;
+    const int64_t step = static_cast<int64_t>(uniform(r.step)) * p.plan.rows * line;
     m = -INFINITY;
     l = 0.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) o[j] = make_float2(0.f, 0.f);
-    const auto slot = [&](int s) {
-      return p.slots + ((r.first + static_cast<int64_t>(s) * r.step) * p.plan.rows + r.row) * line;
-    };
-    for (int s = lane; s < count; s += 64) m = fmaxf(m, slot(s)[0]);
-    for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
-    const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll 4
-    for (int s = from; s < count; s += by) {
-      const float* at = slot(s);
-      const float2 ml = *reinterpret_cast<const float2*>(at);
-      const float w = __builtin_amdgcn_exp2f(ml.x - base);
-      l += w * ml.y;
+    // eight shares at a time, all of their values on the way before the first is used
+    for (int s0 = from; s0 < count; s0 += 8 * by) {
+      float2 ml[8], x[8][4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (2 * lane + 128 * j < latent) {
-          const float2 x = *reinterpret_cast<const float2*>(at + 2 + 2 * lane + 128 * j);
-          o[j].x += w * x.x;
-          o[j].y += w * x.y;
+      for (int u = 0; u < 8; ++u) {
+        const int s = s0 + u * by;
+        ml[u] = make_float2(-INFINITY, 0.f);
+        if (s < count) ml[u] = *reinterpret_cast<const float2*>(row + s * step);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          x[u][j] = make_float2(0.f, 0.f);
+          if (128 * j < latent && s < count && 2 * lane + 128 * j < latent)
+            x[u][j] = *reinterpret_cast<const float2*>(row + s * step + 2 + 2 * lane + 128 * j);
         }
+      }
+      float now = m;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) now = fmaxf(now, ml[u].x);
+      const float base = now == -INFINITY ? 0.f : now, old = __builtin_amdgcn_exp2f(m - base);
+      m = now;
+      l *= old;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        o[j].x *= old;
+        o[j].y *= old;
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float w = __builtin_amdgcn_exp2f(ml[u].x - base);
+        l += w * ml[u].y;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          o[j].x += w * x[u][j].x;
+          o[j].y += w * x[u][j].y;
+        }
+      }
     }
   };
+  typedef typename Elem<T>::Frag Frag;
+  // the first 8 pieces of the wave's first value rows come while the shares are joined
+  const T* wv = reinterpret_cast<const T*>(p.w_v) + (static_cast<int64_t>(h) * p.value + lr) * latent + kVec * g;
+  const auto pieces = [&](int c0, int f, Frag (&a)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (c0 < p.value && f + 4 * kVec * j < latent)
+        a[j] = *reinterpret_cast<const Frag*>(wv + static_cast<int64_t>(c0) * latent + f + 4 * kVec * j);
+  };
+  Frag ahead[8];
+  pieces(16 * wave, 0, ahead);
   float2 o[4];
   float m, l;
-  if (tokens == 1) {
-    join(t0, wave, 4, o, m, l);
+  if (tokens <= 2) {
+    // the waves of a token (4, or 2 of two tokens) leave their shares' sums in LDS
+    const int per = 4 / tokens, t = wave / per;
+    join(t0 + t < end ? t0 + t : t0, wave - t * per, per, o, m, l);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (2 * lane + 128 * j < latent) {
-        halves[wave][2 * lane + 128 * j] = o[j].x;
-        halves[wave][2 * lane + 128 * j + 1] = o[j].y;
-      }
-    if (lane == 0) halves[wave][latent] = l;
+      if (2 * lane + 128 * j < latent) *reinterpret_cast<float2*>(&halves[wave][2 + 2 * lane + 128 * j]) = o[j];
+    if (lane == 0) *reinterpret_cast<float2*>(&halves[wave][0]) = make_float2(m, l);
     __syncthreads();
-    l = halves[0][latent] + halves[1][latent] + halves[2][latent] + halves[3][latent];
-    const float by = l == 0.f ? 0.f : 1.f / l;
-    for (int c = tid; c < latent; c += 256)
-      put(0, c, (halves[0][c] + halves[1][c] + halves[2][c] + halves[3][c]) * by);
+    for (int i = tid; i < tokens * latent; i += 256) {
+      const int row = tokens == 1 || i < latent ? 0 : 1, c = i - row * latent, w0 = row * per;
+      float top = -INFINITY, sum = 0.f, x = 0.f;
+      for (int w = w0; w < w0 + per; ++w) top = fmaxf(top, halves[w][0]);
+      const float base = top == -INFINITY ? 0.f : top;
+      for (int w = w0; w < w0 + per; ++w) {
+        const float by = __builtin_amdgcn_exp2f(halves[w][0] - base);
+        sum += by * halves[w][1];
+        x += by * halves[w][2 + c];
+      }
+      put(row, c, sum == 0.f ? 0.f : x / sum);
+    }
   } else {
     for (int t = wave; t < tokens; t += 4) {
       if (t0 + t >= end) break;
@@ -239,19 +405,21 @@ __global__ __launch_bounds__(256) void latent_out_kernel(LatentAttendParams p, i
   __syncthreads();
   // columns past the tokens hold anything: a column's sum is its own
   for (int c0 = 16 * wave; c0 < p.value; c0 += 64) {
-    const T* w = reinterpret_cast<const T*>(p.w_v) + (static_cast<int64_t>(h) * p.value + c0 + lr) * latent + kVec * g;
     f32x4 acc{0.f, 0.f, 0.f, 0.f};
     for (int f = 0; f < latent; f += 8 * 4 * kVec) {
-      typename Elem<T>::Frag a[8];
+      Frag a[8];
+      if (c0 == 16 * wave && f == 0) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (f + 4 * kVec * j < latent) a[j] = *reinterpret_cast<const typename Elem<T>::Frag*>(w + f + 4 * kVec * j);
+        for (int j = 0; j < 8; ++j) a[j] = ahead[j];
+      } else {
+        pieces(c0, f, a);
+      }
 #pragma unroll
       for (int j = 0; j < 8; ++j)
         if (f + 4 * kVec * j < latent) {
 #pragma unroll
           for (int i = 0; i < kParts; ++i)
-            acc = mma(a[j], *reinterpret_cast<const typename Elem<T>::Frag*>(&rows[i][lr][f + 4 * kVec * j + kVec * g]), acc);
+            acc = mma(a[j], *reinterpret_cast<const Frag*>(&rows[i][lr][f + 4 * kVec * j + kVec * g]), acc);
         }
     }
     const int64_t t = t0 + lr;
@@ -277,21 +445,21 @@ LatentSizes latent_sizes(bool bf16, const LatentPages& c, const SeqBatch& b, int
   SharePlan& plan = z.plan;
   const int64_t requests = std::min<int64_t>(b.n_seqs, b.n_tokens), rows = b.n_tokens * heads;
   const int64_t mean = (rows + requests - 1) / requests;
-  const bool two = bf16 && c.latent <= 128;
-  plan.rows = mean <= 16 ? 16 : mean <= 32 ? 32 : mean <= 64 || !two ? 64 : 128;
-  plan.row_groups = plan.rows >= 64 ? 4 : plan.rows / 16;
+  plan.rows = mean <= 16 ? 16 : mean <= 32 || c.latent > 256 ? 32 : mean <= 64 || c.latent > 128 ? 64 : 128;
+  plan.row_groups = plan.rows / 16;
   plan.heads = 1;
   plan.per_token = heads;
   plan.cut = 1;
   plan.cap = std::min<int64_t>(static_cast<int64_t>(c.cols) * c.page, (int64_t{1} << 31) - 128);
   const int64_t tiles = rows / plan.rows + requests;
   const int64_t goal = std::max(tiles, share_goal(std::min<int64_t>(tiles, 2 * kFill - 1)));
-  const int block = bf16 ? 64 : 32;
-  const int64_t most = std::max<int64_t>(1, ((plan.cap + block - 1) / block + 1) / 2);  // shares of two blocks each
+  const int block = latent_block(bf16);
+  const int64_t most = std::max<int64_t>(1, (plan.cap + block - 1) / block);  // shares of a block each
   plan.grid = tiles > goal / most ? goal : tiles * most;
   const auto up = [](size_t n) { return (n + 255) & ~size_t{255}; };
   const size_t eb = bf16 ? 2 : 4, parts = bf16 ? 2 : 1;
   z.absorbed = up(static_cast<size_t>(rows) * parts * (c.latent + c.turned) * eb);
+  z.shares = up(static_cast<size_t>(plan.grid) * sizeof(LatentShare));
   z.parts = up(static_cast<size_t>(rows) * sizeof(RowParts));
   z.slots = up(static_cast<size_t>(plan.grid) * plan.rows * (c.latent + 2) * sizeof(float));
   return z;
@@ -300,23 +468,22 @@ LatentSizes latent_sizes(bool bf16, const LatentPages& c, const SeqBatch& b, int
 template <typename T, int kTokens>
 static void query_as(const LatentAttendParams& p, hipStream_t stream) {
   const int64_t y = (p.batch.n_tokens + kTokens - 1) / kTokens;
-  hipLaunchKernelGGL((latent_query_kernel<T, kTokens>), dim3(p.heads, static_cast<unsigned>(y)), dim3(256), 0, stream, p);
+  hipLaunchKernelGGL((latent_query_kernel<T, kTokens>), dim3(p.heads + 1, static_cast<unsigned>(y)), dim3(256), 0, stream, p);
 }
 template <typename T>
 static hipError_t attend_as(const LatentAttendParams& p, hipStream_t stream) {
   const int64_t rows = p.batch.n_tokens * p.heads;
-  if (rows <= 512) {
+  if (rows <= 256) {
     query_as<T, 1>(p, stream);
-  } else if (rows <= 2048) {
-    query_as<T, 4>(p, stream);
   } else {
-    query_as<T, 8>(p, stream);
+    query_as<T, 4>(p, stream);
   }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   e = launch_latent_core(sizeof(T) == 2, p, stream);
   if (e != hipSuccess) return e;
-  const int tokens = rows <= 512 ? 1 : static_cast<int>(std::min<int64_t>(16, (rows + 255) / 256));
+  // a workgroup a CU while there are so few tokens
+  const int tokens = static_cast<int>(std::min<int64_t>(std::max<int64_t>(1, rows / 256), 16));
   const int64_t y = (p.batch.n_tokens + tokens - 1) / tokens;
   hipLaunchKernelGGL((latent_out_kernel<T>), dim3(p.heads, static_cast<unsigned>(y)), dim3(256), 0, stream, p, tokens);
   return hipGetLastError();

@@ -166,8 +166,9 @@ scd_status_t scd_latent_attend(const scd_latent_cache_t* cache, const scd_batch_
   p.scale = static_cast<float>(softmax_scale * kLog2e);
   char* ws = static_cast<char*>(workspace);
   p.absorbed = ws;
-  p.parts = reinterpret_cast<RowParts*>(ws + z.absorbed);
-  p.slots = reinterpret_cast<float*>(ws + z.absorbed + z.parts);
+  p.shares = reinterpret_cast<LatentShare*>(ws + z.absorbed);
+  p.parts = reinterpret_cast<RowParts*>(ws + z.absorbed + z.shares);
+  p.slots = reinterpret_cast<float*>(ws + z.absorbed + z.shares + z.parts);
   return launched(launch_latent_attend(dtype == SCD_BF16, p, stream), "latent attend");
 }
 

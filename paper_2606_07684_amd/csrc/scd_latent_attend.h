@@ -13,79 +13,78 @@
 namespace scd {
 using namespace dev;
 
-// kWide: the widest latent that this instance takes; NT: 16-row tiles of a wave.
-template <typename T, int kWide, int NT>
+// kWide: the widest latent that this instance takes; kWaves waves, of which kHalves share a row's value channels: a
+// wave's chain of LDS reads, scores, weights and products is far longer than its instructions take to issue, so a CU
+// needs two on every SIMD, and where rows are few they are had by halves of the channels (both form the scores).
+template <typename T, int kWide, int kWaves, int kHalves>
 struct LatentShape {
   static constexpr int kParts = sizeof(T) == 2 ? 2 : 1;         // summands of an absorbed query
   static constexpr int kVec = Elem<T>::kVec;
   static constexpr int kMostTurned = 64;
-  static constexpr int kBlock = 2 * Elem<T>::kStep;             // positions of an LDS block
+  static constexpr int kBlock = latent_block(sizeof(T) == 2);   // positions of an LDS block: two steps of a wave
   // 16-byte pieces of an LDS row: an odd number, so that a column's pieces lie in different banks
   static constexpr int kPieces = (kWide + kMostTurned) / kVec + 1;
-  typedef dev::Copies<kBlock, kPieces> Copies;
+  typedef dev::Copies<kBlock, kPieces, kWaves> Copies;
   static constexpr int kRow = kPieces * kVec;                   // elements
   static constexpr int kBlockBytes = Copies::kBytes;
   static constexpr int kRing = kBlockBytes * 4 <= 110 * 1024 ? 4 : kBlockBytes * 3 <= 150 * 1024 ? 3 : 2;
   static constexpr int kIds = 1024;
-  static constexpr int kFrags = (kWide + kMostTurned) / (4 * kVec), kTiles = kWide / 16;
-  typedef AttendCore<T, kFrags, kTiles, NT, kParts, kRow, kRow> Core;
+  static constexpr int kFrags = (kWide + kMostTurned) / (4 * kVec), kTiles = kWide / 16 / kHalves;
+  typedef AttendCore<T, kFrags, kTiles, 1, kParts, kRow, kRow> Core;
   static constexpr int kLds = kRing * kBlockBytes + kIds * 4;
 };
 
-template <typename T, int kWide, int NT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void latent_attend_kernel(LatentAttendParams p) {
-  typedef LatentShape<T, kWide, NT> S;
+template <typename T, int kWide, int kWaves, int kHalves>
+__global__ __launch_bounds__(64 * kWaves) void latent_attend_kernel(LatentAttendParams p) {
+  typedef LatentShape<T, kWide, kWaves, kHalves> S;
   typedef typename S::Core Core;
   constexpr int kStep = Elem<T>::kStep, kVec = S::kVec;
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  __shared__ ShareLds lds;
   int* ids = reinterpret_cast<int*>(smem + S::kRing * S::kBlockBytes);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lr = lane & 15, g = lane >> 4;
 
-  const int64_t cap = p.plan.cap;
-  const auto length = [&](const Span& s, int) {
-    const int64_t n = s.pos0 + (s.end - s.begin);
-    return n < 0 ? int64_t{0} : (n > cap ? cap : n);
-  };
-  Share sh;
-  if (!find_share<256>(p.batch, p.plan, S::kBlock, 2, blockIdx.x, lds, tid, length, sh)) return;
-  sh.len = uniform(sh.len);
+  const LatentShare sh = p.shares[blockIdx.x];
+  if (sh.b < 0) return;
+  const int64_t begin = sh.begin, held = sh.held;
+  int64_t len = held + sh.tokens;
+  len = len < 0 ? 0 : (len > p.plan.cap ? p.plan.cap : len);
 
   const int width = p.cache.latent + p.cache.turned;
-  const int n_rows = static_cast<int>(sh.span.end - sh.span.begin) * p.heads;
+  const int n_rows = sh.tokens * p.heads;
   const int row0 = sh.tile * p.plan.rows;
   const int tile_rows = n_rows - row0 < p.plan.rows ? n_rows - row0 : p.plan.rows;
   // positions the tile's last row attends to, and this share's blocks of them
-  int64_t seen = sh.span.pos0 + (row0 + tile_rows - 1) / p.heads + 1;
-  seen = seen < 0 ? 0 : (seen > sh.len ? sh.len : seen);
+  int64_t seen = held + (row0 + tile_rows - 1) / p.heads + 1;
+  seen = seen < 0 ? 0 : (seen > len ? len : seen);
   const int blocks = static_cast<int>((seen + S::kBlock - 1) / S::kBlock);
   const int first = static_cast<int>(static_cast<int64_t>(blocks) * sh.part / sh.parts);
   const int last = static_cast<int>(static_cast<int64_t>(blocks) * (sh.part + 1) / sh.parts);
-  const int64_t unit = sh.first + static_cast<int64_t>(sh.part) * sh.tiles;
+  const int64_t slot = sh.first + static_cast<int64_t>(sh.part) * sh.tiles;
   if (sh.part == 0 && tid < tile_rows)
-    p.parts[sh.span.begin * p.heads + row0 + tid] =
-        RowParts{static_cast<int>(sh.first), sh.tiles, sh.parts, tid};
+    p.parts[begin * p.heads + row0 + tid] =
+        RowParts{sh.first, sh.tiles, sh.parts, tid};
 
-  // waves side by side over the tile's rows, and, where rows are few, over a block's two steps
-  const int wr = wave % p.plan.row_groups, wp = wave / p.plan.row_groups;
-  const bool both = p.plan.row_groups == 4;
+  // waves side by side over the tile's rows, over halves of the value channels, and, where rows are few, over a
+  // block's two steps
+  const int groups = p.plan.row_groups, wr = wave % groups, rest = wave / groups;
+  const int wc = rest % kHalves, wp = rest / kHalves;
+  const bool both = groups * kHalves == kWaves;
   const bool works = both || wp < 2;
 
   Core core;
   core.clear();
   int lowest = 0x7fffffff;  // of the tile's limits
   {
-    const int64_t low = sh.span.pos0 + row0 / p.heads;
+    const int64_t low = held + row0 / p.heads;
     lowest = low < -1 ? -1 : (low >= seen ? static_cast<int>(seen) - 1 : static_cast<int>(low));
   }
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    int row = (wr * NT + n) * 16 + lr;
+  {
+    int row = wr * 16 + lr;
     row = row0 + (row < tile_rows ? row : tile_rows - 1);
-    const int64_t at = sh.span.pos0 + row / p.heads;
-    core.limit[n] = at < 0 ? -1 : (at >= sh.len ? static_cast<int>(sh.len) - 1 : static_cast<int>(at));
-    const T* q = reinterpret_cast<const T*>(p.absorbed) + (sh.span.begin * p.heads + row) * (S::kParts * width);
+    const int64_t at = held + row / p.heads;
+    core.limit[0] = at < 0 ? -1 : (at >= len ? static_cast<int>(len) - 1 : static_cast<int>(at));
+    const T* q = reinterpret_cast<const T*>(p.absorbed) + (begin * p.heads + row) * (S::kParts * width);
 #pragma unroll
     for (int i = 0; i < S::kParts; ++i)
 #pragma unroll
@@ -93,7 +92,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
         union { u32x4 u; typename Core::Frag v; } x;
         x.u = u32x4{0, 0, 0, 0};
         if (works && 4 * kVec * f < width) x.u = *reinterpret_cast<const u32x4*>(q + i * width + 4 * kVec * f + kVec * g);
-        core.q[n][i][f] = x.v;
+        core.q[0][i][f] = x.v;
       }
   }
 
@@ -104,7 +103,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     int window = column(first);
     const auto fill = [&] {
       const int64_t cols = p.cache.cols;
-      for (int i = tid; i < S::kIds; i += 256) {
+      for (int i = tid; i < S::kIds; i += 64 * kWaves) {
         const int64_t col = static_cast<int64_t>(window) + i;
         const int id = col < cols ? p.cache.table[sh.b * cols + col] : -1;
         ids[i] = id >= 0 && id < p.cache.n_pages ? id : -1;
@@ -118,30 +117,28 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     const uint32_t row_bytes = static_cast<uint32_t>(width * sizeof(T));
     const uint64_t page_bytes = static_cast<uint64_t>(row_bytes) << lg;
     const int mask = (1 << lg) - 1;
-    uint32_t place[S::Copies::kMine];
-    int page[S::Copies::kMine];
+    uint32_t place[S::Copies::kMine];  // the page (one of four at most) in the upper bits
 #pragma unroll
     for (int j = 0; j < S::Copies::kMine; ++j) {
       const int row = S::Copies::row(wave, j, lane);
-      page[j] = row >> lg;
-      place[j] = (row & mask) * row_bytes + 16 * S::Copies::piece(wave, j, lane, pieces);
+      place[j] = ((row & mask) * row_bytes + 16 * S::Copies::piece(wave, j, lane, pieces)) | (row >> lg) << 28;
     }
     const int last_column = static_cast<int>((seen - 1) >> lg);
-    const auto fetch = [&](int block, int slot) {
+    const auto fetch = [&](int block, int ring) {
       const int pos0 = block * S::kBlock, col0 = pos0 >> lg;
       const uint32_t in_page = (pos0 & mask) * row_bytes;  // a page of more than a block
       int id[S::Copies::kMine];
 #pragma unroll
       for (int j = 0; j < S::Copies::kMine; ++j) {
         // columns behind the last one that is seen are its page again
-        const int col = col0 + page[j];
+        const int col = col0 + static_cast<int>(place[j] >> 28);
         id[j] = ids[(col < last_column ? col : last_column) - window];
       }
 #pragma unroll
       for (int j = 0; j < S::Copies::kMine; ++j) {
         const uint32_t p0 = id[j] < 0 ? 0 : id[j];  // a hole's rows are left out: any page will do
-        copy16(p.cache.pages + (p0 * page_bytes + (in_page + place[j])),
-               smem + slot * S::kBlockBytes + S::Copies::index(wave, j) * 1024);
+        copy16(p.cache.pages + (p0 * page_bytes + (in_page + (place[j] & 0xfffffff))),
+               smem + ring * S::kBlockBytes + S::Copies::index(wave, j) * 1024);
       }
     };
     constexpr int kAhead = S::kRing - 1;
@@ -151,7 +148,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
     };
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) fetch(first + i < last ? first + i : last - 1, i);
-    int slot = 0;
+    int ring = 0;
     for (int block = first; block < last; ++block) {
       wait_copies<(kAhead - 1) * S::Copies::kMine>();
       lds_barrier();
@@ -162,10 +159,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
         fill();
         __syncthreads();
       }
-      fetch(next, slot == 0 ? S::kRing - 1 : slot - 1);
+      fetch(next, ring == 0 ? S::kRing - 1 : ring - 1);
       if (works) {
         const int pos = block * S::kBlock;
-        const T* rows = reinterpret_cast<const T*>(smem + slot * S::kBlockBytes);
+        const T* rows = reinterpret_cast<const T*>(smem + ring * S::kBlockBytes);
         // holes among the block's pages, a bit for every 16 positions
         const int col = static_cast<int>((static_cast<int64_t>(pos) + 16 * (lane & 3)) >> lg) - window;
         const int holes = static_cast<int>(__ballot(lane < S::kBlock / 16 && pos + 16 * lane < seen && ids[col] < 0));
@@ -174,80 +171,77 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
           const T* at = rows + st * kStep * S::kRow;
           const int bits = holes >> (st * (kStep / 16));
           if (careful) {
-            core.template step<true>(at, at, 1.f, pos + st * kStep, bits, lane);
+            core.template step<true>(at, at + wc * (kWide / kHalves), 1.f, pos + st * kStep, bits, lane);
           } else {
-            core.template step<false>(at, at, 1.f, pos + st * kStep, bits, lane);
+            core.template step<false>(at, at + wc * (kWide / kHalves), 1.f, pos + st * kStep, bits, lane);
           }
         }
       }
-      slot = slot + 1 == S::kRing ? 0 : slot + 1;
+      ring = ring + 1 == S::kRing ? 0 : ring + 1;
     }
     wait_copies<0>();
   }
 
-  // the two steps' halves become one through LDS, in which no copy is under way any more
-  constexpr int kLine = kWide + 4;
+  // what the two steps' waves have becomes one through LDS, in which no copy is under way any more
+  constexpr int kLine = kWide + 4, kMine = kWide / kHalves;
+  float total = core.sum(0);
   if (!both) {
-    float* rest = reinterpret_cast<float*>(smem);
+    float* row = reinterpret_cast<float*>(smem) + (wr * 16 + lr) * kLine;
     lds_barrier();
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      float* row = rest + ((wr * NT + n) * 16 + lr) * kLine;
-      if (wp == 1) {
-        const float total = core.sum(n);
-        if (g == 0) {
-          row[kWide] = core.m[n];
-          row[kWide + 1] = total;
-        }
-#pragma unroll
-        for (int c = 0; c < S::kTiles; ++c) *reinterpret_cast<f32x4*>(row + 16 * c + 4 * g) = core.o[n][c];
+    if (wp == 1) {
+      if (g == 0) {
+        row[kWide] = core.m[0];
+        row[kWide + 1] = total;
       }
+#pragma unroll
+      for (int c = 0; c < S::kTiles; ++c) *reinterpret_cast<f32x4*>(row + wc * kMine + 16 * c + 4 * g) = core.o[0][c];
     }
     lds_barrier();
     if (wp != 0) return;
+    const float other = row[kWide], now = fmaxf(core.m[0], other), base = now == -INFINITY ? 0.f : now;
+    const float mine = __builtin_amdgcn_exp2f(core.m[0] - base), its = __builtin_amdgcn_exp2f(other - base);
+    total = total * mine + row[kWide + 1] * its;
+    core.m[0] = now;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-      const float* row = rest + ((wr * NT + n) * 16 + lr) * kLine;
-      const float other = row[kWide], now = fmaxf(core.m[n], other), base = now == -INFINITY ? 0.f : now;
-      const float mine = __builtin_amdgcn_exp2f(core.m[n] - base), its = __builtin_amdgcn_exp2f(other - base);
-      core.l[n] = core.sum(n) * mine + row[kWide + 1] * its;
-      core.m[n] = now;
+    for (int c = 0; c < S::kTiles; ++c) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(row + wc * kMine + 16 * c + 4 * g);
 #pragma unroll
-      for (int c = 0; c < S::kTiles; ++c) {
-        const f32x4 x = *reinterpret_cast<const f32x4*>(row + 16 * c + 4 * g);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) core.o[n][c][i] = core.o[n][c][i] * mine + x[i] * its;
-      }
+      for (int i = 0; i < 4; ++i) core.o[0][c][i] = core.o[0][c][i] * mine + x[i] * its;
     }
   }
-  const int line = p.cache.latent + 2;
+  const int line = p.cache.latent + 2, row = wr * 16 + lr;
+  if (row < tile_rows) {
+    // lines of latent + 2 values: two-float stores keep to their alignment
+    float* out = p.slots + (slot * p.plan.rows + row) * line;
+    if (g == 0 && wc == 0) *reinterpret_cast<float2*>(out) = make_float2(core.m[0], total);
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int row = (wr * NT + n) * 16 + lr;
-    const float total = both ? core.sum(n) : core.l[n];
-    if (row < tile_rows) {
-      // lines of latent + 2 values: two-float stores keep to their alignment
-      float* out = p.slots + (unit * p.plan.rows + row) * line;
-      if (g == 0) *reinterpret_cast<float2*>(out) = make_float2(core.m[n], total);
-#pragma unroll
-      for (int c = 0; c < S::kTiles; ++c)
-        if (16 * c < p.cache.latent) {
-          float2* to = reinterpret_cast<float2*>(out + 2 + 16 * c + 4 * g);
-          to[0] = make_float2(core.o[n][c][0], core.o[n][c][1]);
-          to[1] = make_float2(core.o[n][c][2], core.o[n][c][3]);
-        }
-    }
+    for (int c = 0; c < S::kTiles; ++c)
+      if (wc * kMine + 16 * c < p.cache.latent) {
+        float2* to = reinterpret_cast<float2*>(out + 2 + wc * kMine + 16 * c + 4 * g);
+        to[0] = make_float2(core.o[0][c][0], core.o[0][c][1]);
+        to[1] = make_float2(core.o[0][c][2], core.o[0][c][3]);
+      }
   }
 }
 
-template <typename T, int kWide, int NT>
+template <typename T, int kWide, int kWaves, int kHalves>
 hipError_t launch_latent_shape(const LatentAttendParams& p, hipStream_t stream) {
-  typedef LatentShape<T, kWide, NT> S;
-  constexpr int join = 32 * (kWide + 4) * 4 * NT;
-  static_assert(join <= S::kRing * S::kBlockBytes, "the halves' join fits the ring");
-  hipLaunchKernelGGL((latent_attend_kernel<T, kWide, NT>), dim3(static_cast<unsigned>(p.plan.grid)), dim3(256), S::kLds,
-                     stream, p);
+  typedef LatentShape<T, kWide, kWaves, kHalves> S;
+  static_assert((kHalves == 1 ? 64 : 32) * (kWide + 4) * 4 <= S::kRing * S::kBlockBytes, "the steps' join fits the ring");
+  static_assert(S::kTiles % 4 == 0, "value tiles are read by fours");
+  hipLaunchKernelGGL((latent_attend_kernel<T, kWide, kWaves, kHalves>), dim3(static_cast<unsigned>(p.plan.grid)),
+                     dim3(64 * kWaves), S::kLds, stream, p);
   return hipGetLastError();
+}
+// Few rows with halves of the channels, more without: 64 rows are four waves for each of a block's steps, 128 eight
+// (above 128 channels registers are too few for that, and up to 64 there is nothing to halve); latents above 256 channels, whose queries alone are 144 registers, up to 32 rows in four waves.
+template <typename T>
+hipError_t launch_latent_as(const LatentAttendParams& p, hipStream_t stream) {
+  if (p.cache.latent <= 64) return launch_latent_shape<T, 64, 8, 1>(p, stream);
+  if (p.cache.latent <= 128)
+    return p.plan.rows >= 64 ? launch_latent_shape<T, 128, 8, 1>(p, stream) : launch_latent_shape<T, 128, 8, 2>(p, stream);
+  if (p.cache.latent <= 256) return launch_latent_shape<T, 256, 8, 2>(p, stream);
+  return launch_latent_shape<T, 512, 4, 2>(p, stream);
 }
 
 hipError_t launch_latent_core_bf16(const LatentAttendParams& p, hipStream_t stream);
