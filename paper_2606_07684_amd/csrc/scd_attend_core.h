@@ -87,8 +87,8 @@ __device__ inline float row_top(float x) {
 }
 
 // kFrags pieces of 4 kVec channels that a score contracts, kTiles tiles of 16 value channels, NT tiles of 16
-// query rows, a query as kParts summands; kKeyRow, kValueRow elements between LDS rows.
-template <typename T, int kFrags, int kTiles, int NT, int kParts, int kKeyRow, int kValueRow>
+// query rows, the queries' first kLow pieces with a second summand; kKeyRow, kValueRow elements between LDS rows.
+template <typename T, int kFrags, int kTiles, int NT, int kLow, int kKeyRow, int kValueRow>
 struct AttendCore {
   typedef typename Elem<T>::Frag Frag;
   static constexpr int kStep = Elem<T>::kStep, kVec = Elem<T>::kVec, kSub = kStep / 16;
@@ -96,7 +96,7 @@ struct AttendCore {
   // most steps neither compare scores across lanes nor scale what they have.
   static constexpr float kSlack = 8.f;
 
-  Frag q[NT][kParts][kFrags];
+  Frag q[NT][kFrags], low[NT][kLow > 0 ? kLow : 1];
   f32x4 o[NT][kTiles];
   float m[NT], l[NT];  // l: this lane's positions only
   int limit[NT];       // last position the lane's row attends to
@@ -130,9 +130,11 @@ struct AttendCore {
       for (int t = 0; t < kSub; ++t) {
         const Frag a = *reinterpret_cast<const Frag*>(row + 16 * t * kKeyRow + 4 * kVec * f);
 #pragma unroll
-        for (int i = 0; i < kParts; ++i)
+        for (int n = 0; n < NT; ++n) s[t][n] = mma(a, q[n][f], s[t][n]);
+        if (f < kLow) {
 #pragma unroll
-          for (int n = 0; n < NT; ++n) s[t][n] = mma(a, q[n][i][f], s[t][n]);
+          for (int n = 0; n < NT; ++n) s[t][n] = mma(a, low[n][f < kLow ? f : 0], s[t][n]);
+        }
       }
     bool odd = false;
     if constexpr (kCareful) {

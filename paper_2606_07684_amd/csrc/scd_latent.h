@@ -62,6 +62,11 @@ struct LatentShare {
   int64_t begin, held;  // first packed row, tokens held before
 };
 
+// Elements of an absorbed query: latent and turned channels, in bf16 the latent ones' second summands behind them.
+__host__ __device__ inline int query_width(bool bf16, int latent, int turned) {
+  return bf16 ? 2 * latent + turned : latent + turned;
+}
+
 struct LatentAttendParams {
   LatentPages cache;
   SeqBatch batch;
@@ -71,7 +76,7 @@ struct LatentAttendParams {
   const char* w_v;
   int32_t heads, plain, value;
   float scale;          // of the scores, times log2(e)
-  char* absorbed;       // [n_tokens * heads][parts of q][latent + turned]
+  char* absorbed;       // [n_tokens * heads][query_width]
   LatentShare* shares;  // [grid]
   RowParts* parts;      // [n_tokens * heads]
   float* slots;         // [grid][rows][latent + 2]

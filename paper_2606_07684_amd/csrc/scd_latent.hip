@@ -80,104 +80,136 @@ hipError_t launch_latent_append(bool bf16, const LatentAppendParams& p, hipStrea
 }
 
 // ---- queries into the latents' space -------------------------------------------------------------------
-__device__ inline void put_query(uint16_t* row, int width, int i, float x) {
-  // two bf16 summands hold 16 bits of a query: a score's error then stays below what the rounding of the
-  // result to bf16 adds, as in a product of unrounded queries
+// Channel i of an absorbed query of `width` channels, the first `latent` of them products.
+__device__ inline void put_query(uint16_t* row, int latent, int width, int i, float x) {
+  // Two bf16 summands hold 16 bits of a product: a score's error then stays below what the rounding of the
+  // result to bf16 adds, as in a product of unrounded queries.  The turned channels are the query's own.
   const __bf16 high = static_cast<__bf16>(x);
   row[i] = __builtin_bit_cast(uint16_t, high);
-  row[width + i] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(x - static_cast<float>(high)));
+  if (i < latent) row[width + i] = __builtin_bit_cast(uint16_t, static_cast<__bf16>(x - static_cast<float>(high)));
 }
-__device__ inline void put_query(float* row, int, int i, float x) { row[i] = x; }
+__device__ inline void put_query(float* row, int, int, int i, float x) { row[i] = x; }
 
 // What every workgroup of the attention takes, by one workgroup beside those of the queries: there it costs
 // nothing, and the attention, whose start is a chain of memory accesses, finds it with one.
 __device__ inline void plan_shares(const LatentAttendParams& p, int block, int tid) {
+  // a request among 256 after another
+  struct Entry { int64_t begin, held, first; int tokens, tiles, blocks; };
+  __shared__ Entry entries[256];
   __shared__ int64_t sums[2][4];
-  __shared__ int64_t before[256];
-  const int lane = tid & 63, wave = tid >> 6;
-  const auto span = [&](int b) { return span_of(p.batch, b); };
-  const auto tiles_of = [&](const Span& s) { return div_ceil((s.end - s.begin) * p.heads, p.plan.rows); };
-  const auto blocks_of = [&](const Span& s) {
-    int64_t n = s.pos0 + (s.end - s.begin);
-    n = n < 0 ? 0 : (n > p.plan.cap ? p.plan.cap : n);
-    return (n + block - 1) >> (31 - __builtin_clz(block));
+  const int lane = tid & 63, wave = tid >> 6, shift = 31 - __builtin_clz(block);
+  const auto load = [&](int b) {
+    Entry e{0, 0, 0, 0, 0, 0};
+    if (b < p.batch.n_seqs) {
+      const Span s = span_of(p.batch, b);
+      e.begin = s.begin;
+      e.held = s.pos0;
+      e.tokens = static_cast<int>(s.end - s.begin);
+      int64_t n = s.pos0 + e.tokens;
+      n = n < 0 ? 0 : (n > p.plan.cap ? p.plan.cap : n);
+      e.blocks = static_cast<int>((n + block - 1) >> shift);
+      e.tiles = static_cast<int>((static_cast<uint32_t>(e.tokens) * static_cast<uint32_t>(p.heads) + p.plan.rows - 1) /
+                                 static_cast<uint32_t>(p.plan.rows));
+    }
+    return e;
   };
-  int64_t tiles = 0, work = 0;
-  for (int b = tid; b < p.batch.n_seqs; b += 256) {
-    const Span s = span(b);
-    const int64_t n = tiles_of(s);
-    tiles += n;
-    work += n * blocks_of(s);
+  // sum over the workgroup of x and y, both below 2^31 a thread of a wave at least
+  const auto total_of = [&](int64_t x, int64_t y, int64_t& tx, int64_t& ty) {
+    for (int o = 32; o > 0; o >>= 1) {
+      x += __shfl_xor(x, o);
+      y += __shfl_xor(y, o);
+    }
+    __syncthreads();  // the last sums' readers are done
+    if (lane == 0) {
+      sums[0][wave] = x;
+      sums[1][wave] = y;
+    }
+    __syncthreads();
+    tx = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
+    ty = sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
+  };
+  Entry mine = load(tid);
+  const bool one_round = p.batch.n_seqs <= 256;
+  int64_t tiles = mine.tiles, work = static_cast<int64_t>(mine.tiles) * mine.blocks, most = 0;
+  for (int b = 256 + tid; b < p.batch.n_seqs; b += 256) {
+    const Entry e = load(b);
+    tiles += e.tiles;
+    work += static_cast<int64_t>(e.tiles) * e.blocks;
   }
-  for (int o = 32; o > 0; o >>= 1) {
-    tiles += __shfl_xor(tiles, o);
-    work += __shfl_xor(work, o);
-  }
-  if (lane == 0) {
-    sums[0][wave] = tiles;
-    sums[1][wave] = work;
-  }
-  __syncthreads();
-  tiles = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
-  work = sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
-  int64_t chunk = int64_t{1} << 40;
+  total_of(tiles, work, tiles, work);
+  uint32_t chunk = 0x7fffffff;
   if (tiles < 2 * kFill) {
     const int64_t room = share_goal(tiles) - tiles;
-    chunk = room > 0 ? div_ceil(work, room) : chunk;
-    chunk = chunk < 1 ? 1 : chunk;
+    if (room > 0) chunk = static_cast<uint32_t>(div_ceil(work, room));
+    if (chunk < 1) chunk = 1;
   }
-  const auto shares_of = [&](const Span& s) {
-    const int64_t n = blocks_of(s);
-    return tiles_of(s) * (n <= chunk ? 1 : div_ceil(n, chunk));
+  const auto parts_of = [&](const Entry& e) {
+    const uint32_t n = e.blocks;
+    return n <= chunk ? 1u : (n + chunk - 1) / chunk;
   };
-  int64_t total = 0;
-  for (int b = tid; b < p.batch.n_seqs; b += 256) total += shares_of(span(b));
-  for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
-  __syncthreads();
-  if (lane == 0) sums[0][wave] = total;
-  __syncthreads();
-  total = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
-  total = total < p.plan.grid ? total : p.plan.grid;
-  for (int64_t w = total + tid; w < p.plan.grid; w += 256) p.shares[w].b = -1;
-  // 256 requests after another: where their shares begin, then the workgroups that take them
-  int64_t first = 0;
-  for (int b0 = 0; b0 < p.batch.n_seqs; b0 += 256) {
-    const int64_t mine = b0 + tid < p.batch.n_seqs ? shares_of(span(b0 + tid)) : 0;
-    int64_t sum = mine;
+  int64_t total = static_cast<int64_t>(mine.tiles) * parts_of(mine);
+  for (int b = 256 + tid; b < p.batch.n_seqs; b += 256) {
+    const Entry e = load(b);
+    total += static_cast<int64_t>(e.tiles) * parts_of(e);
+  }
+  int64_t sum = total;  // of the first round: where a request's shares begin
+  if (one_round) {
     for (int o = 1; o < 64; o <<= 1) {
       const int64_t other = __shfl_up(sum, o);
       if (lane >= o) sum += other;
     }
     __syncthreads();
-    if (lane == 63) sums[1][wave] = sum;
+    if (lane == 63) sums[0][wave] = sum;
+    mine.first = sum - total;
     __syncthreads();
-    int64_t ahead = first;
-    for (int w = 0; w < wave; ++w) ahead += sums[1][w];
-    before[tid] = ahead + sum - mine;
-    const int64_t next = first + sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
-    __syncthreads();
-    for (int64_t w = tid; w < total; w += 256) {
-      const int64_t unit = xcd_remap(static_cast<int>(w), static_cast<int>(total));
-      if (unit < first || unit >= next) continue;
-      int lo = 0, hi = 255;  // the last request whose shares begin at or before the unit
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (before[mid] <= unit) lo = mid; else hi = mid - 1;
+    for (int w = 0; w < wave; ++w) mine.first += sums[0][w];
+    total = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
+  } else {
+    total_of(total, most, total, most);
+  }
+  total = total < p.plan.grid ? total : p.plan.grid;
+  for (int64_t w = total + tid; w < p.plan.grid; w += 256) p.shares[w].b = -1;
+  int64_t first = 0;
+  for (int b0 = 0; b0 < p.batch.n_seqs; b0 += 256) {
+    int64_t next = total;
+    if (!one_round) {
+      mine = load(b0 + tid);
+      const int64_t n = static_cast<int64_t>(mine.tiles) * parts_of(mine);
+      sum = n;
+      for (int o = 1; o < 64; o <<= 1) {
+        const int64_t other = __shfl_up(sum, o);
+        if (lane >= o) sum += other;
       }
-      const int b = b0 + lo;
-      const Span s = span(b);
-      const int64_t local = unit - before[lo], n = tiles_of(s), blocks = blocks_of(s);
+      __syncthreads();
+      if (lane == 63) sums[1][wave] = sum;
+      __syncthreads();
+      mine.first = first + sum - n;
+      for (int w = 0; w < wave; ++w) mine.first += sums[1][w];
+      next = first + sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
+    }
+    entries[tid] = mine;
+    __syncthreads();
+    for (int w = tid; w < total; w += 256) {
+      const int64_t unit = xcd_remap(w, static_cast<int>(total));
+      if (unit < first || unit >= next) continue;
+      int lo = 0, hi = p.batch.n_seqs - b0 < 256 ? p.batch.n_seqs - b0 - 1 : 255;
+      while (lo < hi) {  // the last request whose shares begin at or before the unit
+        const int mid = (lo + hi + 1) >> 1;
+        if (entries[mid].first <= unit) lo = mid; else hi = mid - 1;
+      }
+      const Entry e = entries[lo];
+      const uint32_t local = static_cast<uint32_t>(unit - e.first);
       LatentShare out;
-      out.b = b;
-      out.tokens = static_cast<int>(s.end - s.begin);
-      out.tiles = static_cast<int>(n);
-      out.part = static_cast<int>(div_up_to(local, n));
-      out.tile = static_cast<int>(local - out.part * n);
-      out.parts = static_cast<int>(blocks <= chunk ? 1 : div_ceil(blocks, chunk));
-      out.first = static_cast<int>(before[lo] + out.tile);
+      out.b = b0 + lo;
+      out.tokens = e.tokens;
+      out.tiles = e.tiles;
+      out.part = static_cast<int>(local / static_cast<uint32_t>(e.tiles));
+      out.tile = static_cast<int>(local) - out.part * e.tiles;
+      out.parts = static_cast<int>(parts_of(e));
+      out.first = static_cast<int>(e.first) + out.tile;
       out.pad = 0;
-      out.begin = s.begin;
-      out.held = s.pos0;
+      out.begin = e.begin;
+      out.held = e.held;
       p.shares[w] = out;
     }
     first = next;
@@ -185,7 +217,7 @@ __device__ inline void plan_shares(const LatentAttendParams& p, int block, int t
   }
 }
 
-// absorbed_h = scale [ q_h[:plain] W_k,h | q_h[plain:] ]: workgroup (h, a few tokens), eight latent channels a
+// absorbed_h = [ q_h[:plain] W_k,h | q_h[plain:] ], of the other sign for a negative scale: workgroup (h, a few tokens), eight latent channels a
 // thread, the matrix's rows dealt to groups of threads whose sums meet in LDS.  The matrix is read once for
 // kTokens tokens; with few tokens that read is the call.
 template <typename T, int kTokens>
@@ -222,7 +254,7 @@ __global__ __launch_bounds__(256) void latent_query_kernel(LatentAttendParams p)
     const int t = i / wide, c = i - t * wide;
     float y = 0.f;
     if (t < n) y = load1(reinterpret_cast<const T*>(p.q.data) + (t0 + t) * p.q.token + h * p.q.head + c);
-    q[t][c] = y * p.scale;
+    q[t][c] = p.scale < 0.f ? -y : y;
   }
   __syncthreads();
   float acc[kTokens][8];
@@ -265,7 +297,7 @@ __global__ __launch_bounds__(256) void latent_query_kernel(LatentAttendParams p)
     }
   }
   __syncthreads();
-  constexpr int kParts = sizeof(T) == 2 ? 2 : 1;
+  const int line = query_width(sizeof(T) == 2, latent, turned);
   for (int i = tid; i < n * width; i += 256) {
     const int t = i / width, c = i - t * width;
     float y = 0.f;
@@ -274,7 +306,7 @@ __global__ __launch_bounds__(256) void latent_query_kernel(LatentAttendParams p)
     } else {
       y = q[t][p.plain + c - latent];
     }
-    put_query(reinterpret_cast<T*>(p.absorbed) + ((t0 + t) * p.heads + h) * (kParts * width), width, c, y);
+    put_query(reinterpret_cast<T*>(p.absorbed) + ((t0 + t) * p.heads + h) * line, latent, width, c, y);
   }
 }
 
@@ -292,9 +324,8 @@ __global__ __launch_bounds__(256) void latent_out_kernel(LatentAttendParams p, i
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lr = lane & 15, g = lane >> 4;
   const int h = blockIdx.x, latent = p.cache.latent, line = latent + 2;
   const int64_t t0 = static_cast<int64_t>(blockIdx.y) * tokens;
-  int64_t end = p.batch.n_tokens;
-  if (p.batch.cu != nullptr) end = std::min<int64_t>(end, p.batch.cu[p.batch.n_seqs]);
-  if (t0 >= end) return;
+  // rows behind the last request are left alone: joined like the others (their entries are checked), not stored
+  const int32_t stop = p.batch.cu != nullptr ? p.batch.cu[p.batch.n_seqs] : 0x7fffffff;
 
   const auto put = [&](int t, int c, float x) {
     if constexpr (sizeof(T) == 2) {
@@ -309,7 +340,8 @@ __global__ __launch_bounds__(256) void latent_out_kernel(LatentAttendParams p, i
   const auto join = [&](int64_t t, int from, int by, float2 (&o)[4], float& m, float& l) {
     const RowParts r = p.parts[t * p.heads + h];
     const int64_t last = r.first + static_cast<int64_t>(r.count - 1) * r.step;
-    const bool fits = r.first >= 0 && r.step >= 0 && r.row >= 0 && r.row < p.plan.rows && last < p.plan.grid;
+    const bool fits = r.first >= 0 && r.step >= 0 && r.row >= 0 && r.row < p.plan.rows && last < p.plan.grid &&
+                      r.count <= p.plan.grid;
     const int count = uniform(fits ? r.count : 0);
     const float* row = p.slots + (static_cast<int64_t>(uniform(r.first)) * p.plan.rows + uniform(r.row)) * line;
     const int64_t step = static_cast<int64_t>(uniform(r.step)) * p.plan.rows * line;
@@ -356,7 +388,7 @@ __global__ __launch_bounds__(256) void latent_out_kernel(LatentAttendParams p, i
     }
   };
   typedef typename Elem<T>::Frag Frag;
-  // the first 8 pieces of the wave's first value rows come while the shares are joined
+  // the first 8 pieces of the wave's first two tiles of value rows come while the shares are joined
   const T* wv = reinterpret_cast<const T*>(p.w_v) + (static_cast<int64_t>(h) * p.value + lr) * latent + kVec * g;
   const auto pieces = [&](int c0, int f, Frag (&a)[8]) {
 #pragma unroll
@@ -364,14 +396,15 @@ __global__ __launch_bounds__(256) void latent_out_kernel(LatentAttendParams p, i
       if (c0 < p.value && f + 4 * kVec * j < latent)
         a[j] = *reinterpret_cast<const Frag*>(wv + static_cast<int64_t>(c0) * latent + f + 4 * kVec * j);
   };
-  Frag ahead[8];
-  pieces(16 * wave, 0, ahead);
+  Frag ahead[2][8];
+  pieces(16 * wave, 0, ahead[0]);
+  pieces(16 * wave + 64, 0, ahead[1]);
   float2 o[4];
   float m, l;
   if (tokens <= 2) {
     // the waves of a token (4, or 2 of two tokens) leave their shares' sums in LDS
     const int per = 4 / tokens, t = wave / per;
-    join(t0 + t < end ? t0 + t : t0, wave - t * per, per, o, m, l);
+    join(t0 + t < p.batch.n_tokens ? t0 + t : t0, wave - t * per, per, o, m, l);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
       if (2 * lane + 128 * j < latent) *reinterpret_cast<float2*>(&halves[wave][2 + 2 * lane + 128 * j]) = o[j];
@@ -391,7 +424,7 @@ __global__ __launch_bounds__(256) void latent_out_kernel(LatentAttendParams p, i
     }
   } else {
     for (int t = wave; t < tokens; t += 4) {
-      if (t0 + t >= end) break;
+      if (t0 + t >= p.batch.n_tokens) break;
       join(t0 + t, 0, 1, o, m, l);
       const float by = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
@@ -408,9 +441,9 @@ __global__ __launch_bounds__(256) void latent_out_kernel(LatentAttendParams p, i
     f32x4 acc{0.f, 0.f, 0.f, 0.f};
     for (int f = 0; f < latent; f += 8 * 4 * kVec) {
       Frag a[8];
-      if (c0 == 16 * wave && f == 0) {
+      if (c0 < 128 && f == 0) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) a[j] = ahead[j];
+        for (int j = 0; j < 8; ++j) a[j] = c0 < 64 ? ahead[0][j] : ahead[1][j];
       } else {
         pieces(c0, f, a);
       }
@@ -423,7 +456,7 @@ __global__ __launch_bounds__(256) void latent_out_kernel(LatentAttendParams p, i
         }
     }
     const int64_t t = t0 + lr;
-    if (lr < tokens && t < end) {
+    if (lr < tokens && t < p.batch.n_tokens && t < stop) {
       T* out = reinterpret_cast<T*>(p.out.data) + t * p.out.token + h * p.out.head + c0 + 4 * g;
       if (p.out.wide) {
         if constexpr (sizeof(T) == 2) {
@@ -457,8 +490,7 @@ LatentSizes latent_sizes(bool bf16, const LatentPages& c, const SeqBatch& b, int
   const int64_t most = std::max<int64_t>(1, (plan.cap + block - 1) / block);  // shares of a block each
   plan.grid = tiles > goal / most ? goal : tiles * most;
   const auto up = [](size_t n) { return (n + 255) & ~size_t{255}; };
-  const size_t eb = bf16 ? 2 : 4, parts = bf16 ? 2 : 1;
-  z.absorbed = up(static_cast<size_t>(rows) * parts * (c.latent + c.turned) * eb);
+  z.absorbed = up(static_cast<size_t>(rows) * query_width(bf16, c.latent, c.turned) * (bf16 ? 2 : 4));
   z.shares = up(static_cast<size_t>(plan.grid) * sizeof(LatentShare));
   z.parts = up(static_cast<size_t>(rows) * sizeof(RowParts));
   z.slots = up(static_cast<size_t>(plan.grid) * plan.rows * (c.latent + 2) * sizeof(float));

@@ -18,7 +18,6 @@ using namespace dev;
 // needs two on every SIMD, and where rows are few they are had by halves of the channels (both form the scores).
 template <typename T, int kWide, int kWaves, int kHalves>
 struct LatentShape {
-  static constexpr int kParts = sizeof(T) == 2 ? 2 : 1;         // summands of an absorbed query
   static constexpr int kVec = Elem<T>::kVec;
   static constexpr int kMostTurned = 64;
   static constexpr int kBlock = latent_block(sizeof(T) == 2);   // positions of an LDS block: two steps of a wave
@@ -30,7 +29,9 @@ struct LatentShape {
   static constexpr int kRing = kBlockBytes * 4 <= 110 * 1024 ? 4 : kBlockBytes * 3 <= 150 * 1024 ? 3 : 2;
   static constexpr int kIds = 1024;
   static constexpr int kFrags = (kWide + kMostTurned) / (4 * kVec), kTiles = kWide / 16 / kHalves;
-  typedef AttendCore<T, kFrags, kTiles, 1, kParts, kRow, kRow> Core;
+  // bf16 queries in the latents' space have a second summand
+  static constexpr int kLow = sizeof(T) == 2 ? kWide / (4 * kVec) : 0;
+  typedef AttendCore<T, kFrags, kTiles, 1, kLow, kRow, kRow> Core;
   static constexpr int kLds = kRing * kBlockBytes + kIds * 4;
 };
 
@@ -79,21 +80,11 @@ __global__ __launch_bounds__(64 * kWaves) void latent_attend_kernel(LatentAttend
     const int64_t low = held + row0 / p.heads;
     lowest = low < -1 ? -1 : (low >= seen ? static_cast<int>(seen) - 1 : static_cast<int>(low));
   }
+  int my_row = wr * 16 + lr;
+  my_row = row0 + (my_row < tile_rows ? my_row : tile_rows - 1);
   {
-    int row = wr * 16 + lr;
-    row = row0 + (row < tile_rows ? row : tile_rows - 1);
-    const int64_t at = held + row / p.heads;
+    const int64_t at = held + my_row / p.heads;
     core.limit[0] = at < 0 ? -1 : (at >= len ? static_cast<int>(len) - 1 : static_cast<int>(at));
-    const T* q = reinterpret_cast<const T*>(p.absorbed) + (begin * p.heads + row) * (S::kParts * width);
-#pragma unroll
-    for (int i = 0; i < S::kParts; ++i)
-#pragma unroll
-      for (int f = 0; f < S::kFrags; ++f) {
-        union { u32x4 u; typename Core::Frag v; } x;
-        x.u = u32x4{0, 0, 0, 0};
-        if (works && 4 * kVec * f < width) x.u = *reinterpret_cast<const u32x4*>(q + i * width + 4 * kVec * f + kVec * g);
-        core.q[0][i][f] = x.v;
-      }
   }
 
   if (first < last) {
@@ -146,8 +137,43 @@ __global__ __launch_bounds__(64 * kWaves) void latent_attend_kernel(LatentAttend
     const auto covered = [&](int block) {
       return (((static_cast<int64_t>(block) + 1) * S::kBlock - 1) >> lg) < static_cast<int64_t>(window) + S::kIds;
     };
+    // The tile's queries come by way of the ring's end, 16 bytes a lane of every row once: the waves that share a row
+    // and rows' pieces in memory order would fetch it many times.  The blocks that fit in front of them are on their
+    // way meanwhile.
+    const int line = query_width(sizeof(T) == 2, p.cache.latent, p.cache.turned), query_pieces = line / kVec | 1;
+    const int query_bytes = tile_rows * query_pieces * 16;
+    char* queries = smem + S::kRing * S::kBlockBytes - ((query_bytes + 1023) & ~1023);
+    const int early = static_cast<int>(queries - smem) / S::kBlockBytes < kAhead
+                          ? static_cast<int>(queries - smem) / S::kBlockBytes : kAhead;
+    const char* from = p.absorbed + (begin * p.heads + row0) * (line * static_cast<int64_t>(sizeof(T)));
+    for (int i = wave * 64; i < tile_rows * query_pieces; i += 64 * kWaves) {
+      const int row = (i + lane) / query_pieces, piece = i + lane - row * query_pieces;
+      if (row < tile_rows && piece < line / kVec) copy16(from + (row * line + kVec * piece) * sizeof(T), queries + 16 * i);
+    }
+    for (int i = 0; i < early; ++i) fetch(first + i < last ? first + i : last - 1, i);
+    if (early == kAhead) {
+      wait_copies<kAhead * S::Copies::kMine>();
+    } else {
+      wait_copies<0>();
+    }
+    lds_barrier();
+    const T* q = reinterpret_cast<const T*>(queries) + (my_row - row0) * query_pieces * kVec;
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) fetch(first + i < last ? first + i : last - 1, i);
+    for (int f = 0; f < S::kFrags; ++f) {
+      union { u32x4 u; typename Core::Frag v; } x, y;
+      x.u = y.u = u32x4{0, 0, 0, 0};
+      if (4 * kVec * f < width) x.u = *reinterpret_cast<const u32x4*>(q + 4 * kVec * f + kVec * g);
+      core.q[0][f] = x.v;
+      if (f < S::kLow) {
+        if (4 * kVec * f < p.cache.latent) y.u = *reinterpret_cast<const u32x4*>(q + width + 4 * kVec * f + kVec * g);
+        core.low[0][f < S::kLow ? f : 0] = y.v;
+      }
+    }
+    if (early < kAhead) {
+      lds_barrier();
+      for (int i = early; i < kAhead; ++i) fetch(first + i < last ? first + i : last - 1, i);
+    }
+    const float scale = fabsf(p.scale);
     int ring = 0;
     for (int block = first; block < last; ++block) {
       wait_copies<(kAhead - 1) * S::Copies::kMine>();
@@ -171,9 +197,9 @@ __global__ __launch_bounds__(64 * kWaves) void latent_attend_kernel(LatentAttend
           const T* at = rows + st * kStep * S::kRow;
           const int bits = holes >> (st * (kStep / 16));
           if (careful) {
-            core.template step<true>(at, at + wc * (kWide / kHalves), 1.f, pos + st * kStep, bits, lane);
+            core.template step<true>(at, at + wc * (kWide / kHalves), scale, pos + st * kStep, bits, lane);
           } else {
-            core.template step<false>(at, at + wc * (kWide / kHalves), 1.f, pos + st * kStep, bits, lane);
+            core.template step<false>(at, at + wc * (kWide / kHalves), scale, pos + st * kStep, bits, lane);
           }
         }
       }
@@ -228,6 +254,8 @@ template <typename T, int kWide, int kWaves, int kHalves>
 hipError_t launch_latent_shape(const LatentAttendParams& p, hipStream_t stream) {
   typedef LatentShape<T, kWide, kWaves, kHalves> S;
   static_assert((kHalves == 1 ? 64 : 32) * (kWide + 4) * 4 <= S::kRing * S::kBlockBytes, "the steps' join fits the ring");
+  static_assert((kWaves * 16 / (kHalves == 2 ? 2 : 1)) * (((S::kLow > 0 ? 2 : 1) * kWide + 64) / S::kVec + 1) * 16 + 1024 <=
+                    S::kRing * S::kBlockBytes, "the queries fit the ring");
   static_assert(S::kTiles % 4 == 0, "value tiles are read by fours");
   hipLaunchKernelGGL((latent_attend_kernel<T, kWide, kWaves, kHalves>), dim3(static_cast<unsigned>(p.plan.grid)),
                      dim3(64 * kWaves), S::kLds, stream, p);

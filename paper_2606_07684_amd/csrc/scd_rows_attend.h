@@ -27,7 +27,7 @@ struct RowsShape {
   static constexpr int kRing = kBlockBytes * 3 <= 80 * 1024 ? 3 : kBlockBytes * 2 <= 80 * 1024 ? 2 :
                                kBlockBytes * 3 <= 156 * 1024 ? 3 : 2;
   static constexpr int kMine = KeyCopies::kMine + ValueCopies::kMine;
-  typedef AttendCore<T, kKey / (4 * kVec), kValue / 16, NT, 1, kKeyPieces * kVec, kValuePieces * kVec> Core;
+  typedef AttendCore<T, kKey / (4 * kVec), kValue / 16, NT, 0, kKeyPieces * kVec, kValuePieces * kVec> Core;
 };
 
 // Rows that do not start on 16 bytes, element by element.
@@ -121,7 +121,7 @@ __global__ __launch_bounds__(256, 2) void rows_attend_kernel(RowsAttendParams p)
         // a negative scale is its magnitude and queries of the other sign
         if (p.scale < 0.f) x.u ^= sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
       }
-      core.q[n][0][f] = x.v;
+      core.q[n][f] = x.v;
     }
   }
 
