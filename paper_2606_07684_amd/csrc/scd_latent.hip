@@ -505,7 +505,7 @@ static void query_as(const LatentAttendParams& p, hipStream_t stream) {
 template <typename T>
 static hipError_t attend_as(const LatentAttendParams& p, hipStream_t stream) {
   const int64_t rows = p.batch.n_tokens * p.heads;
-  if (rows <= 256) {
+  if (rows <= 1024) {
     query_as<T, 1>(p, stream);
   } else {
     query_as<T, 4>(p, stream);

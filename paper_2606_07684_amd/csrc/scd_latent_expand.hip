@@ -19,17 +19,48 @@ __device__ inline f32x16 mma32(const f32x4& a, const f32x4& b, f32x16 c) {
   return c;
 }
 
+// 16 bytes of a row, element by element where it does not start on 16 bytes.
+__device__ inline void put(uint16_t* out, bool wide, const u32x4& x) {
+  if (wide) {
+    *reinterpret_cast<u32x4*>(out) = x;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) out[e] = static_cast<uint16_t>(x[e >> 1] >> (16 * (e & 1)));
+  }
+}
+__device__ inline void put(float* out, bool wide, const u32x4& x) {
+  if (wide) {
+    *reinterpret_cast<u32x4*>(out) = x;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) out[e] = __uint_as_float(x[e]);
+  }
+}
+
+template <typename T, int kWide>
+struct ExpandShape {
+  static constexpr int kVec = Elem<T>::kVec, kRows = sizeof(T) == 2 && kWide <= 256 ? 64 : 32;
+  static constexpr int kBuffers = sizeof(T) == 2 || kWide <= 256 ? 2 : 1;
+  static constexpr int kPieces = (kWide + 64) / kVec + 1;  // of an LDS row, odd
+  typedef dev::Copies<kRows, kPieces> Copies;
+  // a wave's results on their way out: 32 channels a row, and 16 bytes that keep rows off each other's banks
+  static constexpr int kOutRow = 32 * sizeof(T) + 16, kOutBytes = kRows * kOutRow;
+  static constexpr int kTiles = 8;                         // whose rows' places are looked up at once
+  static constexpr int kLds = kBuffers * Copies::kBytes + 4 * kOutBytes;
+};
+
 template <typename T, int kWide>
 __global__ __launch_bounds__(256) void latent_expand_kernel(LatentExpandParams p, int64_t tiles) {
-  constexpr int kVec = Elem<T>::kVec, kRows = sizeof(T) == 2 ? 64 : 32, kSub = kRows / 32;
-  constexpr int kPieces = (kWide + 64) / kVec + 1, kRow = kPieces * kVec;
-  constexpr int kFrags = kWide / (2 * kVec), kFixed = (kWide == 128 ? 32 : kWide / 2) / (2 * kVec);
+  typedef ExpandShape<T, kWide> S;
+  constexpr int kVec = S::kVec, kRows = S::kRows, kSub = kRows / 32, kRow = S::kPieces * kVec;
+  constexpr int kFrags = kWide / (2 * kVec), kSure = (kWide == 64 ? 32 : kWide / 2) / (2 * kVec);
   typedef typename Elem<T>::Frag Frag;
   extern __shared__ __attribute__((aligned(16))) char smem[];
-  __shared__ int64_t places[3][kRows];  // byte of a row in the pages, -1: a hole, -2: no such row
+  __shared__ int64_t places[S::kTiles][kRows];  // byte of a row in the pages, -1: a hole, -2: no such row
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, col = lane & 31;
-  const int latent = p.cache.latent, width = latent + p.cache.turned, frags = latent / (2 * kVec);
+  const int latent = p.cache.latent, width = latent + p.cache.turned;
+  char* const mine = smem + S::kBuffers * S::Copies::kBytes + wave * S::kOutBytes;
 
   // the wave's 32 channels: of a head's keys, or of its values
   const int per_head = (p.plain + p.value) / 32;
@@ -45,111 +76,117 @@ __global__ __launch_bounds__(256) void latent_expand_kernel(LatentExpandParams p
     const T* at = reinterpret_cast<const T*>(values ? p.w_v : p.w_k) +
                   (static_cast<int64_t>(head) * (values ? p.value : p.plain) + c0 + row_of_lds(col)) * latent + kVec * half;
 #pragma unroll
-    for (int f = 0; f < kFrags; ++f)
-      if (f < kFixed || f < frags) w[f] = *reinterpret_cast<const Frag*>(at + 2 * kVec * f);
+    for (int f = 0; f < kFrags; ++f) {
+      if (f < kSure || 2 * kVec * f < latent) w[f] = *reinterpret_cast<const Frag*>(at + 2 * kVec * f);
+    }
   }
   const Rows& rows = values ? p.v : p.k;
 
-  const auto resolve = [&](int64_t tile, int64_t* to) {
-    if (tid >= kRows) return;
-    const int64_t t = tile * kRows + tid;
-    int64_t place = -2;
-    if (t < p.batch.n_tokens) {
-      int b = 0;
-      int64_t begin = 0;
-      bool mine = true;
-      if (p.batch.cu != nullptr) {
-        int hi = p.batch.n_seqs - 1;  // the last request that begins at or before t
-        while (b < hi) {
-          const int mid = (b + hi + 1) >> 1;
-          if (p.batch.cu[mid] <= t) b = mid; else hi = mid - 1;
-        }
-        begin = p.batch.cu[b];
-        mine = t < p.batch.cu[p.batch.n_seqs];
+  const auto resolve = [&](int64_t t) -> int64_t {
+    if (t >= p.batch.n_tokens) return -2;
+    int b = 0;
+    int64_t begin = 0;
+    if (p.batch.cu != nullptr) {
+      if (t >= p.batch.cu[p.batch.n_seqs]) return -2;
+      int hi = p.batch.n_seqs - 1;  // the last request that begins at or before t
+      while (b < hi) {
+        const int mid = (b + hi + 1) >> 1;
+        if (p.batch.cu[mid] <= t) b = mid; else hi = mid - 1;
       }
-      if (mine) {
-        const int64_t pos = t - begin + (p.batch.pos0 != nullptr ? p.batch.pos0[b] : 0);
-        const int64_t column = pos >> p.cache.page_log2;
-        place = -1;
-        if (pos >= 0 && column < p.cache.cols) {
-          const int id = p.cache.table[static_cast<int64_t>(b) * p.cache.cols + column];
-          if (id >= 0 && id < p.cache.n_pages)
-            place = ((static_cast<int64_t>(id) << p.cache.page_log2) + (pos & (p.cache.page - 1))) *
-                    (width * static_cast<int64_t>(sizeof(T)));
-        }
-      }
+      begin = p.batch.cu[b];
     }
-    to[tid] = place;
+    const int64_t pos = t - begin + (p.batch.pos0 != nullptr ? p.batch.pos0[b] : 0);
+    const int64_t column = pos >> p.cache.page_log2;
+    if (pos < 0 || column >= p.cache.cols) return -1;
+    const int id = p.cache.table[static_cast<int64_t>(b) * p.cache.cols + column];
+    if (id < 0 || id >= p.cache.n_pages) return -1;
+    return ((static_cast<int64_t>(id) << p.cache.page_log2) + (pos & (p.cache.page - 1))) *
+           (width * static_cast<int64_t>(sizeof(T)));
   };
   const int pieces = width / kVec;
   const auto fetch = [&](const int64_t* from, int buffer) {
-    constexpr int kCopies = (kRows * kPieces + 63) / 64;
-    for (int j = wave; j < kCopies; j += 4) {
-      const int slot = j * 64 + lane, row = slot / kPieces, piece = slot - row * kPieces;
-      if (row < kRows && piece < pieces) {
-        const int64_t place = from[row];
-        copy16(p.cache.pages + (place < 0 ? 0 : place) + 16 * piece, smem + buffer * (kRows * kPieces * 16) + j * 1024);
-      }
+#pragma unroll
+    for (int j = 0; j < S::Copies::kMine; ++j) {
+      const int64_t place = from[S::Copies::row(wave, j, lane)];
+      copy16(p.cache.pages + (place < 0 ? 0 : place) + 16 * S::Copies::piece(wave, j, lane, pieces),
+             smem + buffer * S::Copies::kBytes + S::Copies::index(wave, j) * 1024);
     }
   };
 
-  int64_t tile = blockIdx.y;
-  resolve(tile, places[0]);
-  __syncthreads();
-  fetch(places[0], 0);
-  for (int it = 0; tile < tiles; ++it, tile += gridDim.y) {
-    const int now = it % 3, next = (it + 1) % 3;
-    resolve(tile + gridDim.y, places[next]);
-    wait_copies<0>();
+  constexpr int kPer = 32 / kVec, kAt = 64 / kPer;  // pieces of a result's row, rows of a store
+  const int64_t step = gridDim.y;
+  int it = 0;  // of the buffer
+  for (int64_t tile0 = blockIdx.y; tile0 < tiles; tile0 += S::kTiles * step) {
+    // places of the next kTiles tiles' rows; the last readers are done
     lds_barrier();
-    if (tile + gridDim.y < tiles) fetch(places[next], (it + 1) & 1);
-    if (!works) continue;
-    const T* at = reinterpret_cast<const T*>(smem + (it & 1) * (kRows * kPieces * 16));
-    f32x16 acc[kSub];
-#pragma unroll
-    for (int s = 0; s < kSub; ++s)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) acc[s][i] = 0.f;
-#pragma unroll
-    for (int f = 0; f < kFrags; ++f)
-      if (f < kFixed || f < frags) {
+    for (int i = tid; i < S::kTiles * kRows; i += 256) {
+      const int64_t tile = tile0 + (i / kRows) * step;
+      places[i / kRows][i % kRows] = resolve(tile * kRows + i % kRows);
+    }
+    __syncthreads();
+    fetch(places[0], it);
+    // The first copies have landed when all has; from then on at most the stores may be under way that every
+    // working wave issues, at least, behind a tile's copies.  (Where rows are missing there are fewer, and then the
+    // tiles behind have no rows either.)
+    for (int k = 0; k < S::kTiles && tile0 + k * step < tiles; ++k) {
+      if (S::kBuffers == 2 && k > 0 && works) wait_copies<kRows / kAt>(); else wait_copies<0>();
+      lds_barrier();
+      const int64_t tile = tile0 + k * step;
+      const char* from = smem + it * S::Copies::kBytes;
+      const bool more = k + 1 < S::kTiles && tile + step < tiles;
+      if (S::kBuffers == 2) {
+        it ^= 1;
+        if (more) fetch(places[k + 1], it);
+      }
+      if (works) {
+        const T* at = reinterpret_cast<const T*>(from) + col * kRow + kVec * half;
+        f32x16 acc[kSub];
 #pragma unroll
         for (int s = 0; s < kSub; ++s)
-          acc[s] = mma32(w[f], *reinterpret_cast<const Frag*>(at + (32 * s + col) * kRow + 2 * kVec * f + kVec * half), acc[s]);
-      }
 #pragma unroll
-    for (int s = 0; s < kSub; ++s) {
-      const int64_t place = places[now][32 * s + col];
-      if (place == -2) continue;
-      float x[16];
+          for (int i = 0; i < 16; ++i) acc[s][i] = 0.f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x[i] = place < 0 ? 0.f : acc[s][i];
-      T* out = reinterpret_cast<T*>(rows.data) + (tile * kRows + 32 * s + col) * rows.token + head * rows.head + c0 + 16 * half;
-      store8(out, rows.wide, x);
-      store8(out + 8, rows.wide, x + 8);
-    }
-    if (!values && c0 == 0) {
-      // the shared key behind this head's own channels
-      const int per_row = p.cache.turned / kVec;
-      for (int i = lane; i < kRows * per_row; i += 64) {
-        const int row = i / per_row, piece = i - row * per_row;
-        const int64_t place = places[now][row];
-        if (place == -2) continue;
-        uint4 x = *reinterpret_cast<const uint4*>(at + row * kRow + latent + kVec * piece);
-        if (place < 0) x = make_uint4(0, 0, 0, 0);
-        T* out = reinterpret_cast<T*>(rows.data) + (tile * kRows + row) * rows.token + head * rows.head + p.plain + kVec * piece;
-        if (rows.wide) {
-          *reinterpret_cast<uint4*>(out) = x;
-        } else {
-          const uint32_t bits[4] = {x.x, x.y, x.z, x.w};
-          for (int e = 0; e < kVec; ++e) {
-            if constexpr (sizeof(T) == 2) {
-              out[e] = static_cast<uint16_t>(bits[e >> 1] >> (16 * (e & 1)));
-            } else {
-              out[e] = __uint_as_float(bits[e]);
-            }
+        for (int f = 0; f < kFrags; ++f)
+          if (f < kSure || 2 * kVec * f < latent) {  // behind the latent lies the shared key
+#pragma unroll
+            for (int s = 0; s < kSub; ++s)
+              acc[s] = mma32(w[f], *reinterpret_cast<const Frag*>(at + 32 * s * kRow + 2 * kVec * f), acc[s]);
+          }
+        // out through LDS: whole runs of a row's 32 channels at a time
+#pragma unroll
+        for (int s = 0; s < kSub; ++s) {
+          const bool hole = places[k][32 * s + col] < 0;
+          float x[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x[i] = hole ? 0.f : acc[s][i];
+          T* to = reinterpret_cast<T*>(mine + (32 * s + col) * S::kOutRow) + 16 * half;
+          store8(to, true, x);
+          store8(to + 8, true, x + 8);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int j = 0; j < kRows / kAt; ++j) {
+          const int row = j * kAt + lane / kPer, piece = lane % kPer;
+          const u32x4 x = *reinterpret_cast<const u32x4*>(mine + row * S::kOutRow + 16 * piece);
+          T* out = reinterpret_cast<T*>(rows.data) + (tile * kRows + row) * rows.token + head * rows.head + c0 + kVec * piece;
+          if (places[k][row] != -2) put(out, rows.wide, x);
+        }
+        if (!values && c0 == 0) {
+          // the shared key behind this head's own channels
+          const int per_row = p.cache.turned / kVec;
+          for (int i = lane; i < kRows * per_row; i += 64) {
+            const int row = i / per_row, piece = i - row * per_row;
+            const int64_t place = places[k][row];
+            u32x4 x = *reinterpret_cast<const u32x4*>(from + row * (kRow * sizeof(T)) + (latent + kVec * piece) * sizeof(T));
+            if (place < 0) x = u32x4{0, 0, 0, 0};
+            T* out = reinterpret_cast<T*>(rows.data) + (tile * kRows + row) * rows.token + head * rows.head + p.plain + kVec * piece;
+            if (place != -2) put(out, rows.wide, x);
           }
         }
+      }
+      if (S::kBuffers == 1) {
+        lds_barrier();  // the only buffer is read
+        if (more) fetch(places[k + 1], 0);
       }
     }
   }
@@ -157,16 +194,18 @@ __global__ __launch_bounds__(256) void latent_expand_kernel(LatentExpandParams p
 
 template <typename T, int kWide>
 static hipError_t expand_as(const LatentExpandParams& p, hipStream_t stream) {
-  constexpr int kRows = sizeof(T) == 2 ? 64 : 32, kPieces = (kWide + 64) / Elem<T>::kVec + 1;
-  const int64_t tiles = (p.batch.n_tokens + kRows - 1) / kRows;
+  typedef ExpandShape<T, kWide> S;
+  static_assert(S::kLds + S::kTiles * S::kRows * 8 <= 160 * 1024, "LDS of a CU");
+  const int64_t tiles = (p.batch.n_tokens + S::kRows - 1) / S::kRows;
   const int x = (p.heads * ((p.plain + p.value) / 32) + 3) / 4;
   const int64_t y = std::min<int64_t>(tiles, std::min<int64_t>(65535, std::max(1, 1024 / x)));
-  hipLaunchKernelGGL((latent_expand_kernel<T, kWide>), dim3(x, static_cast<unsigned>(y)), dim3(256),
-                     2 * kRows * kPieces * 16, stream, p, tiles);
+  hipLaunchKernelGGL((latent_expand_kernel<T, kWide>), dim3(x, static_cast<unsigned>(y)), dim3(256), S::kLds, stream, p,
+                     tiles);
   return hipGetLastError();
 }
 
 hipError_t launch_latent_expand(bool bf16, const LatentExpandParams& p, hipStream_t stream) {
+  if (p.cache.latent <= 64) return bf16 ? expand_as<uint16_t, 64>(p, stream) : expand_as<float, 64>(p, stream);
   if (p.cache.latent <= 128) return bf16 ? expand_as<uint16_t, 128>(p, stream) : expand_as<float, 128>(p, stream);
   if (p.cache.latent <= 256) return bf16 ? expand_as<uint16_t, 256>(p, stream) : expand_as<float, 256>(p, stream);
   return bf16 ? expand_as<uint16_t, 512>(p, stream) : expand_as<float, 512>(p, stream);

@@ -300,6 +300,24 @@ def test_expand(dtype, shape, lens, pos0, how):
     assert np.array_equal(f64(k[:-2, :, plain:]), want[0][..., plain:])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("r", [32, 64, 96, 160, 256, 384])
+def test_expand_keeps_rows_and_channels_apart(dtype, r):
+    """A key or a latent that is not finite reaches its own row only, and a key no product."""
+    c = Case(dtype, [70], [0], 2, 64, 32, r, 32, 16)
+    k, v = (torch.empty(70, 2, d, dtype=DT[dtype], device="cuda") for d in (96, 32))
+    scd.scd_latent_expand(c.cache, c.batch, c.w_k, c.w_v, k, v)
+    clean = k.clone(), v.clone()
+    c.pages[c.table[0][1], 3, r + 5] = float("nan")
+    c.pages[c.table[0][2], 4, 7] = float("inf")
+    scd.scd_latent_expand(c.cache, c.batch, c.w_k, c.w_v, k, v)
+    assert torch.isnan(k[19, :, 69]).all()
+    k[19, :, 69] = clean[0][19, :, 69]
+    assert not torch.isfinite(k[36, :, :64]).any() and not torch.isfinite(v[36]).any()
+    k[36], v[36] = clean[0][36], clean[1][36]
+    assert torch.equal(k, clean[0]) and torch.equal(v, clean[1])
+
+
 # ---- together ----------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_prompt_then_tokens(dtype):
