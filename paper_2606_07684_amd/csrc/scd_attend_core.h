@@ -62,6 +62,15 @@ __device__ inline void read_values4(uint32_t at, s16x4 (&h)[8]) {
       : "memory");
 }
 
+// Between matrix instructions and, behind a branch, the first use of their results: the compiler inserts the wait
+// states that such a use needs within a block, but was seen to leave them out across one (the last of 16 results
+// was then read a few cycles before it was written).
+__device__ inline void settle() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_nop 15\n\ts_nop 3" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // Whether one of the 16-byte piece's values is not finite.
 __device__ inline bool odd_piece(const uint16_t* p) {
   const uint4 v = *reinterpret_cast<const uint4*>(p);

@@ -455,6 +455,7 @@ __global__ __launch_bounds__(256) void latent_out_kernel(LatentAttendParams p, i
             acc = mma(a[j], *reinterpret_cast<const Frag*>(&rows[i][lr][f + 4 * kVec * j + kVec * g]), acc);
         }
     }
+    settle();
     const int64_t t = t0 + lr;
     if (lr < tokens && t < p.batch.n_tokens && t < stop) {
       T* out = reinterpret_cast<T*>(p.out.data) + t * p.out.token + h * p.out.head + c0 + 4 * g;

@@ -206,6 +206,7 @@ __global__ __launch_bounds__(64 * kWaves) void latent_attend_kernel(LatentAttend
       ring = ring + 1 == S::kRing ? 0 : ring + 1;
     }
     wait_copies<0>();
+    settle();
   }
 
   // what the two steps' waves have becomes one through LDS, in which no copy is under way any more

@@ -53,10 +53,13 @@ template <typename T, int kWide>
 __global__ __launch_bounds__(256) void latent_expand_kernel(LatentExpandParams p, int64_t tiles) {
   typedef ExpandShape<T, kWide> S;
   constexpr int kVec = S::kVec, kRows = S::kRows, kSub = kRows / 32, kRow = S::kPieces * kVec;
-  constexpr int kFrags = kWide / (2 * kVec), kSure = (kWide == 64 ? 32 : kWide / 2) / (2 * kVec);
+  constexpr int kFrags = kWide / (2 * kVec);
   typedef typename Elem<T>::Frag Frag;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   __shared__ int64_t places[S::kTiles][kRows];  // byte of a row in the pages, -1: a hole, -2: no such row
+  __shared__ int partly[S::kTiles];             // whether some of a tile's rows have no place
+  constexpr int kStaged = 256;                  // requests whose bounds are kept in LDS
+  __shared__ int bounds[kStaged + 1], starts[kStaged];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, col = lane & 31;
   const int latent = p.cache.latent, width = latent + p.cache.turned;
@@ -77,25 +80,40 @@ __global__ __launch_bounds__(256) void latent_expand_kernel(LatentExpandParams p
                   (static_cast<int64_t>(head) * (values ? p.value : p.plain) + c0 + row_of_lds(col)) * latent + kVec * half;
 #pragma unroll
     for (int f = 0; f < kFrags; ++f) {
-      if (f < kSure || 2 * kVec * f < latent) w[f] = *reinterpret_cast<const Frag*>(at + 2 * kVec * f);
+      union { u32x4 u; Frag v; } x;
+      x.u = u32x4{0, 0, 0, 0};  // the pieces that lie there are the latent's last one again
+      if (2 * kVec * f < latent) x.u = *reinterpret_cast<const u32x4*>(at + 2 * kVec * f);
+      w[f] = x.v;
     }
   }
   const Rows& rows = values ? p.v : p.k;
 
+  const bool staged = p.batch.n_seqs <= kStaged;
+  if (staged) {
+    for (int b = tid; b <= p.batch.n_seqs; b += 256) {
+      bounds[b] = p.batch.cu != nullptr ? p.batch.cu[b] : (b == 0 ? 0 : 0x7fffffff);
+      if (b < p.batch.n_seqs) starts[b] = p.batch.pos0 != nullptr ? p.batch.pos0[b] : 0;
+    }
+  }
   const auto resolve = [&](int64_t t) -> int64_t {
     if (t >= p.batch.n_tokens) return -2;
-    int b = 0;
-    int64_t begin = 0;
-    if (p.batch.cu != nullptr) {
+    int b = 0, hi = p.batch.n_seqs - 1;  // the last request that begins at or before t
+    int64_t pos;
+    if (staged) {
+      if (t >= bounds[p.batch.n_seqs]) return -2;
+      while (b < hi) {
+        const int mid = (b + hi + 1) >> 1;
+        if (bounds[mid] <= t) b = mid; else hi = mid - 1;
+      }
+      pos = t - bounds[b] + starts[b];
+    } else {
       if (t >= p.batch.cu[p.batch.n_seqs]) return -2;
-      int hi = p.batch.n_seqs - 1;  // the last request that begins at or before t
       while (b < hi) {
         const int mid = (b + hi + 1) >> 1;
         if (p.batch.cu[mid] <= t) b = mid; else hi = mid - 1;
       }
-      begin = p.batch.cu[b];
+      pos = t - p.batch.cu[b] + (p.batch.pos0 != nullptr ? p.batch.pos0[b] : 0);
     }
-    const int64_t pos = t - begin + (p.batch.pos0 != nullptr ? p.batch.pos0[b] : 0);
     const int64_t column = pos >> p.cache.page_log2;
     if (pos < 0 || column >= p.cache.cols) return -1;
     const int id = p.cache.table[static_cast<int64_t>(b) * p.cache.cols + column];
@@ -103,25 +121,56 @@ __global__ __launch_bounds__(256) void latent_expand_kernel(LatentExpandParams p
     return ((static_cast<int64_t>(id) << p.cache.page_log2) + (pos & (p.cache.page - 1))) *
            (width * static_cast<int64_t>(sizeof(T)));
   };
-  const int pieces = width / kVec;
+  // a row's latent, its last piece again up to kWide channels, and the shared key behind them
+  const auto source = [&](int piece) {
+    constexpr int kLatent = kWide / kVec;
+    const int mine = latent / kVec, key = p.cache.turned / kVec;
+    return piece < kLatent ? (piece < mine ? piece : mine - 1) : mine + (piece - kLatent < key ? piece - kLatent : key - 1);
+  };
   const auto fetch = [&](const int64_t* from, int buffer) {
 #pragma unroll
     for (int j = 0; j < S::Copies::kMine; ++j) {
       const int64_t place = from[S::Copies::row(wave, j, lane)];
-      copy16(p.cache.pages + (place < 0 ? 0 : place) + 16 * S::Copies::piece(wave, j, lane, pieces),
+      copy16(p.cache.pages + (place < 0 ? 0 : place) + 16 * source(S::Copies::piece(wave, j, lane, S::kPieces)),
              smem + buffer * S::Copies::kBytes + S::Copies::index(wave, j) * 1024);
     }
   };
 
   constexpr int kPer = 32 / kVec, kAt = 64 / kPer;  // pieces of a result's row, rows of a store
+  constexpr int kStores = kRows / kAt;
+  // heads' shared keys: rows of the tile dealt to the waves of the workgroup that has the first channels of a head
+  const int first_group = blockIdx.x * 4;
+  const int key_head = (first_group + per_head - 1) / per_head;  // the only one, as a head has four groups at least
+  const bool keys = p.plain + p.value >= 128 ? key_head * per_head < first_group + 4 && key_head < p.heads : false;
+  const int key_pieces = p.cache.turned / kVec;
+  // where a lane's pieces of a tile go, from its first row's channels on
+  const bool near = rows.token < (int64_t{1} << 23);  // a tile's rows lie within 32 bits
+  uint32_t out_at[kStores];
+#pragma unroll
+  for (int j = 0; j < kStores; ++j)
+    out_at[j] = static_cast<uint32_t>((j * kAt + lane / kPer) * rows.token + kVec * (lane % kPer)) * sizeof(T);
+  char* const out_first = rows.data + (static_cast<int64_t>(head) * rows.head + c0) * sizeof(T);
+
+  // row `row` of a tile's shared keys, behind every head's own channels
+  const auto put_key = [&](int64_t tile, int h, int row, int piece, const char* from, int64_t place) {
+    if (place == -2) return;
+    u32x4 x = *reinterpret_cast<const u32x4*>(from + (row * kRow + kWide + kVec * piece) * sizeof(T));
+    if (place < 0) x = u32x4{0, 0, 0, 0};
+    put(reinterpret_cast<T*>(p.k.data) + (tile * kRows + row) * p.k.token + h * p.k.head + p.plain + kVec * piece, p.k.wide, x);
+  };
+
   const int64_t step = gridDim.y;
   int it = 0;  // of the buffer
   for (int64_t tile0 = blockIdx.y; tile0 < tiles; tile0 += S::kTiles * step) {
     // places of the next kTiles tiles' rows; the last readers are done
-    lds_barrier();
+    __syncthreads();
+    if (tid < S::kTiles) partly[tid] = 0;
+    __syncthreads();
     for (int i = tid; i < S::kTiles * kRows; i += 256) {
       const int64_t tile = tile0 + (i / kRows) * step;
-      places[i / kRows][i % kRows] = resolve(tile * kRows + i % kRows);
+      const int64_t place = resolve(tile * kRows + i % kRows);
+      places[i / kRows][i % kRows] = place;
+      if (place < 0) partly[i / kRows] = 1;
     }
     __syncthreads();
     fetch(places[0], it);
@@ -129,11 +178,12 @@ __global__ __launch_bounds__(256) void latent_expand_kernel(LatentExpandParams p
     // working wave issues, at least, behind a tile's copies.  (Where rows are missing there are fewer, and then the
     // tiles behind have no rows either.)
     for (int k = 0; k < S::kTiles && tile0 + k * step < tiles; ++k) {
-      if (S::kBuffers == 2 && k > 0 && works) wait_copies<kRows / kAt>(); else wait_copies<0>();
+      if (S::kBuffers == 2 && k > 0 && works) wait_copies<kStores>(); else wait_copies<0>();
       lds_barrier();
       const int64_t tile = tile0 + k * step;
       const char* from = smem + it * S::Copies::kBytes;
       const bool more = k + 1 < S::kTiles && tile + step < tiles;
+      const bool whole = uniform(partly[k]) == 0;
       if (S::kBuffers == 2) {
         it ^= 1;
         if (more) fetch(places[k + 1], it);
@@ -147,41 +197,51 @@ __global__ __launch_bounds__(256) void latent_expand_kernel(LatentExpandParams p
           for (int i = 0; i < 16; ++i) acc[s][i] = 0.f;
 #pragma unroll
         for (int f = 0; f < kFrags; ++f)
-          if (f < kSure || 2 * kVec * f < latent) {  // behind the latent lies the shared key
 #pragma unroll
-            for (int s = 0; s < kSub; ++s)
-              acc[s] = mma32(w[f], *reinterpret_cast<const Frag*>(at + 32 * s * kRow + 2 * kVec * f), acc[s]);
-          }
+          for (int s = 0; s < kSub; ++s)
+            acc[s] = mma32(w[f], *reinterpret_cast<const Frag*>(at + 32 * s * kRow + 2 * kVec * f), acc[s]);
+        settle();
         // out through LDS: whole runs of a row's 32 channels at a time
 #pragma unroll
         for (int s = 0; s < kSub; ++s) {
-          const bool hole = places[k][32 * s + col] < 0;
           float x[16];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) x[i] = hole ? 0.f : acc[s][i];
+          for (int i = 0; i < 16; ++i) x[i] = acc[s][i];
+          if (!whole && places[k][32 * s + col] < 0) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] = 0.f;
+          }
           T* to = reinterpret_cast<T*>(mine + (32 * s + col) * S::kOutRow) + 16 * half;
           store8(to, true, x);
           store8(to + 8, true, x + 8);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        const char* piece = mine + (lane / kPer) * S::kOutRow + 16 * (lane % kPer);
+        u32x4 x[kStores];
 #pragma unroll
-        for (int j = 0; j < kRows / kAt; ++j) {
-          const int row = j * kAt + lane / kPer, piece = lane % kPer;
-          const u32x4 x = *reinterpret_cast<const u32x4*>(mine + row * S::kOutRow + 16 * piece);
-          T* out = reinterpret_cast<T*>(rows.data) + (tile * kRows + row) * rows.token + head * rows.head + c0 + kVec * piece;
-          if (places[k][row] != -2) put(out, rows.wide, x);
-        }
-        if (!values && c0 == 0) {
-          // the shared key behind this head's own channels
-          const int per_row = p.cache.turned / kVec;
-          for (int i = lane; i < kRows * per_row; i += 64) {
-            const int row = i / per_row, piece = i - row * per_row;
-            const int64_t place = places[k][row];
-            u32x4 x = *reinterpret_cast<const u32x4*>(from + row * (kRow * sizeof(T)) + (latent + kVec * piece) * sizeof(T));
-            if (place < 0) x = u32x4{0, 0, 0, 0};
-            T* out = reinterpret_cast<T*>(rows.data) + (tile * kRows + row) * rows.token + head * rows.head + p.plain + kVec * piece;
-            if (place != -2) put(out, rows.wide, x);
+        for (int j = 0; j < kStores; ++j) x[j] = *reinterpret_cast<const u32x4*>(piece + j * kAt * S::kOutRow);
+        char* out = out_first + tile * kRows * rows.token * static_cast<int64_t>(sizeof(T));
+        if (whole && rows.wide && near) {
+#pragma unroll
+          for (int j = 0; j < kStores; ++j) *reinterpret_cast<u32x4*>(out + out_at[j]) = x[j];
+        } else {
+#pragma unroll
+          for (int j = 0; j < kStores; ++j) {
+            const int row = j * kAt + lane / kPer;
+            T* to = reinterpret_cast<T*>(out) + row * rows.token + kVec * (lane % kPer);
+            if (places[k][row] != -2) put(to, rows.wide, x[j]);
           }
+        }
+      }
+      if (keys) {
+        for (int i = tid; i < kRows * key_pieces; i += 256) {
+          const int row = i / key_pieces, piece = i - row * key_pieces;
+          put_key(tile, key_head, row, piece, from, places[k][row]);
+        }
+      } else if (works && !values && c0 == 0) {
+        for (int i = lane; i < kRows * key_pieces; i += 64) {
+          const int row = i / key_pieces, piece = i - row * key_pieces;
+          put_key(tile, head, row, piece, from, places[k][row]);
         }
       }
       if (S::kBuffers == 1) {

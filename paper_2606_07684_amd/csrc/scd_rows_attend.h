@@ -187,6 +187,7 @@ __global__ __launch_bounds__(256, 2) void rows_attend_kernel(RowsAttendParams p)
     for (; block < last && block < whole; ++block) run(block, IntC<0>{});
     for (; block < last; ++block) run(block, IntC<1>{});
     wait_copies<0>();
+    settle();
   }
 
   constexpr int kLine = kValue + 4;
