@@ -84,13 +84,126 @@ __device__ inline int plan_scan(int x, PlanLds& lds, int tid, int& total) {
   return before + sum - x;
 }
 
+// The same call where no request writes to more than two pages, as in a step of one token or few each: a thread a
+// request, all it knows in registers, four dependent memory accesses in all (lengths, entries, counts, results).
+// False, and nothing done, where some request writes to more.
+struct FewLds {
+  PlanLds scan;
+  int shared, pages[2 * kPlanThreads], writer[2 * kPlanThreads];  // entries of pages that others name too
+  int free[2 * kPlanThreads];
+};
+__device__ inline bool reserve_few(const PagePool& p, const SeqBatch& batch, const PageMoves& m, FewLds& lds, int tid) {
+  // the lowest pages' counts come meanwhile
+  int first[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) first[e] = 4 * tid + e < p.n_pages ? p.refs[4 * tid + e] : 1;
+  if (tid == 0) lds.shared = 0;
+  int lo = 0, n_columns = 0, held = 0;
+  bool wrong = false;
+  if (tid < p.n_seqs) {
+    const Span s = span_of(batch, tid);
+    held = p.held[tid];
+    const int64_t n = s.end - s.begin;
+    if (n > 0) {
+      const int64_t hi = div_up_to(held < 0 ? 0 : held + n + p.page - 1, p.page);
+      lo = held < 0 ? 0 : held / p.page;
+      wrong = held < 0 || hi > p.cols;
+      const int64_t columns = wrong ? 0 : hi - lo;
+      n_columns = columns > 2 ? 3 : static_cast<int>(columns);
+    }
+  }
+  if (__syncthreads_or(n_columns > 2)) return false;
+  const int refused = __syncthreads_count(wrong);
+  if (refused > 0) {
+    if (tid < 4) m.status[tid] = tid == 3 ? refused : 0;
+    return true;
+  }
+  const int64_t row = static_cast<int64_t>(tid) * p.cols + lo;
+  int id[2], refs[2];
+  bool missing[2], left[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) id[e] = e < n_columns ? p.table[row + e] : 0;
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    missing[e] = e < n_columns && (id[e] < 0 || id[e] >= p.n_pages);
+    refs[e] = e < n_columns && !missing[e] ? p.refs[id[e]] : 0;
+    if (refs[e] > 1) {
+      const int at = atomicAdd(&lds.shared, 1);
+      lds.pages[at] = id[e];
+      lds.writer[at] = tid;
+    }
+  }
+  __syncthreads();
+  const int shared = lds.shared;
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    left[e] = false;
+    if (refs[e] > 1) {
+      int writers = 0, last = -1;
+      for (int i = 0; i < shared; ++i)
+        if (lds.pages[i] == id[e]) {
+          ++writers;
+          last = lds.writer[i] > last ? lds.writer[i] : last;
+        }
+      left[e] = tid != last || refs[e] > writers;
+    }
+  }
+  // begun pages that are left are the only ones whose contents move: a request has one at most, its first
+  const bool moved = left[0] && static_cast<int64_t>(lo) * p.page < held;
+  const int taken = (missing[0] || left[0]) + (missing[1] || left[1]);
+  int total;
+  const int before = plan_scan(taken | (moved ? 1 : 0) << 16, lds.scan, tid, total);
+  const int wanted = total & 0xffff, moves = total >> 16;
+  int found = 0;
+  for (int id0 = 0; id0 < p.n_pages && found < wanted; id0 += 4 * kPlanThreads) {
+    const int at0 = id0 + 4 * tid;
+    bool open[4];
+    int n = 0, all;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      open[e] = at0 + e < p.n_pages && (id0 == 0 ? first[e] : p.refs[at0 + e]) <= 0;
+      n += open[e];
+    }
+    int at = found + plan_scan(n, lds.scan, tid, all);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (open[e]) {
+        if (at < 2 * kPlanThreads) lds.free[at] = at0 + e;
+        ++at;
+      }
+    found += all;
+  }
+  if (found < wanted || moves > m.capacity) {
+    if (tid < 4) m.status[tid] = tid == 2 ? std::max(wanted - found, 1) : 0;
+    return true;
+  }
+  __syncthreads();
+  int take = before & 0xffff;
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    if (!missing[e] && !left[e]) continue;
+    const int to = lds.free[take++];
+    p.table[row + e] = to;
+    p.refs[to] = 1;
+    if (left[e]) atomicSub(p.refs + id[e], 1);
+    if (e == 0 && moved) {
+      m.pairs[2 * static_cast<int64_t>(before >> 16)] = id[0];
+      m.pairs[2 * static_cast<int64_t>(before >> 16) + 1] = to;
+    }
+  }
+  if (tid < 4) m.status[tid] = tid == 0 ? moves : 0;
+  return true;
+}
+
 // Pages that the new tokens of every request go to, one workgroup for all.  A missing page is taken, and so
 // is one in place of a page that others name too; where that holds earlier positions its contents are to be
 // moved (a move is listed).  If all that name a page are to write to it, the last of them keeps it.
 __global__ __launch_bounds__(kPlanThreads) void pages_reserve_kernel(PagePool p, SeqBatch batch, PageMoves m, int32_t* ws) {
   __shared__ PlanLds lds;
+  __shared__ FewLds few;
   __shared__ int refused;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (p.n_seqs <= kPlanThreads && reserve_few(p, batch, m, few, tid)) return;
   int32_t* writers = ws;                        // [n_pages] requests that write to a shared page
   int32_t* keeper = writers + p.n_pages;        // [n_pages] the last of them
   int32_t* free = keeper + p.n_pages;           // [n_pages] free pages, lowest first

@@ -11,6 +11,13 @@ namespace dev {
 // below 2^32 work-items.
 constexpr int64_t kMaxGrid = int64_t{1} << 23;
 
+// a / b for a >= 0, b > 0; in 32 bits where both fit, which takes a tenth of the time.
+__device__ inline int64_t div_up_to(int64_t a, int64_t b) {
+  if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+  return a / b;
+}
+__device__ inline int64_t div_ceil(int64_t a, int64_t b) { return div_up_to(a + b - 1, b); }
+
 // Rows of request b, kept inside the batch whatever cu holds.
 struct Span {
   int64_t begin, end;
