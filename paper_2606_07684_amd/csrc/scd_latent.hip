@@ -90,6 +90,17 @@ __device__ inline void put_query(uint16_t* row, int latent, int width, int i, fl
 }
 __device__ inline void put_query(float* row, int, int, int i, float x) { row[i] = x; }
 
+// Sums of the lanes up to each lane.
+__device__ inline int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);  // from 1, 2, 4, 8 lanes before, in rows of 16
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);  // rows 1 and 3: from the row before
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);  // rows 2 and 3: from lane 31
+  return x;
+}
+
 // What every workgroup of the attention takes, by one workgroup beside those of the queries: there it costs
 // nothing, and the attention, whose start is a chain of memory accesses, finds it with one.
 __device__ inline void plan_shares(const LatentAttendParams& p, int block, int tid) {
@@ -128,71 +139,25 @@ __device__ inline void plan_shares(const LatentAttendParams& p, int block, int t
     tx = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
     ty = sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
   };
-  Entry mine = load(tid);
-  const bool one_round = p.batch.n_seqs <= 256;
-  int64_t tiles = mine.tiles, work = static_cast<int64_t>(mine.tiles) * mine.blocks, most = 0;
-  for (int b = 256 + tid; b < p.batch.n_seqs; b += 256) {
-    const Entry e = load(b);
-    tiles += e.tiles;
-    work += static_cast<int64_t>(e.tiles) * e.blocks;
-  }
-  total_of(tiles, work, tiles, work);
-  uint32_t chunk = 0x7fffffff;
-  if (tiles < 2 * kFill) {
-    const int64_t room = share_goal(tiles) - tiles;
-    if (room > 0) chunk = static_cast<uint32_t>(div_ceil(work, room));
-    if (chunk < 1) chunk = 1;
-  }
-  const auto parts_of = [&](const Entry& e) {
+  const auto chunk_of = [](int64_t tiles, int64_t work) {
+    uint32_t chunk = 0x7fffffff;
+    if (tiles < 2 * kFill) {
+      const int64_t room = share_goal(tiles) - tiles;
+      if (room > 0) chunk = static_cast<uint32_t>(div_ceil(work, room));
+      if (chunk < 1) chunk = 1;
+    }
+    return chunk;
+  };
+  const auto parts_of = [](const Entry& e, uint32_t chunk) {
     const uint32_t n = e.blocks;
     return n <= chunk ? 1u : (n + chunk - 1) / chunk;
   };
-  int64_t total = static_cast<int64_t>(mine.tiles) * parts_of(mine);
-  for (int b = 256 + tid; b < p.batch.n_seqs; b += 256) {
-    const Entry e = load(b);
-    total += static_cast<int64_t>(e.tiles) * parts_of(e);
-  }
-  int64_t sum = total;  // of the first round: where a request's shares begin
-  if (one_round) {
-    for (int o = 1; o < 64; o <<= 1) {
-      const int64_t other = __shfl_up(sum, o);
-      if (lane >= o) sum += other;
-    }
-    __syncthreads();
-    if (lane == 63) sums[0][wave] = sum;
-    mine.first = sum - total;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) mine.first += sums[0][w];
-    total = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
-  } else {
-    total_of(total, most, total, most);
-  }
-  total = total < p.plan.grid ? total : p.plan.grid;
-  for (int64_t w = total + tid; w < p.plan.grid; w += 256) p.shares[w].b = -1;
-  int64_t first = 0;
-  for (int b0 = 0; b0 < p.batch.n_seqs; b0 += 256) {
-    int64_t next = total;
-    if (!one_round) {
-      mine = load(b0 + tid);
-      const int64_t n = static_cast<int64_t>(mine.tiles) * parts_of(mine);
-      sum = n;
-      for (int o = 1; o < 64; o <<= 1) {
-        const int64_t other = __shfl_up(sum, o);
-        if (lane >= o) sum += other;
-      }
-      __syncthreads();
-      if (lane == 63) sums[1][wave] = sum;
-      __syncthreads();
-      mine.first = first + sum - n;
-      for (int w = 0; w < wave; ++w) mine.first += sums[1][w];
-      next = first + sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
-    }
-    entries[tid] = mine;
-    __syncthreads();
+  // the workgroups whose shares are [first, next), of the requests b0 .. b0 + count - 1 in `entries`
+  const auto deal = [&](int b0, int count, int64_t first, int64_t next, int total, uint32_t chunk) {
     for (int w = tid; w < total; w += 256) {
-      const int64_t unit = xcd_remap(w, static_cast<int>(total));
+      const int64_t unit = xcd_remap(w, total);
       if (unit < first || unit >= next) continue;
-      int lo = 0, hi = p.batch.n_seqs - b0 < 256 ? p.batch.n_seqs - b0 - 1 : 255;
+      int lo = 0, hi = count - 1;
       while (lo < hi) {  // the last request whose shares begin at or before the unit
         const int mid = (lo + hi + 1) >> 1;
         if (entries[mid].first <= unit) lo = mid; else hi = mid - 1;
@@ -205,16 +170,74 @@ __device__ inline void plan_shares(const LatentAttendParams& p, int block, int t
       out.tiles = e.tiles;
       out.part = static_cast<int>(local / static_cast<uint32_t>(e.tiles));
       out.tile = static_cast<int>(local) - out.part * e.tiles;
-      out.parts = static_cast<int>(parts_of(e));
+      out.parts = static_cast<int>(parts_of(e, chunk));
       out.first = static_cast<int>(e.first) + out.tile;
       out.pad = 0;
       out.begin = e.begin;
       out.held = e.held;
       p.shares[w] = out;
     }
-    first = next;
+  };
+  const auto none = [&](int64_t from) {
+    for (int64_t w = from + tid; w < p.plan.grid; w += 256) p.shares[w].b = -1;
+  };
+  const int64_t most = (p.batch.n_tokens * p.heads / p.plan.rows + p.batch.n_seqs) * ((p.plan.cap + block - 1) >> shift);
+  if (p.batch.n_seqs <= 64 && most < int64_t{1} << 31) {
+    // one wave's lanes hold the requests, sums in 32 bits
+    if (wave == 0) {
+      Entry e = load(lane);
+      const int tiles = __builtin_amdgcn_readlane(wave_scan(e.tiles), 63);
+      const int work = __builtin_amdgcn_readlane(wave_scan(e.tiles * e.blocks), 63);
+      const uint32_t chunk = chunk_of(tiles, work);
+      const int shares = e.tiles * static_cast<int>(parts_of(e, chunk)), sum = wave_scan(shares);
+      e.first = sum - shares;
+      entries[lane] = e;
+      if (lane == 63) {
+        sums[0][0] = sum;
+        sums[0][1] = chunk;
+      }
+    }
     __syncthreads();
+    const int64_t total = sums[0][0] < p.plan.grid ? sums[0][0] : p.plan.grid;
+    deal(0, p.batch.n_seqs, 0, total, static_cast<int>(total), static_cast<uint32_t>(sums[0][1]));
+    none(total);
+    return;
   }
+  int64_t tiles = 0, work = 0, total = 0, rest = 0;
+  for (int b = tid; b < p.batch.n_seqs; b += 256) {
+    const Entry e = load(b);
+    tiles += e.tiles;
+    work += static_cast<int64_t>(e.tiles) * e.blocks;
+  }
+  total_of(tiles, work, tiles, work);
+  const uint32_t chunk = chunk_of(tiles, work);
+  for (int b = tid; b < p.batch.n_seqs; b += 256) {
+    const Entry e = load(b);
+    total += static_cast<int64_t>(e.tiles) * parts_of(e, chunk);
+  }
+  total_of(total, rest, total, rest);
+  total = total < p.plan.grid ? total : p.plan.grid;
+  int64_t first = 0;
+  for (int b0 = 0; b0 < p.batch.n_seqs; b0 += 256) {
+    Entry mine = load(b0 + tid);
+    const int64_t n = static_cast<int64_t>(mine.tiles) * parts_of(mine, chunk);
+    int64_t sum = n;
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t other = __shfl_up(sum, o);
+      if (lane >= o) sum += other;
+    }
+    __syncthreads();  // the last round's readers are done
+    if (lane == 63) sums[1][wave] = sum;
+    __syncthreads();
+    mine.first = first + sum - n;
+    for (int w = 0; w < wave; ++w) mine.first += sums[1][w];
+    const int64_t next = first + sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
+    entries[tid] = mine;
+    __syncthreads();
+    deal(b0, p.batch.n_seqs - b0 < 256 ? p.batch.n_seqs - b0 : 256, first, next, static_cast<int>(total), chunk);
+    first = next;
+  }
+  none(total);
 }
 
 // absorbed_h = [ q_h[:plain] W_k,h | q_h[plain:] ], of the other sign for a negative scale: workgroup (h, a few tokens), eight latent channels a
@@ -226,6 +249,7 @@ __global__ __launch_bounds__(256) void latent_query_kernel(LatentAttendParams p)
   __shared__ float q[kTokens][256 + 64];
   __shared__ __attribute__((aligned(16))) float sums[kTokens * 2048];
   const int tid = threadIdx.x, h = static_cast<int>(blockIdx.x) - 1;
+  if (h >= p.heads) return;
   if (h < 0) {
     if (blockIdx.y == 0) plan_shares(p, latent_block(sizeof(T) == 2), tid);
     return;
@@ -315,14 +339,15 @@ __global__ __launch_bounds__(256) void latent_query_kernel(LatentAttendParams p)
 // of it).  One or two tokens' shares are dealt to the four waves, more tokens are dealt as they are.  The joined
 // rows, as two bf16 summands, are the right operands of the product with W_v,h, whose rows come from memory
 // as they lie.
-template <typename T>
+template <typename T, int kMost>
 __global__ __launch_bounds__(256) void latent_out_kernel(LatentAttendParams p, int tokens) {
-  constexpr int kParts = sizeof(T) == 2 ? 2 : 1, kMost = 512;
+  constexpr int kParts = sizeof(T) == 2 ? 2 : 1, kPairs = kMost / 128;
   constexpr int kVec = Elem<T>::kVec, kRow = kMost + kVec;  // 16-byte pieces of a row: odd
   __shared__ __attribute__((aligned(16))) T rows[kParts][16][kRow];
   __shared__ float halves[4][kMost + 2];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, lr = lane & 15, g = lane >> 4;
   const int h = blockIdx.x, latent = p.cache.latent, line = latent + 2;
+  if (h >= p.heads) return;
   const int64_t t0 = static_cast<int64_t>(blockIdx.y) * tokens;
   // rows behind the last request are left alone: joined like the others (their entries are checked), not stored
   const int32_t stop = p.batch.cu != nullptr ? p.batch.cu[p.batch.n_seqs] : 0x7fffffff;
@@ -337,7 +362,7 @@ __global__ __launch_bounds__(256) void latent_out_kernel(LatentAttendParams p, i
     }
   };
   // shares from, from + by, ... of a token's row: their sum in the lane's channels 2 lane + 128 j
-  const auto join = [&](int64_t t, int from, int by, float2 (&o)[4], float& m, float& l) {
+  const auto join = [&](int64_t t, int from, int by, float2 (&o)[kPairs], float& m, float& l) {
     const RowParts r = p.parts[t * p.heads + h];
     const int64_t last = r.first + static_cast<int64_t>(r.count - 1) * r.step;
     const bool fits = r.first >= 0 && r.step >= 0 && r.row >= 0 && r.row < p.plan.rows && last < p.plan.grid &&
@@ -348,19 +373,19 @@ __global__ __launch_bounds__(256) void latent_out_kernel(LatentAttendParams p, i
     m = -INFINITY;
     l = 0.f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) o[j] = make_float2(0.f, 0.f);
+    for (int j = 0; j < kPairs; ++j) o[j] = make_float2(0.f, 0.f);
     // eight shares at a time, all of their values on the way before the first is used
     for (int s0 = from; s0 < count; s0 += 8 * by) {
-      float2 ml[8], x[8][4];
+      float2 ml[8], x[8][kPairs];
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         const int s = s0 + u * by;
         ml[u] = make_float2(-INFINITY, 0.f);
         if (s < count) ml[u] = *reinterpret_cast<const float2*>(row + s * step);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < kPairs; ++j) {
           x[u][j] = make_float2(0.f, 0.f);
-          if (128 * j < latent && s < count && 2 * lane + 128 * j < latent)
+          if (s < count && 2 * lane + 128 * j < latent)
             x[u][j] = *reinterpret_cast<const float2*>(row + s * step + 2 + 2 * lane + 128 * j);
         }
       }
@@ -371,7 +396,7 @@ __global__ __launch_bounds__(256) void latent_out_kernel(LatentAttendParams p, i
       m = now;
       l *= old;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < kPairs; ++j) {
         o[j].x *= old;
         o[j].y *= old;
       }
@@ -380,7 +405,7 @@ __global__ __launch_bounds__(256) void latent_out_kernel(LatentAttendParams p, i
         const float w = __builtin_amdgcn_exp2f(ml[u].x - base);
         l += w * ml[u].y;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < kPairs; ++j) {
           o[j].x += w * x[u][j].x;
           o[j].y += w * x[u][j].y;
         }
@@ -399,14 +424,14 @@ __global__ __launch_bounds__(256) void latent_out_kernel(LatentAttendParams p, i
   Frag ahead[2][8];
   pieces(16 * wave, 0, ahead[0]);
   pieces(16 * wave + 64, 0, ahead[1]);
-  float2 o[4];
+  float2 o[kPairs];
   float m, l;
   if (tokens <= 2) {
     // the waves of a token (4, or 2 of two tokens) leave their shares' sums in LDS
     const int per = 4 / tokens, t = wave / per;
     join(t0 + t < p.batch.n_tokens ? t0 + t : t0, wave - t * per, per, o, m, l);
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < kPairs; ++j)
       if (2 * lane + 128 * j < latent) *reinterpret_cast<float2*>(&halves[wave][2 + 2 * lane + 128 * j]) = o[j];
     if (lane == 0) *reinterpret_cast<float2*>(&halves[wave][0]) = make_float2(m, l);
     __syncthreads();
@@ -428,7 +453,7 @@ __global__ __launch_bounds__(256) void latent_out_kernel(LatentAttendParams p, i
       join(t0 + t, 0, 1, o, m, l);
       const float by = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
+      for (int j = 0; j < kPairs; ++j)
         if (2 * lane + 128 * j < latent) {
           put(t, 2 * lane + 128 * j, o[j].x * by);
           put(t, 2 * lane + 128 * j + 1, o[j].y * by);
@@ -498,10 +523,18 @@ LatentSizes latent_sizes(bool bf16, const LatentPages& c, const SeqBatch& b, int
   return z;
 }
 
+// From half a megabyte of matrices on, a multiple of the XCDs that workgroups are dealt to: a head's workgroups, one behind
+// another in y, then share one, and its matrix is read into one L2.  Queries of 16 tokens of 32 heads, 2 MB: 8.0 us spread
+// over all XCDs, 6.8 so; of 37 fp32 tokens of 8 heads, 128 KB: 4.8 spread, 6.7 so.
+static unsigned heads_grid(int heads, int64_t matrix_bytes) {
+  return matrix_bytes < int64_t{1} << 19 ? heads : (heads + kNumXcd - 1) / kNumXcd * kNumXcd;
+}
+
 template <typename T, int kTokens>
 static void query_as(const LatentAttendParams& p, hipStream_t stream) {
   const int64_t y = (p.batch.n_tokens + kTokens - 1) / kTokens;
-  hipLaunchKernelGGL((latent_query_kernel<T, kTokens>), dim3(p.heads + 1, static_cast<unsigned>(y)), dim3(256), 0, stream, p);
+  hipLaunchKernelGGL((latent_query_kernel<T, kTokens>), dim3(heads_grid(p.heads + 1, int64_t{p.heads} * p.plain * p.cache.latent * sizeof(T)),
+                                                               static_cast<unsigned>(y)), dim3(256), 0, stream, p);
 }
 template <typename T>
 static hipError_t attend_as(const LatentAttendParams& p, hipStream_t stream) {
@@ -518,7 +551,14 @@ static hipError_t attend_as(const LatentAttendParams& p, hipStream_t stream) {
   // a workgroup a CU while there are so few tokens
   const int tokens = static_cast<int>(std::min<int64_t>(std::max<int64_t>(1, rows / 256), 16));
   const int64_t y = (p.batch.n_tokens + tokens - 1) / tokens;
-  hipLaunchKernelGGL((latent_out_kernel<T>), dim3(p.heads, static_cast<unsigned>(y)), dim3(256), 0, stream, p, tokens);
+  const dim3 grid(heads_grid(p.heads, int64_t{p.heads} * p.value * p.cache.latent * sizeof(T)), static_cast<unsigned>(y));
+  if (p.cache.latent <= 128) {
+    hipLaunchKernelGGL((latent_out_kernel<T, 128>), grid, dim3(256), 0, stream, p, tokens);
+  } else if (p.cache.latent <= 256) {
+    hipLaunchKernelGGL((latent_out_kernel<T, 256>), grid, dim3(256), 0, stream, p, tokens);
+  } else {
+    hipLaunchKernelGGL((latent_out_kernel<T, 512>), grid, dim3(256), 0, stream, p, tokens);
+  }
   return hipGetLastError();
 }
 

@@ -9,6 +9,7 @@ namespace {
 
 using namespace scd;
 
+constexpr int64_t kMostWorkgroups = (int64_t{1} << 23) - 1;  // of 512 threads: below 2^32 in a launch
 constexpr double kLog2e = 1.4426950408889634;
 
 scd_status_t check_latent_shape(const scd_latent_cache_t* c) {
@@ -151,6 +152,7 @@ scd_status_t scd_latent_attend(const scd_latent_cache_t* cache, const scd_batch_
   SCD_TRY(check_rows(out, "out", q->n_heads, value_dim, dtype, batch->n_tokens, true));
   if (batch->n_tokens == 0) return ok();
   const LatentSizes z = latent_sizes(dtype == SCD_BF16, pages_of(cache), batch_of(batch), q->n_heads);
+  if (z.plan.grid > kMostWorkgroups) return fail(SCD_ERR_UNSUPPORTED, "the call needs more than 2^23 workgroups");
   SCD_TRY(check_workspace(workspace, workspace_bytes, z.total()));
   LatentAttendParams p{};
   p.cache = pages_of(cache);
@@ -178,6 +180,7 @@ static scd_status_t check_held(const scd_batch_t* batch, const scd_batch_t* held
   SCD_TRY(check_batch(held));
   if (held->n_seqs != batch->n_seqs)
     return fail(SCD_ERR_SHAPE, "held has %d requests, the batch %d", held->n_seqs, batch->n_seqs);
+  if (held->n_tokens > (int64_t{1} << 31) - 128) return fail(SCD_ERR_UNSUPPORTED, "held has more than 2^31 - 128 rows");
   return SCD_OK;
 }
 
@@ -220,6 +223,7 @@ scd_status_t scd_rows_attend(const scd_batch_t* batch, const scd_batch_t* held, 
   p.v = rows_of(v, dtype);
   const RowsSizes z = rows_sizes(dtype == SCD_BF16, rows_wide(p.k, p.v), batch_of(batch), held->n_tokens, q->n_heads,
                                  k->n_heads, value_dim);
+  if (z.plan.grid > kMostWorkgroups) return fail(SCD_ERR_UNSUPPORTED, "the call needs more than 2^23 workgroups");
   SCD_TRY(check_workspace(workspace, workspace_bytes, scd_rows_attend_workspace_bytes(batch, held, dtype, q->n_heads,
                                                                                       k->n_heads, key_dim, value_dim)));
   p.batch = batch_of(batch);

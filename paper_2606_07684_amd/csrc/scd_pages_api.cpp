@@ -37,6 +37,7 @@ scd_status_t check_moves(const scd_moves_t* m, int64_t need) {
 
 scd_status_t check_list(const int32_t* list, int32_t n, const char* name) {
   if (n < 0) return fail(SCD_ERR_SHAPE, "%s has %d entries", name, n);
+  if (n > 1 << 20) return fail(SCD_ERR_UNSUPPORTED, "%s has more than 2^20 entries", name);
   if (n > 0 && list == nullptr) return fail(SCD_ERR_NULL, "%s is NULL", name);
   if (reinterpret_cast<uintptr_t>(list) % 4 != 0) return fail(SCD_ERR_ALIGN, "%s is not aligned to its entries", name);
   return SCD_OK;
