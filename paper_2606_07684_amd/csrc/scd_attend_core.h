@@ -340,8 +340,8 @@ __device__ inline void wait_copies() {
 }
 
 // ---- shares ------------------------------------------------------------------------------------------
-// A request's query rows make tiles, its positions blocks of kBlock.  While there are fewer tiles than twice what
-// fills the chip, every tile's positions are cut into shares of at most `chunk` blocks, so that the shares of all
+// A request's query rows make tiles, its positions blocks of kBlock.  While there are fewer than kWholeTiles tiles,
+// every tile's positions are cut into shares of at most `chunk` blocks, so that the shares of all
 // tiles are no more than the goal:  sum ceil(blocks / chunk) <= sum blocks / chunk + tiles <= goal.
 struct Share {
   Span span;
@@ -404,8 +404,8 @@ __device__ inline bool find_share(const SeqBatch& s, const SharePlan& p, int blo
       t[1] += n * of.blocks(span, b);
     }, total);
     const int64_t tiles = total[0] * p.heads, work = total[1] * p.heads;
-    if (tiles < 2 * kFill) {
-      const int64_t room = share_goal(tiles) - tiles;
+    if (tiles < kWholeTiles) {
+      const int64_t room = share_goal(tiles, p.fill) - tiles;
       chunk = room > 0 ? div_ceil(work, room) : chunk;
       chunk = chunk < least ? least : chunk;
     }

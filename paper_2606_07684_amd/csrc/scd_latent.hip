@@ -139,10 +139,10 @@ __device__ inline void plan_shares(const LatentAttendParams& p, int block, int t
     tx = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
     ty = sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
   };
-  const auto chunk_of = [](int64_t tiles, int64_t work) {
+  const auto chunk_of = [&](int64_t tiles, int64_t work) {
     uint32_t chunk = 0x7fffffff;
-    if (tiles < 2 * kFill) {
-      const int64_t room = share_goal(tiles) - tiles;
+    if (tiles < kWholeTiles) {
+      const int64_t room = share_goal(tiles, p.plan.fill) - tiles;
       if (room > 0) chunk = static_cast<uint32_t>(div_ceil(work, room));
       if (chunk < 1) chunk = 1;
     }
@@ -509,9 +509,10 @@ LatentSizes latent_sizes(bool bf16, const LatentPages& c, const SeqBatch& b, int
   plan.heads = 1;
   plan.per_token = heads;
   plan.cut = 1;
+  plan.fill = 256;  // eight waves and most of a CU's LDS each
   plan.cap = std::min<int64_t>(static_cast<int64_t>(c.cols) * c.page, (int64_t{1} << 31) - 128);
   const int64_t tiles = rows / plan.rows + requests;
-  const int64_t goal = std::max(tiles, share_goal(std::min<int64_t>(tiles, 2 * kFill - 1)));
+  const int64_t goal = std::max(tiles, share_goal(std::min<int64_t>(tiles, kWholeTiles - 1), plan.fill));
   const int block = latent_block(bf16);
   const int64_t most = std::max<int64_t>(1, (plan.cap + block - 1) / block);  // shares of a block each
   plan.grid = tiles > goal / most ? goal : tiles * most;

@@ -1,7 +1,7 @@
 // The dense keys and values of cached latents (gfx950), for prompts: k_h = [W_k,h c | key], v_h = W_v,h c.
 //
 // A wave keeps 32 rows of the heads' matrices in registers for the whole call and takes tiles of cached rows
-// from LDS, so the matrices are read once a workgroup and the latents once for every 128 channels; what is
+// from LDS, so the matrices are read once a workgroup and the latents once for every 256 channels; what is
 // written, heads x (plain + turned + value) channels a row, is 20 times what is read and bounds the call.
 #include <algorithm>
 
@@ -39,18 +39,20 @@ __device__ inline void put(float* out, bool wide, const u32x4& x) {
 
 template <typename T, int kWide>
 struct ExpandShape {
-  static constexpr int kVec = Elem<T>::kVec, kRows = sizeof(T) == 2 && kWide <= 256 ? 64 : 32;
+  static constexpr int kWaves = sizeof(T) == 4 && kWide == 512 ? 4 : 8;  // the latter's matrices are 256 registers
+  static constexpr int kThreads = 64 * kWaves;
+  static constexpr int kVec = Elem<T>::kVec, kRows = 32;
   static constexpr int kBuffers = sizeof(T) == 2 || kWide <= 256 ? 2 : 1;
   static constexpr int kPieces = (kWide + 64) / kVec + 1;  // of an LDS row, odd
-  typedef dev::Copies<kRows, kPieces> Copies;
+  typedef dev::Copies<kRows, kPieces, kWaves> Copies;
   // a wave's results on their way out: 32 channels a row, and 16 bytes that keep rows off each other's banks
   static constexpr int kOutRow = 32 * sizeof(T) + 16, kOutBytes = kRows * kOutRow;
-  static constexpr int kTiles = 8;                         // whose rows' places are looked up at once
-  static constexpr int kLds = kBuffers * Copies::kBytes + 4 * kOutBytes;
+  static constexpr int kTiles = 16;                        // whose rows' places are looked up at once
+  static constexpr int kLds = kBuffers * Copies::kBytes + kWaves * kOutBytes;
 };
 
 template <typename T, int kWide>
-__global__ __launch_bounds__(256) void latent_expand_kernel(LatentExpandParams p, int64_t tiles) {
+__global__ __launch_bounds__((ExpandShape<T, kWide>::kThreads)) void latent_expand_kernel(LatentExpandParams p, int64_t tiles) {
   typedef ExpandShape<T, kWide> S;
   constexpr int kVec = S::kVec, kRows = S::kRows, kSub = kRows / 32, kRow = S::kPieces * kVec;
   constexpr int kFrags = kWide / (2 * kVec);
@@ -67,7 +69,7 @@ __global__ __launch_bounds__(256) void latent_expand_kernel(LatentExpandParams p
 
   // the wave's 32 channels: of a head's keys, or of its values
   const int per_head = (p.plain + p.value) / 32;
-  const int group = blockIdx.x * 4 + wave;
+  const int group = blockIdx.x * S::kWaves + wave;
   const bool works = group < p.heads * per_head;
   const int head = works ? group / per_head : 0;
   int c0 = works ? (group - head * per_head) * 32 : 0;
@@ -90,7 +92,7 @@ __global__ __launch_bounds__(256) void latent_expand_kernel(LatentExpandParams p
 
   const bool staged = p.batch.n_seqs <= kStaged;
   if (staged) {
-    for (int b = tid; b <= p.batch.n_seqs; b += 256) {
+    for (int b = tid; b <= p.batch.n_seqs; b += S::kThreads) {
       bounds[b] = p.batch.cu != nullptr ? p.batch.cu[b] : (b == 0 ? 0 : 0x7fffffff);
       if (b < p.batch.n_seqs) starts[b] = p.batch.pos0 != nullptr ? p.batch.pos0[b] : 0;
     }
@@ -139,9 +141,9 @@ __global__ __launch_bounds__(256) void latent_expand_kernel(LatentExpandParams p
   constexpr int kPer = 32 / kVec, kAt = 64 / kPer;  // pieces of a result's row, rows of a store
   constexpr int kStores = kRows / kAt;
   // heads' shared keys: rows of the tile dealt to the waves of the workgroup that has the first channels of a head
-  const int first_group = blockIdx.x * 4;
-  const int key_head = (first_group + per_head - 1) / per_head;  // the only one, as a head has four groups at least
-  const bool keys = p.plain + p.value >= 128 ? key_head * per_head < first_group + 4 && key_head < p.heads : false;
+  const int first_group = blockIdx.x * S::kWaves;
+  const int key_head = (first_group + per_head - 1) / per_head;  // the only one, if a head has as many groups as there are waves
+  const bool keys = per_head >= S::kWaves && key_head * per_head < first_group + S::kWaves && key_head < p.heads;
   const int key_pieces = p.cache.turned / kVec;
   // where a lane's pieces of a tile go, from its first row's channels on
   const bool near = rows.token < (int64_t{1} << 23);  // a tile's rows lie within 32 bits
@@ -166,7 +168,7 @@ __global__ __launch_bounds__(256) void latent_expand_kernel(LatentExpandParams p
     __syncthreads();
     if (tid < S::kTiles) partly[tid] = 0;
     __syncthreads();
-    for (int i = tid; i < S::kTiles * kRows; i += 256) {
+    for (int i = tid; i < S::kTiles * kRows; i += S::kThreads) {
       const int64_t tile = tile0 + (i / kRows) * step;
       const int64_t place = resolve(tile * kRows + i % kRows);
       places[i / kRows][i % kRows] = place;
@@ -234,7 +236,7 @@ __global__ __launch_bounds__(256) void latent_expand_kernel(LatentExpandParams p
         }
       }
       if (keys) {
-        for (int i = tid; i < kRows * key_pieces; i += 256) {
+        for (int i = tid; i < kRows * key_pieces; i += S::kThreads) {
           const int row = i / key_pieces, piece = i - row * key_pieces;
           put_key(tile, key_head, row, piece, from, places[k][row]);
         }
@@ -257,9 +259,9 @@ static hipError_t expand_as(const LatentExpandParams& p, hipStream_t stream) {
   typedef ExpandShape<T, kWide> S;
   static_assert(S::kLds + S::kTiles * S::kRows * 8 <= 160 * 1024, "LDS of a CU");
   const int64_t tiles = (p.batch.n_tokens + S::kRows - 1) / S::kRows;
-  const int x = (p.heads * ((p.plain + p.value) / 32) + 3) / 4;
+  const int x = (p.heads * ((p.plain + p.value) / 32) + S::kWaves - 1) / S::kWaves;
   const int64_t y = std::min<int64_t>(tiles, std::min<int64_t>(65535, std::max(1, 1024 / x)));
-  hipLaunchKernelGGL((latent_expand_kernel<T, kWide>), dim3(x, static_cast<unsigned>(y)), dim3(256), S::kLds, stream, p,
+  hipLaunchKernelGGL((latent_expand_kernel<T, kWide>), dim3(x, static_cast<unsigned>(y)), dim3(S::kThreads), S::kLds, stream, p,
                      tiles);
   return hipGetLastError();
 }

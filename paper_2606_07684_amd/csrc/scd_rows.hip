@@ -6,41 +6,78 @@
 namespace scd {
 using namespace dev;
 
-// out = (sum_s 2^(m_s - m) o_s) / (sum_s 2^(m_s - m) l_s): a wave a query row, two channels a lane.
-template <typename T>
+// out = (sum_s 2^(m_s - m) o_s) / (sum_s 2^(m_s - m) l_s): kWaves waves a query row, which deal its shares among them
+// and meet in LDS, two channels a lane, eight shares' values on the way at once.
+template <typename T, int kWaves>
 __global__ __launch_bounds__(256) void rows_join_kernel(RowsAttendParams p, int64_t rows) {
-  const int lane = threadIdx.x & 63, line = p.value + 2;
-  int64_t end = p.batch.n_tokens;
-  if (p.batch.cu != nullptr) end = std::min<int64_t>(end, p.batch.cu[p.batch.n_seqs]);
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6); i < rows;
-       i += static_cast<int64_t>(gridDim.x) * 4) {
+  __shared__ float halves[4][128 + 2];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, line = p.value + 2;
+  const int32_t stop = p.batch.cu != nullptr ? p.batch.cu[p.batch.n_seqs] : 0x7fffffff;
+  constexpr int kRows = 4 / kWaves;
+  for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * kRows; i0 < rows; i0 += static_cast<int64_t>(gridDim.x) * kRows) {
+    const int64_t i = i0 + (kWaves == 1 ? wave : 0);
+    if (i >= rows) return;
     const int64_t t = i / p.q.n_heads;
-    if (t >= end) return;
+    if (t >= stop) return;  // behind the last request, and so is what follows
     const RowParts r = p.parts[i];
     const int64_t last = r.first + static_cast<int64_t>(r.count - 1) * r.step;
-    if (r.count <= 1 || r.first < 0 || r.step < 0 || r.row < 0 || r.row >= p.plan.rows || last >= p.plan.grid) continue;
-    const auto slot = [&](int s) {
-      return p.slots + ((r.first + static_cast<int64_t>(s) * r.step) * p.plan.rows + r.row) * line;
-    };
+    if (r.count <= 1 || r.first < 0 || r.step < 0 || r.row < 0 || r.row >= p.plan.rows || last >= p.plan.grid ||
+        r.count > p.plan.grid)
+      continue;
+    const int count = uniform(r.count);
+    const float* row = p.slots + (static_cast<int64_t>(uniform(r.first)) * p.plan.rows + uniform(r.row)) * line + 2 * lane;
+    const int64_t step = static_cast<int64_t>(uniform(r.step)) * p.plan.rows * line;
+    const bool mine = 2 * lane < p.value;
     float m = -INFINITY, l = 0.f;
-    for (int s = lane; s < r.count; s += 64) m = fmaxf(m, slot(s)[0]);
-    for (int x = 32; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor(m, x));
-    const float base = m == -INFINITY ? 0.f : m;
     float2 o = make_float2(0.f, 0.f);
-#pragma unroll 4
-    for (int s = 0; s < r.count; ++s) {
-      const float* at = slot(s);
-      const float2 ml = *reinterpret_cast<const float2*>(at);
-      const float w = __builtin_amdgcn_exp2f(ml.x - base);
-      l += w * ml.y;
-      if (2 * lane < p.value) {
-        const float2 x = *reinterpret_cast<const float2*>(at + 2 + 2 * lane);
-        o.x += w * x.x;
-        o.y += w * x.y;
+    for (int s0 = kWaves == 1 ? 0 : wave; s0 < count; s0 += 8 * kWaves) {
+      float2 ml[8], x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int s = s0 + u * kWaves;
+        ml[u] = make_float2(-INFINITY, 0.f);
+        x[u] = make_float2(0.f, 0.f);
+        if (s < count) ml[u] = *reinterpret_cast<const float2*>(row + s * step - 2 * lane);
+        if (s < count && mine) x[u] = *reinterpret_cast<const float2*>(row + s * step + 2);
+      }
+      float now = m;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) now = fmaxf(now, ml[u].x);
+      const float base = now == -INFINITY ? 0.f : now, old = __builtin_amdgcn_exp2f(m - base);
+      m = now;
+      l *= old;
+      o.x *= old;
+      o.y *= old;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float w = __builtin_amdgcn_exp2f(ml[u].x - base);
+        l += w * ml[u].y;
+        o.x += w * x[u].x;
+        o.y += w * x[u].y;
+      }
+    }
+    if constexpr (kWaves == 4) {
+      __syncthreads();  // the last row's readers are done
+      if (lane == 0) *reinterpret_cast<float2*>(&halves[wave][0]) = make_float2(m, l);
+      if (mine) *reinterpret_cast<float2*>(&halves[wave][2 + 2 * lane]) = o;
+      __syncthreads();
+      if (wave != 0) continue;
+      const float now = fmaxf(fmaxf(halves[0][0], halves[1][0]), fmaxf(halves[2][0], halves[3][0]));
+      const float base = now == -INFINITY ? 0.f : now;
+      l = 0.f;
+      o = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float by = __builtin_amdgcn_exp2f(halves[w][0] - base);
+        l += by * halves[w][1];
+        if (mine) {
+          o.x += by * halves[w][2 + 2 * lane];
+          o.y += by * halves[w][3 + 2 * lane];
+        }
       }
     }
     const float by = l == 0.f ? 0.f : 1.f / l;
-    if (2 * lane < p.value) {
+    if (mine) {
       T* out = reinterpret_cast<T*>(p.out.data) + t * p.out.token + (i - t * p.q.n_heads) * p.out.head + 2 * lane;
       store1(out, o.x * by);
       store1(out + 1, o.y * by);
@@ -61,11 +98,15 @@ RowsSizes rows_sizes(bool bf16, bool wide, const SeqBatch& b, int64_t held_rows,
   plan.cap = held_rows;
   const int64_t least = ((rows + plan.rows - 1) / plan.rows) * kv_heads;
   const int64_t tiles = (rows / plan.rows + requests) * kv_heads;
-  plan.cut = least < 2 * kFill;
+  // Two workgroups share a CU.  Few rows are cut for both, as their call is the rows' fetch: 16 requests of 8000 positions,
+  // 8 key heads, 114 us (169 cut for one each).  Tiles of 128 rows are cut for one each, as joins weigh more: a prompt of
+  // 512 tokens 33 us (37 cut for two).
+  plan.fill = plan.rows == 128 ? 256 : 512;
+  plan.cut = least < kWholeTiles;
   plan.grid = tiles;
   if (!plan.cut) return z;
   const int block = plan.rows == 128 || !bf16 ? 32 : 64;
-  const int64_t goal = std::max(tiles, share_goal(std::min<int64_t>(tiles, 2 * kFill - 1)));
+  const int64_t goal = std::max(tiles, share_goal(std::min<int64_t>(tiles, kWholeTiles - 1), plan.fill));
   const int64_t most = std::max<int64_t>(1, ((held_rows + block - 1) / block + 1) / 2);  // shares of two blocks each
   plan.grid = tiles > goal / most ? goal : tiles * most;
   if (most == 1) {
@@ -83,12 +124,21 @@ hipError_t launch_rows_attend(bool bf16, const RowsAttendParams& p, hipStream_t 
                        : bf16             ? launch_rows_bf16(p, stream)
                                           : launch_rows_f32(p, stream);
   if (e != hipSuccess || !p.plan.cut) return e;
+  // four waves a row while there are few rows, which then have many shares (one request of 8000 positions 41 -> 17 us);
+  // with 4096 rows (a prompt of 128 tokens) a wave a row is faster, 17 us to 25
   const int64_t rows = p.batch.n_tokens * p.q.n_heads;
-  const unsigned blocks = static_cast<unsigned>(std::min<int64_t>((rows + 3) / 4, kMaxGrid));
+  const bool few = rows <= 1024;
+  const unsigned blocks = static_cast<unsigned>(std::min<int64_t>(few ? rows : (rows + 3) / 4, kMaxGrid));
   if (bf16) {
-    hipLaunchKernelGGL((rows_join_kernel<uint16_t>), dim3(blocks), dim3(256), 0, stream, p, rows);
+    if (few) {
+      hipLaunchKernelGGL((rows_join_kernel<uint16_t, 4>), dim3(blocks), dim3(256), 0, stream, p, rows);
+    } else {
+      hipLaunchKernelGGL((rows_join_kernel<uint16_t, 1>), dim3(blocks), dim3(256), 0, stream, p, rows);
+    }
+  } else if (few) {
+    hipLaunchKernelGGL((rows_join_kernel<float, 4>), dim3(blocks), dim3(256), 0, stream, p, rows);
   } else {
-    hipLaunchKernelGGL((rows_join_kernel<float>), dim3(blocks), dim3(256), 0, stream, p, rows);
+    hipLaunchKernelGGL((rows_join_kernel<float, 1>), dim3(blocks), dim3(256), 0, stream, p, rows);
   }
   return hipGetLastError();
 }
