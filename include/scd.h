@@ -549,7 +549,8 @@ scd_status_t scd_rows_attend(const scd_batch_t* batch, const scd_batch_t* held, 
  * counts the table entries that name a page (0: free), held [n_seqs] is what every request holds (its pos0 in the
  * next batch).  All are int32 in device memory; an entry outside [0, n_pages) names nothing.  Fresh pages are the
  * lowest free ones, to requests in their order and a request's positions in theirs, so results depend on the arguments
- * alone.  The calls take a pool one after another: on one stream, or ordered by the caller. */
+ * alone.  The calls take a pool one after another: on one stream, or ordered by the caller.  n_pages, n_seqs and
+ * max_pages are up to 2^30. */
 typedef struct {
   int32_t n_pages;
   int32_t n_seqs;

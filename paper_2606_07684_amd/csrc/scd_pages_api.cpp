@@ -11,6 +11,10 @@ scd_status_t check_pool(const scd_pages_t* p, const char* name) {
   if (p->n_pages < 1 || p->n_seqs < 1 || p->max_pages < 1)
     return fail(SCD_ERR_SHAPE, "%s needs n_pages, n_seqs and max_pages >= 1 (got %d, %d, %d)", name, p->n_pages,
                 p->n_seqs, p->max_pages);
+  // the kernels step 32-bit indexes by up to 4096
+  if (p->n_pages > 1 << 30 || p->n_seqs > 1 << 30 || p->max_pages > 1 << 30)
+    return fail(SCD_ERR_UNSUPPORTED, "%s: n_pages, n_seqs and max_pages up to 2^30 (got %d, %d, %d)", name, p->n_pages,
+                p->n_seqs, p->max_pages);
   if (p->page_tokens < 1) return fail(SCD_ERR_SHAPE, "page_tokens must be >= 1 (got %d)", p->page_tokens);
   const struct {
     const void* p;
