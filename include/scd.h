@@ -503,9 +503,10 @@ scd_status_t scd_latent_append(const scd_latent_cache_t* cache, const scd_batch_
  * q [n_tokens, n_heads, plain_dim + turned_dim], out [n_tokens, n_heads, value_dim], not overlapping q.  Sums and
  * the softmax are fp32.  In bf16 calls queries in the latents' space and the weighted latents are held as two
  * bf16 summands, weights of the softmax are rounded to bf16 (their sum is of unrounded ones).  A row with no
- * position to attend to is zero.  A position whose latent or key is not finite makes the rows that attend to it
- * not finite, and no others.  One call takes one token a request or a chunk of them; for prompts of some hundred
- * tokens scd_latent_expand and scd_rows_attend do a half to a third of the arithmetic.
+ * position to attend to is zero.  A position whose latent or key is not finite reaches the rows that attend to it
+ * (which it makes not finite, unless its scores are -inf and its latent finite), and no others.  One call takes one
+ * token a request or a chunk of them; for prompts of a hundred tokens and more scd_latent_expand and scd_rows_attend do
+ * less arithmetic, (plain_dim + turned_dim + value_dim) / (2 latent_dim + turned_dim) of it and the expansion.
  * n_tokens up to 65535, n_tokens * n_heads below 2^27, cached positions below 2^31 - 128.
  * `workspace` (device, 16-byte aligned, caller-owned, any contents) holds
  * scd_latent_attend_workspace_bytes(cache, batch, dtype, n_heads) bytes, which depend on the sizes alone, so
@@ -533,7 +534,7 @@ scd_status_t scd_latent_expand(const scd_latent_cache_t* cache, const scd_batch_
  * head h reads KV head h / (n_heads / n_kv_heads); out [batch.n_tokens, n_heads, value_dim], overlapping no input.
  * key_dim a multiple of 32 up to 192, value_dim up to 128.  Sums and the softmax are fp32, weights are rounded to
  * bf16 in bf16 calls.  A row with no position to attend to is zero.  Keys and values behind a row's position do not
- * reach it, whatever they hold; a value that is not finite makes its channel NaN in the rows that attend to it.
+ * reach it, whatever they hold; a value that is not finite makes its channel not finite in the rows that attend to it.
  * Fastest where all rows and strides are multiples of 16 bytes.  The workspace is as of scd_latent_attend; where it is
  * 0 bytes it may be NULL. */
 size_t scd_rows_attend_workspace_bytes(const scd_batch_t* batch, const scd_batch_t* held, int32_t dtype, int32_t n_heads,

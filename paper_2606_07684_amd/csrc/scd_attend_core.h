@@ -419,6 +419,7 @@ __device__ inline bool find_share(const SeqBatch& s, const SharePlan& p, int blo
   const int64_t per_head = total[0];
   if (per_head == 0 || workgroup >= per_head * p.heads) return false;
   const int64_t unit = xcd_remap(workgroup, static_cast<int>(per_head * p.heads));
+  if (unit >= p.grid) return false;  // more rows than the batch has, by boundaries that fall: the workspace ends here
   out.head = static_cast<int>(div_up_to(unit, per_head));
   const int64_t left = unit - out.head * per_head;
   Located at;

@@ -198,7 +198,7 @@ __device__ inline void plan_shares(const LatentAttendParams& p, int block, int t
       }
     }
     __syncthreads();
-    const int64_t total = sums[0][0] < p.plan.grid ? sums[0][0] : p.plan.grid;
+    const int64_t total = sums[0][0] < 0 ? 0 : (sums[0][0] < p.plan.grid ? sums[0][0] : p.plan.grid);
     deal(0, p.batch.n_seqs, 0, total, static_cast<int>(total), static_cast<uint32_t>(sums[0][1]));
     none(total);
     return;
