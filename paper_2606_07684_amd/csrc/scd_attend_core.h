@@ -340,9 +340,11 @@ __device__ inline void wait_copies() {
 }
 
 // ---- shares ------------------------------------------------------------------------------------------
-// A request's query rows make tiles, its positions blocks of kBlock.  While there are fewer than kWholeTiles tiles,
+// A request's query rows make tiles, its positions blocks of kBlock.  While there are fewer than plan.whole tiles,
 // every tile's positions are cut into shares of at most `chunk` blocks, so that the shares of all
-// tiles are no more than the goal:  sum ceil(blocks / chunk) <= sum blocks / chunk + tiles <= goal.
+// tiles are no more than the goal, by either of  sum ceil(blocks / chunk) <= sum blocks / chunk + tiles  and
+// sum ceil(blocks / chunk) <= tiles ceil(most blocks / chunk):  the first where lengths differ, the second, which cuts
+// equal tiles evenly, where they do not (512 rows behind 8000 positions, 32 heads, 256 us by the first alone, 143 so).
 struct Share {
   Span span;
   int64_t len;     // positions of the request
@@ -350,7 +352,7 @@ struct Share {
   int64_t first;   // unit of the tile's first share; share s is unit first + s * tiles
 };
 struct ShareLds {
-  int64_t wave[2][16];
+  int64_t wave[3][16];
   LocateLds found;
 };
 
@@ -372,8 +374,9 @@ template <int kThreads, typename Length>
 __device__ inline bool find_share(const SeqBatch& s, const SharePlan& p, int block, int least, int workgroup,
                                   ShareLds& lds, int tid, Length length, Share& out) {
   const Tiles<Length> of{p, length, block};
-  const auto all = [&](auto count, int64_t (&total)[2]) {
-    total[0] = total[1] = 0;
+  // two sums and a maximum over the requests
+  const auto all = [&](auto count, int64_t (&total)[3]) {
+    total[0] = total[1] = total[2] = 0;
     if (s.n_seqs == 1) {
       count(span_of(s, 0), 0, total);
       return;
@@ -382,31 +385,34 @@ __device__ inline bool find_share(const SeqBatch& s, const SharePlan& p, int blo
     for (int o = 32; o > 0; o >>= 1) {
       total[0] += __shfl_xor(total[0], o);
       total[1] += __shfl_xor(total[1], o);
+      const int64_t other = __shfl_xor(total[2], o);
+      total[2] = other > total[2] ? other : total[2];
     }
     __syncthreads();  // the last sum's readers are done
-    if ((tid & 63) == 0) {
-      lds.wave[0][tid >> 6] = total[0];
-      lds.wave[1][tid >> 6] = total[1];
-    }
+    if ((tid & 63) == 0)
+      for (int i = 0; i < 3; ++i) lds.wave[i][tid >> 6] = total[i];
     __syncthreads();
-    total[0] = total[1] = 0;
+    total[0] = total[1] = total[2] = 0;
     for (int w = 0; w < kThreads / 64; ++w) {
       total[0] += lds.wave[0][w];
       total[1] += lds.wave[1][w];
+      total[2] = lds.wave[2][w] > total[2] ? lds.wave[2][w] : total[2];
     }
   };
-  int64_t chunk = int64_t{1} << 40, total[2];
+  int64_t chunk = int64_t{1} << 40, total[3];
   if (p.cut) {
-    // all tiles, and all blocks of all tiles
-    all([&](const Span& span, int b, int64_t (&t)[2]) {
-      const int64_t n = of.tiles(span);
+    // all tiles, all blocks of all tiles, and those of the longest
+    all([&](const Span& span, int b, int64_t (&t)[3]) {
+      const int64_t n = of.tiles(span), blocks = of.blocks(span, b);
       t[0] += n;
-      t[1] += n * of.blocks(span, b);
+      t[1] += n * blocks;
+      t[2] = n > 0 && blocks > t[2] ? blocks : t[2];
     }, total);
     const int64_t tiles = total[0] * p.heads, work = total[1] * p.heads;
-    if (tiles < kWholeTiles) {
-      const int64_t room = share_goal(tiles, p.fill) - tiles;
-      chunk = room > 0 ? div_ceil(work, room) : chunk;
+    if (tiles > 0 && tiles < p.whole) {
+      const int64_t goal = share_goal(tiles, p.fill);
+      const int64_t mixed = div_ceil(work, goal - tiles), even = div_ceil(total[2], div_up_to(goal, tiles));
+      chunk = mixed < even ? mixed : even;
       chunk = chunk < least ? least : chunk;
     }
   }
@@ -415,7 +421,7 @@ __device__ inline bool find_share(const SeqBatch& s, const SharePlan& p, int blo
     return n <= chunk ? int64_t{1} : div_ceil(n, chunk);
   };
   // heads one after another, each with all requests' shares; every head has as many
-  all([&](const Span& span, int b, int64_t (&t)[2]) { t[0] += of.tiles(span) * parts_of(span, b); }, total);
+  all([&](const Span& span, int b, int64_t (&t)[3]) { t[0] += of.tiles(span) * parts_of(span, b); }, total);
   const int64_t per_head = total[0];
   if (per_head == 0 || workgroup >= per_head * p.heads) return false;
   const int64_t unit = xcd_remap(workgroup, static_cast<int>(per_head * p.heads));

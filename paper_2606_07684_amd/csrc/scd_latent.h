@@ -38,15 +38,15 @@ struct SharePlan {
   int32_t per_token;    // query rows a token has in a tile's head
   int32_t cut;          // whether tiles are cut at all
   int32_t fill;         // workgroups that fill the chip: its 256 CUs, times those that one holds at once
+  int32_t whole;        // tiles from which on none is cut
   int64_t cap;          // positions a request can hold
   int64_t grid;         // workgroups launched: a bound on the shares
 };
 
-// Shares that a call's tiles may be cut into, a multiple of the workgroups that fill the chip; from kWholeTiles on tiles
-// stay whole.
-constexpr int kWholeTiles = 512;
+// Shares that fewer than `whole` tiles may be cut into: a multiple of the workgroups that fill the chip, two a tile at
+// least.
 __host__ __device__ inline int64_t share_goal(int64_t tiles, int fill) {
-  return tiles >= kWholeTiles ? tiles : static_cast<int64_t>((2 * static_cast<uint32_t>(tiles) + fill - 1) / fill) * fill;
+  return static_cast<int64_t>((2 * static_cast<uint32_t>(tiles) + fill - 1) / fill) * fill;
 }
 
 // A query row's shares in the workspace, left by the first of them: share s is slot first + s * step.

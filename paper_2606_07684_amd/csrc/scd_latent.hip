@@ -139,14 +139,13 @@ __device__ inline void plan_shares(const LatentAttendParams& p, int block, int t
     tx = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
     ty = sums[1][0] + sums[1][1] + sums[1][2] + sums[1][3];
   };
-  const auto chunk_of = [&](int64_t tiles, int64_t work) {
-    uint32_t chunk = 0x7fffffff;
-    if (tiles < kWholeTiles) {
-      const int64_t room = share_goal(tiles, p.plan.fill) - tiles;
-      if (room > 0) chunk = static_cast<uint32_t>(div_ceil(work, room));
-      if (chunk < 1) chunk = 1;
-    }
-    return chunk;
+  // as of find_share, from the tiles, all their blocks and those of the longest
+  const auto chunk_of = [&](int64_t tiles, int64_t work, int64_t longest) {
+    if (tiles <= 0 || tiles >= p.plan.whole) return 0x7fffffffu;
+    const int64_t goal = share_goal(tiles, p.plan.fill);
+    const int64_t mixed = div_ceil(work, goal - tiles), even = div_ceil(longest, div_up_to(goal, tiles));
+    const int64_t chunk = mixed < even ? mixed : even;
+    return chunk < 1 ? 1u : static_cast<uint32_t>(chunk);
   };
   const auto parts_of = [](const Entry& e, uint32_t chunk) {
     const uint32_t n = e.blocks;
@@ -188,7 +187,12 @@ __device__ inline void plan_shares(const LatentAttendParams& p, int block, int t
       Entry e = load(lane);
       const int tiles = __builtin_amdgcn_readlane(wave_scan(e.tiles), 63);
       const int work = __builtin_amdgcn_readlane(wave_scan(e.tiles * e.blocks), 63);
-      const uint32_t chunk = chunk_of(tiles, work);
+      int longest = e.tiles > 0 ? e.blocks : 0;
+      for (int o = 32; o > 0; o >>= 1) {
+        const int other = __shfl_xor(longest, o);
+        longest = other > longest ? other : longest;
+      }
+      const uint32_t chunk = chunk_of(tiles, work, longest);
       const int shares = e.tiles * static_cast<int>(parts_of(e, chunk)), sum = wave_scan(shares);
       e.first = sum - shares;
       entries[lane] = e;
@@ -203,14 +207,23 @@ __device__ inline void plan_shares(const LatentAttendParams& p, int block, int t
     none(total);
     return;
   }
-  int64_t tiles = 0, work = 0, total = 0, rest = 0;
+  int64_t tiles = 0, work = 0, longest = 0, total = 0, rest = 0;
   for (int b = tid; b < p.batch.n_seqs; b += 256) {
     const Entry e = load(b);
     tiles += e.tiles;
     work += static_cast<int64_t>(e.tiles) * e.blocks;
+    longest = e.tiles > 0 && e.blocks > longest ? e.blocks : longest;
   }
   total_of(tiles, work, tiles, work);
-  const uint32_t chunk = chunk_of(tiles, work);
+  for (int o = 32; o > 0; o >>= 1) {
+    const int64_t other = __shfl_xor(longest, o);
+    longest = other > longest ? other : longest;
+  }
+  __syncthreads();  // the sums' readers are done
+  if (lane == 0) sums[0][wave] = longest;
+  __syncthreads();
+  for (int w = 0; w < 4; ++w) longest = sums[0][w] > longest ? sums[0][w] : longest;
+  const uint32_t chunk = chunk_of(tiles, work, longest);
   for (int b = tid; b < p.batch.n_seqs; b += 256) {
     const Entry e = load(b);
     total += static_cast<int64_t>(e.tiles) * parts_of(e, chunk);
@@ -505,6 +518,11 @@ LatentSizes latent_sizes(bool bf16, const LatentPages& c, const SeqBatch& b, int
   const int64_t requests = std::min<int64_t>(b.n_seqs, b.n_tokens), rows = b.n_tokens * heads;
   const int64_t mean = (rows + requests - 1) / requests;
   plan.rows = mean <= 16 ? 16 : mean <= 32 || c.latent > 256 ? 32 : mean <= 64 || c.latent > 128 ? 64 : 128;
+  // Few tiles are more tiles of half the height, but not below what a token of 32 heads has, whose rows a second tile would
+  // fetch again (us, halved | whole): two tokens of 16 requests of 1000 32 | 37, of 4000 41 | 44; 64 tokens behind 2000 46 |
+  // 51; 5 tokens of 4 requests, 64 heads, r = 128, 29 | 32; a token of 16 of 4000 at r = 512 58 | 61.  The other sides: 128
+  // tokens behind 2000 70 | 69, 200 115 | 100; a token of 16 requests of 1K to 16K, 32 heads, 50 | 44.
+  if (plan.rows > (c.latent > 256 ? 16 : 32) && rows <= 32 * plan.rows) plan.rows /= 2;
   plan.row_groups = plan.rows / 16;
   plan.heads = 1;
   plan.per_token = heads;
@@ -512,7 +530,8 @@ LatentSizes latent_sizes(bool bf16, const LatentPages& c, const SeqBatch& b, int
   plan.fill = 256;  // eight waves and most of a CU's LDS each
   plan.cap = std::min<int64_t>(static_cast<int64_t>(c.cols) * c.page, (int64_t{1} << 31) - 128);
   const int64_t tiles = rows / plan.rows + requests;
-  const int64_t goal = std::max(tiles, share_goal(std::min<int64_t>(tiles, kWholeTiles - 1), plan.fill));
+  plan.whole = 512;
+  const int64_t goal = std::max(tiles, share_goal(std::min<int64_t>(tiles, plan.whole - 1), plan.fill));
   const int block = latent_block(bf16);
   const int64_t most = std::max<int64_t>(1, (plan.cap + block - 1) / block);  // shares of a block each
   plan.grid = tiles > goal / most ? goal : tiles * most;

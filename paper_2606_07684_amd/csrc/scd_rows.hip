@@ -98,15 +98,20 @@ RowsSizes rows_sizes(bool bf16, bool wide, const SeqBatch& b, int64_t held_rows,
   plan.cap = held_rows;
   const int64_t least = ((rows + plan.rows - 1) / plan.rows) * kv_heads;
   const int64_t tiles = (rows / plan.rows + requests) * kv_heads;
-  // Two workgroups share a CU.  Few rows are cut for both, as their call is the rows' fetch: 16 requests of 8000 positions,
-  // 8 key heads, 114 us (169 cut for one each).  Tiles of 128 rows are cut for one each, as joins weigh more: a prompt of
-  // 512 tokens 33 us (37 cut for two).
-  plan.fill = plan.rows == 128 ? 256 : 512;
-  plan.cut = least < kWholeTiles;
+  // Joins cost a prompt more than idle CUs do: it is cut for one workgroup a CU, and not from 256 tiles on.  Where requests
+  // hold many more positions than query rows, bf16 calls are cut for the two workgroups that a CU takes (fp32 ones fill
+  // it), to 448 tiles.  In us, this rule's side first.  Prompts of 32 heads of 192 and 128: 512 tokens 34 | 37 cut for two,
+  // 1000 tokens (256 tiles) 43 whole | 56 cut, 1500 behind 3000 175 | 194; fp32 of 500 tokens 64 whole | 87, 256 behind
+  // 2000 139 | 153 for two.  Long: 512 rows behind 8000 115 for two | 143, 1000 behind 8000 209 cut | 264; a token of 10
+  // requests of 4000 174 cut | 193; 256 behind 1000, not long, 34 | 39 for two.
+  const bool lengthy = bf16 && held_rows > 3 * b.n_tokens && held_rows >= 2048 * requests;
+  plan.fill = lengthy ? 512 : 256;
+  plan.whole = lengthy ? 448 : 256;
+  plan.cut = least < plan.whole;
   plan.grid = tiles;
   if (!plan.cut) return z;
   const int block = plan.rows == 128 || !bf16 ? 32 : 64;
-  const int64_t goal = std::max(tiles, share_goal(std::min<int64_t>(tiles, kWholeTiles - 1), plan.fill));
+  const int64_t goal = std::max(tiles, share_goal(std::min<int64_t>(tiles, plan.whole - 1), plan.fill));
   const int64_t most = std::max<int64_t>(1, ((held_rows + block - 1) / block + 1) / 2);  // shares of two blocks each
   plan.grid = tiles > goal / most ? goal : tiles * most;
   if (most == 1) {
