@@ -264,7 +264,8 @@ hipError_t launch_latent_shape(const LatentAttendParams& p, hipStream_t stream) 
   return hipGetLastError();
 }
 // Few rows with halves of the channels, more without: 64 rows are four waves for each of a block's steps, 128 eight
-// (above 128 channels registers are too few for that, and up to 64 there is nothing to halve); latents above 256 channels, whose queries alone are 144 registers, up to 32 rows in four waves.
+// (above 128 channels registers are too few for that, and up to 64 there is nothing to halve); latents above 256 channels, whose queries
+// alone are 144 registers, up to 32 rows in four waves.
 template <typename T>
 hipError_t launch_latent_as(const LatentAttendParams& p, hipStream_t stream) {
   if (p.cache.latent <= 64) return launch_latent_shape<T, 64, 8, 1>(p, stream);

@@ -30,7 +30,7 @@ struct PagesCopyParams {
 };
 static_assert(sizeof(PagesCopyParams) <= 4096, "kernel argument block");
 
-size_t pages_workspace(int64_t n_pages, int64_t n_seqs);
+size_t pages_workspace(int64_t n_pages);
 hipError_t launch_pages_free(const PagePool& p, int n, const int32_t* seqs, hipStream_t stream);
 hipError_t launch_pages_fork(const PagePool& p, int n, const int32_t* src, const int32_t* dst, hipStream_t stream);
 hipError_t launch_pages_reserve(const PagePool& p, const SeqBatch& b, const PageMoves& m, int32_t* ws, hipStream_t stream);

@@ -48,7 +48,7 @@ scd_status_t check_list(const int32_t* list, int32_t n, const char* name) {
 }
 
 scd_status_t check_workspace(const scd_pages_t* p, const void* ws, size_t bytes) {
-  const size_t need = pages_workspace(p->n_pages, p->n_seqs);
+  const size_t need = pages_workspace(p->n_pages);
   if (ws == nullptr) return fail(SCD_ERR_NULL, "workspace is NULL");
   if (!aligned16(ws)) return fail(SCD_ERR_ALIGN, "workspace is not 16-byte aligned");
   if (bytes < need) return fail(SCD_ERR_SHAPE, "workspace_bytes %zu < %zu needed", bytes, need);
@@ -66,7 +66,7 @@ extern "C" {
 
 size_t scd_pages_workspace_bytes(const scd_pages_t* pages) {
   if (check_pool(pages, "pages") != SCD_OK) return 0;
-  return pages_workspace(pages->n_pages, pages->n_seqs);
+  return pages_workspace(pages->n_pages);
 }
 
 scd_status_t scd_pages_free(const scd_pages_t* pages, int32_t n, const int32_t* seqs, hipStream_t stream) {

@@ -102,6 +102,24 @@ def test_reserve_many_requests(n):
     b.compact()
 
 
+def test_reserve_long_prompts_of_many_requests():
+    """Columns of more requests than threads, shared pages among them; then calls that change nothing."""
+    rng = random.Random(8)
+    n = 1300
+    b = Both(9000, n, 12)
+    b.reserve([rng.choice([0, 1, 16, 17, 100, 150]) if i % 3 else 0 for i in range(n)])
+    empty, full = ([i for i in range(n) if (b.pool.held[i] > 0) == held] for held in (False, True))
+    b.fork([rng.choice(full) for _ in empty], empty)
+    b.reserve([rng.choice([0, 1, 1, 5, 40]) for _ in range(n)])
+    late = [0] * n
+    late[1200] = 13 * 16
+    assert b.reserve(late)[3] == 1
+    assert b.reserve([12 * 16 - h for h in b.pool.held])[2] > 0
+    b.free(rng.sample(range(n), 700))
+    b.reserve([rng.choice([0, 1, 33]) if h < 150 else 0 for h in b.pool.held])
+    b.compact()
+
+
 # ---- past 4 GiB --------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_latent_cache_past_4_gib(dtype):
