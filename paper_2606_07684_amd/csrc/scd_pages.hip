@@ -4,7 +4,7 @@
 // numbers alone: the lowest free pages, to requests in their order and a request's positions in theirs.  All
 // of it is integers, a few hundred to some ten thousand, so the calls are chains of dependent memory accesses
 // of one workgroup (a workgroup a request where requests are on their own); the contents are moved by
-// pages_copy_kernel, which HBM bounds.  48 forks of 16 requests: free and fork 4.8 us each, reserve 10.8, and the copy of
+// pages_copy_kernel, which HBM bounds.  48 forks of 16 requests: free and fork 4.8 us each, reserve 11 to 12, and the copy of
 // their 48 pages of 32 layers, 126 MB read and written, 20; 124 pages of 16 layers, 520 MB, 112 us, 4.7 TB/s.
 #include <algorithm>
 
