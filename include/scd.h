@@ -501,9 +501,8 @@ scd_status_t scd_latent_append(const scd_latent_cache_t* cache, const scd_batch_
  *   a = W_k,h^T q_i,h[:plain_dim],  s_j = softmax_scale (a . c_j + q_i,h[plain_dim:] . k_j),  j <= pos0[b] + i
  *   out_i,h = W_v,h sum_j p_j c_j,  p = softmax(s)
  * q [n_tokens, n_heads, plain_dim + turned_dim], out [n_tokens, n_heads, value_dim], not overlapping q.  Sums and
- * the softmax are fp32.  In bf16 calls queries in the latents' space and the weighted latents are held as two
- * bf16 summands, weights of the softmax are rounded to bf16 (their sum is of unrounded ones).  A row with no
- * position to attend to is zero.  A position whose latent or key is not finite reaches the rows that attend to it
+ * the softmax are fp32.  In bf16 calls queries in the latents' space, the softmax's weights and the weighted latents
+ * are held as two bf16 summands, 16 bits.  A row with no position to attend to is zero.  A position whose latent or key is not finite reaches the rows that attend to it
  * (which it makes not finite, unless its scores are -inf and its latent finite), and no others.  One call takes one
  * token a request or a chunk of them; for prompts of a hundred tokens and more scd_latent_expand and scd_rows_attend do
  * less arithmetic, (plain_dim + turned_dim + value_dim) / (2 latent_dim + turned_dim) of it and the expansion.
@@ -532,8 +531,9 @@ scd_status_t scd_latent_expand(const scd_latent_cache_t* cache, const scd_batch_
  *   out_i = sum_j p_j v_j,  p = softmax over j of softmax_scale (q_i . k_j),  position j <= position i
  * q [batch.n_tokens, n_heads, key_dim], k [held.n_tokens, n_kv_heads, key_dim], v [.., n_kv_heads, value_dim], query
  * head h reads KV head h / (n_heads / n_kv_heads); out [batch.n_tokens, n_heads, value_dim], overlapping no input.
- * key_dim a multiple of 32 up to 192, value_dim up to 128.  Sums and the softmax are fp32, weights are rounded to
- * bf16 in bf16 calls.  A row with no position to attend to is zero.  Keys and values behind a row's position do not
+ * key_dim a multiple of 32 up to 192, value_dim up to 128.  Sums and the softmax are fp32.  In bf16 calls its weights
+ * are held as two bf16 summands, 16 bits; calls of more than 64 query rows a KV head and request on average, of 16-byte
+ * rows, round them to bf16 once (the sum that divides is of unrounded ones).  A row with no position to attend to is zero.  Keys and values behind a row's position do not
  * reach it, whatever they hold; a value that is not finite makes its channel not finite in the rows that attend to it.
  * Fastest where all rows and strides are multiples of 16 bytes.  The workspace is as of scd_latent_attend; where it is
  * 0 bytes it may be NULL. */

@@ -71,6 +71,13 @@ __device__ inline void settle() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// Two values rounded to bf16 by one instruction.
+__device__ inline uint32_t both_bf16(float x, float y) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{x, y}), bf16x2));
+}
+
 // Whether one of the 16-byte piece's values is not finite.
 __device__ inline bool odd_piece(const uint16_t* p) {
   const uint4 v = *reinterpret_cast<const uint4*>(p);
@@ -104,6 +111,14 @@ struct AttendCore {
   // A row's base m follows its largest score once that is ahead by more than this: weights stay below 2^8, and
   // most steps neither compare scores across lanes nor scale what they have.
   static constexpr float kSlack = 8.f;
+  // Whether a bf16 call's weight is two bf16 summands, 16 bits.  With one, 8 bits, results are off by what one more
+  // rounding to bf16 would add (relative error against 64 bits 2.3e-3 over dense rows, 1.8e-3 to 1.9e-3 over latents;
+  // 1.66e-3 with two, which is the result's own rounding).  The second summand is a product more, which hides behind the
+  // memory in tiles of one 16-row tile a wave (a token of 64 requests of 8000 positions 368 us either way, 64 rows behind
+  // 8000 54 | 55; over latents a token of 16 requests of 1K to 16K 45 | 46, 200 tokens behind 2000 102 | 108), and not in
+  // prompts' tiles of two, whose matrix instructions are the call (2048 rows behind 6144 320 | 400 us, 512 behind 8000
+  // 120 | 139): those round weights once.
+  static constexpr bool kRest = NT == 1;
 
   Frag q[NT][kFrags], low[NT][kLow > 0 ? kLow : 1];
   f32x4 o[NT][kTiles];
@@ -122,7 +137,7 @@ struct AttendCore {
 
   // Positions pos .. pos + kStep - 1 at LDS rows k, v; scale >= 0.  kCareful: some row leaves some of them out
   // (behind its limit, or in a hole: bit t of `holes` for positions 16 t on); weights there are zero and values
-  // that are not finite do not count.  A value that is not finite makes its channel NaN for the rows that attend
+  // that are not finite do not count.  The sum that divides is of the weights themselves, not of their summands.  A value that is not finite makes its channel NaN for the rows that attend
   // to it.
   template <bool kCareful>
   __device__ void step(const T* k, const T* v, float scale, int pos, int holes, int lane) {
@@ -195,11 +210,7 @@ struct AttendCore {
           l[n] += w;
         }
     }
-    if (kCareful && odd) {
-      weigh<true>(v, s, pos, holes, lr, g);
-    } else {
-      weigh<false>(v, s, pos, holes, lr, g);
-    }
+    weigh<kCareful>(v, s, odd, pos, holes, lr, g);
   }
 
   // The row's sum over the lanes that hold its positions.
@@ -214,57 +225,83 @@ struct AttendCore {
     return pos + 16 * t + 4 * g + i <= limit[n] && !(holes >> t & 1);
   }
 
-  // Tiles kTile .. kTile + 3 and those behind them.
-  template <int kTile, bool kOdd>
-  __device__ void weigh_tiles(uint32_t at, const bf16x8 (&w)[NT], const bf16x8 (&ones)[NT]) {
+  // Tiles kTile .. kTile + 3 and those behind them.  odd (of all lanes alike): some value is not finite; such values are
+  // taken out and counted beside the product.
+  template <int kTile, bool kCareful>
+  __device__ void weigh_tiles(uint32_t at, const bf16x8 (&w)[NT], const bf16x8 (&rest)[NT], bool odd, int pos, int holes,
+                              int g) {
     if constexpr (kTile < kTiles) {
-      s16x4 h[8];
-      read_values4<32 * kTile, 32 * kValueRow>(at, h);
+      union { s16x4 h[8]; bf16x8 v[4]; uint32_t u[16]; } a;
+      read_values4<32 * kTile, 32 * kValueRow>(at, a.h);
+      if (kCareful && odd) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        union { s16x4 h[2]; bf16x8 v; uint16_t u[8]; } a;
-        a.h[0] = h[2 * c];
-        a.h[1] = h[2 * c + 1];
-        if constexpr (kOdd) {
-          union { bf16x8 v; uint16_t u[8]; } flag;
+        for (int c = 0; c < 4; ++c) {
+          union { bf16x8 v; uint32_t u[4]; } flag;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const bool bad = (a.u[e] & 0x7f80) == 0x7f80;
-            flag.u[e] = bad ? 0x3f80 : 0;
-            if (bad) a.u[e] = 0;
+          for (int e = 0; e < 4; ++e) {
+            // two values' exponents at once: all ones carry into the bit above them
+            const uint32_t top = ((a.u[4 * c + e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+            const uint32_t bad = top | (top - (top >> 15));
+            flag.u[e] = bad & 0x3f803f80u;
+            a.u[4 * c + e] &= ~bad;
           }
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            const f32x4 x = mma(flag.v, ones[n], f32x4{0.f, 0.f, 0.f, 0.f});
+            asm volatile("" : "+v"(pos));  // formed again for every tile: registers are short
+            bf16x8 ones;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) ones[e] = static_cast<__bf16>(seen(n, e >> 2, e & 3, pos, holes, g) ? 1.f : 0.f);
+            const f32x4 x = mma(flag.v, ones, f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
             for (int i = 0; i < 4; ++i)
               if (x[i] > 0.f) o[n][kTile + c][i] = __builtin_nanf("");
           }
+          __builtin_amdgcn_sched_barrier(0);
         }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) o[n][kTile + c] = mma(a.v, w[n], o[n][kTile + c]);
       }
-      weigh_tiles<kTile + 4, kOdd>(at, w, ones);
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) o[n][kTile + c] = mma(a.v[c], w[n], o[n][kTile + c]);
+      if constexpr (kRest) {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int n = 0; n < NT; ++n) o[n][kTile + c] = mma(a.v[c], rest[n], o[n][kTile + c]);
+      }
+      weigh_tiles<kTile + 4, kCareful>(at, w, rest, odd, pos, holes, g);
+    }
+  }
+
+  template <bool kCareful>
+  __device__ void weigh(const T* v, const f32x4 (&s)[kSub][NT], bool odd, int pos, int holes, int lr, int g) {
+    if constexpr (sizeof(T) == 2) {
+      bf16x8 w[NT], rest[NT];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        union { uint32_t u[4]; bf16x8 v; } high, low;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x = s[e >> 1][n][2 * (e & 1)], y = s[e >> 1][n][2 * (e & 1) + 1];
+          high.u[e] = both_bf16(x, y);
+          if constexpr (kRest) low.u[e] = both_bf16(x - bf16_lo(high.u[e]), y - bf16_hi(high.u[e]));
+        }
+        w[n] = high.v;
+        if constexpr (kRest) rest[n] = low.v;
+      }
+      const uint32_t at = static_cast<uint32_t>(
+          reinterpret_cast<uintptr_t>((lds_s16x4_t)(v + (4 * g + (lr >> 2)) * kValueRow + 4 * (lr & 3))));
+      weigh_tiles<0, kCareful>(at, w, rest, odd, pos, holes, g);
+    } else if (kCareful && odd) {
+      weigh_f32<true>(v, s, pos, holes, lr, g);
+    } else {
+      weigh_f32<false>(v, s, pos, holes, lr, g);
     }
   }
 
   template <bool kOdd>
-  __device__ void weigh(const T* v, const f32x4 (&s)[kSub][NT], int pos, int holes, int lr, int g) {
-    if constexpr (sizeof(T) == 2) {
-      bf16x8 w[NT], ones[NT];
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          // one rounding of a weight to bf16, 8 bits: over many positions it averages out, and the sum that
-          // divides is of unrounded weights
-          w[n][e] = static_cast<__bf16>(s[e >> 2][n][e & 3]);
-          if constexpr (kOdd) ones[n][e] = static_cast<__bf16>(seen(n, e >> 2, e & 3, pos, holes, g) ? 1.f : 0.f);
-        }
-      const uint32_t at = static_cast<uint32_t>(
-          reinterpret_cast<uintptr_t>((lds_s16x4_t)(v + (4 * g + (lr >> 2)) * kValueRow + 4 * (lr & 3))));
-      weigh_tiles<0, kOdd>(at, w, ones);
-    } else {
+  __device__ void weigh_f32(const T* v, const f32x4 (&s)[kSub][NT], int pos, int holes, int lr, int g) {
+    if constexpr (sizeof(T) == 4) {
       const T* at = v + 4 * g * kValueRow + lr;
 #pragma unroll
       for (int c = 0; c < kTiles; ++c)
