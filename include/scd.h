@@ -533,8 +533,9 @@ scd_status_t scd_latent_expand(const scd_latent_cache_t* cache, const scd_batch_
  * head h reads KV head h / (n_heads / n_kv_heads); out [batch.n_tokens, n_heads, value_dim], overlapping no input.
  * key_dim a multiple of 32 up to 192, value_dim up to 128.  Sums and the softmax are fp32.  In bf16 calls its weights
  * are held as two bf16 summands, 16 bits; calls of more than 64 query rows a KV head and request on average, of 16-byte
- * rows, round them to bf16 once (the sum that divides is of unrounded ones).  A row with no position to attend to is zero.  Keys and values behind a row's position do not
- * reach it, whatever they hold; a value that is not finite makes its channel not finite in the rows that attend to it.
+ * rows, round them to bf16 once (the sum that divides is of unrounded ones).  A row with no position to attend to is
+ * zero.  Keys and values behind a row's position do not reach it, whatever they hold; a value that is not finite makes
+ * its channel not finite in the rows that attend to it, a key whose scores are -inf takes its position out of them.
  * Fastest where all rows and strides are multiples of 16 bytes.  The workspace is as of scd_latent_attend; where it is
  * 0 bytes it may be NULL. */
 size_t scd_rows_attend_workspace_bytes(const scd_batch_t* batch, const scd_batch_t* held, int32_t dtype, int32_t n_heads,

@@ -363,8 +363,9 @@ struct Copies {
     const int r = (index(wave, j) * 64 + lane) / kPieces;
     return r < kRows ? r : kRows - 1;
   }
+  static __device__ int piece(int wave, int j, int lane) { return (index(wave, j) * 64 + lane) % kPieces; }
   static __device__ int piece(int wave, int j, int lane, int pieces) {
-    const int c = (index(wave, j) * 64 + lane) % kPieces;
+    const int c = piece(wave, j, lane);
     return c < pieces ? c : pieces - 1;
   }
 };

@@ -77,6 +77,7 @@ struct LatentAttendParams {
   const char* w_v;
   int32_t heads, plain, value;
   float scale;          // of the scores, times log2(e)
+  char* zeros;          // 256 bytes of them
   char* absorbed;       // [n_tokens * heads][query_width]
   LatentShare* shares;  // [grid]
   RowParts* parts;      // [n_tokens * heads]
@@ -102,8 +103,8 @@ __host__ __device__ constexpr int latent_block(bool bf16) { return bf16 ? 64 : 3
 // Absorbed queries, attention over the latents, the shares' join with the value matrices applied.
 struct LatentSizes {
   SharePlan plan;
-  size_t absorbed, shares, parts, slots;  // bytes of the workspace
-  size_t total() const { return absorbed + shares + parts + slots; }
+  size_t zeros, absorbed, shares, parts, slots;  // bytes of the workspace
+  size_t total() const { return zeros + absorbed + shares + parts + slots; }
 };
 LatentSizes latent_sizes(bool bf16, const LatentPages& c, const SeqBatch& b, int heads);
 hipError_t launch_latent_attend(bool bf16, const LatentAttendParams& p, hipStream_t stream);

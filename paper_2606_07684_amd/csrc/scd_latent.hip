@@ -265,7 +265,10 @@ __global__ __launch_bounds__(256) void latent_query_kernel(LatentAttendParams p)
   const int tid = threadIdx.x, h = static_cast<int>(blockIdx.x) - 1;
   if (h >= p.heads) return;
   if (h < 0) {
-    if (blockIdx.y == 0) plan_shares(p, latent_block(sizeof(T) == 2), tid);
+    if (blockIdx.y == 0) {
+      if (tid < 64) reinterpret_cast<uint32_t*>(p.zeros)[tid] = 0;
+      plan_shares(p, latent_block(sizeof(T) == 2), tid);
+    }
     return;
   }
   const int64_t t0 = static_cast<int64_t>(blockIdx.y) * kTokens;
@@ -537,6 +540,7 @@ LatentSizes latent_sizes(bool bf16, const LatentPages& c, const SeqBatch& b, int
   const int64_t most = std::max<int64_t>(1, (plan.cap + block - 1) / block);  // shares of a block each
   plan.grid = tiles > goal / most ? goal : tiles * most;
   const auto up = [](size_t n) { return (n + 255) & ~size_t{255}; };
+  z.zeros = 256;
   z.absorbed = up(static_cast<size_t>(rows) * query_width(bf16, c.latent, c.turned) * (bf16 ? 2 : 4));
   z.shares = up(static_cast<size_t>(plan.grid) * sizeof(LatentShare));
   z.parts = up(static_cast<size_t>(rows) * sizeof(RowParts));

@@ -167,10 +167,11 @@ scd_status_t scd_latent_attend(const scd_latent_cache_t* cache, const scd_batch_
   p.value = value_dim;
   p.scale = static_cast<float>(softmax_scale * kLog2e);
   char* ws = static_cast<char*>(workspace);
-  p.absorbed = ws;
-  p.shares = reinterpret_cast<LatentShare*>(ws + z.absorbed);
-  p.parts = reinterpret_cast<RowParts*>(ws + z.absorbed + z.shares);
-  p.slots = reinterpret_cast<float*>(ws + z.absorbed + z.shares + z.parts);
+  p.zeros = ws;
+  p.absorbed = p.zeros + z.zeros;
+  p.shares = reinterpret_cast<LatentShare*>(p.absorbed + z.absorbed);
+  p.parts = reinterpret_cast<RowParts*>(p.absorbed + z.absorbed + z.shares);
+  p.slots = reinterpret_cast<float*>(p.absorbed + z.absorbed + z.shares + z.parts);
   return launched(launch_latent_attend(dtype == SCD_BF16, p, stream), "latent attend");
 }
 

@@ -30,13 +30,16 @@ struct LatentShape {
   static constexpr int kRing = kBlockBytes * 4 <= 110 * 1024 ? 4 : kBlockBytes * 3 <= 150 * 1024 ? 3 : 2;
   static constexpr int kIds = 1024;
   static constexpr int kFrags = (kWide + kMostTurned) / (4 * kVec), kTiles = kWide / 16 / kHalves;
+  static constexpr int kLatentFrags = kWide / (4 * kVec);
   // bf16 queries in the latents' space have a second summand
-  static constexpr int kLow = sizeof(T) == 2 ? kWide / (4 * kVec) : 0;
+  static constexpr int kLow = sizeof(T) == 2 ? kLatentFrags : 0;
   typedef AttendCore<T, kFrags, kTiles, 1, kLow, kRow, kRow> Core;
   static constexpr int kLds = kRing * kBlockBytes + kIds * 4;
 };
 
-template <typename T, int kWide, int kWaves, int kHalves>
+// kPadded: cached rows have a narrower latent or key than kWide and 64 channels.  LDS then holds zeros for the rest, so that
+// no product of the queries' zeros there is one with an infinity.
+template <typename T, int kWide, int kWaves, int kHalves, bool kPadded>
 __global__ __launch_bounds__(64 * kWaves) void latent_attend_kernel(LatentAttendParams p) {
   typedef LatentShape<T, kWide, kWaves, kHalves> S;
   typedef typename S::Core Core;
@@ -62,7 +65,7 @@ __global__ __launch_bounds__(64 * kWaves) void latent_attend_kernel(LatentAttend
   const int blocks = static_cast<int>((seen + S::kBlock - 1) / S::kBlock);
   const int first = static_cast<int>(static_cast<int64_t>(blocks) * sh.part / sh.parts);
   const int last = static_cast<int>(static_cast<int64_t>(blocks) * (sh.part + 1) / sh.parts);
-  const int64_t slot = sh.first + static_cast<int64_t>(sh.part) * sh.tiles;
+  const int64_t slot = uniform(sh.first + static_cast<int64_t>(sh.part) * sh.tiles);
   if (sh.part == 0 && tid < tile_rows)
     p.parts[begin * p.heads + row0 + tid] =
         RowParts{sh.first, sh.tiles, sh.parts, tid};
@@ -104,16 +107,23 @@ __global__ __launch_bounds__(64 * kWaves) void latent_attend_kernel(LatentAttend
     fill();
     __syncthreads();
 
-    // a lane's pieces: the page of their row among the block's, their place in it, the column among the window's
-    const int pieces = width / kVec;
+    // A lane's pieces: the page of their row among the block's, their place in it, the column among the window's.  An LDS
+    // row is a latent of kWide channels and a key of 64.
     const uint32_t row_bytes = static_cast<uint32_t>(width * sizeof(T));
     const uint64_t page_bytes = static_cast<uint64_t>(row_bytes) << lg;
     const int mask = (1 << lg) - 1;
-    uint32_t place[S::Copies::kMine];  // the page (one of four at most) in the upper bits
+    uint32_t place[S::Copies::kMine];  // the page (one of four at most) in bits 28 and 29, bit 31: zeros
 #pragma unroll
     for (int j = 0; j < S::Copies::kMine; ++j) {
-      const int row = S::Copies::row(wave, j, lane);
-      place[j] = ((row & mask) * row_bytes + 16 * S::Copies::piece(wave, j, lane, pieces)) | (row >> lg) << 28;
+      const int row = S::Copies::row(wave, j, lane), at = (row & mask) * row_bytes;
+      if constexpr (kPadded) {
+        const int piece = S::Copies::piece(wave, j, lane);
+        const bool key = piece >= kWide / kVec;
+        const int of = key ? piece - kWide / kVec : piece, have = (key ? p.cache.turned : p.cache.latent) / kVec;
+        place[j] = of < have ? (at + 16 * (of + (key ? p.cache.latent / kVec : 0))) | (row >> lg) << 28 : 1u << 31;
+      } else {
+        place[j] = (at + 16 * S::Copies::piece(wave, j, lane, (kWide + S::kMostTurned) / kVec)) | (row >> lg) << 28;
+      }
     }
     const int last_column = static_cast<int>((seen - 1) >> lg);
     const auto fetch = [&](int block, int ring) {
@@ -123,13 +133,14 @@ __global__ __launch_bounds__(64 * kWaves) void latent_attend_kernel(LatentAttend
 #pragma unroll
       for (int j = 0; j < S::Copies::kMine; ++j) {
         // columns behind the last one that is seen are its page again
-        const int col = col0 + static_cast<int>(place[j] >> 28);
+        const int col = col0 + static_cast<int>(kPadded ? place[j] >> 28 & 3 : place[j] >> 28);
         id[j] = ids[(col < last_column ? col : last_column) - window];
       }
 #pragma unroll
       for (int j = 0; j < S::Copies::kMine; ++j) {
         const uint32_t p0 = id[j] < 0 ? 0 : id[j];  // a hole's rows are left out: any page will do
-        copy16(p.cache.pages + (p0 * page_bytes + (in_page + (place[j] & 0xfffffff))),
+        const char* at = p.cache.pages + (p0 * page_bytes + (in_page + (place[j] & 0xfffffff)));
+        copy16(kPadded && static_cast<int>(place[j]) < 0 ? p.zeros : at,
                smem + ring * S::kBlockBytes + S::Copies::index(wave, j) * 1024);
       }
     };
@@ -163,10 +174,12 @@ __global__ __launch_bounds__(64 * kWaves) void latent_attend_kernel(LatentAttend
     for (int f = 0; f < S::kFrags; ++f) {
       union { u32x4 u; typename Core::Frag v; } x, y;
       x.u = y.u = u32x4{0, 0, 0, 0};
-      if (4 * kVec * f < width) x.u = *reinterpret_cast<const u32x4*>(q + 4 * kVec * f + kVec * g);
+      const int of = f < S::kLatentFrags ? f : f - S::kLatentFrags;
+      if (!kPadded || 4 * kVec * of < (f < S::kLatentFrags ? p.cache.latent : p.cache.turned))
+        x.u = *reinterpret_cast<const u32x4*>(q + (f < S::kLatentFrags ? 0 : p.cache.latent) + 4 * kVec * of + kVec * g);
       core.q[0][f] = x.v;
       if (f < S::kLow) {
-        if (4 * kVec * f < p.cache.latent) y.u = *reinterpret_cast<const u32x4*>(q + width + 4 * kVec * f + kVec * g);
+        if (!kPadded || 4 * kVec * f < p.cache.latent) y.u = *reinterpret_cast<const u32x4*>(q + width + 4 * kVec * f + kVec * g);
         core.low[0][f < S::kLow ? f : 0] = y.v;
       }
     }
@@ -212,17 +225,19 @@ __global__ __launch_bounds__(64 * kWaves) void latent_attend_kernel(LatentAttend
 
   // what the two steps' waves have becomes one through LDS, in which no copy is under way any more
   constexpr int kLine = kWide + 4, kMine = kWide / kHalves;
+  // the lane's place, which the loop above has no registers to keep
+  const int at_lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u)), at_row = at_lane & 15, at_g = at_lane >> 4;
   float total = core.sum(0);
   if (!both) {
-    float* row = reinterpret_cast<float*>(smem) + (wr * 16 + lr) * kLine;
+    float* row = reinterpret_cast<float*>(smem) + (wr * 16 + at_row) * kLine;
     lds_barrier();
     if (wp == 1) {
-      if (g == 0) {
+      if (at_g == 0) {
         row[kWide] = core.m[0];
         row[kWide + 1] = total;
       }
 #pragma unroll
-      for (int c = 0; c < S::kTiles; ++c) *reinterpret_cast<f32x4*>(row + wc * kMine + 16 * c + 4 * g) = core.o[0][c];
+      for (int c = 0; c < S::kTiles; ++c) *reinterpret_cast<f32x4*>(row + wc * kMine + 16 * c + 4 * at_g) = core.o[0][c];
     }
     lds_barrier();
     if (wp != 0) return;
@@ -232,20 +247,20 @@ __global__ __launch_bounds__(64 * kWaves) void latent_attend_kernel(LatentAttend
     core.m[0] = now;
 #pragma unroll
     for (int c = 0; c < S::kTiles; ++c) {
-      const f32x4 x = *reinterpret_cast<const f32x4*>(row + wc * kMine + 16 * c + 4 * g);
+      const f32x4 x = *reinterpret_cast<const f32x4*>(row + wc * kMine + 16 * c + 4 * at_g);
 #pragma unroll
       for (int i = 0; i < 4; ++i) core.o[0][c][i] = core.o[0][c][i] * mine + x[i] * its;
     }
   }
-  const int line = p.cache.latent + 2, row = wr * 16 + lr;
+  const int line = p.cache.latent + 2, row = wr * 16 + at_row;
   if (row < tile_rows) {
     // lines of latent + 2 values: two-float stores keep to their alignment
     float* out = p.slots + (slot * p.plan.rows + row) * line;
-    if (g == 0 && wc == 0) *reinterpret_cast<float2*>(out) = make_float2(core.m[0], total);
+    if (at_g == 0 && wc == 0) *reinterpret_cast<float2*>(out) = make_float2(core.m[0], total);
 #pragma unroll
     for (int c = 0; c < S::kTiles; ++c)
       if (wc * kMine + 16 * c < p.cache.latent) {
-        float2* to = reinterpret_cast<float2*>(out + 2 + wc * kMine + 16 * c + 4 * g);
+        float2* to = reinterpret_cast<float2*>(out + 2 + wc * kMine + 16 * c + 4 * at_g);
         to[0] = make_float2(core.o[0][c][0], core.o[0][c][1]);
         to[1] = make_float2(core.o[0][c][2], core.o[0][c][3]);
       }
@@ -259,8 +274,12 @@ hipError_t launch_latent_shape(const LatentAttendParams& p, hipStream_t stream) 
   static_assert((kWaves * 16 / (kHalves == 2 ? 2 : 1)) * (((S::kLow > 0 ? 2 : 1) * kWide + 64) / S::kVec + 1) * 16 + 1024 <=
                     S::kRing * S::kBlockBytes, "the queries fit the ring");
   static_assert(S::kTiles % 4 == 0, "value tiles are read by fours");
-  hipLaunchKernelGGL((latent_attend_kernel<T, kWide, kWaves, kHalves>), dim3(static_cast<unsigned>(p.plan.grid)),
-                     dim3(64 * kWaves), S::kLds, stream, p);
+  const dim3 grid(static_cast<unsigned>(p.plan.grid)), block(64 * kWaves);
+  if (p.cache.latent == kWide && p.cache.turned == S::kMostTurned) {
+    hipLaunchKernelGGL((latent_attend_kernel<T, kWide, kWaves, kHalves, false>), grid, block, S::kLds, stream, p);
+  } else {
+    hipLaunchKernelGGL((latent_attend_kernel<T, kWide, kWaves, kHalves, true>), grid, block, S::kLds, stream, p);
+  }
   return hipGetLastError();
 }
 // Few rows with halves of the channels, more without: 64 rows are four waves for each of a block's steps, 128 eight

@@ -112,7 +112,7 @@ __global__ __launch_bounds__(256, 2) void rows_attend_kernel(RowsAttendParams p)
     for (int f = 0; f < kKey / (4 * kVec); ++f) {
       union { T t[kVec]; u32x4 u; typename Core::Frag v; } x;
       x.u = u32x4{0, 0, 0, 0};
-      if (works && 4 * kVec * f < p.key) {
+      if (works) {
         const T* from = q + 4 * kVec * f + kVec * g;
         if (p.q.wide) {
           x.u = *reinterpret_cast<const u32x4*>(from);
@@ -132,7 +132,7 @@ __global__ __launch_bounds__(256, 2) void rows_attend_kernel(RowsAttendParams p)
     const T* keys = reinterpret_cast<const T*>(p.k.data) + held.begin * p.k.token + sh.head * p.k.head;
     const T* vals = reinterpret_cast<const T*>(p.v.data) + held.begin * p.v.token + sh.head * p.v.head;
     // where a lane's pieces lie from the block's first row on
-    const int key_pieces = p.key / kVec, value_pieces = p.value / kVec;
+    const int key_pieces = kKey / kVec, value_pieces = p.value / kVec;
     const uint32_t key_stride = static_cast<uint32_t>(p.k.token * sizeof(T)), value_stride = static_cast<uint32_t>(p.v.token * sizeof(T));
     uint32_t key_at[S::KeyCopies::kMine], value_at[S::ValueCopies::kMine];
     if constexpr (kWide) {
@@ -273,16 +273,24 @@ hipError_t launch_rows_shape(const RowsAttendParams& p, hipStream_t stream) {
                      S::kRing * S::kBlockBytes, stream, p);
   return hipGetLastError();
 }
+// Keys of every width have an instance of their own: a padded one would multiply zeros of the query by whatever lies
+// behind a key's row, and by infinities of its last piece.  Values are padded: their columns past the row are not stored.
+template <typename T, int kKey, int NT, bool kWide>
+hipError_t launch_rows_key(const RowsAttendParams& p, hipStream_t stream) {
+  return p.value <= 64 ? launch_rows_shape<T, kKey, 64, NT, kWide>(p, stream)
+                       : launch_rows_shape<T, kKey, 128, NT, kWide>(p, stream);
+}
 template <typename T, int NT, bool kWide>
 hipError_t launch_rows_as(const RowsAttendParams& p, hipStream_t stream) {
-  if (p.value <= 64) {
-    if (p.key <= 64) return launch_rows_shape<T, 64, 64, NT, kWide>(p, stream);
-    if (p.key <= 128) return launch_rows_shape<T, 128, 64, NT, kWide>(p, stream);
-    return launch_rows_shape<T, 192, 64, NT, kWide>(p, stream);
+  switch (p.key) {
+    case 32: return launch_rows_key<T, 32, NT, kWide>(p, stream);
+    case 64: return launch_rows_key<T, 64, NT, kWide>(p, stream);
+    case 96: return launch_rows_key<T, 96, NT, kWide>(p, stream);
+    case 128: return launch_rows_key<T, 128, NT, kWide>(p, stream);
+    case 160: return launch_rows_key<T, 160, NT, kWide>(p, stream);
+    case 192: return launch_rows_key<T, 192, NT, kWide>(p, stream);
   }
-  if (p.key <= 64) return launch_rows_shape<T, 64, 128, NT, kWide>(p, stream);
-  if (p.key <= 128) return launch_rows_shape<T, 128, 128, NT, kWide>(p, stream);
-  return launch_rows_shape<T, 192, 128, NT, kWide>(p, stream);
+  return hipErrorInvalidValue;  // refused before
 }
 
 hipError_t launch_rows_bf16(const RowsAttendParams& p, hipStream_t stream);

@@ -1,0 +1,65 @@
+"""Infinities in keys and latents reach what the formulas say, at widths that kernels pad and at full ones."""
+import pytest
+import torch
+
+import paper_2606_07684_amd as scd
+from tests.latent_util import DT
+from tests.test_gpu_attend_close import _latent_close, _rows_close
+from tests.test_gpu_latent import Case as Latent
+from tests.test_gpu_rows import Case as Rows
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.fail("GPU tests need a visible MI355X")
+    scd.load_library()
+    yield
+    torch.cuda.synchronize()
+
+
+# ---- scores of -inf ---------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("r", [32, 64, 96, 128, 160, 256, 288, 512])
+@pytest.mark.parametrize("dr", [32, 64])
+def test_latent_keys_of_minus_infinity(dtype, r, dr):
+    """A shared key that makes a position's scores -inf takes it out, at every width: the same as a key so low that its
+    weight is zero."""
+    c = Latent(dtype, [70, 1], [3, 200], heads=2, plain=32, value=32, r=r, dr=dr, page=16)
+    c.q[..., 32:] = c.q[..., 32:].abs().clamp(min=0.5)
+    for channel in sorted({0, 1, dr // 2 - 1, dr // 2, dr - 8, dr - 1}):
+        pages = c.pages.clone()
+        both = []
+        for low in (float("-inf"), -1e6):
+            c.pages.copy_(pages)
+            for b, p in ((0, 5), (0, 40), (0, 63), (1, 0), (1, 17), (1, 200)):
+                c.pages[c.table[b][p // 16], p % 16, r + channel] = low
+            both.append(c.attend())
+        assert torch.isfinite(both[1]).all()
+        assert torch.equal(*both), channel
+        _latent_close(c, both[1])
+        c.pages.copy_(pages)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("key", [32, 64, 96, 128, 160, 192])
+@pytest.mark.parametrize("value", [32, 96, 128])
+@pytest.mark.parametrize("stray", [0, 1])
+def test_rows_keys_of_minus_infinity(dtype, key, value, stray):
+    c = Rows(dtype, [100, 1, 2], [30, 300, 7], heads=4, kv_heads=2, key=key, value=value)
+    c.q.copy_(c.q.abs().clamp(min=0.5))
+    room = torch.zeros(*c.k.shape[:2], key + stray, dtype=DT[dtype], device="cuda")
+    for channel in sorted({0, key // 2, key - 8, key - 1}):
+        both = []
+        for low in (float("-inf"), -1e6):
+            k = room[..., :key]  # with `stray` rows that start on an element only
+            k.copy_(c.k)
+            for p in (0, 31, 64, 100, 129, 130, 200, 430):
+                k[p, :, channel] = low
+            both.append(c.attend(k=k))
+        assert torch.equal(*both), channel
+        kept, c.k = c.k, k
+        _rows_close(c, both[1])
+        c.k = kept
