@@ -56,7 +56,7 @@ template <typename T, int kWide>
 __global__ __launch_bounds__((ExpandShape<T, kWide>::kThreads)) void latent_expand_kernel(LatentExpandParams p, int64_t tiles) {
   typedef ExpandShape<T, kWide> S;
   constexpr int kVec = S::kVec, kRows = S::kRows, kSub = kRows / 32, kRow = S::kPieces * kVec;
-  constexpr int kFrags = kWide / (2 * kVec);
+  constexpr int kFrags = kWide / (2 * kVec), kSure = kWide == 64 ? 32 : kWide / 2 + 32;  // channels that any latent has
   typedef typename Elem<T>::Frag Frag;
   extern __shared__ __attribute__((aligned(16))) char smem[];
   __shared__ int64_t places[S::kTiles][kRows];  // byte of a row in the pages, -1: a hole, -2: no such row
@@ -198,11 +198,17 @@ __global__ __launch_bounds__((ExpandShape<T, kWide>::kThreads)) void latent_expa
         for (int s = 0; s < kSub; ++s)
 #pragma unroll
           for (int i = 0; i < 16; ++i) acc[s][i] = 0.f;
+        // pieces that the latent does not have are left out: there the matrix is zeros and the row its last piece again,
+        // and an infinity of it would be NaN
 #pragma unroll
-        for (int f = 0; f < kFrags; ++f)
+        for (int c = 0; c < kWide; c += 32)
+          if (c < kSure || c < latent) {
 #pragma unroll
-          for (int s = 0; s < kSub; ++s)
-            acc[s] = mma32(w[f], *reinterpret_cast<const Frag*>(at + 32 * s * kRow + 2 * kVec * f), acc[s]);
+            for (int f = c / (2 * kVec); f < (c + 32) / (2 * kVec); ++f)
+#pragma unroll
+              for (int s = 0; s < kSub; ++s)
+                acc[s] = mma32(w[f], *reinterpret_cast<const Frag*>(at + 32 * s * kRow + 2 * kVec * f), acc[s]);
+          }
         settle();
         // out through LDS: whole runs of a row's 32 channels at a time
 #pragma unroll

@@ -63,3 +63,24 @@ def test_rows_keys_of_minus_infinity(dtype, key, value, stray):
         kept, c.k = c.k, k
         _rows_close(c, both[1])
         c.k = kept
+
+
+# ---- expansion ----------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("r", [32, 64, 96, 128, 160, 256, 288, 512])
+def test_expand_infinities(dtype, r):
+    """A latent's infinity is its products' infinity, at every width."""
+    c = Latent(dtype, [70], [0], 2, 64, 32, r, 32, 16)
+    k, v = (torch.empty(70, 2, d, dtype=DT[dtype], device="cuda") for d in (96, 32))
+    for channel in sorted({0, r // 2, r - 8, r - 1}):
+        pages = c.pages.clone()
+        w_k, w_v = (torch.where(w == 0, 1.0, w).to(DT[dtype]) for w in (c.w_k, c.w_v))
+        scd.scd_latent_expand(c.cache, c.batch, w_k, w_v, k, v)
+        clean = k.clone(), v.clone()
+        for p, x in ((0, float("inf")), (37, float("-inf")), (69, float("inf"))):
+            c.pages[c.table[0][p // 16], p % 16, channel] = x
+            clean[0][p, :, :64] = torch.sign(w_k[..., channel]) * x
+            clean[1][p] = torch.sign(w_v[..., channel]) * x
+        scd.scd_latent_expand(c.cache, c.batch, w_k, w_v, k, v)
+        assert torch.equal(k, clean[0]) and torch.equal(v, clean[1]), channel
+        c.pages.copy_(pages)
