@@ -5,7 +5,9 @@ import pytest
 import torch
 
 import paper_2606_07684_amd as scd
+from synth import workloads as W
 from tests import attend_error as E
+from tests import parity_util as U
 from tests.latent_util import DT, f64, ints, randn
 from tests.test_gpu_latent import SHAPES
 from tests.test_gpu_latent import Case as Latent
@@ -156,3 +158,44 @@ def test_latent_not_finite_where_seen(dtype, bad):
     got = c.attend()
     assert torch.equal(got[:20], clean[:20]) and torch.equal(got[40:], clean[40:])
     assert not torch.isfinite(got[20:40]).any()
+
+
+# ---- dense rows as they lie --------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,pos0,group", [([3, 5], [400, 700], 2), ([100, 120], [380, 600], 2), ([1], [1200], 1)])
+def test_rows_of_16_bytes_past_4_gib(dtype, lens, pos0, group):
+    """Rows 2^21 elements apart, which are fetched 16 bytes at a time: the last ones lie behind 4 GiB."""
+    c = Rows(dtype, lens, pos0, heads=2 * group, kv_heads=2, key=96, value=64)
+    apart = 1 << 21
+    assert (c.k.shape[0] - 1) * apart * c.k.element_size() > 1 << 32
+
+    def far(x):
+        t, h, d = x.shape
+        y = torch.empty(t * apart, dtype=x.dtype, device="cuda").as_strided((t, h, d), (apart, d, 1))
+        y.copy_(x)
+        return y
+    near = c.attend()
+    _rows_close(c, near)
+    assert torch.equal(c.attend(k=far(c.k), v=far(c.v)), near)
+
+
+@pytest.mark.parametrize("name,layers", [("SMALL_BF16", (0, 1, 3, 4)), ("SMALL_F32", (0, 2))])
+def test_rows_that_decode_and_patch_wrote(name, layers):
+    """The codec's caches of Reuse and Patch layers, [tokens, heads * head_dim], read as they are."""
+    wl = getattr(W, name)
+    inp = U.Inputs(wl, "cuda")
+    out = U.run_gpu(wl, inp, scd.scd_rope_table(U.model_of(wl), wl.max_position), which=("decode", "patch"))
+    total = np.diff(wl.cu_seqlens).tolist()
+    for new in ([1] * len(total), [min(n, 70 + 40 * b) for b, n in enumerate(total)]):
+        c = Rows(wl.dtype, new, [a - b for a, b in zip(total, new)], heads=4 * wl.n_kv_heads, kv_heads=wl.n_kv_heads,
+                 key=wl.head_dim, value=wl.head_dim)
+        for layer in layers:
+            c.k, c.v = (out[x][layer].view(-1, wl.n_kv_heads, wl.head_dim) for x in ("k_cache", "v_cache"))
+            _rows_close(c)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_of_nobody(dtype):
+    """Requests none of which holds a row."""
+    c = Rows(dtype, [3, 90], [5, 0], rows=[0, 0], heads=4, kv_heads=2)
+    assert c.k.shape[0] == 0 and not c.attend().any()
