@@ -22,7 +22,7 @@ SOURCES = ["scd_gemm.hip", "scd_patch.hip", "scd_decode.hip", "scd_encode.hip", 
            "scd_attend_rows.hip", "scd_attend_prompt.hip", "scd_serve_api.cpp", "scd_latent.hip",
            "scd_latent_attend_bf16.hip", "scd_latent_attend_f32.hip", "scd_latent_expand.hip",
            "scd_latent_api.cpp", "scd_rows.hip", "scd_rows_attend_bf16.hip", "scd_rows_attend_f32.hip",
-           "scd_rows_attend_odd.hip",            "scd_pages.hip", "scd_pages_api.cpp"]
+           "scd_rows_attend_odd.hip", "scd_pages.hip", "scd_pages_api.cpp"]
 
 FLAGS = [
     f"--offload-arch={ARCH}",

@@ -109,6 +109,8 @@ struct LatentSizes {
 LatentSizes latent_sizes(bool bf16, const LatentPages& c, const SeqBatch& b, int heads);
 hipError_t launch_latent_attend(bool bf16, const LatentAttendParams& p, hipStream_t stream);
 hipError_t launch_latent_core(bool bf16, const LatentAttendParams& p, hipStream_t stream);
+hipError_t launch_latent_core_bf16(const LatentAttendParams& p, hipStream_t stream);
+hipError_t launch_latent_core_f32(const LatentAttendParams& p, hipStream_t stream);
 
 struct RowsSizes {
   SharePlan plan;

@@ -594,8 +594,6 @@ hipError_t launch_latent_attend(bool bf16, const LatentAttendParams& p, hipStrea
   return bf16 ? attend_as<uint16_t>(p, stream) : attend_as<float>(p, stream);
 }
 
-hipError_t launch_latent_core_bf16(const LatentAttendParams& p, hipStream_t stream);
-hipError_t launch_latent_core_f32(const LatentAttendParams& p, hipStream_t stream);
 hipError_t launch_latent_core(bool bf16, const LatentAttendParams& p, hipStream_t stream) {
   return bf16 ? launch_latent_core_bf16(p, stream) : launch_latent_core_f32(p, stream);
 }

@@ -294,7 +294,4 @@ hipError_t launch_latent_as(const LatentAttendParams& p, hipStream_t stream) {
   return launch_latent_shape<T, 512, 4, 2>(p, stream);
 }
 
-hipError_t launch_latent_core_bf16(const LatentAttendParams& p, hipStream_t stream);
-hipError_t launch_latent_core_f32(const LatentAttendParams& p, hipStream_t stream);
-
 }  // namespace scd

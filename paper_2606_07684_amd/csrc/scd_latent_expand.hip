@@ -55,7 +55,7 @@ struct ExpandShape {
 template <typename T, int kWide>
 __global__ __launch_bounds__((ExpandShape<T, kWide>::kThreads)) void latent_expand_kernel(LatentExpandParams p, int64_t tiles) {
   typedef ExpandShape<T, kWide> S;
-  constexpr int kVec = S::kVec, kRows = S::kRows, kSub = kRows / 32, kRow = S::kPieces * kVec;
+  constexpr int kVec = S::kVec, kRows = S::kRows, kRow = S::kPieces * kVec;
   constexpr int kFrags = kWide / (2 * kVec), kSure = kWide == 64 ? 32 : kWide / 2 + 32;  // channels that any latent has
   typedef typename Elem<T>::Frag Frag;
   extern __shared__ __attribute__((aligned(16))) char smem[];
@@ -193,11 +193,9 @@ __global__ __launch_bounds__((ExpandShape<T, kWide>::kThreads)) void latent_expa
       }
       if (works) {
         const T* at = reinterpret_cast<const T*>(from) + col * kRow + kVec * half;
-        f32x16 acc[kSub];
+        f32x16 acc;
 #pragma unroll
-        for (int s = 0; s < kSub; ++s)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[s][i] = 0.f;
+        for (int i = 0; i < 16; ++i) acc[i] = 0.f;
         // pieces that the latent does not have are left out: there the matrix is zeros and the row its last piece again,
         // and an infinity of it would be NaN
 #pragma unroll
@@ -205,40 +203,35 @@ __global__ __launch_bounds__((ExpandShape<T, kWide>::kThreads)) void latent_expa
           if (c < kSure || c < latent) {
 #pragma unroll
             for (int f = c / (2 * kVec); f < (c + 32) / (2 * kVec); ++f)
-#pragma unroll
-              for (int s = 0; s < kSub; ++s)
-                acc[s] = mma32(w[f], *reinterpret_cast<const Frag*>(at + 32 * s * kRow + 2 * kVec * f), acc[s]);
+              acc = mma32(w[f], *reinterpret_cast<const Frag*>(at + 2 * kVec * f), acc);
           }
         settle();
         // out through LDS: whole runs of a row's 32 channels at a time
+        float x[16];
 #pragma unroll
-        for (int s = 0; s < kSub; ++s) {
-          float x[16];
+        for (int i = 0; i < 16; ++i) x[i] = acc[i];
+        if (!whole && places[k][col] < 0) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) x[i] = acc[s][i];
-          if (!whole && places[k][32 * s + col] < 0) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] = 0.f;
-          }
-          T* to = reinterpret_cast<T*>(mine + (32 * s + col) * S::kOutRow) + 16 * half;
-          store8(to, true, x);
-          store8(to + 8, true, x + 8);
+          for (int i = 0; i < 16; ++i) x[i] = 0.f;
         }
+        T* to = reinterpret_cast<T*>(mine + col * S::kOutRow) + 16 * half;
+        store8(to, true, x);
+        store8(to + 8, true, x + 8);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         const char* piece = mine + (lane / kPer) * S::kOutRow + 16 * (lane % kPer);
-        u32x4 x[kStores];
+        u32x4 y[kStores];
 #pragma unroll
-        for (int j = 0; j < kStores; ++j) x[j] = *reinterpret_cast<const u32x4*>(piece + j * kAt * S::kOutRow);
+        for (int j = 0; j < kStores; ++j) y[j] = *reinterpret_cast<const u32x4*>(piece + j * kAt * S::kOutRow);
         char* out = out_first + tile * kRows * rows.token * static_cast<int64_t>(sizeof(T));
         if (whole && rows.wide && near) {
 #pragma unroll
-          for (int j = 0; j < kStores; ++j) *reinterpret_cast<u32x4*>(out + out_at[j]) = x[j];
+          for (int j = 0; j < kStores; ++j) *reinterpret_cast<u32x4*>(out + out_at[j]) = y[j];
         } else {
 #pragma unroll
           for (int j = 0; j < kStores; ++j) {
             const int row = j * kAt + lane / kPer;
-            T* to = reinterpret_cast<T*>(out) + row * rows.token + kVec * (lane % kPer);
-            if (places[k][row] != -2) put(to, rows.wide, x[j]);
+            T* row_at = reinterpret_cast<T*>(out) + row * rows.token + kVec * (lane % kPer);
+            if (places[k][row] != -2) put(row_at, rows.wide, y[j]);
           }
         }
       }
