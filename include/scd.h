@@ -502,10 +502,13 @@ scd_status_t scd_latent_append(const scd_latent_cache_t* cache, const scd_batch_
  *   out_i,h = W_v,h sum_j p_j c_j,  p = softmax(s)
  * q [n_tokens, n_heads, plain_dim + turned_dim], out [n_tokens, n_heads, value_dim], not overlapping q.  Sums and
  * the softmax are fp32.  In bf16 calls queries in the latents' space, the softmax's weights and the weighted latents
- * are held as two bf16 summands, 16 bits.  A row with no position to attend to is zero.  A position whose latent or key is not finite reaches the rows that attend to it
- * (which it makes not finite, unless its scores are -inf and its latent finite), and no others.  One call takes one
- * token a request or a chunk of them; for prompts of a hundred tokens and more scd_latent_expand and scd_rows_attend do
- * less arithmetic, (plain_dim + turned_dim + value_dim) / (2 latent_dim + turned_dim) of it and the expansion.
+ * are held as two bf16 summands, 16 bits.  A row with no position to attend to is zero.  A position whose latent or key
+ * is not finite reaches the rows that attend to it (which it makes not finite, unless its scores are -inf and its latent
+ * finite: that takes it out of them), and no others.  One call takes one
+ * token a request or a chunk of them.  scd_latent_expand and scd_rows_attend take (plain_dim + turned_dim + value_dim) /
+ * (2 latent_dim + turned_dim) of the arithmetic, and the expansion beside it: less only where 2 latent_dim is well above
+ * plain_dim + value_dim and new tokens are many for the positions expanded (32 heads of 128 + 64 and 128 channels,
+ * latent_dim 256: from about 100 tokens behind 2000 positions, from fewer than 16 behind 200).
  * n_tokens up to 65535, n_tokens * n_heads below 2^27, cached positions below 2^31 - 128.
  * `workspace` (device, 16-byte aligned, caller-owned, any contents) holds
  * scd_latent_attend_workspace_bytes(cache, batch, dtype, n_heads) bytes, which depend on the sizes alone, so

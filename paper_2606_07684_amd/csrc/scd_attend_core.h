@@ -113,11 +113,11 @@ struct AttendCore {
   static constexpr float kSlack = 8.f;
   // Whether a bf16 call's weight is two bf16 summands, 16 bits.  With one, 8 bits, results are off by what one more
   // rounding to bf16 would add (relative error against 64 bits 2.3e-3 over dense rows, 1.8e-3 to 1.9e-3 over latents;
-  // 1.66e-3 with two, which is the result's own rounding).  The second summand is a product more, which hides behind the
-  // memory in tiles of one 16-row tile a wave (a token of 64 requests of 8000 positions 368 us either way, 64 rows behind
-  // 8000 54 | 55; over latents a token of 16 requests of 1K to 16K 45 | 46, 200 tokens behind 2000 102 | 108), and not in
-  // prompts' tiles of two, whose matrix instructions are the call (2048 rows behind 6144 320 | 400 us, 512 behind 8000
-  // 120 | 139): those round weights once.
+  // 1.66e-3 with two, which is the result's own rounding).  The second summand is a product more.  In tiles of one 16-row
+  // tile a wave its time is hidden behind the memory or small (a token of 64 requests of 8000 positions 368 us either way,
+  // 64 rows behind 8000 54 | 55; over latents a token of 16 requests of 1K to 16K 45 | 46, 200 tokens behind 2000 102 |
+  // 108).  In prompts' tiles of two it adds all of it (2048 rows behind 6144 320 | 400 us, 512 behind 8000 120 | 139):
+  // those round weights once.
   static constexpr bool kRest = NT == 1;
 
   Frag q[NT][kFrags], low[NT][kLow > 0 ? kLow : 1];
@@ -137,8 +137,8 @@ struct AttendCore {
 
   // Positions pos .. pos + kStep - 1 at LDS rows k, v; scale >= 0.  kCareful: some row leaves some of them out
   // (behind its limit, or in a hole: bit t of `holes` for positions 16 t on); weights there are zero and values
-  // that are not finite do not count.  The sum that divides is of the weights themselves, not of their summands.  A value that is not finite makes its channel NaN for the rows that attend
-  // to it.
+  // that are not finite do not count.  A value that is not finite makes its channel NaN for the rows that attend
+  // to it.  The sum that divides is of the weights themselves, not of their bf16 summands.
   template <bool kCareful>
   __device__ void step(const T* k, const T* v, float scale, int pos, int holes, int lane) {
     const int lr = lane & 15, g = lane >> 4;

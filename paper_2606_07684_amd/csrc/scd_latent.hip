@@ -9,8 +9,9 @@ using namespace dev;
 
 // ---- append ------------------------------------------------------------------------------------------
 // A wave a token: the latent's bits as they are, the shared key a channel a lane, turned in fp32 and rounded
-// once.  Bound by HBM for prompts (30000 tokens of 256 + 64 channels 14 us, 2.7 TB/s) and by three memory accesses one after
-// the other (owner, page, row) for a few tokens (64 tokens 3.3 us).
+// once.  Bound by three memory accesses one after the other (owner, page, row): all of the call for a few tokens (64
+// tokens 3.3 us), and of a prompt what its waves spend most of their time on, a token each (30000 tokens of 256 + 64
+// channels 14 us, 2.7 TB/s of the 5 that a copy reaches).
 template <typename T>
 __global__ __launch_bounds__(256) void latent_append_kernel(LatentAppendParams p) {
   constexpr int kVec = 16 / sizeof(T);
@@ -355,7 +356,7 @@ __global__ __launch_bounds__(256) void latent_query_kernel(LatentAttendParams p)
 // out_h = W_v,h (sum_s 2^(m_s - m) o_s) / (sum_s 2^(m_s - m) l_s) over a row's shares s: workgroup (h, tokens
 // of it).  One or two tokens' shares are dealt to the four waves, more tokens are dealt as they are.  The joined
 // rows, as two bf16 summands, are the right operands of the product with W_v,h, whose rows come from memory
-// as they lie.  Bound by latency: shares' places, shares, product (16 tokens of 32 heads 9.8 us).
+// as they lie.  Bound by latency: shares' places, shares, product (16 tokens of 32 heads 9.9 us).
 template <typename T, int kMost>
 __global__ __launch_bounds__(256) void latent_out_kernel(LatentAttendParams p, int tokens) {
   constexpr int kParts = sizeof(T) == 2 ? 2 : 1, kPairs = kMost / 128;
@@ -523,9 +524,9 @@ LatentSizes latent_sizes(bool bf16, const LatentPages& c, const SeqBatch& b, int
   const int64_t mean = (rows + requests - 1) / requests;
   plan.rows = mean <= 16 ? 16 : mean <= 32 || c.latent > 256 ? 32 : mean <= 64 || c.latent > 128 ? 64 : 128;
   // Few tiles are more tiles of half the height, but not below what a token of 32 heads has, whose rows a second tile would
-  // fetch again (us, halved | whole): two tokens of 16 requests of 1000 32 | 37, of 4000 41 | 44; 64 tokens behind 2000 46 |
-  // 51; 5 tokens of 4 requests, 64 heads, r = 128, 29 | 32; a token of 16 of 4000 at r = 512 58 | 61.  The other sides: 128
-  // tokens behind 2000 70 | 69, 200 115 | 100; a token of 16 requests of 1K to 16K, 32 heads, 50 | 44.
+  // fetch again (us, halved | whole): two tokens of 16 requests of 1000 32 | 37, of 4000 41 | 45; 64 tokens behind 2000 47 |
+  // 51; 5 tokens of 4 requests, 64 heads, r = 128, 29 | 32; a token of 16 of 4000 at r = 512 60 | 61.  The other sides: 128
+  // tokens behind 2000 70 | 71, 200 118 | 105; a token of 16 requests of 1K to 16K, 32 heads, 51 | 45.
   if (plan.rows > (c.latent > 256 ? 16 : 32) && rows <= 32 * plan.rows) plan.rows /= 2;
   plan.row_groups = plan.rows / 16;
   plan.heads = 1;
@@ -564,8 +565,8 @@ static void query_as(const LatentAttendParams& p, hipStream_t stream) {
 template <typename T>
 static hipError_t attend_as(const LatentAttendParams& p, hipStream_t stream) {
   const int64_t rows = p.batch.n_tokens * p.heads;
-  // one token a workgroup or four, whole calls in us: 16 tokens of 16 heads 28.9 | 31.1, a token of 64 requests of 32
-  // heads 51.9 | 48.5, 200 tokens 109 | 100
+  // one token a workgroup or four, whole calls in us: 16 tokens of 16 heads 28.5 | 31.2, a token of 64 requests of 32
+  // heads 47.9 | 45.8, 200 tokens 115 | 105
   if (rows <= 1024) {
     query_as<T, 1>(p, stream);
   } else {
@@ -575,8 +576,8 @@ static hipError_t attend_as(const LatentAttendParams& p, hipStream_t stream) {
   if (e != hipSuccess) return e;
   e = launch_latent_core(sizeof(T) == 2, p, stream);
   if (e != hipSuccess) return e;
-  // a workgroup a CU while there are so few tokens: a token of 16 requests of 32 heads 34.8 us (16 tokens a workgroup 41.4,
-  // one 36.4), of 64 requests 48.7 (51.5, 67.1)
+  // a workgroup a CU while there are so few tokens: a token of 16 requests of 32 heads 34.0 us (16 tokens a workgroup 41.6,
+  // one 36.2), of 64 requests 45.7 (48.2, 63.7)
   const int tokens = static_cast<int>(std::min<int64_t>(std::max<int64_t>(1, rows / 256), 16));
   const int64_t y = (p.batch.n_tokens + tokens - 1) / tokens;
   const dim3 grid(heads_grid(p.heads, int64_t{p.heads} * p.value * p.cache.latent * sizeof(T)), static_cast<unsigned>(y));

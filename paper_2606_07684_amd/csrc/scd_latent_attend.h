@@ -6,7 +6,7 @@
 // out of LDS, for the weighted sum.  With 16 to 64 query rows a position the arithmetic is a fifth to a half
 // of what the matrix cores do in the time a row takes to arrive, so the call is bound by HBM while there are
 // enough positions, and a workgroup a CU with two blocks in flight is what keeps HBM busy.  A token of 16 requests of 1K to
-// 16K positions, 32 heads, r = 256: 30 us, of which 6 to 7 before the first block, then 4.4 TB/s of cached rows.
+// 16K positions, 32 heads, r = 256: 31.5 to 32 us, of which 6 to 7 before the first block, then some 4 TB/s of cached rows.
 #pragma once
 
 #include "scd_attend_core.h"

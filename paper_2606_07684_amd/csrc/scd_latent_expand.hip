@@ -3,7 +3,7 @@
 // A wave keeps 32 rows of the heads' matrices in registers for the whole call and takes tiles of cached rows
 // from LDS, so the matrices are read once a workgroup and the latents once for every 256 channels; what is
 // written, heads x (plain + turned + value) channels a row, is 20 times what is read and bounds the call: 20000 positions of
-// 28 heads, r = 96, 103 us, 3.6 TB/s; of 32 heads, r = 256, 171 us, 2.5 TB/s and 490 TFLOP/s.
+// 28 heads, r = 96, 98 to 104 us, 3.6 TB/s; of 32 heads, r = 256, 136 to 140 us, 3.1 TB/s and 610 TFLOP/s.
 #include <algorithm>
 
 #include "scd_attend_core.h"

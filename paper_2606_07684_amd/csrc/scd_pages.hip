@@ -16,7 +16,8 @@ using namespace dev;
 
 constexpr int kPlanThreads = 1024, kPlanWaves = kPlanThreads / 64;
 
-// Whether value v is among list[0 .. n).
+// Whether value v is among list[0 .. n).  Every workgroup reads the list, so that calls of many requests take the square
+// of their number: 1000 freed 9 us and forked 13, 10000 29 and 61, 100000 1.2 and 3.4 ms.
 template <int kThreads>
 __device__ inline bool listed(const int32_t* list, int n, int v, int tid) {
   int found = 0;

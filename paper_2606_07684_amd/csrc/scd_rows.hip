@@ -101,9 +101,9 @@ RowsSizes rows_sizes(bool bf16, bool wide, const SeqBatch& b, int64_t held_rows,
   // Joins cost a prompt more than idle CUs do: it is cut for one workgroup a CU, and not from 256 tiles on.  Where requests
   // hold many more positions than query rows, bf16 calls are cut for the two workgroups that a CU takes (fp32 ones fill
   // it), to 448 tiles.  In us, this rule's side first.  Prompts of 32 heads of 192 and 128: 512 tokens 34 | 37 cut for two,
-  // 1000 tokens (256 tiles) 43 whole | 56 cut, 1500 behind 3000 175 | 194; fp32 of 500 tokens 64 whole | 87, 256 behind
-  // 2000 139 | 153 for two.  Long: 512 rows behind 8000 115 for two | 143, 1000 behind 8000 209 cut | 264; a token of 10
-  // requests of 4000 174 cut | 193; 256 behind 1000, not long, 34 | 39 for two.
+  // 1000 tokens (256 tiles) 44 whole | 55 cut, 1500 behind 3000 174 | 193; fp32 of 500 tokens 63 whole | 86, 256 behind
+  // 2000 137 | 150 for two.  Long: 512 rows behind 8000 114 for two | 144, 1000 behind 8000 205 cut | 264; a token of 10
+  // requests of 4000 175 cut | 191; 256 behind 1000, not long, 35 | 39 for two.
   const bool lengthy = bf16 && held_rows > 3 * b.n_tokens && held_rows >= 2048 * requests;
   plan.fill = lengthy ? 512 : 256;
   plan.whole = lengthy ? 448 : 256;

@@ -3,9 +3,10 @@
 // A workgroup takes a tile of query rows of one KV head (its group's heads side by side) and goes through the
 // positions in blocks that four waves fetch into LDS ahead of the arithmetic.  With 128 rows the matrix cores
 // and the LDS reads of the right operands take about the same time, and the softmax's exponentials and maxima run
-// beside them in the other workgroup of the CU.  2048 rows behind 6144 positions, 32 heads of 192 and 128: 337 us, 890
-// TFLOP/s, the matrix cores busy 37% of the time, the vector units 36%, LDS 30%, on the two waves a SIMD that 255 registers
-// leave.  A token of 64 requests of 8000 positions, 8 key heads: 369 us, 5.7 TB/s.
+// beside them in the other workgroup of the CU.  2048 rows behind 6144 positions, 32 heads of 192 and 128: 320 to 344 us,
+// 875 to 940 TFLOP/s, the matrix cores busy 38% of the time, the vector units 36%, LDS 31%, on two waves a SIMD: within a
+// wave the products wait for the keys, the exponentials for the scores, the values' products for both, and for their own
+// reads out of LDS.  A token of 64 requests of 8000 positions, 8 key heads: 368 us, 5.7 TB/s.
 #pragma once
 
 #include "scd_attend_core.h"
